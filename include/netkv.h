@@ -21,6 +21,9 @@
  *   netkv_schedule_streams_evolving  the same with LRU-managed caches that change with
  *                                    every dispatch (Sec. VI-B), set by netkv_lru_init
  *
+ * and the KV blocks themselves, next to their placement: netkv_attn_prompt, netkv_kv_store,
+ * netkv_kv_load, netkv_attn_decode and netkv_kv_evict.
+ *
  * Conventions for every call:
  *   - Pointers named d_* are device pointers owned by the caller; the library never
  *     frees them and keeps no reference after the call returns.  Other pointers are
@@ -60,10 +63,11 @@ typedef enum {
 
 /* Bits OR-ed into *d_status by the kernels. */
 #define NETKV_DEV_EDOMAIN 1 /* utilisation outside [0,1) or NaN; zero-length request;
-                               hash value 0 in a chain or key list; M[r][d] > len/16 */
+                               hash value 0 in a chain or key list; M[r][d] > len/16;
+                               infinity or NaN stored into a KV block */
 #define NETKV_DEV_EFULL 2   /* a hash table had no free slot, a probe ran the whole table,
                                or a cache index is inconsistent */
-#define NETKV_DEV_ERANGE 4  /* a request, prefill rank or snapshot index out of range */
+#define NETKV_DEV_ERANGE 4  /* a request, prefill rank, snapshot, row or page index out of range */
 
 /* ------------------------------------------------------------------ topology
  * The cluster is a four-level tree (Sec. III-A): fanout[0] instances per node,
@@ -485,6 +489,132 @@ typedef struct netkv_copy {
   uint64_t bytes;
 } netkv_copy;
 netkv_status netkv_copy_group_async(const netkv_copy* copies, uint32_t n, netkv_stream_t stream);
+
+/* ------------------------------------------------------------------ KV blocks
+ * The blocks that a decision moves, as data: keys and values of 16 tokens (the block of
+ * Sec. III-B) of one KV head, held in 8 bits with one fp32 scale for each block and head.
+ * At the paper's 70B shape a token then takes 41,040 bytes a pair of shards instead of
+ * 81,920 (Eq. 1 with one byte an element plus 4 bytes a block and head), which halves s_eff
+ * of Eq. 2.  The prefill instance runs netkv_attn_prompt and netkv_kv_store, the decode
+ * instance netkv_attn_decode on the blocks it received, and netkv_kv_evict gives blocks up
+ * when m_d of Eq. 5 is short.  Nothing here is part of the paper, which moves blocks as bytes.
+ *
+ * A page holds one block of every KV head:
+ *   d_k, d_v              [n_pages][kv_heads][16][head_dim] codes, 16-byte aligned
+ *   d_k_scale, d_v_scale  [n_pages][kv_heads] fp32; value = code * scale
+ * A sequence's tokens are in the pages of its row of d_table, [n_seqs][table_width] int32:
+ * token t in page d_table[seq][t / 16], row t % 16.  Entries past a sequence's last block are
+ * not read.  A page number outside [0, n_pages) sets ERANGE; the block then counts as absent
+ * (not written; zeros when loaded; no keys in the attention).  Pages may be shared by
+ * sequences that read them; a page that a call writes must be written for one sequence only.
+ *
+ * Activations are fp16 or bf16 rows (netkv_dtype) of heads * head_dim values, head by head; a
+ * row's stride is given in values, a multiple of 8, and rows start on 16 bytes.  head_dim is
+ * 64 or 128.  heads is a multiple of kv_heads: query head h reads KV head h / (heads/kv_heads).
+ * Offsets d_*_off [n_seqs+1] uint64 number a packed batch's rows as d_chain_off does blocks; a
+ * pair that decreases or passes the row count sets ERANGE and counts as no rows.
+ */
+#define NETKV_BLOCK_TOKENS 16
+typedef enum { NETKV_F16 = 0, NETKV_BF16 = 1 } netkv_dtype;
+typedef enum {
+  NETKV_KV_INT8 = 0, /* two's complement, -127 .. 127; scale = max|x| / 127 */
+  NETKV_KV_E4M3 = 1  /* 8-bit floats, up to 448; scale = max|x| / 448 */
+} netkv_kv_format;
+
+typedef struct {
+  void* d_k;
+  void* d_v;
+  float* d_k_scale;
+  float* d_v_scale;
+  uint32_t n_pages;  /* 1 .. 2^31 - 1 */
+  uint32_t kv_heads; /* 1 .. 1024 */
+  uint32_t head_dim; /* 64 or 128 */
+  uint32_t format;   /* netkv_kv_format */
+} netkv_kv_pages;    /* 48 bytes; read during the call */
+
+/* Writes new tokens into blocks: rows [d_off[i], d_off[i+1]) of d_k and d_v become tokens
+ * d_start[i], d_start[i] + 1, ... of sequence i (d_start NULL: 0).
+ *   - A block without earlier tokens gets scale = max|x| / c over its new rows and codes
+ *     rn(x * (1 / scale)), all in fp32.  Blocks whose largest value is below 2^-100 are held
+ *     as zeros with scale 0.
+ *   - A block that holds tokens before d_start[i] keeps its scale where that is the larger
+ *     one; where it grows, the earlier codes become rn(code * (old / new)).
+ *   - Rows of a block past the last new token keep what they hold.
+ * Infinities and NaN set EDOMAIN and are held as zeros.  Tokens past the table set ERANGE and
+ * are not written.  At most 2^31 - 1 rows and 2^24 - 1 sequences. */
+netkv_status netkv_kv_store(const netkv_kv_pages* pages, uint32_t dtype, const void* d_k,
+                            uint64_t k_stride, const void* d_v, uint64_t v_stride,
+                            uint32_t n_seqs, const uint64_t* d_off, uint64_t rows,
+                            const uint32_t* d_start, const int32_t* d_table,
+                            uint32_t table_width, int* d_status, netkv_stream_t stream);
+
+/* The reverse: tokens d_start[i], d_start[i] + 1, ... of sequence i into rows [d_off[i],
+ * d_off[i+1]) of d_k and d_v, each value code * scale in fp32, rounded once.  A prefill reads
+ * a cached prefix this way.  Rows of tokens past the table set ERANGE and are not written. */
+netkv_status netkv_kv_load(const netkv_kv_pages* pages, uint32_t dtype, void* d_k,
+                           uint64_t k_stride, void* d_v, uint64_t v_stride, uint32_t n_seqs,
+                           const uint64_t* d_off, uint64_t rows, const uint32_t* d_start,
+                           const int32_t* d_table, uint32_t table_width, int* d_status,
+                           netkv_stream_t stream);
+
+/* Causal attention of packed prompts.  Sequence i has Lq = d_q_off[i+1] - d_q_off[i] query rows
+ * and Lk keys by d_k_off (the same offsets for whole prompts; Lk > Lq where a cached prefix
+ * stands before the rows).  Row r of the sequence sees keys j <= r + Lk - Lq:
+ *     out = sum_j softmax_j(scale * q_r . k_j) v_j,   lse = log sum_j exp(scale * q_r . k_j)
+ * A row that sees no key (Lk < Lq) gives 0 and -inf.  Products are of 16-bit values with fp32
+ * sums; the softmax is in fp32; its weights are rounded to the inputs' type for the second
+ * product.  d_lse [q_rows][heads] fp32 or NULL.  Rows outside every sequence are not written.
+ * Values of a sequence's own v have to be finite: an infinity or NaN may reach rows that do
+ * not see it.  What lies outside the sequence reaches nothing.  scale is finite and > 0.
+ * At most 2^31 - 1 rows of either kind and 2^24 - 1 sequences. */
+netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint64_t q_stride,
+                               const void* d_k, uint64_t k_stride, const void* d_v,
+                               uint64_t v_stride, uint32_t heads, uint32_t kv_heads,
+                               uint32_t head_dim, uint32_t n_seqs, const uint64_t* d_q_off,
+                               const uint64_t* d_k_off, uint64_t q_rows, uint64_t k_rows,
+                               float scale, void* d_out, uint64_t out_stride, float* d_lse,
+                               int* d_status, netkv_stream_t stream);
+
+/* Workspace of netkv_attn_decode, 16-byte aligned; 0 for sizes out of range.  with_mass: the
+ * call gives d_mass_out. */
+size_t netkv_attn_decode_workspace_size(const netkv_kv_pages* pages, uint32_t n_seqs,
+                                        uint32_t heads, uint32_t table_width, int with_mass);
+
+/* Attention of one query row a sequence over its blocks: row i of d_q sees tokens
+ * [0, d_len[i]) of sequence i.
+ *     out = sum_t softmax_t(scale * q . k_t) v_t,  lse as for netkv_attn_prompt
+ * A sequence without tokens gives 0 and -inf.  A length past the table sets ERANGE and is cut.
+ *   d_lse       [n_seqs][heads] fp32 or NULL
+ *   d_mass_in, d_mass_out  [n_seqs][table_width] fp32 or NULL (both or d_mass_in only NULL):
+ *               mass_out[i][j] = mass_in[i][j] + the softmax weights of block j's tokens,
+ *               summed over the heads, for the blocks that sequence i has; other entries are
+ *               not written.  d_mass_in NULL: 0.  The two may be the same buffer.
+ *   d_ws        caller-owned, netkv_attn_decode_workspace_size bytes; needs no initial value;
+ *               calls that overlap on the GPU need distinct ones
+ * Codes past the last token of a block reach nothing.  At most 2^24 - 1 sequences. */
+netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t dtype, const void* d_q,
+                               uint64_t q_stride, uint32_t heads, uint32_t n_seqs,
+                               const uint32_t* d_len, const int32_t* d_table,
+                               uint32_t table_width, float scale, void* d_out,
+                               uint64_t out_stride, float* d_lse, const float* d_mass_in,
+                               float* d_mass_out, void* d_ws, size_t ws_bytes, int* d_status,
+                               netkv_stream_t stream);
+
+/* Cuts block tables to a budget.  Sequence i has n = ceil(d_len[i] / 16) blocks and keeps
+ * max(d_budget[i], sink + recent) of them: the first `sink`, the last `recent` (>= 1: the
+ * block that is being filled stays) and, of those between, the ones of largest d_mass; among
+ * equals the lowest index goes first.  NaN counts as the largest.
+ *   d_table_out, d_mass_out  [n_seqs][table_width]: what stays, in order, then -1 and 0
+ *   d_len_out                [n_seqs]: d_len less 16 for each block that went
+ *   d_freed                  [n_seqs][table_width]: the pages that went, in order, then -1
+ *   d_n_freed                [n_seqs]
+ * The rows' outputs may not be the inputs' buffers.  A length past the table sets ERANGE and
+ * is cut. */
+netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table, const uint32_t* d_len,
+                            const float* d_mass, uint32_t table_width, const uint32_t* d_budget,
+                            uint32_t sink, uint32_t recent, int32_t* d_table_out,
+                            uint32_t* d_len_out, float* d_mass_out, int32_t* d_freed,
+                            uint32_t* d_n_freed, int* d_status, netkv_stream_t stream);
 
 /* Library version, for the bindings' load check. */
 uint32_t netkv_version(void);

@@ -1,0 +1,417 @@
+// The 8-bit KV blocks: new keys and values into blocks, blocks back into rows, and the
+// eviction of blocks by the attention weight that they have drawn.
+//
+// A block is 16 tokens of one KV head (Sec. III-B's B_tok) with one scale s = max|x| / c,
+// c = 127 (int8) or 448 (e4m3): code = rn(x * (1 / s)), value = code * s.  Dividing once a
+// block and multiplying an element costs one more rounding than x / s, 2^-24 of a value that
+// is kept to 2^-8 or 2^-4.
+#include "kv_common.cuh"
+
+namespace {
+
+constexpr uint32_t kWarps = 8;            // warps of a store or load block, one unit each
+constexpr float kSmallest = 7.8886091e-31f;  // 2^-100: blocks below are held as zeros, so that
+                                             // 1 / s stays finite
+
+// A unit is one block of one KV head, its keys or its values, taken by one warp: 16 rows of
+// kDim 16-bit values.  A lane has 8 neighbouring values of a row, kDim / 8 lanes a row.
+struct Unit {
+  uint32_t seq, block, head;
+  bool values;
+};
+
+template <class Count>
+__device__ __forceinline__ Unit unit_of(uint32_t n_seqs, uint32_t kv_heads, Count count) {
+  const uint32_t w = blockIdx.x * kWarps + threadIdx.x / 32, per = 2 * kv_heads;
+  const Found f = find_unit(n_seqs, w / per, count);
+  return {f.seq, f.unit, (w % per) / 2, (w & 1) != 0};
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int d = 16; d; d /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+  return x;
+}
+
+struct StoreArgs {
+  KvArgs kv;
+  const unsigned char* k;
+  const unsigned char* v;
+  uint64_t k_stride, v_stride, rows;
+  const uint64_t* off;
+  const uint32_t* start;
+  const int32_t* table;
+  uint32_t n_seqs, width;
+  int* status;
+};
+
+// Blocks that sequence i's new rows touch, cut to its table.
+__device__ __forceinline__ uint32_t touched(const StoreArgs& a, uint32_t i) {
+  const uint64_t n = row_range(a.off, i, a.rows).count, s = a.start ? a.start[i] : 0;
+  if (n == 0) return 0;
+  const uint64_t end = min((s + n + kBlockTokens - 1) / kBlockTokens, (uint64_t)a.width);
+  return end > s / kBlockTokens ? (uint32_t)(end - s / kBlockTokens) : 0;
+}
+
+// Bad offsets or a table that is too short, said once a sequence.
+__device__ __forceinline__ void check_ranges(const StoreArgs& a) {
+  for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < a.n_seqs;
+       i += (uint64_t)gridDim.x * blockDim.x) {
+    const RowRange r = row_range(a.off, (uint32_t)i, a.rows);
+    const uint64_t s = a.start ? a.start[i] : 0;
+    if (r.bad || (r.count && s + r.count > (uint64_t)a.width * kBlockTokens))
+      flag_status(a.status, NETKV_DEV_ERANGE);
+  }
+}
+
+template <int kDim, bool kBf16, bool kE4m3>
+__global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constant__ StoreArgs a) {
+  constexpr int kLanes = kDim / 8, kRows = 32 / kLanes, kSteps = kBlockTokens / kRows;
+  check_ranges(a);
+  const Unit u = unit_of(a.n_seqs, a.kv.heads, [&](uint32_t i) { return touched(a, i); });
+  if (u.seq >= a.n_seqs) return;
+  const uint32_t lane = threadIdx.x & 31;
+  const uint64_t start = a.start ? a.start[u.seq] : 0;
+  const RowRange r = row_range(a.off, u.seq, a.rows);
+  const uint64_t block = start / kBlockTokens + u.block;
+  const int32_t page = a.table[(uint64_t)u.seq * a.width + block];
+  if (page < 0 || (uint32_t)page >= a.kv.n_pages) {
+    if (lane == 0) flag_status(a.status, NETKV_DEV_ERANGE);
+    return;
+  }
+  const unsigned char* src = u.values ? a.v : a.k;
+  const uint64_t stride = u.values ? a.v_stride : a.k_stride;
+  const uint64_t part = (uint64_t)page * a.kv.heads + u.head;
+  unsigned char* codes = (u.values ? a.kv.v : a.kv.k) + part * (kBlockTokens * kDim);
+  float* scale = (u.values ? a.kv.v_scale : a.kv.k_scale) + part;
+
+  const uint32_t col = (lane % kLanes) * 8, row0 = lane / kLanes;
+  const uint64_t pos0 = block * kBlockTokens;
+  const bool merges = pos0 < start;  // the block has tokens from earlier calls
+  uint4 x[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const uint64_t pos = pos0 + row0 + i * kRows;
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (pos >= start && pos < start + r.count)
+      x[i] = __ldcs(reinterpret_cast<const uint4*>(
+          src + ((r.first + (pos - start)) * stride + (uint64_t)u.head * kDim + col) * 2));
+  }
+  const float was = merges ? *scale : 0.f;
+  float largest = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&x[i]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 y = unpack16<kBf16>(w[j]);
+      // infinities and NaN have no code: they are held as zeros
+      if (!(fabsf(y.x) <= 3.4e38f)) w[j] &= 0xffff0000u, odd = true;
+      if (!(fabsf(y.y) <= 3.4e38f)) w[j] &= 0x0000ffffu, odd = true;
+      const float2 z = unpack16<kBf16>(w[j]);
+      largest = fmaxf(largest, fmaxf(fabsf(z.x), fabsf(z.y)));
+    }
+  }
+  if (odd) flag_status(a.status, NETKV_DEV_EDOMAIN);
+  largest = warp_max(largest);
+  const float fresh = largest < kSmallest ? 0.f : largest / (kE4m3 ? 448.f : 127.f);
+  const float now = fmaxf(was, fresh);
+  const float inv = now > 0.f ? 1.f / now : 0.f;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const uint32_t row = row0 + i * kRows;
+    const uint64_t pos = pos0 + row;
+    uint2* to = reinterpret_cast<uint2*>(codes + row * kDim + col);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[i]);
+    if (pos >= start && pos < start + r.count) {
+      uint32_t c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 y = unpack16<kBf16>(w[j]);
+        c[j] = encode2<kE4m3>(y.x * inv, y.y * inv);
+      }
+      *to = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    } else if (pos < start && now > was) {
+      // the block's scale grew: its earlier codes follow
+      const float ratio = was / now;
+      const uint2 old = *to;
+      const uint32_t q[4] = {old.x & 0xffff, old.x >> 16, old.y & 0xffff, old.y >> 16};
+      uint32_t c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 y = decode2<kE4m3>(q[j]);
+        c[j] = encode2<kE4m3>(y.x * ratio, y.y * ratio);
+      }
+      *to = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    }
+  }
+  if (lane == 0) *scale = now;
+}
+
+// Rows from blocks: the reverse walk, its output rows through StoreArgs' k and v.
+template <int kDim, bool kBf16, bool kE4m3>
+__global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant__ StoreArgs a) {
+  constexpr int kLanes = kDim / 8, kRows = 32 / kLanes, kSteps = kBlockTokens / kRows;
+  check_ranges(a);
+  const Unit u = unit_of(a.n_seqs, a.kv.heads, [&](uint32_t i) { return touched(a, i); });
+  if (u.seq >= a.n_seqs) return;
+  const uint32_t lane = threadIdx.x & 31;
+  const uint64_t start = a.start ? a.start[u.seq] : 0;
+  const RowRange r = row_range(a.off, u.seq, a.rows);
+  const uint64_t block = start / kBlockTokens + u.block;
+  const int32_t page = a.table[(uint64_t)u.seq * a.width + block];
+  const bool there = page >= 0 && (uint32_t)page < a.kv.n_pages;
+  if (!there && lane == 0) flag_status(a.status, NETKV_DEV_ERANGE);
+  unsigned char* dst = const_cast<unsigned char*>(u.values ? a.v : a.k);
+  const uint64_t stride = u.values ? a.v_stride : a.k_stride;
+  const uint64_t part = (uint64_t)(there ? page : 0) * a.kv.heads + u.head;
+  const unsigned char* codes = (u.values ? a.kv.v : a.kv.k) + part * (kBlockTokens * kDim);
+  const float s = there ? (u.values ? a.kv.v_scale : a.kv.k_scale)[part] : 0.f;
+  const uint32_t col = (lane % kLanes) * 8, row0 = lane / kLanes;
+  const uint64_t pos0 = block * kBlockTokens;
+  uint2 x[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const uint64_t pos = pos0 + row0 + i * kRows;
+    x[i] = make_uint2(0, 0);
+    if (there && pos >= start && pos < start + r.count)
+      x[i] = *reinterpret_cast<const uint2*>(codes + (row0 + i * kRows) * kDim + col);
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const uint64_t pos = pos0 + row0 + i * kRows;
+    if (pos < start || pos >= start + r.count) continue;
+    const uint32_t q[4] = {x[i].x & 0xffff, x[i].x >> 16, x[i].y & 0xffff, x[i].y >> 16};
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 y = decode2<kE4m3>(q[j]);
+      w[j] = pack16<kBf16>(y.x * s, y.y * s);
+    }
+    *reinterpret_cast<uint4*>(
+        dst + ((r.first + (pos - start)) * stride + (uint64_t)u.head * kDim + col) * 2) =
+        make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// Units of a call: at most one block a sequence more than its rows fill, at either end.
+template <bool kStore>
+netkv_status blocks_call(const netkv_kv_pages* pages, uint32_t dtype, const void* d_k,
+                         uint64_t k_stride, const void* d_v, uint64_t v_stride, uint32_t n_seqs,
+                         const uint64_t* d_off, uint64_t rows, const uint32_t* d_start,
+                         const int32_t* d_table, uint32_t width, int* d_status,
+                         netkv_stream_t stream) {
+  if (!kv_pages_ok(pages) || dtype > NETKV_BF16) return NETKV_EINVAL;
+  if (n_seqs == 0 || rows == 0) return NETKV_OK;
+  const uint64_t row = (uint64_t)pages->kv_heads * pages->head_dim;
+  if (!rows_ok(d_k, k_stride, row) || !rows_ok(d_v, v_stride, row) || !d_off || !d_table ||
+      !aligned_to(d_off, 8) || !aligned_to(d_table, 4) || !aligned_to(d_start, 4) ||
+      !aligned_to(d_status, 4) || width == 0 || width >= (1u << 28) || rows >> 31 ||
+      n_seqs >> 24)
+    return NETKV_EINVAL;
+  const uint64_t units = (rows / kBlockTokens + 2ull * n_seqs) * 2 * pages->kv_heads;
+  const uint64_t grid = (units + kWarps - 1) / kWarps;
+  if (units >> 32 || grid >> 31) return NETKV_EINVAL;
+  const StoreArgs a = {kv_args(pages), (const unsigned char*)d_k, (const unsigned char*)d_v,
+                       k_stride, v_stride, rows, d_off, d_start, d_table, n_seqs, width, d_status};
+  const bool bf = dtype == NETKV_BF16, e4 = pages->format == NETKV_KV_E4M3;
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)grid, kWarps * 32, 0, (cudaStream_t)stream>>>(a);
+  };
+  auto pick = [&](auto dim) {
+    constexpr int kDim = decltype(dim)::value;
+    if (bf && e4) go(kStore ? store_kernel<kDim, true, true> : load_kernel<kDim, true, true>);
+    else if (bf) go(kStore ? store_kernel<kDim, true, false> : load_kernel<kDim, true, false>);
+    else if (e4) go(kStore ? store_kernel<kDim, false, true> : load_kernel<kDim, false, true>);
+    else go(kStore ? store_kernel<kDim, false, false> : load_kernel<kDim, false, false>);
+  };
+  if (pages->head_dim == 64) pick(std::integral_constant<int, 64>());
+  else pick(std::integral_constant<int, 128>());
+  return netkv_launch_status();
+}
+
+// ------------------------------------------------------------------ eviction
+constexpr uint32_t kEvictThreads = 512;
+
+// Weights in the order of unsigned keys; NaN above every number, the two zeros alike.
+__device__ __forceinline__ uint32_t weight_key(float x) {
+  if (x != x) return ~0u;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+struct EvictArgs {
+  const int32_t* table;
+  const uint32_t* len;
+  const float* mass;
+  const uint32_t* budget;
+  uint32_t width, sink, recent;
+  int32_t* table_out;
+  uint32_t* len_out;
+  float* mass_out;
+  int32_t* freed;
+  uint32_t* n_freed;
+  int* status;
+};
+
+// Exclusive sum over the block of two counts at once (16 bits would not hold a chunk's worth of
+// both, so two words); every thread gets its own sums and the totals.
+__device__ __forceinline__ uint2 block_scan(uint2 x, uint2* total, uint2* scratch) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  uint2 y = x;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const uint32_t p = __shfl_up_sync(~0u, y.x, d), q = __shfl_up_sync(~0u, y.y, d);
+    if (lane >= (uint32_t)d) y.x += p, y.y += q;
+  }
+  __syncthreads();  // scratch of an earlier call has been read
+  if (lane == 31) scratch[warp] = y;
+  __syncthreads();
+  uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
+#pragma unroll
+  for (uint32_t w = 0; w < kEvictThreads / 32; ++w) {
+    const uint2 s = scratch[w];
+    if (w < warp) before.x += s.x, before.y += s.y;
+    all.x += s.x, all.y += s.y;
+  }
+  *total = all;
+  return make_uint2(before.x + y.x - x.x, before.y + y.y - x.y);
+}
+
+// One block a sequence.  The evicted blocks are the `gone` smallest of the open ones by
+// (key, index): four passes of a byte each over the keys find the largest evicted key and how
+// many of its equals go, and one ordered pass packs what stays and what goes.
+__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ uint32_t hist[256];
+  __shared__ uint2 scratch[kEvictThreads / 32];
+  __shared__ uint32_t picked[2];
+  const uint32_t seq = blockIdx.x, tid = threadIdx.x;
+  const uint64_t row = (uint64_t)seq * a.width;
+  const uint32_t len = a.len[seq];
+  uint32_t n = len / kBlockTokens + (len % kBlockTokens != 0);
+  if (n > a.width) {
+    if (tid == 0) flag_status(a.status, NETKV_DEV_ERANGE);
+    n = a.width;
+  }
+  const uint64_t held = max((uint64_t)a.budget[seq], (uint64_t)a.sink + a.recent);
+  const uint32_t gone = n > held ? n - (uint32_t)held : 0;
+  const uint32_t lo = gone ? a.sink : 0, hi = gone ? n - a.recent : 0;  // open: [lo, hi)
+
+  uint32_t prefix = 0, left = gone;  // of the keys that begin with prefix, `left` go
+  if (gone) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (uint32_t i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
+      __syncthreads();
+      for (uint32_t i = lo + tid; i < hi; i += kEvictThreads) {
+        const uint32_t key = weight_key(a.mass[row + i]);
+        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))
+          atomicAdd(&hist[(key >> shift) & 255], 1u);
+      }
+      __syncthreads();
+      if (tid < 32) {
+        uint32_t c[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += c[j] = hist[tid * 8 + j];
+        uint32_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const uint32_t x = __shfl_up_sync(~0u, upto, d);
+          if (tid >= (uint32_t)d) upto += x;
+        }
+        uint32_t before = upto - sum;
+        if (before < left && left <= upto) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if (before < left && left <= before + c[j]) {
+              picked[0] = tid * 8 + j;
+              picked[1] = left - before;
+            }
+            before += c[j];
+          }
+        }
+      }
+      __syncthreads();
+      prefix |= picked[0] << shift;
+      left = picked[1];
+    }
+  }
+  uint32_t out = 0, equal = 0;  // evicted and equal to the last key so far
+  for (uint32_t base = 0; base < a.width; base += kEvictThreads) {
+    const uint32_t i = base + tid;
+    const bool in = i < n, open = i >= lo && i < hi;
+    const float m = in ? a.mass[row + i] : 0.f;
+    const int32_t page = in ? a.table[row + i] : -1;
+    const uint32_t key = open ? weight_key(m) : 0;
+    const bool same = open && key == prefix, less = open && key < prefix;
+    uint2 total;
+    const uint2 before = block_scan(make_uint2(less, same), &total, scratch);
+    const uint32_t same_before = equal + before.y;
+    // those of `equal` that went are the first `left` of them
+    const uint32_t gone_before = out + before.x + min(same_before, left);
+    if (in) {
+      if (less || (same && same_before < left)) {
+        a.freed[row + gone_before] = page;
+      } else {
+        a.table_out[row + i - gone_before] = page;
+        a.mass_out[row + i - gone_before] = m;
+      }
+    }
+    out += total.x;
+    equal += total.y;
+  }
+  // the tails: entries past what stays and past what goes
+  for (uint32_t i = tid; i < a.width; i += kEvictThreads) {
+    if (i >= n - gone) a.table_out[row + i] = -1, a.mass_out[row + i] = 0.f;
+    if (i >= gone) a.freed[row + i] = -1;
+  }
+  if (tid == 0) {
+    a.len_out[seq] = (uint32_t)min((uint64_t)len, (uint64_t)n * kBlockTokens) - gone * kBlockTokens;
+    a.n_freed[seq] = gone;
+  }
+}
+
+}  // namespace
+
+extern "C" netkv_status netkv_kv_store(const netkv_kv_pages* pages, uint32_t dtype,
+                                       const void* d_k, uint64_t k_stride, const void* d_v,
+                                       uint64_t v_stride, uint32_t n_seqs, const uint64_t* d_off,
+                                       uint64_t rows, const uint32_t* d_start,
+                                       const int32_t* d_table, uint32_t table_width,
+                                       int* d_status, netkv_stream_t stream) {
+  return blocks_call<true>(pages, dtype, d_k, k_stride, d_v, v_stride, n_seqs, d_off, rows,
+                           d_start, d_table, table_width, d_status, stream);
+}
+
+extern "C" netkv_status netkv_kv_load(const netkv_kv_pages* pages, uint32_t dtype, void* d_k,
+                                      uint64_t k_stride, void* d_v, uint64_t v_stride,
+                                      uint32_t n_seqs, const uint64_t* d_off, uint64_t rows,
+                                      const uint32_t* d_start, const int32_t* d_table,
+                                      uint32_t table_width, int* d_status, netkv_stream_t stream) {
+  return blocks_call<false>(pages, dtype, d_k, k_stride, d_v, v_stride, n_seqs, d_off, rows,
+                            d_start, d_table, table_width, d_status, stream);
+}
+
+extern "C" netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table,
+                                       const uint32_t* d_len, const float* d_mass,
+                                       uint32_t table_width, const uint32_t* d_budget,
+                                       uint32_t sink, uint32_t recent, int32_t* d_table_out,
+                                       uint32_t* d_len_out, float* d_mass_out, int32_t* d_freed,
+                                       uint32_t* d_n_freed, int* d_status, netkv_stream_t stream) {
+  if (n_seqs == 0) return NETKV_OK;
+  const void* p[] = {d_table, d_len,      d_mass,  d_budget, d_table_out,
+                     d_len_out, d_mass_out, d_freed, d_n_freed};
+  for (const void* x : p)
+    if (!x || !aligned_to(x, 4)) return NETKV_EINVAL;
+  if (!aligned_to(d_status, 4) || table_width == 0 || table_width >= (1u << 28) || recent == 0 ||
+      n_seqs >> 31)
+    return NETKV_EINVAL;
+  // rows are packed while others of the same row are still read
+  if ((const void*)d_table == d_table_out || (const void*)d_mass == d_mass_out ||
+      (const void*)d_table == d_freed || d_table_out == d_freed)
+    return NETKV_EINVAL;
+  const EvictArgs a = {d_table,     d_len,     d_mass,     d_budget, table_width, sink,    recent,
+                       d_table_out, d_len_out, d_mass_out, d_freed,  d_n_freed,   d_status};
+  evict_kernel<<<n_seqs, kEvictThreads, 0, (cudaStream_t)stream>>>(a);
+  return netkv_launch_status();
+}

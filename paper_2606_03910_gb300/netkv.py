@@ -41,7 +41,10 @@ EXPORTS = ("netkv_topology_create", "netkv_topology_destroy", "netkv_topology_qu
            "netkv_schedule_streams_load",
            "netkv_lru_state_bytes", "netkv_lru_init", "netkv_lru_export",
            "netkv_schedule_streams_evolving",
-           "netkv_copy_async", "netkv_copy_group_async", "netkv_version")
+           "netkv_copy_async", "netkv_copy_group_async",
+           "netkv_kv_store", "netkv_kv_load", "netkv_attn_prompt",
+           "netkv_attn_decode_workspace_size", "netkv_attn_decode", "netkv_kv_evict",
+           "netkv_version")
 
 
 class NetKVError(RuntimeError):
@@ -124,10 +127,49 @@ _lib.netkv_schedule_streams_evolving.argtypes = [_P, _U32, _P, _U32, _P, _P, _P,
                                                  _P, _P, _P, _P, _P, _P, _P]
 _lib.netkv_copy_async.argtypes = [_P, _P, C.c_size_t, _P]
 _lib.netkv_copy_group_async.argtypes = [_P, _U32, _P]
+class KvPages(C.Structure):
+    """netkv_kv_pages over four tensors, which it keeps: codes [n_pages, kv_heads, 16, dim] of
+    torch.int8 or torch.float8_e4m3fn, and fp32 scales [n_pages, kv_heads]."""
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p),
+                ("d_v_scale", C.c_void_p), ("n_pages", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("format", C.c_uint32)]
+
+    def __init__(self, k, v, k_scale, v_scale):
+        fmt = str(k.dtype).replace("torch.", "")
+        if fmt not in _KV_FORMATS or v.dtype != k.dtype:
+            raise TypeError(f"KV pages of {k.dtype} and {v.dtype}: int8 or float8_e4m3fn expected")
+        if k.dim() != 4 or k.shape[2] != NETKV_BLOCK_TOKENS or v.shape != k.shape:
+            raise ValueError("KV pages are [n_pages, kv_heads, 16, dim]")
+        if k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+            raise ValueError("KV scales are [n_pages, kv_heads]")
+        for t in (k, v, k_scale, v_scale):
+            if not t.is_contiguous():
+                raise ValueError("KV pages and scales are contiguous")
+        _f32(k_scale)
+        _f32(v_scale)
+        super().__init__(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                         k.shape[0], k.shape[1], k.shape[3], _KV_FORMATS[fmt])
+        self.tensors = (k, v, k_scale, v_scale)
+        self.ref = C.byref(self)
+
+
+NETKV_BLOCK_TOKENS = 16
+NETKV_F16, NETKV_BF16 = 0, 1
+NETKV_KV_INT8, NETKV_KV_E4M3 = 0, 1
+_KV_FORMATS = {"int8": NETKV_KV_INT8, "float8_e4m3fn": NETKV_KV_E4M3}
+_lib.netkv_kv_store.argtypes = [_P, _U32, _P, _U64, _P, _U64, _U32, _P, _U64, _P, _P, _U32, _P, _P]
+_lib.netkv_kv_load.argtypes = _lib.netkv_kv_store.argtypes
+_lib.netkv_attn_prompt.argtypes = [_U32, _P, _U64, _P, _U64, _P, _U64, _U32, _U32, _U32, _U32, _P,
+                                   _P, _U64, _U64, C.c_float, _P, _U64, _P, _P, _P]
+_lib.netkv_attn_decode_workspace_size.argtypes = [_P, _U32, _U32, _U32, C.c_int]
+_lib.netkv_attn_decode_workspace_size.restype = C.c_size_t
+_lib.netkv_attn_decode.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _P, _P, _U32, C.c_float, _P,
+                                   _U64, _P, _P, _P, _P, C.c_size_t, _P, _P]
+_lib.netkv_kv_evict.argtypes = [_U32, _P, _P, _P, _U32, _P, _U32, _U32, _P, _P, _P, _P, _P, _P, _P]
 for _f in EXPORTS:
     if _f not in ("netkv_version", "netkv_prefix_match_workspace_size", "netkv_cache_index_bytes",
                   "netkv_schedule_workspace_size", "netkv_schedule_inflight_workspace_size",
-                  "netkv_lru_state_bytes"):
+                  "netkv_lru_state_bytes", "netkv_attn_decode_workspace_size"):
         getattr(_lib, _f).restype = C.c_int
 
 
@@ -373,6 +415,145 @@ def netkv_copy_group_async(copies, stream=None) -> None:
     flat = [v for dst, src, nbytes in copies for v in (_ptr(dst) or 0, _ptr(src) or 0, int(nbytes))]
     _check("netkv_copy_group_async", _lib.netkv_copy_group_async(
         (_U64 * len(flat))(*flat), len(flat) // 3, _stream(stream)))
+
+
+# ---- KV blocks: tensors carry their sizes, so these take them from the tensors and check that
+# they fit together; everything else is checked behind the entry points.
+def _f32(t) -> None:
+    if t is not None and str(t.dtype) != "torch.float32":
+        raise TypeError(f"float32 tensor expected, got {t.dtype}")
+
+
+def _rows(t, width=None):
+    """(dtype code, address, row stride) of rows [rows, heads, dim]; a row is contiguous."""
+    code = _DTYPES.get(str(t.dtype))
+    if code is None:
+        raise TypeError(f"float16 or bfloat16 rows expected, got {t.dtype}")
+    n, heads, dim = t.shape
+    s = t.stride()
+    if (dim > 1 and s[2] != 1) or (heads > 1 and s[1] != dim):
+        raise ValueError("a row's heads have to lie one after another")
+    if width is not None and (heads, dim) != width:
+        raise ValueError(f"rows of {(heads, dim)}, {width} expected")
+    return code, t.data_ptr(), s[0] if n > 1 else heads * dim
+
+
+_DTYPES = {"torch.float16": NETKV_F16, "torch.bfloat16": NETKV_BF16}
+
+
+def _same(first, *rest) -> None:
+    if any(r != first for r in rest):
+        raise TypeError("tensors of one dtype expected")
+
+
+def _ints(t, bits: int, n=None) -> Optional[int]:
+    """The address of a contiguous integer tensor, of n entries where n is given."""
+    if t is None:
+        return None
+    if t.dtype.is_floating_point or t.element_size() * 8 != bits:
+        raise TypeError(f"{bits}-bit integers expected, got {t.dtype}")
+    if not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"a contiguous tensor of {n} entries expected, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _table(t, n_seqs: int):
+    if t.dim() != 2 or t.shape[0] != n_seqs:
+        raise ValueError(f"a block table of {n_seqs} rows expected, got {tuple(t.shape)}")
+    return _ints(t, 32), t.shape[1]
+
+
+def _plane(t, shape) -> Optional[int]:
+    """The address of a contiguous fp32 tensor of that shape."""
+    if t is None:
+        return None
+    _f32(t)
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"a contiguous tensor of {tuple(shape)} expected, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _kv_move(fn: str, pages: KvPages, k, v, off, start, table, status, stream) -> None:
+    width = (pages.kv_heads, pages.head_dim)
+    dt, kp, ks = _rows(k, width)
+    dv, vp, vs = _rows(v, width)
+    _same(dt, dv)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError("as many rows of keys as of values expected")
+    n = off.numel() - 1
+    tp, tw = _table(table, n)
+    _check(fn, getattr(_lib, fn)(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, 64), k.shape[0],
+                                 _ints(start, 32, n), tp, tw, _ptr(status), _stream(stream)))
+
+
+def netkv_kv_store(pages: KvPages, k, v, off, start, table, status=None, stream=None) -> None:
+    """New tokens into 8-bit blocks: rows k, v [rows, kv_heads, dim]; see include/netkv.h."""
+    _kv_move("netkv_kv_store", pages, k, v, off, start, table, status, stream)
+
+
+def netkv_kv_load(pages: KvPages, k, v, off, start, table, status=None, stream=None) -> None:
+    """Tokens from 8-bit blocks into the rows k, v; see include/netkv.h."""
+    _kv_move("netkv_kv_load", pages, k, v, off, start, table, status, stream)
+
+
+def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=None,
+                      stream=None) -> None:
+    """Causal attention of packed prompts: q, out [q_rows, heads, dim], k, v [k_rows, kv_heads,
+    dim]; scale defaults to dim ** -0.5.  See include/netkv.h."""
+    heads, dim = q.shape[1:]
+    kv_heads = k.shape[1]
+    dt, qp, qs = _rows(q)
+    dk, kp, ks = _rows(k, (kv_heads, dim))
+    dv, vp, vs = _rows(v, (kv_heads, dim))
+    do, op, os_ = _rows(out, (heads, dim))
+    _same(dt, dk, dv, do)
+    if k.shape[0] != v.shape[0] or out.shape[0] != q.shape[0]:
+        raise ValueError("as many rows of keys as of values, and of out as of q, expected")
+    n = q_off.numel() - 1
+    _check("netkv_attn_prompt", _lib.netkv_attn_prompt(
+        dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, 64),
+        _ints(k_off, 64, n + 1), q.shape[0], k.shape[0], dim ** -0.5 if scale is None else scale,
+        op, os_, _plane(lse, (q.shape[0], heads)), _ptr(status), _stream(stream)))
+
+
+def netkv_attn_decode_workspace_size(pages: KvPages, n_seqs: int, heads: int, table_width: int,
+                                     with_mass: bool = False) -> int:
+    return int(_lib.netkv_attn_decode_workspace_size(pages.ref, int(n_seqs), int(heads),
+                                                     int(table_width), int(bool(with_mass))))
+
+
+def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=None, mass_out=None,
+                      scale=None, workspace=None, status=None, stream=None) -> None:
+    """One query row a sequence over its blocks: q, out [n_seqs, heads, dim]; see
+    include/netkv.h."""
+    n, heads, dim = q.shape
+    dt, qp, qs = _rows(q, (heads, pages.head_dim))
+    do, op, os_ = _rows(out, (heads, dim))
+    _same(dt, do)
+    if out.shape[0] != n:
+        raise ValueError("as many rows of out as of q expected")
+    tp, tw = _table(table, n)
+    ws_bytes = 0 if workspace is None else _nbytes(workspace)
+    _check("netkv_attn_decode", _lib.netkv_attn_decode(
+        pages.ref, dt, qp, qs, heads, n, _ints(length, 32, n), tp, tw,
+        dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, (n, heads)),
+        _plane(mass_in, (n, tw)), _plane(mass_out, (n, tw)), _ptr(workspace), ws_bytes,
+        _ptr(status), _stream(stream)))
+
+
+def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_out, length_out,
+                   mass_out, freed, n_freed, status=None, stream=None) -> None:
+    """Block tables cut to a budget by accumulated attention weight; see include/netkv.h."""
+    n = length.numel()
+    tp, tw = _table(table, n)
+    to, two = _table(table_out, n)
+    fr, twf = _table(freed, n)
+    if two != tw or twf != tw:
+        raise ValueError("tables of one width expected")
+    _check("netkv_kv_evict", _lib.netkv_kv_evict(
+        n, tp, _ints(length, 32, n), _plane(mass, (n, tw)), tw, _ints(budget, 32, n), int(sink),
+        int(recent), to, _ints(length_out, 32, n), _plane(mass_out, (n, tw)), fr,
+        _ints(n_freed, 32, n), _ptr(status), _stream(stream)))
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:
