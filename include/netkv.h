@@ -68,6 +68,7 @@ typedef enum {
 #define NETKV_DEV_EFULL 2   /* a hash table had no free slot, a probe ran the whole table,
                                or a cache index is inconsistent */
 #define NETKV_DEV_ERANGE 4  /* a request, prefill rank, snapshot, row or page index out of range */
+#define NETKV_DEV_ETIMEOUT 8 /* a kernel waited too long for its own copies and gave up */
 
 /* ------------------------------------------------------------------ topology
  * The cluster is a four-level tree (Sec. III-A): fanout[0] instances per node,
