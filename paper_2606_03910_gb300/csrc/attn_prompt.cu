@@ -1,75 +1,500 @@
 // Causal attention of packed prompts with grouped heads.
+//
+// Bound: 4 kDim flops a visible (query, key) pair on the tensor cores; the exponentials, one a
+// pair, come next (16 a clock and SM against 512 clocks of products for 128 x 128 pairs).
+//
+// A block takes two tiles of 128 query rows that read the same keys: two heads of a group where
+// the group is even, else two neighbouring row blocks of one head.  Keys and values come in
+// tiles of 128 rows by TMA, through a ring that serves both.  One thread issues the products,
+//     S_t = Q_t K^T (fp32, in TMEM)   O_t += P_t V (P_t from TMEM, in S_t's place)
+// so that one tile's products run while four warps take the other tile's softmax: a thread has
+// a row, reads its 128 scores, and writes the weights back as 16-bit values.  The products of
+// one issuing thread complete in order, so S_t of the next keys may follow P_t V at once.
+// The running maximum is left behind until a score passes it by 2^8 (kLag): weights of up to
+// 2^8 are as exact, and the output is then rescaled only a few times a row.
+#include <cuda.h>
+
 #include "kv_common.cuh"
 
 namespace {
 
+constexpr int kRows = 128, kKeys = 128;  // of a tile
+constexpr float kLag = 8.f;              // in powers of two
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kSoftmaxWarps = 8;
+constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // and a warp for the loads, one for the products
+// Registers: the launch has kThreads * kLaunchRegs, of which the softmax warps, that hold a row
+// of scores each thread, take more than the others.
+constexpr int kLaunchRegs = 168, kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
+
 struct PromptArgs {
-  const unsigned char* q;
-  const unsigned char* k;
-  const unsigned char* v;
   unsigned char* out;
-  uint64_t q_stride, k_stride, v_stride, out_stride;  // in values
+  uint64_t out_stride;  // in values
   const uint64_t* q_off;
   const uint64_t* k_off;
   uint64_t q_rows, k_rows;
   uint32_t heads, group, n_seqs;
-  float scale;
+  uint32_t head_pairs;  // 1: a block's tiles are two heads; 0: two row blocks of a head
+  uint32_t tiles;       // row tiles (pairs of them) that the grid has
+  float scale2;         // scale * log2(e)
   float* lse;
   int* status;
 };
 
-// One warp a (query row, head): the keys one after another with a running maximum and sum.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+  return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+// Waits for a phase, two seconds' clocks at most; once one thread of the block has given up,
+// nobody waits any longer and the block runs to its end.
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
+  if (try_wait(bar, parity)) return;
+  const long long t0 = clock64();
+  while (!try_wait(bar, parity)) {
+    if (*late) return;
+    if (clock64() - t0 > 4000000000ll) {
+      *late = 1;
+      return;
+    }
+  }
+}
+
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
+                                         uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+      "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Operands of 128-byte swizzled rows of 64 values.  Queries and keys (the inner dimension
+// along a row): groups of 8 rows 1024 bytes apart.  Values (the inner dimension across rows):
+// the same groups along the inner dimension, and 64 columns every 128 rows.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t columns_every) {
+  return (uint64_t)((at & 0x3ffff) >> 4) | (uint64_t)(columns_every >> 4) << 16 |
+         (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp32 sums of 128 rows by n columns
+__device__ __forceinline__ constexpr uint32_t product(bool bf16, bool b_across, uint32_t n) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_across ? 1u << 16 : 0u) | (n >> 3) << 17 |
+         (128u >> 4) << 24;
+}
+__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t what,
+                                         bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t what,
+                                         bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(what), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                   bar)
+               : "memory");
+}
+__device__ __forceinline__ void after_sync() {
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void before_sync() {
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t at, float* x) {  // 32 columns of the warp's lanes
+  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, "
+      "%8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, "
+      "%24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]),
+        "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, "
+      "%8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, "
+      "%24, %25, %26, %27, %28, %29, %30, %31};"
+      :
+      : "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+        "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+        "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_loaded() {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_stored() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// Stages of the ring: 32 KB each at 128 wide, with 64 KB of queries.
+template <int kDim>
+constexpr int kStages = kDim == 128 ? 4 : 6;
+
+template <int kDim>
+struct Shared {
+  alignas(1024) unsigned char q[2][kRows * kDim * 2];
+  alignas(1024) unsigned char kv[kStages<kDim>][kKeys * kDim * 2];
+  alignas(8) uint64_t q_full, kv_full[kStages<kDim>], kv_empty[kStages<kDim>], landed;
+  uint64_t s_full[2], p_full[2], o_full[2];
+  uint32_t tmem;
+  int late;
+};
+
+// One of a block's two tiles: 128 rows of one head.
+struct Tile {
+  uint32_t head;
+  int64_t row;    // the first, within the sequence
+  int64_t sees;   // keys that the first row sees; each next one sees one more (< 1: none)
+  uint32_t rows;  // 0 .. 128
+  uint32_t steps; // key tiles
+};
+
 template <int kDim, bool kBf16>
-__global__ void __launch_bounds__(256) prompt_kernel(const __grid_constant__ PromptArgs a) {
-  const uint32_t lane = threadIdx.x & 31, head = blockIdx.y;
-  if (head == 0)
-    for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < a.n_seqs; i += gridDim.x * blockDim.x)
-      if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
-        flag_status(a.status, NETKV_DEV_ERANGE);
-  const Found f = find_unit(a.n_seqs, blockIdx.x * 8 + threadIdx.x / 32, [&](uint32_t i) {
-    return (uint32_t)row_range(a.q_off, i, a.q_rows).count;
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_kernel(const __grid_constant__ PromptArgs a, const __grid_constant__ CUtensorMap map_q,
+                  const __grid_constant__ CUtensorMap map_k,
+                  const __grid_constant__ CUtensorMap map_v) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Shared<kDim>& sh = *reinterpret_cast<Shared<kDim>*>(smem);
+  constexpr int kRing = kStages<kDim>, kHalves = kDim / 64;
+  constexpr uint32_t kBox = 128 * 128;  // bytes of 128 rows of 64 values
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+
+  for (uint32_t i = blockIdx.x * kThreads + tid; i < a.n_seqs; i += gridDim.x * kThreads)
+    if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
+      flag_status(a.status, NETKV_DEV_ERANGE);
+
+  // The last row blocks come first: they see the most keys.
+  const uint32_t columns = a.head_pairs ? a.heads / 2 : a.heads, block_rows = a.head_pairs ? 128 : 256;
+  const Found f = find_unit(a.n_seqs, a.tiles - 1 - blockIdx.x / columns, [&](uint32_t i) {
+    return (uint32_t)((row_range(a.q_off, i, a.q_rows).count + block_rows - 1) / block_rows);
   });
   if (f.seq >= a.n_seqs) return;
   const RowRange rq = row_range(a.q_off, f.seq, a.q_rows), rk = row_range(a.k_off, f.seq, a.k_rows);
-  const int64_t sees = min((int64_t)rk.count, (int64_t)f.unit + 1 + (int64_t)rk.count - (int64_t)rq.count);
-  constexpr int kPer = kDim / 32;
-  float q[kPer], o[kPer] = {}, m = -INFINITY, l = 0.f;
-  const uint64_t row = rq.first + f.unit;
-#pragma unroll
-  for (int i = 0; i < kPer; i += 2) {
-    const float2 x = unpack16<kBf16>(*reinterpret_cast<const uint32_t*>(
-        a.q + (row * a.q_stride + (uint64_t)head * kDim + lane * kPer + i) * 2));
-    q[i] = x.x * a.scale, q[i + 1] = x.y * a.scale;
-  }
-  const uint64_t col = (uint64_t)(head / a.group) * kDim + lane * kPer;
-  for (int64_t j = 0; j < sees; ++j) {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPer; i += 2) {
-      const float2 x = unpack16<kBf16>(
-          *reinterpret_cast<const uint32_t*>(a.k + ((rk.first + j) * a.k_stride + col + i) * 2));
-      s += x.x * q[i] + x.y * q[i + 1];
+  const uint32_t column = blockIdx.x % columns;
+  auto tile_of = [&](uint32_t t) {
+    Tile x;
+    x.head = a.head_pairs ? column * 2 + t : column;
+    x.row = (int64_t)f.unit * block_rows + (a.head_pairs ? 0 : t * 128);
+    x.rows = (uint32_t)min((int64_t)128, max((int64_t)0, (int64_t)rq.count - x.row));
+    x.sees = (int64_t)rk.count - (int64_t)rq.count + x.row + 1;
+    const int64_t last = min((int64_t)rk.count, x.sees + (int64_t)x.rows - 1);
+    x.steps = x.rows && last > 0 ? (uint32_t)((last + kKeys - 1) / kKeys) : 0;
+    return x;
+  };
+  const uint32_t kv_head = (a.head_pairs ? column * 2 : column) / a.group;
+  const uint32_t steps0 = tile_of(0).steps, steps1 = tile_of(1).steps, steps = max(steps0, steps1);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      bar_init(smem_addr(&sh.q_full), 1);
+      bar_init(smem_addr(&sh.landed), 1);
+      for (int i = 0; i < kRing; ++i) {
+        bar_init(smem_addr(&sh.kv_full[i]), 1);
+        bar_init(smem_addr(&sh.kv_empty[i]), 1);
+      }
+      for (int t = 0; t < 2; ++t) {
+        bar_init(smem_addr(&sh.s_full[t]), 1);
+        bar_init(smem_addr(&sh.p_full[t]), 128);
+        bar_init(smem_addr(&sh.o_full[t]), 1);
+      }
+      sh.late = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-#pragma unroll
-    for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
-    const float next = fmaxf(m, s), keep = __expf(m - next), p = __expf(s - next);
-    m = next;
-    l = l * keep + p;
-#pragma unroll
-    for (int i = 0; i < kPer; i += 2) {
-      const float2 x = unpack16<kBf16>(
-          *reinterpret_cast<const uint32_t*>(a.v + ((rk.first + j) * a.v_stride + col + i) * 2));
-      o[i] = o[i] * keep + p * x.x;
-      o[i + 1] = o[i + 1] * keep + p * x.y;
-    }
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+                     smem_addr(&sh.tmem))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    before_sync();
   }
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = sh.tmem;
+  volatile int* late = &sh.late;
+  // columns: S of the two tiles, then their O
+  auto s_at = [&](uint32_t t) { return tmem + t * 128; };
+  auto o_at = [&](uint32_t t) { return tmem + 256 + t * kDim; };
+
+  if (warp >= kSoftmaxWarps) {
+   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+   if (warp == kSoftmaxWarps) {
+    // ---- loads: the queries, then K 0, V 0, K 1, V 1, ...
+    if (steps) {
+      if (lane == 0) {
+        bar_expect(smem_addr(&sh.q_full), 2 * kRows * kDim * 2);
+        for (uint32_t t = 0; t < 2; ++t) {
+          const Tile x = tile_of(t);
+          for (int h = 0; h < kHalves; ++h)
+            load_box(smem_addr(sh.q[t]) + h * kBox, &map_q, h * 64, x.head,
+                     (int)(rq.first + x.row), smem_addr(&sh.q_full));
+        }
+      }
+      for (uint32_t i = 0; i < 2 * steps && !*late; ++i) {
+        const uint32_t st = i % kRing, full = smem_addr(&sh.kv_full[st]);
+        if (i >= kRing) wait(smem_addr(&sh.kv_empty[st]), (i / kRing - 1) & 1, late);
+        const int64_t key = (int64_t)(i / 2) * kKeys;
+        const bool values = i & 1;
+        // values past the sequence's end are another's and meet weights of 0: an infinity or a
+        // NaN among them would not vanish, so the rows are cleared before they are handed on
+        const int64_t own = (int64_t)rk.count - key;
+        const bool clear = values && own < kKeys;
+        const uint32_t bar = clear ? smem_addr(&sh.landed) : full;
+        if (lane == 0) {
+          bar_expect(bar, kKeys * kDim * 2);
+          for (int h = 0; h < kHalves; ++h)
+            load_box(smem_addr(sh.kv[st]) + h * kBox, values ? &map_v : &map_k, h * 64, kv_head,
+                     (int)(rk.first + key), bar);
+        }
+        if (clear) {  // the last tile only
+          wait(bar, 0, late);
+          for (int h = 0; h < kHalves; ++h)
+            for (uint32_t x = (uint32_t)own * 8 + lane; x < kKeys * 8; x += 32)
+              reinterpret_cast<uint4*>(sh.kv[st] + h * kBox)[x] = make_uint4(0, 0, 0, 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(full);
+        }
+        __syncwarp();
+      }
+    }
+   } else if (warp == kSoftmaxWarps + 1) {
+    // ---- products
+    if (lane == 0 && steps) {
+      constexpr uint32_t kScores = product(kBf16, false, kKeys), kSums = product(kBf16, true, kDim);
+      auto scores = [&](uint32_t t, uint32_t i) {  // S_t from the ring's i-th tile
+        const uint32_t q = smem_addr(sh.q[t]), k = smem_addr(sh.kv[i % kRing]);
 #pragma unroll
-  for (int i = 0; i < kPer; i += 2)
-    *reinterpret_cast<uint32_t*>(
-        a.out + (row * a.out_stride + (uint64_t)head * kDim + lane * kPer + i) * 2) =
-        pack16<kBf16>(o[i] * inv, o[i + 1] * inv);
-  if (lane == 0 && a.lse) a.lse[row * a.heads + head] = l == 0.f ? -INFINITY : m + logf(l);
+        for (int x = 0; x < kDim / 16; ++x) {
+          const uint32_t off = x / 4 * kBox + x % 4 * 32;
+          mma_smem(s_at(t), operand(q + off, 16), operand(k + off, 16), kScores, x > 0);
+        }
+        commit(smem_addr(&sh.s_full[t]));
+      };
+      auto sums = [&](uint32_t t, uint32_t i, bool add) {
+        const uint32_t v = smem_addr(sh.kv[i % kRing]);
+#pragma unroll
+        for (int x = 0; x < kKeys / 16; ++x)
+          mma_tmem(o_at(t), s_at(t) + x * 8, operand(v + x * 2048, kBox), kSums, add || x > 0);
+      };
+      auto arrived = [&](uint32_t i) {
+        wait(smem_addr(&sh.kv_full[i % kRing]), (i / kRing) & 1, late);
+      };
+      wait(smem_addr(&sh.q_full), 0, late);
+      arrived(0);
+      after_sync();
+      for (uint32_t t = 0; t < 2; ++t)
+        if (t ? steps1 : steps0) scores(t, 0);
+      if (steps > 1) commit(smem_addr(&sh.kv_empty[0]));
+      for (uint32_t j = 0; j < steps && !*late; ++j) {
+        arrived(2 * j + 1);
+        if (j + 1 < steps) arrived(2 * j + 2);
+        for (uint32_t t = 0; t < 2; ++t) {
+          const uint32_t n = t ? steps1 : steps0;
+          if (j >= n) continue;
+          wait(smem_addr(&sh.p_full[t]), j & 1, late);
+          after_sync();
+          sums(t, 2 * j + 1, j > 0);
+          if (j + 1 < n) scores(t, 2 * j + 2);
+          else commit(smem_addr(&sh.o_full[t]));
+        }
+        // (nothing is signalled after the last products, which the softmax warps wait for)
+        if (j + 1 < steps) {
+          commit(smem_addr(&sh.kv_empty[(2 * j + 1) % kRing]));
+          commit(smem_addr(&sh.kv_empty[(2 * j + 2) % kRing]));
+        }
+      }
+    }
+   }
+  } else {
+    // ---- softmax: a thread has a row of its tile
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const uint32_t t = warp / 4, row = tid % 128, lanes = (warp % 4) * 32 << 16;
+    const Tile x = tile_of(t);
+    const int64_t visible = min((int64_t)rk.count, x.sees + (int64_t)row);  // keys of this row
+    float m = -INFINITY, l = 0.f;
+    for (uint32_t j = 0; j < x.steps; ++j) {
+      float s[kKeys];
+      wait(smem_addr(&sh.s_full[t]), j & 1, late);
+      after_sync();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tmem_load(s_at(t) + lanes + i * 32, s + i * 32);
+      tmem_loaded();
+      const int64_t rest = visible - (int64_t)j * kKeys;
+      const int seen = (int)max((int64_t)0, min((int64_t)kKeys, rest));
+      if (__any_sync(~0u, seen < kKeys)) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i)
+          if (i >= seen) s[i] = -INFINITY;
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i) top = fmaxf(top, s[i]);
+      const bool follow = (top - m) * a.scale2 > kLag;  // also the first maximum
+      if (__any_sync(~0u, follow)) {
+        float to = 1.f;
+        if (follow) {
+          to = m == -INFINITY ? 0.f : ex2((m - top) * a.scale2);
+          m = top;
+        }
+        __syncwarp();
+        l *= to;
+        if (j) {  // S_t is complete, and so is P_t V before it
+#pragma unroll
+          for (int i = 0; i < kDim / 32; ++i) {
+            float o[32];
+            tmem_load(o_at(t) + lanes + i * 32, o);
+            tmem_loaded();
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] *= to;
+            tmem_store(o_at(t) + lanes + i * 32, reinterpret_cast<const uint32_t*>(o));
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m * a.scale2;
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t p[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float u = ex2(fmaf(s[h * 64 + 2 * i], a.scale2, -base));
+          const float w = ex2(fmaf(s[h * 64 + 2 * i + 1], a.scale2, -base));
+          sum0 += u;
+          sum1 += w;
+          p[i] = pack16<kBf16>(u, w);
+        }
+        tmem_store(s_at(t) + lanes + h * 32, p);
+      }
+      l += sum0 + sum1;
+      tmem_stored();
+      before_sync();
+      bar_arrive(smem_addr(&sh.p_full[t]));
+    }
+    // ---- the row's output
+    const bool mine = row < x.rows;
+    const uint64_t at = rq.first + x.row + row;
+    if (x.steps) {
+      wait(smem_addr(&sh.o_full[t]), 0, late);
+      after_sync();
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < kDim / 32; ++i) {
+      float o[32];
+      __syncwarp();
+      if (x.steps) {
+        tmem_load(o_at(t) + lanes + i * 32, o);
+        tmem_loaded();
+      }
+      if (mine) {
+        uint4* dst = reinterpret_cast<uint4*>(
+            a.out + (at * a.out_stride + (uint64_t)x.head * kDim + i * 32) * 2);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          uint32_t w[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+            w[z] = x.steps && l != 0.f ? pack16<kBf16>(o[y * 8 + z * 2] * inv, o[y * 8 + z * 2 + 1] * inv) : 0u;
+          dst[y] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+    if (mine && a.lse)
+      a.lse[at * a.heads + x.head] = l == 0.f ? -INFINITY : m * a.scale2 * kLn2 + logf(l);
+    before_sync();
+  }
+  __syncthreads();
+  if (warp == 0) {
+    if (*late) {  // what is still in flight gets a moment to end
+      const long long t0 = clock64();
+      while (clock64() - t0 < 20000000ll) {
+      }
+    }
+    __syncwarp();
+    after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
+  }
+}
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                            const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                            CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                            CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static const Encode found = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (Encode)p;
+  }();
+  return found;
+}
+
+// Rows of heads * dim values as boxes of 128 rows by 64 values of one head.
+bool row_map(CUtensorMap* map, bool bf16, const void* p, uint64_t stride, uint32_t heads,
+             uint32_t dim, uint64_t rows) {
+  const cuuint64_t dims[3] = {dim, heads, rows ? rows : 1};
+  const cuuint64_t strides[2] = {dim * 2ull, stride * 2};
+  const cuuint32_t box[3] = {64, 1, 128}, step[3] = {1, 1, 1};
+  return encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                   const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -93,15 +518,44 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
       !d_q_off || !d_k_off || !aligned_to(d_q_off, 8) || !aligned_to(d_k_off, 8) ||
       !aligned_to(d_lse, 4) || !aligned_to(d_status, 4))
     return NETKV_EINVAL;
-  const PromptArgs a = {(const unsigned char*)d_q, (const unsigned char*)d_k,
-                        (const unsigned char*)d_v, (unsigned char*)d_out, q_stride, k_stride,
-                        v_stride, out_stride, d_q_off, d_k_off, q_rows, k_rows, heads,
-                        heads / kv_heads, n_seqs, scale, d_lse, d_status};
-  auto go = [&](auto kernel) {
-    kernel<<<dim3((unsigned)((q_rows + 7) / 8), heads), 256, 0, (cudaStream_t)stream>>>(a);
-  };
+  PromptArgs a = {};
+  a.out = (unsigned char*)d_out;
+  a.out_stride = out_stride;
+  a.q_off = d_q_off;
+  a.k_off = d_k_off;
+  a.q_rows = q_rows;
+  a.k_rows = k_rows;
+  a.heads = heads;
+  a.group = heads / kv_heads;
+  a.n_seqs = n_seqs;
+  a.head_pairs = a.group % 2 == 0;
+  a.scale2 = scale * kLog2e;
+  a.lse = d_lse;
+  a.status = d_status;
+  const uint64_t block_rows = a.head_pairs ? 128 : 256;
+  // a sequence ends at most one tile that it does not fill
+  const uint64_t tiles = q_rows / block_rows + n_seqs, grid = tiles * (a.head_pairs ? heads / 2 : heads);
+  if (grid >> 31) return NETKV_EINVAL;
+  a.tiles = (uint32_t)tiles;
+  if (!encoder()) return NETKV_ECUDA;
   const bool bf = dtype == NETKV_BF16;
-  if (head_dim == 64) go(bf ? prompt_kernel<64, true> : prompt_kernel<64, false>);
-  else go(bf ? prompt_kernel<128, true> : prompt_kernel<128, false>);
-  return netkv_launch_status();
+  CUtensorMap q, k, v;
+  if (!row_map(&q, bf, d_q, q_stride, heads, head_dim, q_rows) ||
+      !row_map(&k, bf, k_rows ? d_k : d_q, k_rows ? k_stride : q_stride, k_rows ? kv_heads : 1,
+               head_dim, k_rows) ||
+      !row_map(&v, bf, k_rows ? d_v : d_q, k_rows ? v_stride : q_stride, k_rows ? kv_heads : 1,
+               head_dim, k_rows))
+    return NETKV_EINVAL;
+  auto go = [&](auto kernel, size_t bytes) -> netkv_status {
+    // a launch with fewer registers than the warps share out would never end
+    cudaFuncAttributes has;
+    NETKV_CUDA_TRY(cudaFuncGetAttributes(&has, kernel));
+    if (has.numRegs < kLaunchRegs) return NETKV_ECUDA;
+    NETKV_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    kernel<<<(unsigned)grid, kThreads, bytes, (cudaStream_t)stream>>>(a, q, k, v);
+    return netkv_launch_status();
+  };
+  if (head_dim == 64)
+    return go(bf ? prompt_kernel<64, true> : prompt_kernel<64, false>, sizeof(Shared<64>));
+  return go(bf ? prompt_kernel<128, true> : prompt_kernel<128, false>, sizeof(Shared<128>));
 }
