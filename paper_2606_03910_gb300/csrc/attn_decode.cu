@@ -23,9 +23,14 @@
 
 namespace {
 
-constexpr uint32_t kCtas = 304;     // two blocks an SM on 152 SMs
 constexpr uint32_t kWarps = 4;
-constexpr uint32_t kStages = 4;     // pages in flight a warp
+// Blocks of the grid: three an SM on 152 SMs, two where the sums of two tiles leave no room for
+// a third; and pages in flight a warp, 12 KB or 16 KB of them.
+template <int kTiles>
+constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
+constexpr uint32_t kMostCtas = 456;
+template <int kDim, int kTiles>
+constexpr uint32_t kStages = (kTiles == 1 ? 3 : 4) * (128 / kDim);
 constexpr uint32_t kMinPages = 8;   // a block's run at least: two pages a warp
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
@@ -44,10 +49,11 @@ struct DecodeArgs {
   float* lse;
   const float* mass_in;
   float* mass_out;
-  float* part_o;    // [kCtas][2][kTiles * 8][kDim]
-  float* part_ml;   // [kCtas][2][kTiles * 8][2]
+  float* part_o;    // [ctas][2][kTiles * 8][kDim]
+  float* part_ml;   // [ctas][2][kTiles * 8][2]
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
+  uint32_t ctas;
   int* status;
 };
 
@@ -55,6 +61,19 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A kernel that follows another of the same call starts while that one ends: what it reads of
+// the call's own it reads after follow().
+__device__ __forceinline__ void follow() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_follow() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 __device__ __forceinline__ uint32_t pages_of(const DecodeArgs& a, uint32_t seq) {
@@ -80,7 +99,7 @@ __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, uint32_t units) {
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
   r.total = sum * units;
-  r.ctas = (uint32_t)min((uint64_t)kCtas, max((uint64_t)1, r.total / kMinPages));
+  r.ctas = (uint32_t)min((uint64_t)a.ctas, max((uint64_t)1, r.total / kMinPages));
   return r;
 }
 
@@ -176,24 +195,27 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {
 template <int kDim, int kTiles>
 struct Shared {
   static constexpr int kHeads = kTiles * 8;
+  static constexpr uint32_t kRing = kStages<kDim, kTiles>;
   static constexpr int kGroupFloats = 16 * kHeads + 8;  // of 16 dims; the 8 spread the banks
-  alignas(128) unsigned char ring[kWarps][kStages][2][kBlockTokens * kDim];
+  alignas(128) unsigned char ring[kWarps][kRing][2][kBlockTokens * kDim];
   float o[kWarps][kDim / 16 * kGroupFloats];
   float m[kWarps][kHeads], l[kWarps][kHeads];
-  alignas(8) uint64_t full[kWarps][kStages];
+  alignas(8) uint64_t full[kWarps][kRing];
 };
 
 template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
     decode_kernel(const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   using Sh = Shared<kDim, kTiles>;
   Sh& sh = *reinterpret_cast<Sh*>(smem);
   constexpr int kHeads = kTiles * 8, kSteps = kDim / 16, kPart = kBlockTokens * kDim;
+  constexpr uint32_t kRing = Sh::kRing;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, r = lane / 4, c = lane % 4;
   const uint32_t units = a.kv.heads * a.chunks;
+  let_follow();
 
-  if (lane < kStages)
+  if (lane < kRing)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&sh.full[warp][lane]))
                  : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -240,7 +262,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   auto issue = [&](uint32_t k) {  // the k-th page of the segment into the ring
     const int32_t p = __shfl_sync(~0u, k / 32 == batch ? page0 : page1, k % 32);
     if (lane == 0) {
-      const uint32_t st = issued % kStages, bar = smem_addr(&sh.full[warp][st]);
+      const uint32_t st = issued % kRing, bar = smem_addr(&sh.full[warp][st]);
       if (p >= 0) {
         const uint64_t at = ((uint64_t)p * a.kv.heads + kv_head) * kPart;
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
@@ -273,7 +295,7 @@ __global__ void __launch_bounds__(kWarps * 32)
     page2 = page_at(64 + lane);
     scales(page0, &ks0, &vs0);
     scales(page1, &ks1, &vs1);
-    for (uint32_t k = 0; k < mine && k < kStages; ++k) issue(k);
+    for (uint32_t k = 0; k < mine && k < kRing; ++k) issue(k);
   };
 
   begin(next);
@@ -330,8 +352,8 @@ __global__ void __launch_bounds__(kWarps * 32)
         scales(page1, &ks1, &vs1);
         page2 = page_at((batch + 2) * 32 + lane);
       }
-      const uint32_t st = taken % kStages, bar = smem_addr(&sh.full[warp][st]);
-      if (!wait(bar, (taken / kStages) & 1, late)) late = true;
+      const uint32_t st = taken % kRing, bar = smem_addr(&sh.full[warp][st]);
+      if (!wait(bar, (taken / kRing) & 1, late)) late = true;
       ++taken;
       const int32_t page = __shfl_sync(~0u, page0, k % 32);
       if (page >= 0) {
@@ -363,7 +385,8 @@ __global__ void __launch_bounds__(kWarps * 32)
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            s[t][i] = r + (i / 2) * 8 < valid ? s[t][i] * (ks * f[t][i & 1]) : -INFINITY;
+            s[t][i] *= ks * f[t][i & 1];
+            if (valid < kBlockTokens && r + (i / 2) * 8 >= valid) s[t][i] = -INFINITY;
             above |= s[t][i] > m[t][i & 1] + kLag;
           }
         if (__any_sync(~0u, above)) {
@@ -406,17 +429,16 @@ __global__ void __launch_bounds__(kWarps * 32)
           for (int i = 0; i < 4; ++i) x[i] = ex2(s[t][i] - m[t][i & 1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) l[t][j] += x[j] + x[j + 2];
-          if (kMass) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float sum = x[j] + x[j + 2];
-#pragma unroll
-              for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
-              const uint32_t h = head0 + t * 8 + 2 * c + j;
-              if (r == 0 && h < a.group)
-                a.block2[((uint64_t)seg.seq * a.width + block) * a.heads + kv_head * a.group + h] =
-                    m[t][j] + log2f(sum);
-            }
+          if (kMass) {  // over the tokens: odd threads r take head 2 c + 1, even ones 2 c
+            const float sum0 = x[0] + x[2], sum1 = x[1] + x[3];
+            float sum = r & 1 ? sum1 : sum0;
+            sum += __shfl_xor_sync(~0u, r & 1 ? sum0 : sum1, 4);
+            sum += __shfl_xor_sync(~0u, sum, 8);
+            sum += __shfl_xor_sync(~0u, sum, 16);
+            const uint32_t h = head0 + t * 8 + 2 * c + r;
+            if (r < 2 && h < a.group)
+              a.block2[((uint64_t)seg.seq * a.width + block) * a.heads + kv_head * a.group + h] =
+                  (r & 1 ? m[t][1] : m[t][0]) + lg2(sum);
           }
           p[t][0] = transpose8x8(pack16<false>(x[0] * w, x[1] * w));
           p[t][1] = transpose8x8(pack16<false>(x[2] * w, x[3] * w));
@@ -431,7 +453,7 @@ __global__ void __launch_bounds__(kWarps * 32)
           const uint32_t* src = reinterpret_cast<const uint32_t*>(vp + row * kDim + r * (kDim / 8));
           if (kWords == 4) *reinterpret_cast<uint4*>(v[i]) = *reinterpret_cast<const uint4*>(src);
           else *reinterpret_cast<uint2*>(v[i]) = *reinterpret_cast<const uint2*>(src);
-          if (row >= valid) {
+          if (valid < kBlockTokens && row >= valid) {
 #pragma unroll
             for (int j = 0; j < kWords; ++j) v[i][j] = 0;
           }
@@ -458,7 +480,7 @@ __global__ void __launch_bounds__(kWarps * 32)
         }
       }
       __syncwarp();
-      if (k + kStages < mine) issue(k + kStages);
+      if (k + kRing < mine) issue(k + kRing);
     }
 
     // ---- the warps' sums
@@ -542,11 +564,17 @@ __global__ void __launch_bounds__(kWarps * 32)
 }
 
 // Joins the segments that runs share: one block a (boundary between runs, head of the unit),
-// where the boundary is the first inside its segment.
+// where the boundary is the first inside its segment.  The parts' weights first, then eight
+// groups of threads (a thread has four dims) over every eighth part: a long sequence alone on
+// the card has a part from each run, 456 for one unit.
+constexpr uint32_t kJoin = 256;
 template <int kDim, int kTiles, bool kBf16, bool kMass>
-__global__ void __launch_bounds__(kDim) join_kernel(const __grid_constant__ DecodeArgs a) {
-  constexpr int kHeads = kTiles * 8;
-  const uint32_t units = a.kv.heads * a.chunks, dim = threadIdx.x, h = blockIdx.y;
+__global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ DecodeArgs a) {
+  constexpr int kHeads = kTiles * 8, kLanes = kDim / 4, kGroups = kJoin / kLanes;
+  __shared__ float weight[kCtas<kTiles>], reduce[kJoin / 32][2];
+  __shared__ float4 sums[kGroups][kLanes];
+  const uint32_t units = a.kv.heads * a.chunks, tid = threadIdx.x, h = blockIdx.y;
+  let_follow();
   const Runs runs = runs_of(a, units);
   const uint32_t cut = blockIdx.x + 1;
   if (cut >= runs.ctas) return;
@@ -556,22 +584,58 @@ __global__ void __launch_bounds__(kDim) join_kernel(const __grid_constant__ Deco
   const uint32_t head0 = s.unit % a.chunks * kHeads;
   if (head0 + h >= a.group) return;
   const uint64_t end = at + s.pages;
-  float top = -INFINITY, sum = 0.f, all = 0.f;
-  for (uint32_t c = cut - 1; c < runs.ctas && runs.start(c) < end; ++c) {
-    const uint32_t slot = c * 2 + (runs.start(c) >= at ? 0 : 1);
-    const float m = a.part_ml[(slot * kHeads + h) * 2], l = a.part_ml[(slot * kHeads + h) * 2 + 1];
-    const float o = a.part_o[((uint64_t)slot * kHeads + h) * kDim + dim];
-    const float to = fmaxf(top, m);
-    const float x = top == -INFINITY ? 0.f : ex2(top - to), y = m == -INFINITY ? 0.f : ex2(m - to);
-    sum = sum * x + l * y;
-    all = all * x + o * y;
-    top = to;
+  // runs that start before the end, less those before cut - 1
+  const uint32_t parts =
+      (uint32_t)min((uint64_t)runs.ctas, (end * runs.ctas + runs.total - 1) / runs.total) - (cut - 1);
+  const uint32_t second = runs.start(cut - 1) < at;  // the segment is that run's last one
+  auto slot = [&](uint32_t i) {
+    return ((uint64_t)(cut - 1 + i) * 2 + (i == 0 ? second : 0)) * kHeads + h;
+  };
+  follow();
+  float top = -INFINITY, sum = 0.f;
+  for (uint32_t i = tid; i < parts; i += kJoin) top = fmaxf(top, a.part_ml[slot(i) * 2]);
+#pragma unroll
+  for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  if (tid % 32 == 0) reduce[tid / 32][0] = top;
+  __syncthreads();
+  top = reduce[0][0];
+#pragma unroll
+  for (int w = 1; w < (int)kJoin / 32; ++w) top = fmaxf(top, reduce[w][0]);
+  for (uint32_t i = tid; i < parts; i += kJoin) {
+    const float m = a.part_ml[slot(i) * 2], l = a.part_ml[slot(i) * 2 + 1];
+    const float w = m == -INFINITY ? 0.f : ex2(m - top);
+    weight[i] = w;
+    // a part of NaN scores has no maximum, but its sum says so
+    sum += m == -INFINITY && l == l ? 0.f : w * l;
+  }
+#pragma unroll
+  for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+  if (tid % 32 == 0) reduce[tid / 32][1] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < (int)kJoin / 32; ++w) sum += reduce[w][1];
+  const uint32_t lane = tid % kLanes, group = tid / kLanes;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (uint32_t i = group; i < parts; i += kGroups) {
+    const float4 x = reinterpret_cast<const float4*>(a.part_o + slot(i) * kDim)[lane];
+    const float w = weight[i];
+    o.x += w * x.x, o.y += w * x.y, o.z += w * x.z, o.w += w * x.w;
+  }
+  sums[group][lane] = o;
+  __syncthreads();
+  if (group) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) {
+    const float4 x = sums[g][lane];
+    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const uint32_t head = s.unit / a.chunks * a.group + head0 + h;
-  reinterpret_cast<uint16_t*>(a.out)[s.seq * a.out_stride + (uint64_t)head * kDim + dim] =
-      (uint16_t)pack16<kBf16>(all * inv, 0.f);
-  if (dim == 0) {
+  reinterpret_cast<uint2*>(a.out + (s.seq * a.out_stride + (uint64_t)head * kDim) * 2)[lane] =
+      make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
+  if (lane == 0) {
     const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
     if (a.lse) a.lse[(uint64_t)s.seq * a.heads + head] = z * kLn2;
     if (kMass) a.lse2[(uint64_t)s.seq * a.heads + head] = z;
@@ -581,6 +645,7 @@ __global__ void __launch_bounds__(kDim) join_kernel(const __grid_constant__ Deco
 // A block's weight over all heads, in the heads' order: one thread a block.
 __global__ void __launch_bounds__(128) mass_kernel(const __grid_constant__ DecodeArgs a) {
   const uint32_t seq = blockIdx.x, pages = pages_of(a, seq);
+  follow();
   for (uint32_t block = blockIdx.y * 128 + threadIdx.x; block < pages; block += gridDim.y * 128) {
     const uint64_t at = (uint64_t)seq * a.width + block;
     float sum = 0.f;
@@ -590,6 +655,21 @@ __global__ void __launch_bounds__(128) mass_kernel(const __grid_constant__ Decod
     }
     a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum;
   }
+}
+
+template <class Kernel>
+cudaError_t launch_following(Kernel kernel, dim3 grid, unsigned threads, cudaStream_t s,
+                             const DecodeArgs& a) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3(threads);
+  c.stream = s;
+  c.attrs = &early;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, a);
 }
 
 bool sizes_ok(const netkv_kv_pages* pages, uint32_t n_seqs, uint32_t heads, uint32_t width) {
@@ -607,7 +687,7 @@ struct Workspace {
 Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, uint32_t width,
                     bool mass) {
   auto up = [](size_t x) { return (x + 127) / 128 * 128; };
-  const size_t rows = (size_t)kCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
+  const size_t rows = (size_t)kMostCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
   Workspace w;
   w.part_ml = up(rows * p->head_dim * 4);
   w.lse2 = w.part_ml + up(rows * 8);
@@ -666,6 +746,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         (float*)(w + ws.part_ml),
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
+                        per == 8 ? kCtas<1> : kCtas<2>,
                         d_status};
   const cudaStream_t s = (cudaStream_t)stream;
   auto go = [&](auto dim, auto tiles, auto bf, auto e4, auto mass) -> netkv_status {
@@ -674,8 +755,10 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
     constexpr int bytes = (int)sizeof(Shared<kDim, kTiles>);
     NETKV_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    kernel<<<kCtas, kWarps * 32, bytes, s>>>(a);
-    join_kernel<kDim, kTiles, kB, kM><<<dim3(kCtas - 1, min(group, per)), kDim, 0, s>>>(a);
+    kernel<<<kCtas<kTiles>, kWarps * 32, bytes, s>>>(a);
+    if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
+    NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,
+                                    dim3(kCtas<kTiles> - 1, min(group, per)), kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
@@ -697,6 +780,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                                    : widths(std::integral_constant<int, 2>());
   if (st != NETKV_OK) return st;
   if (d_mass_out)
-    mass_kernel<<<dim3(n_seqs, min((table_width + 127) / 128, 1024u)), 128, 0, s>>>(a);
+    NETKV_CUDA_TRY(launch_following(mass_kernel, dim3(n_seqs, min((table_width + 127) / 128, 1024u)),
+                                    128, s, a));
   return netkv_launch_status();
 }
