@@ -24,13 +24,10 @@
 namespace {
 
 constexpr uint32_t kWarps = 4;
-// Blocks of the grid: three an SM on 152 SMs, two where the sums of two tiles leave no room for
-// a third; and pages in flight a warp, 12 KB or 16 KB of them.
-template <int kTiles>
-constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
-constexpr uint32_t kMostCtas = 456;
-template <int kDim, int kTiles>
-constexpr uint32_t kStages = (kTiles == 1 ? 3 : 4) * (128 / kDim);
+constexpr uint32_t kThreads = kWarps * 32 + 32;  // and a warp for the loads
+constexpr uint32_t kCtas = 304;     // two blocks an SM on 152 SMs
+template <int kDim>
+constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
 constexpr uint32_t kMinPages = 8;   // a block's run at least: two pages a warp
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
@@ -49,11 +46,10 @@ struct DecodeArgs {
   float* lse;
   const float* mass_in;
   float* mass_out;
-  float* part_o;    // [ctas][2][kTiles * 8][kDim]
-  float* part_ml;   // [ctas][2][kTiles * 8][2]
+  float* part_o;    // [kCtas][2][kTiles * 8][kDim]
+  float* part_ml;   // [kCtas][2][kTiles * 8][2]
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
-  uint32_t ctas;
   int* status;
 };
 
@@ -99,7 +95,7 @@ __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, uint32_t units) {
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
   r.total = sum * units;
-  r.ctas = (uint32_t)min((uint64_t)a.ctas, max((uint64_t)1, r.total / kMinPages));
+  r.ctas = (uint32_t)min((uint64_t)kCtas, max((uint64_t)1, r.total / kMinPages));
   return r;
 }
 
@@ -147,13 +143,19 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 
-// Waits for a phase of a barrier, a second at most (a hundredth once that has run out).
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, bool late) {
-  if (try_wait(bar, parity)) return true;
+// Waits for a phase of a barrier, a second at most (a hundredth once that has run out for a
+// thread of the block).
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
+  if (try_wait(bar, parity)) return;
   const long long t0 = clock64();
   while (!try_wait(bar, parity))
-    if (clock64() - t0 > (late ? 20000000ll : 2000000000ll)) return false;
-  return true;
+    if (clock64() - t0 > (*late ? 20000000ll : 2000000000ll)) {
+      *late = 1;
+      return;
+    }
+}
+__device__ __forceinline__ void sync_warps() {  // all but the loading one
+  asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
 }
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
@@ -195,17 +197,140 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {
 template <int kDim, int kTiles>
 struct Shared {
   static constexpr int kHeads = kTiles * 8;
-  static constexpr uint32_t kRing = kStages<kDim, kTiles>;
+  static constexpr uint32_t kRing = kStages<kDim>;
   static constexpr int kGroupFloats = 16 * kHeads + 8;  // of 16 dims; the 8 spread the banks
-  alignas(128) unsigned char ring[kWarps][kRing][2][kBlockTokens * kDim];
+  alignas(128) unsigned char ring[kWarps][kRing][2][2][kBlockTokens * kDim];
   float o[kWarps][kDim / 16 * kGroupFloats];
   float m[kWarps][kHeads], l[kWarps][kHeads];
-  alignas(8) uint64_t full[kWarps][kRing];
+  alignas(16) float2 scale[kWarps][kRing][2];  // of keys and values
+  uint2 tokens[kWarps][kRing];                 // of each page; 0 where it is absent
+  alignas(8) uint64_t full[kWarps][kRing], empty[kWarps][kRing];
+  int late;
 };
 
+// The segments of one run, in order.
+struct Walk {
+  Segment s;
+  uint64_t left;  // pages from s on
+  __device__ __forceinline__ void start(const DecodeArgs& a, uint32_t units, const Runs& runs) {
+    const uint64_t first = runs.start(blockIdx.x);
+    left = runs.start(blockIdx.x + 1) - first;
+    if (left == 0) return;
+    s = segment_at(a, units, first);
+    s.count = (uint32_t)min((uint64_t)(s.pages - s.first), left);
+  }
+  __device__ __forceinline__ void next(const DecodeArgs& a, uint32_t units) {
+    left -= s.count;
+    if (left == 0) return;
+    s.first = 0;
+    if (++s.unit == units) {
+      s.unit = 0;
+      do {
+        ++s.seq;
+        s.pages = s.seq < a.n_seqs ? pages_of(a, s.seq) : 1;
+      } while (s.pages == 0);
+      if (s.seq >= a.n_seqs) left = 0;  // lengths that changed under the call
+    }
+    s.count = (uint32_t)min((uint64_t)s.pages, left);
+  }
+};
+
+// 32 pages on their way into the ring: lane j has page j, counted from the 2 * pair-th of a
+// segment's.
+struct Batch {
+  uint32_t count;  // pages; 0: none left
+  uint32_t kv_head, tokens;
+  int32_t page;
+  float2 scale;
+};
+
+// The loading warp: pairs of neighbouring pages, one pair after another to the four warps.  The
+// table's entries are read two batches ahead and the scales one, over the ends of segments too,
+// so that a ring's place is filled as soon as it is free.
+template <int kDim, int kTiles>
+__device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTiles>& sh,
+                                           uint32_t units, const Runs& runs) {
+  constexpr uint32_t kRing = kStages<kDim>, kPart = kBlockTokens * kDim;
+  const uint32_t lane = threadIdx.x & 31;
+  volatile int* late = &sh.late;
+  Walk walk;
+  walk.start(a, units, runs);
+  uint32_t at = 0;  // pages of the present segment that batches have
+  auto take = [&]() {
+    Batch b = {0, 0, 0, -1, make_float2(0.f, 0.f)};
+    if (walk.left && at == walk.s.count) {
+      walk.next(a, units);
+      at = 0;
+    }
+    if (walk.left == 0) return b;
+    b.count = min(walk.s.count - at, 32u);
+    b.kv_head = walk.s.unit / a.chunks;
+    if (lane < b.count) {
+      const uint32_t block = walk.s.first + at + lane;
+      b.page = a.table[(uint64_t)walk.s.seq * a.width + block];
+      b.tokens = min(tokens_of(a, walk.s.seq) - block * kBlockTokens, kBlockTokens);
+    }
+    at += b.count;
+    return b;
+  };
+  auto scales = [&](Batch& b) {
+    if (lane >= b.count) return;
+    if (b.page < 0 || (uint32_t)b.page >= a.kv.n_pages) {
+      flag_status(a.status, NETKV_DEV_ERANGE);
+      b.page = -1;
+      b.tokens = 0;
+      return;
+    }
+    const uint64_t part = (uint64_t)b.page * a.kv.heads + b.kv_head;
+    b.scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
+  };
+  uint32_t given[kWarps] = {};  // pairs that each warp was given
+  Batch b0 = take(), b1 = take();
+  scales(b0);
+  scales(b1);
+  while (b0.count) {
+    const Batch b2 = take();
+    const uint32_t w = lane / 2 % kWarps, pairs = (b0.count + 1) / 2;
+    uint32_t n = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kWarps; ++i)
+      if (i == w) n = given[i];
+    n += lane / 2 / kWarps;
+    for (uint32_t q = 0; q < 32 / (2 * kWarps); ++q) {  // a pair for each warp
+      if (lane / (2 * kWarps) == q && lane / 2 < pairs) {
+        const uint32_t st = n % kRing, bar = smem_addr(&sh.full[w][st]);
+        if (n >= kRing) wait(smem_addr(&sh.empty[w][st]), (n / kRing - 1) & 1, late);
+        if (b0.page >= 0) {
+          const uint64_t from = ((uint64_t)b0.page * a.kv.heads + b0.kv_head) * kPart;
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+              "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][0])),
+              "l"(a.kv.k + from), "r"(kPart), "r"(bar)
+              : "memory");
+          asm volatile(
+              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+              "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][1])),
+              "l"(a.kv.v + from), "r"(kPart), "r"(bar)
+              : "memory");
+        }
+        sh.scale[w][st][lane & 1] = b0.scale;
+        (&sh.tokens[w][st].x)[lane & 1] = b0.tokens;
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                     "r"(b0.page >= 0 ? 2 * kPart : 0)
+                     : "memory");
+      }
+      __syncwarp();
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kWarps; ++i) given[i] += (pairs + kWarps - 1 - i) / kWarps;
+    b0 = b1;
+    b1 = b2;
+    scales(b1);
+  }
+}
+
 template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass>
-__global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
-    decode_kernel(const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) decode_kernel(const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   using Sh = Shared<kDim, kTiles>;
   Sh& sh = *reinterpret_cast<Sh*>(smem);
@@ -215,107 +340,53 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
   const uint32_t units = a.kv.heads * a.chunks;
   let_follow();
 
-  if (lane < kRing)
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&sh.full[warp][lane]))
+  if (warp < kWarps && lane < kRing) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 2;" ::"r"(smem_addr(&sh.full[warp][lane]))
                  : "memory");
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  __syncwarp();
-
-  // rows of sequences without tokens, and lengths past the table
-  for (uint32_t i = blockIdx.x; i < a.n_seqs; i += gridDim.x) {
-    const uint32_t n = a.len[i];
-    if (tid == 0 && n > (uint64_t)a.width * kBlockTokens) flag_status(a.status, NETKV_DEV_ERANGE);
-    if (n) continue;
-    for (uint32_t x = tid; x < a.heads * kDim / 8; x += kWarps * 32)
-      reinterpret_cast<uint4*>(a.out + i * a.out_stride * 2)[x] = make_uint4(0, 0, 0, 0);
-    for (uint32_t h = tid; h < a.heads && a.lse; h += kWarps * 32)
-      a.lse[(uint64_t)i * a.heads + h] = -INFINITY;
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(&sh.empty[warp][lane]))
+                 : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-
+  if (tid == 0) sh.late = 0;
   const Runs runs = runs_of(a, units);
-  if (blockIdx.x >= runs.ctas) return;
-  uint64_t left = runs.start(blockIdx.x + 1) - runs.start(blockIdx.x);
-  if (left == 0) return;
-  Segment next = segment_at(a, units, runs.start(blockIdx.x));
-  next.count = (uint32_t)min((uint64_t)(next.pages - next.first), left);
+  __syncthreads();
+  volatile int* late = &sh.late;
+  if (warp == kWarps) {
+    if (blockIdx.x < runs.ctas) load_pages<kDim, kTiles>(a, sh, units, runs);
+    return;
+  }
+  Walk walk;
+  walk.left = 0;
+  if (blockIdx.x < runs.ctas) walk.start(a, units, runs);
 
-  // A warp's pages of a segment are numbered k = 0, 1, ...: block first + warp + 4 k.  Lane j
-  // keeps the page numbers of k = j, 32 + j and 64 + j past the present 32 and the scales of
-  // the first two, so that neither is waited for in a long segment.
-  uint32_t issued = 0, taken = 0;  // pages of all segments
-  uint32_t mine = 0, kv_head = 0, head0 = 0, batch = 0;
-  int32_t page0 = -1, page1 = -1, page2 = -1;
-  float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
-  Segment seg = next;
-  auto page_at = [&](uint32_t k) -> int32_t {
-    if (k >= mine) return -1;
-    const int32_t p = a.table[(uint64_t)seg.seq * a.width + seg.first + warp + kWarps * k];
-    if (p >= 0 && (uint32_t)p < a.kv.n_pages) return p;
-    flag_status(a.status, NETKV_DEV_ERANGE);
-    return -1;
-  };
-  auto scales = [&](int32_t p, float* ks, float* vs) {
-    const uint64_t at = (uint64_t)(p < 0 ? 0 : p) * a.kv.heads + kv_head;
-    *ks = a.kv.k_scale[at];
-    *vs = a.kv.v_scale[at];
-  };
-  auto issue = [&](uint32_t k) {  // the k-th page of the segment into the ring
-    const int32_t p = __shfl_sync(~0u, k / 32 == batch ? page0 : page1, k % 32);
-    if (lane == 0) {
-      const uint32_t st = issued % kRing, bar = smem_addr(&sh.full[warp][st]);
-      if (p >= 0) {
-        const uint64_t at = ((uint64_t)p * a.kv.heads + kv_head) * kPart;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
-                     "r"(2 * kPart)
-                     : "memory");
-        asm volatile(
-            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-            "[%3];" ::"r"(smem_addr(sh.ring[warp][st][0])),
-            "l"(a.kv.k + at), "r"(kPart), "r"(bar)
-            : "memory");
-        asm volatile(
-            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-            "[%3];" ::"r"(smem_addr(sh.ring[warp][st][1])),
-            "l"(a.kv.v + at), "r"(kPart), "r"(bar)
-            : "memory");
-      } else {  // an absent page keeps its place in the ring
-        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-      }
+  // Queries of a segment: thread (r, c) has head r of each tile, dims by 16 bytes of codes:
+  // 64 h + 16 c + 4 i + 0..3 in step 4 h + i.  Read ahead of their segment.
+  uint4 raw[kTiles][kDim / 32];
+  auto load_queries = [&]() {
+    const uint32_t kv_head = walk.s.unit / a.chunks, head0 = walk.s.unit % a.chunks * kHeads;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const uint32_t h = head0 + t * 8 + r;
+      const uint4* src = reinterpret_cast<const uint4*>(
+          a.q + (walk.s.seq * a.q_stride + ((uint64_t)kv_head * a.group + min(h, a.group - 1)) * kDim) * 2);
+#pragma unroll
+      for (int i = 0; i < kDim / 32; ++i)
+        raw[t][i] = h < a.group ? src[(i / 2) * 8 + c * 2 + i % 2] : make_uint4(0, 0, 0, 0);
     }
-    ++issued;
   };
-  auto begin = [&](const Segment& s) {
-    seg = s;
-    mine = s.count > warp ? (s.count - warp + kWarps - 1) / kWarps : 0;
-    kv_head = s.unit / a.chunks;
-    head0 = s.unit % a.chunks * kHeads;
-    batch = 0;
-    page0 = page_at(lane);
-    page1 = page_at(32 + lane);
-    page2 = page_at(64 + lane);
-    scales(page0, &ks0, &vs0);
-    scales(page1, &ks1, &vs1);
-    for (uint32_t k = 0; k < mine && k < kRing; ++k) issue(k);
-  };
-
-  begin(next);
-  bool first_segment = true, late = false;
-  while (true) {
-    // ---- queries of the segment: thread (r, c) has head r of each tile, dims by 16 bytes of
-    // codes: 64 h + 16 c + 4 i + 0..3 in step 4 h + i
+  if (walk.left) load_queries();
+  uint32_t taken = 0;  // pairs of all segments
+  bool first_segment = true;
+  while (walk.left) {
+    const Segment seg = walk.s;
+    const uint32_t kv_head = seg.unit / a.chunks, head0 = seg.unit % a.chunks * kHeads;
+    const uint32_t all_pairs = (seg.count + 1) / 2;
+    const uint32_t pairs = all_pairs > warp ? (all_pairs - warp + kWarps - 1) / kWarps : 0;
     uint32_t q[kTiles][kSteps][2];
     float f[kTiles][2];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const uint32_t h = head0 + t * 8 + r;
-      const bool real = h < a.group;
-      uint4 raw[kDim / 32];
-      const uint4* src = reinterpret_cast<const uint4*>(
-          a.q + (seg.seq * a.q_stride + ((uint64_t)kv_head * a.group + (real ? h : 0)) * kDim) * 2);
-#pragma unroll
-      for (int i = 0; i < kDim / 32; ++i)
-        raw[i] = real ? src[(i / 2) * 8 + c * 2 + i % 2] : make_uint4(0, 0, 0, 0);
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(raw);
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(raw[t]);
       float largest = 0.f;
 #pragma unroll
       for (int i = 0; i < kDim / 8; ++i) {
@@ -342,60 +413,60 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) m[t][0] = m[t][1] = -INFINITY;
     float v_unit = 0.f, v_inv = 0.f;  // a power of two that the value scales are taken by
-    const uint32_t tokens = tokens_of(a, seg.seq);
 
-    for (uint32_t k = 0; k < mine; ++k) {
-      if (k / 32 != batch) {
-        batch = k / 32;
-        page0 = page1, page1 = page2;
-        ks0 = ks1, vs0 = vs1;
-        scales(page1, &ks1, &vs1);
-        page2 = page_at((batch + 2) * 32 + lane);
-      }
-      const uint32_t st = taken % kRing, bar = smem_addr(&sh.full[warp][st]);
-      if (!wait(bar, (taken / kRing) & 1, late)) late = true;
+    for (uint32_t i = 0; i < pairs; ++i) {
+      const uint32_t st = taken % kRing;
+      wait(smem_addr(&sh.full[warp][st]), (taken / kRing) & 1, late);
       ++taken;
-      const int32_t page = __shfl_sync(~0u, page0, k % 32);
-      if (page >= 0) {
-        const float ks = __shfl_sync(~0u, ks0, k % 32), vs = __shfl_sync(~0u, vs0, k % 32);
-        const uint32_t block = seg.first + warp + kWarps * k, t0 = block * kBlockTokens;
-        const uint32_t valid = min(tokens - t0, kBlockTokens);
-        const unsigned char* kp = sh.ring[warp][st][0];
-        const unsigned char* vp = sh.ring[warp][st][1];
+      const uint32_t at = 2 * (warp + kWarps * i), block = seg.first + at;
+      const uint2 nn = sh.tokens[warp][st];
+      const uint32_t n[2] = {nn.x, nn.y};
+      const bool full = n[0] + n[1] == 2 * kBlockTokens;
+      if (n[0] + n[1]) {
+        const float4 sc = *reinterpret_cast<const float4*>(sh.scale[warp][st]);
+        const float ks[2] = {sc.x, sc.z}, vs[2] = {sc.y, sc.w};
+        const unsigned char(*pg)[2][kPart] = sh.ring[warp][st];
 
-        float s[kTiles][4] = {};
+        float s[2][kTiles][4] = {};
 #pragma unroll
-        for (int h = 0; h < kDim / 64; ++h) {
-          const uint4 x = *reinterpret_cast<const uint4*>(kp + r * kDim + h * 64 + c * 16);
-          const uint4 y = *reinterpret_cast<const uint4*>(kp + (r + 8) * kDim + h * 64 + c * 16);
-          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+        for (int h = 0; h < kDim / 64; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t a0, a1, a2, a3;
-            widen<kE4m3>(xs[i], &a0, &a2);
-            widen<kE4m3>(ys[i], &a1, &a3);
+          for (int g = 0; g < 2; ++g) {
+            const unsigned char* kp = pg[g][0] + h * 64 + c * 16;
+            const uint4 x = *reinterpret_cast<const uint4*>(kp + r * kDim);
+            const uint4 y = *reinterpret_cast<const uint4*>(kp + (r + 8) * kDim);
+            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-              mma(s[t], a0, a1, a2, a3, q[t][h * 4 + i][0], q[t][h * 4 + i][1]);
+            for (int z = 0; z < 4; ++z) {
+              uint32_t a0, a1, a2, a3;
+              widen<kE4m3>(xs[z], &a0, &a2);
+              widen<kE4m3>(ys[z], &a1, &a3);
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t)
+                mma(s[g][t], a0, a1, a2, a3, q[t][h * 4 + z][0], q[t][h * 4 + z][1]);
+            }
           }
-        }
-        // s: tokens r and r + 8, heads 2 c and 2 c + 1 of each tile
+        // s: tokens r and r + 8 of a page, heads 2 c and 2 c + 1 of each tile
         bool above = false;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[t][i] *= ks * f[t][i & 1];
-            if (valid < kBlockTokens && r + (i / 2) * 8 >= valid) s[t][i] = -INFINITY;
-            above |= s[t][i] > m[t][i & 1] + kLag;
-          }
+          for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              s[g][t][z] *= ks[g] * f[t][z & 1];
+              if (!full && r + (z / 2) * 8 >= n[g]) s[g][t][z] = -INFINITY;
+              above |= s[g][t][z] > m[t][z & 1] + kLag;
+            }
         if (__any_sync(~0u, above)) {
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) {
             float to[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              float x = fmaxf(m[t][j], fmaxf(s[t][j], s[t][j + 2]));
+              float x = m[t][j];
+#pragma unroll
+              for (int g = 0; g < 2; ++g) x = fmaxf(x, fmaxf(s[g][t][j], s[g][t][j + 2]));
 #pragma unroll
               for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
               to[j] = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - x);
@@ -405,88 +476,101 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
 #pragma unroll
             for (int j = 0; j < kDim / 16; ++j)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[t][j][i] *= to[i & 1];
+              for (int z = 0; z < 4; ++z) o[t][j][z] *= to[z & 1];
           }
         }
-        if (vs > v_unit) {  // the whole warp; values of other blocks stay within fp16's range
-          const uint32_t e = min(max(__float_as_uint(vs) >> 23, 2u), 252u);
+        if (fmaxf(vs[0], vs[1]) > v_unit) {  // the whole warp
+          const uint32_t e = min(max(__float_as_uint(fmaxf(vs[0], vs[1])) >> 23, 2u), 252u);
           const float unit = __uint_as_float((e + 1) << 23), shrink = v_unit / unit;
 #pragma unroll
           for (int t = 0; t < kTiles; ++t)
 #pragma unroll
             for (int j = 0; j < kDim / 16; ++j)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[t][j][i] *= shrink;
+              for (int z = 0; z < 4; ++z) o[t][j][z] *= shrink;
           v_unit = unit;
           v_inv = __uint_as_float((253 - e) << 23);
         }
-        const float w = vs * v_inv;
-        uint32_t p[kTiles][2];
+        uint32_t p[2][kTiles][2];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          float x[4];
+        for (int g = 0; g < 2; ++g) {
+          const float w = vs[g] * v_inv;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = ex2(s[t][i] - m[t][i & 1]);
+          for (int t = 0; t < kTiles; ++t) {
+            float x[4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) l[t][j] += x[j] + x[j + 2];
-          if (kMass) {  // over the tokens: odd threads r take head 2 c + 1, even ones 2 c
-            const float sum0 = x[0] + x[2], sum1 = x[1] + x[3];
-            float sum = r & 1 ? sum1 : sum0;
-            sum += __shfl_xor_sync(~0u, r & 1 ? sum0 : sum1, 4);
-            sum += __shfl_xor_sync(~0u, sum, 8);
-            sum += __shfl_xor_sync(~0u, sum, 16);
-            const uint32_t h = head0 + t * 8 + 2 * c + r;
-            if (r < 2 && h < a.group)
-              a.block2[((uint64_t)seg.seq * a.width + block) * a.heads + kv_head * a.group + h] =
-                  (r & 1 ? m[t][1] : m[t][0]) + lg2(sum);
+            for (int z = 0; z < 4; ++z) x[z] = ex2(s[g][t][z] - m[t][z & 1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) l[t][j] += x[j] + x[j + 2];
+            if (kMass) {  // over the tokens: odd threads r take head 2 c + 1, even ones 2 c
+              const float sum0 = x[0] + x[2], sum1 = x[1] + x[3];
+              float sum = r & 1 ? sum1 : sum0;
+              sum += __shfl_xor_sync(~0u, r & 1 ? sum0 : sum1, 4);
+              sum += __shfl_xor_sync(~0u, sum, 8);
+              sum += __shfl_xor_sync(~0u, sum, 16);
+              const uint32_t h = head0 + t * 8 + 2 * c + r;
+              if (r < 2 && h < a.group && at + g < seg.count)
+                a.block2[((uint64_t)seg.seq * a.width + block + g) * a.heads +
+                         kv_head * a.group + h] = (r & 1 ? m[t][1] : m[t][0]) + lg2(sum);
+            }
+            p[g][t][0] = transpose8x8(pack16<false>(x[0] * w, x[1] * w));
+            p[g][t][1] = transpose8x8(pack16<false>(x[2] * w, x[3] * w));
           }
-          p[t][0] = transpose8x8(pack16<false>(x[0] * w, x[1] * w));
-          p[t][1] = transpose8x8(pack16<false>(x[2] * w, x[3] * w));
         }
         // values: tokens 2 c, 2 c + 1, 2 c + 8 and 2 c + 9, dims r * kDim / 8 on; zeros past
         // the last token, whose codes may stand for anything
         constexpr int kWords = kDim / 32;
-        uint32_t v[4][kWords];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t row = 2 * c + (i & 1) + (i / 2) * 8;
-          const uint32_t* src = reinterpret_cast<const uint32_t*>(vp + row * kDim + r * (kDim / 8));
-          if (kWords == 4) *reinterpret_cast<uint4*>(v[i]) = *reinterpret_cast<const uint4*>(src);
-          else *reinterpret_cast<uint2*>(v[i]) = *reinterpret_cast<const uint2*>(src);
-          if (valid < kBlockTokens && row >= valid) {
+        for (int g = 0; g < 2; ++g) {
+          uint32_t v[4][kWords];
 #pragma unroll
-            for (int j = 0; j < kWords; ++j) v[i][j] = 0;
+          for (int z = 0; z < 4; ++z) {
+            const uint32_t row = 2 * c + (z & 1) + (z / 2) * 8;
+            const unsigned char* src = pg[g][1] + row * kDim + r * (kDim / 8);
+            if (kWords == 4) {
+              const uint4 y = *reinterpret_cast<const uint4*>(src);
+              v[z][0] = y.x, v[z][1] = y.y, v[z][kWords - 2] = y.z, v[z][kWords - 1] = y.w;
+            } else {
+              const uint2 y = *reinterpret_cast<const uint2*>(src);
+              v[z][0] = y.x, v[z][1] = y.y;
+            }
+            if (!full && row >= n[g]) {
+#pragma unroll
+              for (int j = 0; j < kWords; ++j) v[z][j] = 0;
+            }
           }
+#pragma unroll
+          for (int z = 0; z < kWords; ++z)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {  // tile 2 z + j: dims 4 z + 2 j and the next of the run
+              const uint32_t sel = j ? 0x7362 : 0x5140;
+              uint32_t a0, a1, a2, a3;
+              widen<kE4m3>(__byte_perm(v[0][z], v[1][z], sel), &a0, &a1);
+              widen<kE4m3>(__byte_perm(v[2][z], v[3][z], sel), &a2, &a3);
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t)
+                mma(o[t][2 * z + j], a0, a1, a2, a3, p[g][t][0], p[g][t][1]);
+            }
         }
+      } else if (kMass && r < 2) {
 #pragma unroll
-        for (int i = 0; i < kWords; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {  // tile 2 i + j: dims 4 i + 2 j and the next of the run
-            const uint32_t sel = j ? 0x7362 : 0x5140;
-            uint32_t a0, a1, a2, a3;
-            widen<kE4m3>(__byte_perm(v[0][i], v[1][i], sel), &a0, &a1);
-            widen<kE4m3>(__byte_perm(v[2][i], v[3][i], sel), &a2, &a3);
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) mma(o[t][2 * i + j], a0, a1, a2, a3, p[t][0], p[t][1]);
-          }
-      } else if (kMass && r == 0) {
-        const uint32_t block = seg.first + warp + kWarps * k;
-#pragma unroll
-        for (int i = 0; i < kHeads / 4; ++i) {
-          const uint32_t h = head0 + c + i * 4;
-          if (h < a.group)
-            a.block2[((uint64_t)seg.seq * a.width + block) * a.heads + kv_head * a.group + h] =
+        for (int z = 0; z < kHeads / 4; ++z) {
+          const uint32_t h = head0 + c + z * 4;
+          if (h < a.group && at + r < seg.count)
+            a.block2[((uint64_t)seg.seq * a.width + block + r) * a.heads + kv_head * a.group + h] =
                 -INFINITY;
         }
       }
       __syncwarp();
-      if (k + kRing < mine) issue(k + kRing);
+      if (lane == 0)
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&sh.empty[warp][st]))
+                     : "memory");
     }
 
     // ---- the warps' sums
-    const Segment done = seg;
-    const uint32_t done_kv = kv_head, done_head0 = head0;
-    const bool whole = done.count == done.pages;
+    const bool whole = seg.count == seg.pages;
+    walk.next(a, units);
+    if (walk.left) load_queries();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -506,26 +590,10 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
                 o[t][x][2 * i + j] * v_unit;
           }
       }
-    left -= done.count;
-    if (left) {  // the next segment's pages are on their way while this one is summed up
-      next = {done.seq, done.unit + 1, 0, 0, done.pages};
-      if (next.unit == units) {
-        next.unit = 0;
-        do {
-          ++next.seq;
-          next.pages = next.seq < a.n_seqs ? pages_of(a, next.seq) : 1;
-        } while (next.pages == 0);
-        if (next.seq >= a.n_seqs) left = 0;  // lengths that changed under the call
-      }
-    }
-    if (left) {
-      next.count = (uint32_t)min((uint64_t)next.pages, left);
-      begin(next);
-    }
-    __syncthreads();
+    sync_warps();
     for (uint32_t x = tid; x < kHeads * kDim; x += kWarps * 32) {
       const uint32_t h = x / kDim, dim = x % kDim;
-      if (done_head0 + h >= a.group) break;
+      if (head0 + h >= a.group) break;
       float top = sh.m[0][h];
 #pragma unroll
       for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][h]);
@@ -536,16 +604,16 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
         sum += y * sh.l[w][h];
         all += y * sh.o[w][dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + h];
       }
-      const uint32_t head = done_kv * a.group + done_head0 + h;
+      const uint32_t head = kv_head * a.group + head0 + h;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const uint32_t y = pack16<kBf16>(all * inv, 0.f);
-        reinterpret_cast<uint16_t*>(a.out)[done.seq * a.out_stride + (uint64_t)head * kDim + dim] =
+        reinterpret_cast<uint16_t*>(a.out)[seg.seq * a.out_stride + (uint64_t)head * kDim + dim] =
             (uint16_t)y;
         if (dim == 0) {
           const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
-          if (a.lse) a.lse[(uint64_t)done.seq * a.heads + head] = z * kLn2;
-          if (kMass) a.lse2[(uint64_t)done.seq * a.heads + head] = z;
+          if (a.lse) a.lse[(uint64_t)seg.seq * a.heads + head] = z * kLn2;
+          if (kMass) a.lse2[(uint64_t)seg.seq * a.heads + head] = z;
         }
       } else {
         const uint32_t slot = blockIdx.x * 2 + (first_segment ? 0 : 1);
@@ -556,22 +624,32 @@ __global__ void __launch_bounds__(kWarps * 32, kTiles == 1 ? 3 : 2)
         }
       }
     }
-    if (!left) break;
     first_segment = false;
-    __syncthreads();
+    sync_warps();
   }
-  if (late && lane == 0) flag_status(a.status, NETKV_DEV_ETIMEOUT);
+
+  // rows of sequences without tokens, and lengths past the table
+  for (uint32_t i = blockIdx.x; i < a.n_seqs; i += gridDim.x) {
+    const uint32_t n = a.len[i];
+    if (tid == 0 && n > (uint64_t)a.width * kBlockTokens) flag_status(a.status, NETKV_DEV_ERANGE);
+    if (n) continue;
+    for (uint32_t x = tid; x < a.heads * kDim / 8; x += kWarps * 32)
+      reinterpret_cast<uint4*>(a.out + i * a.out_stride * 2)[x] = make_uint4(0, 0, 0, 0);
+    for (uint32_t h = tid; h < a.heads && a.lse; h += kWarps * 32)
+      a.lse[(uint64_t)i * a.heads + h] = -INFINITY;
+  }
+  if (tid == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
 }
 
 // Joins the segments that runs share: one block a (boundary between runs, head of the unit),
 // where the boundary is the first inside its segment.  The parts' weights first, then eight
 // groups of threads (a thread has four dims) over every eighth part: a long sequence alone on
-// the card has a part from each run, 456 for one unit.
+// the card has a part from each run, 304 for one unit.
 constexpr uint32_t kJoin = 256;
 template <int kDim, int kTiles, bool kBf16, bool kMass>
 __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int kHeads = kTiles * 8, kLanes = kDim / 4, kGroups = kJoin / kLanes;
-  __shared__ float weight[kCtas<kTiles>], reduce[kJoin / 32][2];
+  __shared__ float weight[kCtas], reduce[kJoin / 32][2];
   __shared__ float4 sums[kGroups][kLanes];
   const uint32_t units = a.kv.heads * a.chunks, tid = threadIdx.x, h = blockIdx.y;
   let_follow();
@@ -687,7 +765,7 @@ struct Workspace {
 Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, uint32_t width,
                     bool mass) {
   auto up = [](size_t x) { return (x + 127) / 128 * 128; };
-  const size_t rows = (size_t)kMostCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
+  const size_t rows = (size_t)kCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
   Workspace w;
   w.part_ml = up(rows * p->head_dim * 4);
   w.lse2 = w.part_ml + up(rows * 8);
@@ -746,7 +824,6 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         (float*)(w + ws.part_ml),
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
-                        per == 8 ? kCtas<1> : kCtas<2>,
                         d_status};
   const cudaStream_t s = (cudaStream_t)stream;
   auto go = [&](auto dim, auto tiles, auto bf, auto e4, auto mass) -> netkv_status {
@@ -755,10 +832,10 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
     constexpr int bytes = (int)sizeof(Shared<kDim, kTiles>);
     NETKV_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    kernel<<<kCtas<kTiles>, kWarps * 32, bytes, s>>>(a);
+    kernel<<<kCtas, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
     NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,
-                                    dim3(kCtas<kTiles> - 1, min(group, per)), kJoin, s, a));
+                                    dim3(kCtas - 1, min(group, per)), kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
