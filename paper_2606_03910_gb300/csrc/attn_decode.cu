@@ -829,9 +829,9 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
   auto go = [&](auto dim, auto tiles, auto bf, auto e4, auto mass) -> netkv_status {
     constexpr int kDim = decltype(dim)::value, kTiles = decltype(tiles)::value;
     constexpr bool kB = decltype(bf)::value, kE = decltype(e4)::value, kM = decltype(mass)::value;
-    auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
+    constexpr auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
     constexpr int bytes = (int)sizeof(Shared<kDim, kTiles>);
-    NETKV_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    NETKV_CUDA_TRY(allow_shared<kernel>(bytes));
     kernel<<<kCtas, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
     NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,

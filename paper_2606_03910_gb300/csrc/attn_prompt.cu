@@ -546,16 +546,21 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
       !row_map(&v, bf, k_rows ? d_v : d_q, k_rows ? v_stride : q_stride, k_rows ? kv_heads : 1,
                head_dim, k_rows))
     return NETKV_EINVAL;
-  auto go = [&](auto kernel, size_t bytes) -> netkv_status {
+  auto go = [&](auto dim, auto b) -> netkv_status {
+    constexpr auto kernel = prompt_kernel<decltype(dim)::value, decltype(b)::value>;
+    constexpr size_t bytes = sizeof(Shared<decltype(dim)::value>);
     // a launch with fewer registers than the warps share out would never end
-    cudaFuncAttributes has;
-    NETKV_CUDA_TRY(cudaFuncGetAttributes(&has, kernel));
-    if (has.numRegs < kLaunchRegs) return NETKV_ECUDA;
-    NETKV_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    static const int regs = [] {
+      cudaFuncAttributes has;
+      return cudaFuncGetAttributes(&has, kernel) == cudaSuccess ? has.numRegs : 0;
+    }();
+    if (regs < kLaunchRegs) return NETKV_ECUDA;
+    NETKV_CUDA_TRY(allow_shared<kernel>((int)bytes));
     kernel<<<(unsigned)grid, kThreads, bytes, (cudaStream_t)stream>>>(a, q, k, v);
     return netkv_launch_status();
   };
-  if (head_dim == 64)
-    return go(bf ? prompt_kernel<64, true> : prompt_kernel<64, false>, sizeof(Shared<64>));
-  return go(bf ? prompt_kernel<128, true> : prompt_kernel<128, false>, sizeof(Shared<128>));
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (head_dim == 64) return bf ? go(D64(), std::true_type()) : go(D64(), std::false_type());
+  return bf ? go(D128(), std::true_type()) : go(D128(), std::false_type());
 }

@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "netkv_internal.cuh"
 
 constexpr uint32_t kBlockTokens = NETKV_BLOCK_TOKENS;
@@ -29,6 +31,20 @@ inline bool kv_pages_ok(const netkv_kv_pages* p) {
 inline KvArgs kv_args(const netkv_kv_pages* p) {
   return {(unsigned char*)p->d_k, (unsigned char*)p->d_v, p->d_k_scale, p->d_v_scale, p->n_pages,
           p->kv_heads};
+}
+
+// Allows a kernel its dynamic shared memory, once for each device (0.8 us a time).
+template <auto kKernel>
+inline cudaError_t allow_shared(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 // Rows of heads * dim 16-bit values: 16-byte aligned, strides in values.

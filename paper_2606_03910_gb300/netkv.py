@@ -186,8 +186,8 @@ def current_stream() -> Optional[int]:
     import torch
     if not torch.cuda.is_initialized():
         return None
-    # with the device's index given, torch skips its search for one (3.1 -> 1.6 us a call)
-    return int(torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream)
+    # the raw handle, without a Stream object around it (1.6 -> 0.4 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _stream(s) -> Optional[int]:
@@ -420,70 +420,80 @@ def netkv_copy_group_async(copies, stream=None) -> None:
 # ---- KV blocks: tensors carry their sizes, so these take them from the tensors and check that
 # they fit together; everything else is checked behind the entry points.
 def _f32(t) -> None:
-    if t is not None and str(t.dtype) != "torch.float32":
+    if _code(t) != _F32:
         raise TypeError(f"float32 tensor expected, got {t.dtype}")
 
 
-def _rows(t, width=None):
+_F32, _I32, _I64 = 100, 101, 102
+_NAMED = {"torch.float16": NETKV_F16, "torch.bfloat16": NETKV_BF16, "torch.float32": _F32,
+          "torch.int32": _I32, "torch.uint32": _I32, "torch.int64": _I64, "torch.uint64": _I64}
+_CODES = {}  # of the dtypes seen: a lookup by dtype is a fifth of one by its name
+
+
+def _code(t) -> int:
+    d = t.dtype
+    c = _CODES.get(d)
+    if c is None:
+        c = _CODES[d] = _NAMED.get(str(d), -1)
+    return c
+
+
+def _rows(t, heads: int, dim: int, code: Optional[int] = None):
     """(dtype code, address, row stride) of rows [rows, heads, dim]; a row is contiguous."""
-    code = _DTYPES.get(str(t.dtype))
-    if code is None:
+    c = _code(t)
+    if c != NETKV_BF16 and c != NETKV_F16:
         raise TypeError(f"float16 or bfloat16 rows expected, got {t.dtype}")
-    n, heads, dim = t.shape
-    s = t.stride()
-    if (dim > 1 and s[2] != 1) or (heads > 1 and s[1] != dim):
-        raise ValueError("a row's heads have to lie one after another")
-    if width is not None and (heads, dim) != width:
-        raise ValueError(f"rows of {(heads, dim)}, {width} expected")
-    return code, t.data_ptr(), s[0] if n > 1 else heads * dim
-
-
-_DTYPES = {"torch.float16": NETKV_F16, "torch.bfloat16": NETKV_BF16}
-
-
-def _same(first, *rest) -> None:
-    if any(r != first for r in rest):
+    if code is not None and c != code:
         raise TypeError("tensors of one dtype expected")
+    n, h, d = t.shape
+    if h != heads or d != dim:
+        raise ValueError(f"rows of {(heads, dim)} expected, got {(h, d)}")
+    s, sh, sd = t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1):
+        raise ValueError("a row's heads have to lie one after another")
+    return c, t.data_ptr(), s if n > 1 else h * d
 
 
-def _ints(t, bits: int, n=None) -> Optional[int]:
-    """The address of a contiguous integer tensor, of n entries where n is given."""
+def _ints(t, code: int, n: int) -> Optional[int]:
+    """The address of a contiguous integer tensor of n entries."""
     if t is None:
         return None
-    if t.dtype.is_floating_point or t.element_size() * 8 != bits:
-        raise TypeError(f"{bits}-bit integers expected, got {t.dtype}")
-    if not t.is_contiguous() or (n is not None and t.numel() != n):
+    if _code(t) != code:
+        raise TypeError(f"{32 if code == _I32 else 64}-bit integers expected, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"a contiguous tensor of {n} entries expected, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _table(t, n_seqs: int):
-    if t.dim() != 2 or t.shape[0] != n_seqs:
-        raise ValueError(f"a block table of {n_seqs} rows expected, got {tuple(t.shape)}")
-    return _ints(t, 32), t.shape[1]
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != n_seqs:
+        raise ValueError(f"a block table of {n_seqs} rows expected, got {tuple(shape)}")
+    return _ints(t, _I32, n_seqs * shape[1]), shape[1]
 
 
-def _plane(t, shape) -> Optional[int]:
+def _plane(t, rows: int, width: int) -> Optional[int]:
     """The address of a contiguous fp32 tensor of that shape."""
     if t is None:
         return None
-    _f32(t)
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"a contiguous tensor of {tuple(shape)} expected, got {tuple(t.shape)}")
+    if _code(t) != _F32:
+        raise TypeError(f"float32 tensor expected, got {t.dtype}")
+    if t.shape != (rows, width) or not t.is_contiguous():
+        raise ValueError(f"a contiguous tensor of {(rows, width)} expected, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _kv_move(fn: str, pages: KvPages, k, v, off, start, table, status, stream) -> None:
-    width = (pages.kv_heads, pages.head_dim)
-    dt, kp, ks = _rows(k, width)
-    dv, vp, vs = _rows(v, width)
-    _same(dt, dv)
-    if k.shape[0] != v.shape[0]:
+    heads, dim = pages.kv_heads, pages.head_dim
+    dt, kp, ks = _rows(k, heads, dim)
+    _, vp, vs = _rows(v, heads, dim, dt)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
         raise ValueError("as many rows of keys as of values expected")
     n = off.numel() - 1
     tp, tw = _table(table, n)
-    _check(fn, getattr(_lib, fn)(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, 64), k.shape[0],
-                                 _ints(start, 32, n), tp, tw, _ptr(status), _stream(stream)))
+    _check(fn, getattr(_lib, fn)(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
+                                 _ints(start, _I32, n), tp, tw, _ptr(status), _stream(stream)))
 
 
 def netkv_kv_store(pages: KvPages, k, v, off, start, table, status=None, stream=None) -> None:
@@ -500,24 +510,24 @@ def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=N
                       stream=None) -> None:
     """Causal attention of packed prompts: q, out [q_rows, heads, dim], k, v [k_rows, kv_heads,
     dim]; scale defaults to dim ** -0.5.  See include/netkv.h."""
-    heads, dim = q.shape[1:]
-    kv_heads = k.shape[1]
-    dt, qp, qs = _rows(q)
-    dk, kp, ks = _rows(k, (kv_heads, dim))
-    dv, vp, vs = _rows(v, (kv_heads, dim))
-    do, op, os_ = _rows(out, (heads, dim))
-    _same(dt, dk, dv, do)
-    if k.shape[0] != v.shape[0] or out.shape[0] != q.shape[0]:
+    q_rows, heads, dim = q.shape
+    k_rows, kv_heads, _ = k.shape
+    dt, qp, qs = _rows(q, heads, dim)
+    _, kp, ks = _rows(k, kv_heads, dim, dt)
+    _, vp, vs = _rows(v, kv_heads, dim, dt)
+    _, op, os_ = _rows(out, heads, dim, dt)
+    if v.shape[0] != k_rows or out.shape[0] != q_rows:
         raise ValueError("as many rows of keys as of values, and of out as of q, expected")
     n = q_off.numel() - 1
     _check("netkv_attn_prompt", _lib.netkv_attn_prompt(
-        dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, 64),
-        _ints(k_off, 64, n + 1), q.shape[0], k.shape[0], dim ** -0.5 if scale is None else scale,
-        op, os_, _plane(lse, (q.shape[0], heads)), _ptr(status), _stream(stream)))
+        dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, _I64, n + 1),
+        _ints(k_off, _I64, n + 1), q_rows, k_rows, dim ** -0.5 if scale is None else scale,
+        op, os_, _plane(lse, q_rows, heads), _ptr(status), _stream(stream)))
 
 
 def netkv_attn_decode_workspace_size(pages: KvPages, n_seqs: int, heads: int, table_width: int,
                                      with_mass: bool = False) -> int:
+    """Bytes of the workspace; see include/netkv.h."""
     return int(_lib.netkv_attn_decode_workspace_size(pages.ref, int(n_seqs), int(heads),
                                                      int(table_width), int(bool(with_mass))))
 
@@ -527,17 +537,16 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     """One query row a sequence over its blocks: q, out [n_seqs, heads, dim]; see
     include/netkv.h."""
     n, heads, dim = q.shape
-    dt, qp, qs = _rows(q, (heads, pages.head_dim))
-    do, op, os_ = _rows(out, (heads, dim))
-    _same(dt, do)
+    dt, qp, qs = _rows(q, heads, pages.head_dim)
+    _, op, os_ = _rows(out, heads, dim, dt)
     if out.shape[0] != n:
         raise ValueError("as many rows of out as of q expected")
     tp, tw = _table(table, n)
     ws_bytes = 0 if workspace is None else _nbytes(workspace)
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
-        pages.ref, dt, qp, qs, heads, n, _ints(length, 32, n), tp, tw,
-        dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, (n, heads)),
-        _plane(mass_in, (n, tw)), _plane(mass_out, (n, tw)), _ptr(workspace), ws_bytes,
+        pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n), tp, tw,
+        dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads),
+        _plane(mass_in, n, tw), _plane(mass_out, n, tw), _ptr(workspace), ws_bytes,
         _ptr(status), _stream(stream)))
 
 
@@ -551,9 +560,9 @@ def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_ou
     if two != tw or twf != tw:
         raise ValueError("tables of one width expected")
     _check("netkv_kv_evict", _lib.netkv_kv_evict(
-        n, tp, _ints(length, 32, n), _plane(mass, (n, tw)), tw, _ints(budget, 32, n), int(sink),
-        int(recent), to, _ints(length_out, 32, n), _plane(mass_out, (n, tw)), fr,
-        _ints(n_freed, 32, n), _ptr(status), _stream(stream)))
+        n, tp, _ints(length, _I32, n), _plane(mass, n, tw), tw, _ints(budget, _I32, n), int(sink),
+        int(recent), to, _ints(length_out, _I32, n), _plane(mass_out, n, tw), fr,
+        _ints(n_freed, _I32, n), _ptr(status), _stream(stream)))
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:
