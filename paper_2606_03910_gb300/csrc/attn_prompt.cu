@@ -47,6 +47,25 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two fp32 values in one operation
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ void split(uint64_t x, float* a, float* b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(x), "l"(y), "l"(z));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
+  return d;
+}
 __device__ __forceinline__ uint32_t smem_addr(const void* p) {
   return (uint32_t)__cvta_generic_to_shared(p);
 }
@@ -376,9 +395,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < kKeys; ++i)
           if (i >= seen) s[i] = -INFINITY;
       }
-      float top = m;
+      float tops[4] = {m, s[0], s[1], s[2]};
 #pragma unroll
-      for (int i = 0; i < kKeys; ++i) top = fmaxf(top, s[i]);
+      for (int i = 3; i + 1 < kKeys; i += 2) tops[i / 2 % 4] = fmaxf(tops[i / 2 % 4], fmaxf(s[i], s[i + 1]));
+      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], fmaxf(tops[3], s[kKeys - 1])));
       const bool follow = (top - m) * a.scale2 > kLag;  // also the first maximum
       if (__any_sync(~0u, follow)) {
         float to = 1.f;
@@ -400,22 +420,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      const float base = m == -INFINITY ? 0.f : m * a.scale2;
-      float sum0 = 0.f, sum1 = 0.f;
+      const float base = m == -INFINITY ? 0.f : -m * a.scale2;
+      const uint64_t scale_2 = pair(a.scale2, a.scale2), base_2 = pair(base, base);
+      uint64_t sums_2[2] = {0, 0};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t p[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-          const float u = ex2(fmaf(s[h * 64 + 2 * i], a.scale2, -base));
-          const float w = ex2(fmaf(s[h * 64 + 2 * i + 1], a.scale2, -base));
-          sum0 += u;
-          sum1 += w;
+          float u, w;
+          split(fma2(pair(s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1]), scale_2, base_2), &u, &w);
+          u = ex2(u);
+          w = ex2(w);
+          sums_2[i & 1] = add2(sums_2[i & 1], pair(u, w));
           p[i] = pack16<kBf16>(u, w);
         }
         tmem_store(s_at(t) + lanes + h * 32, p);
       }
-      l += sum0 + sum1;
+      float u, w;
+      split(add2(sums_2[0], sums_2[1]), &u, &w);
+      l += u + w;
       tmem_stored();
       before_sync();
       bar_arrive(smem_addr(&sh.p_full[t]));
