@@ -42,9 +42,10 @@ struct PromptArgs {
   int* status;
 };
 
+// (kept in order: the first half of a row's weights is wanted first)
 __device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 // Two fp32 values in one operation
@@ -125,6 +126,15 @@ __device__ __forceinline__ constexpr uint32_t product(bool bf16, bool b_across, 
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_across ? 1u << 16 : 0u) | (n >> 3) << 17 |
          (128u >> 4) << 24;
 }
+// Products and commits are issued by one thread (`leader`) of a warp whose threads stay together,
+// so that operands are the warp's, not a thread's.
+__device__ __forceinline__ bool elect() {
+  uint32_t yes;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(yes));
+  return yes != 0;
+}
 __device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t what,
                                          bool add) {
   asm volatile(
@@ -187,6 +197,29 @@ __device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
         "r"(at)
       : "memory");
 }
+__device__ __forceinline__ void tmem_load16(uint32_t at, float* x) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, "
+      "%8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]),
+        "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, "
+      "%8, %9, %10, %11, %12, %13, %14, %15};"
+      :
+      : "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+        "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(at)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_loaded() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -194,27 +227,88 @@ __device__ __forceinline__ void tmem_stored() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
-// Stages of the ring: 32 KB each at 128 wide, with 64 KB of queries.
+// Tiles in the ring: 32 KB each at 128 wide, with 64 KB of queries and 32 KB for outputs.
 template <int kDim>
-constexpr int kStages = kDim == 128 ? 4 : 6;
+constexpr int kStages = kDim == 128 ? 4 : 8;
+
+// What a block works on: a row block of one sequence for a column (a pair of heads, or a head).
+struct Item {
+  uint64_t q_first, k_first;  // the sequence's rows
+  uint32_t q_count, k_count;
+  uint32_t row;     // the block's first row within the sequence
+  uint32_t column;
+  uint32_t steps[2];  // key tiles of each of the two tiles
+  int32_t valid;      // 0: nothing to do; -1: no more items
+};
 
 template <int kDim>
 struct Shared {
   alignas(1024) unsigned char q[2][kRows * kDim * 2];
   alignas(1024) unsigned char kv[kStages<kDim>][kKeys * kDim * 2];
-  alignas(8) uint64_t q_full, kv_full[kStages<kDim>], kv_empty[kStages<kDim>], landed;
-  uint64_t s_full[2], p_full[2], o_full[2];
+  alignas(128) unsigned char out[kSoftmaxWarps][32 * 128];
+  alignas(8) uint64_t q_full, q_empty, kv_full[kStages<kDim>], kv_empty[kStages<kDim>], landed;
+  uint64_t s_full[2], p_full[2][2], o_full[2];  // p: the two halves of the keys
+  uint64_t item_full[2], item_empty[2], claimed;
+  alignas(16) uint4 claim;
+  Item item[2];
   uint32_t tmem;
   int late;
 };
 
 // One of a block's two tiles: 128 rows of one head.
 struct Tile {
-  uint32_t head;
-  int64_t row;    // the first, within the sequence
-  int64_t sees;   // keys that the first row sees; each next one sees one more (< 1: none)
-  uint32_t rows;  // 0 .. 128
-  uint32_t steps; // key tiles
+  uint32_t head, rows;  // 0 .. 128 rows
+  int32_t row;          // the first, within the sequence
+};
+__device__ __forceinline__ Tile tile_of(const PromptArgs& a, const Item& x, uint32_t t) {
+  Tile y;
+  y.head = a.head_pairs ? x.column * 2 + t : x.column;
+  y.row = (int32_t)(x.row + (a.head_pairs ? 0 : t * kRows));
+  y.rows = (uint32_t)min(kRows, max(0, (int32_t)x.q_count - y.row));
+  return y;
+}
+
+// The grid's n-th item.  The last row blocks come first: they see the most keys.
+__device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n) {
+  const uint32_t columns = a.head_pairs ? a.heads / 2 : a.heads;
+  const uint32_t block_rows = a.head_pairs ? kRows : 2 * kRows;
+  const Found f = find_unit(a.n_seqs, a.tiles - 1 - n / columns, [&](uint32_t i) {
+    return (uint32_t)((row_range(a.q_off, i, a.q_rows).count + block_rows - 1) / block_rows);
+  });
+  Item x = {};
+  if (f.seq >= a.n_seqs) return x;
+  const RowRange q = row_range(a.q_off, f.seq, a.q_rows), k = row_range(a.k_off, f.seq, a.k_rows);
+  x.q_first = q.first;
+  x.k_first = k.first;
+  x.q_count = (uint32_t)q.count;
+  x.k_count = (uint32_t)k.count;
+  x.row = f.unit * block_rows;
+  x.column = n % columns;
+  x.valid = 1;
+#pragma unroll
+  for (uint32_t t = 0; t < 2; ++t) {
+    const Tile y = tile_of(a, x, t);
+    // keys that the tile's last row sees
+    const int64_t last = min((int64_t)x.k_count, (int64_t)x.k_count - x.q_count + y.row + y.rows);
+    x.steps[t] = y.rows && last > 0 ? (uint32_t)((last + kKeys - 1) / kKeys) : 0;
+  }
+  return x;
+}
+
+// The items of a block, as its warps read them: two places, filled by the planning warp.
+struct Items {
+  uint32_t n = 0;
+  template <class Sh>
+  __device__ __forceinline__ Item next(Sh& sh, volatile int* late) {
+    const uint32_t at = n % 2;
+    wait(smem_addr(&sh.item_full[at]), n / 2 & 1, late);
+    const Item x = sh.item[at];
+    ++n;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.item_empty[at]));
+    if (*late) return Item{0, 0, 0, 0, 0, 0, {0, 0}, -1};
+    return x;
+  }
 };
 
 template <int kDim, bool kBf16>
@@ -224,49 +318,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                   const __grid_constant__ CUtensorMap map_v) {
   extern __shared__ __align__(1024) unsigned char smem[];
   Shared<kDim>& sh = *reinterpret_cast<Shared<kDim>*>(smem);
-  constexpr int kRing = kStages<kDim>, kHalves = kDim / 64;
+  constexpr uint32_t kRing = kStages<kDim>;
+  constexpr int kHalves = kDim / 64;
   constexpr uint32_t kBox = 128 * 128;  // bytes of 128 rows of 64 values
-  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-
-  for (uint32_t i = blockIdx.x * kThreads + tid; i < a.n_seqs; i += gridDim.x * kThreads)
-    if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
-      flag_status(a.status, NETKV_DEV_ERANGE);
-
-  // The last row blocks come first: they see the most keys.
-  const uint32_t columns = a.head_pairs ? a.heads / 2 : a.heads, block_rows = a.head_pairs ? 128 : 256;
-  const Found f = find_unit(a.n_seqs, a.tiles - 1 - blockIdx.x / columns, [&](uint32_t i) {
-    return (uint32_t)((row_range(a.q_off, i, a.q_rows).count + block_rows - 1) / block_rows);
-  });
-  if (f.seq >= a.n_seqs) return;
-  const RowRange rq = row_range(a.q_off, f.seq, a.q_rows), rk = row_range(a.k_off, f.seq, a.k_rows);
-  const uint32_t column = blockIdx.x % columns;
-  auto tile_of = [&](uint32_t t) {
-    Tile x;
-    x.head = a.head_pairs ? column * 2 + t : column;
-    x.row = (int64_t)f.unit * block_rows + (a.head_pairs ? 0 : t * 128);
-    x.rows = (uint32_t)min((int64_t)128, max((int64_t)0, (int64_t)rq.count - x.row));
-    x.sees = (int64_t)rk.count - (int64_t)rq.count + x.row + 1;
-    const int64_t last = min((int64_t)rk.count, x.sees + (int64_t)x.rows - 1);
-    x.steps = x.rows && last > 0 ? (uint32_t)((last + kKeys - 1) / kKeys) : 0;
-    return x;
-  };
-  const uint32_t kv_head = (a.head_pairs ? column * 2 : column) / a.group;
-  const uint32_t steps0 = tile_of(0).steps, steps1 = tile_of(1).steps, steps = max(steps0, steps1);
+  // the whole of TMEM, from column 0: S of the two tiles, then their O
+  constexpr uint32_t kS = 0, kO = 256;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid / 32, 0);
+  volatile int* late = &sh.late;
 
   if (warp == 0) {
     if (lane == 0) {
+      sh.late = 0;
       bar_init(smem_addr(&sh.q_full), 1);
+      bar_init(smem_addr(&sh.q_empty), 1);
       bar_init(smem_addr(&sh.landed), 1);
-      for (int i = 0; i < kRing; ++i) {
+      bar_init(smem_addr(&sh.claimed), 1);
+      for (uint32_t i = 0; i < kRing; ++i) {
         bar_init(smem_addr(&sh.kv_full[i]), 1);
         bar_init(smem_addr(&sh.kv_empty[i]), 1);
       }
       for (int t = 0; t < 2; ++t) {
         bar_init(smem_addr(&sh.s_full[t]), 1);
-        bar_init(smem_addr(&sh.p_full[t]), 128);
+        bar_init(smem_addr(&sh.p_full[t][0]), 128);
+        bar_init(smem_addr(&sh.p_full[t][1]), 128);
         bar_init(smem_addr(&sh.o_full[t]), 1);
+        bar_init(smem_addr(&sh.item_full[t]), 1);
+        bar_init(smem_addr(&sh.item_empty[t]), kSoftmaxWarps + 2);
       }
-      sh.late = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
@@ -278,204 +356,303 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   after_sync();
-  const uint32_t tmem = sh.tmem;
-  volatile int* late = &sh.late;
-  // columns: S of the two tiles, then their O
-  auto s_at = [&](uint32_t t) { return tmem + t * 128; };
-  auto o_at = [&](uint32_t t) { return tmem + 256 + t * kDim; };
+  Items items;
 
   if (warp >= kSoftmaxWarps) {
-   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-   if (warp == kSoftmaxWarps) {
-    // ---- loads: the queries, then K 0, V 0, K 1, V 1, ...
-    if (steps) {
-      if (lane == 0) {
-        bar_expect(smem_addr(&sh.q_full), 2 * kRows * kDim * 2);
-        for (uint32_t t = 0; t < 2; ++t) {
-          const Tile x = tile_of(t);
-          for (int h = 0; h < kHalves; ++h)
-            load_box(smem_addr(sh.q[t]) + h * kBox, &map_q, h * 64, x.head,
-                     (int)(rq.first + x.row), smem_addr(&sh.q_full));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kSoftmaxWarps) {
+      // ---- loads: of each item the queries, then K 0, V 0, K 1, V 1, ...
+      uint32_t i = 0, cleared = 0, with_q = 0;
+      while (true) {
+        const Item x = items.next(sh, late);
+        if (x.valid < 0) break;
+        const uint32_t steps = max(x.steps[0], x.steps[1]);
+        if (steps == 0) continue;
+        const uint32_t kv_head = (a.head_pairs ? x.column * 2 : x.column) / a.group;
+        if (with_q) wait(smem_addr(&sh.q_empty), (with_q - 1) & 1, late);
+        ++with_q;
+        if (lane == 0) {
+          bar_expect(smem_addr(&sh.q_full), 2 * kRows * kDim * 2);
+          for (uint32_t t = 0; t < 2; ++t) {
+            const Tile y = tile_of(a, x, t);
+            for (int h = 0; h < kHalves; ++h)
+              load_box(smem_addr(sh.q[t]) + h * kBox, &map_q, h * 64, y.head,
+                       (int)(x.q_first + y.row), smem_addr(&sh.q_full));
+          }
+        }
+        for (uint32_t j = 0; j < 2 * steps && !*late; ++j, ++i) {
+          const uint32_t st = i % kRing, full = smem_addr(&sh.kv_full[st]);
+          if (i >= kRing) wait(smem_addr(&sh.kv_empty[st]), (i / kRing - 1) & 1, late);
+          const uint32_t key = j / 2 * kKeys;
+          const bool values = j & 1;
+          // values past the sequence's end are another's and meet weights of 0: an infinity or a
+          // NaN among them would not vanish, so the rows are cleared before they are handed on
+          const uint32_t own = x.k_count - key;
+          const bool clear = values && own < kKeys;
+          const uint32_t bar = clear ? smem_addr(&sh.landed) : full;
+          if (lane == 0) {
+            bar_expect(bar, kKeys * kDim * 2);
+            for (int h = 0; h < kHalves; ++h)
+              load_box(smem_addr(sh.kv[st]) + h * kBox, values ? &map_v : &map_k, h * 64, kv_head,
+                       (int)(x.k_first + key), bar);
+          }
+          if (clear) {  // a sequence's last tile only
+            wait(bar, cleared++ & 1, late);
+            for (int h = 0; h < kHalves; ++h)
+              for (uint32_t z = own * 8 + lane; z < kKeys * 8; z += 32)
+                reinterpret_cast<uint4*>(sh.kv[st] + h * kBox)[z] = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(full);
+          }
+          __syncwarp();
         }
       }
-      for (uint32_t i = 0; i < 2 * steps && !*late; ++i) {
-        const uint32_t st = i % kRing, full = smem_addr(&sh.kv_full[st]);
-        if (i >= kRing) wait(smem_addr(&sh.kv_empty[st]), (i / kRing - 1) & 1, late);
-        const int64_t key = (int64_t)(i / 2) * kKeys;
-        const bool values = i & 1;
-        // values past the sequence's end are another's and meet weights of 0: an infinity or a
-        // NaN among them would not vanish, so the rows are cleared before they are handed on
-        const int64_t own = (int64_t)rk.count - key;
-        const bool clear = values && own < kKeys;
-        const uint32_t bar = clear ? smem_addr(&sh.landed) : full;
-        if (lane == 0) {
-          bar_expect(bar, kKeys * kDim * 2);
-          for (int h = 0; h < kHalves; ++h)
-            load_box(smem_addr(sh.kv[st]) + h * kBox, values ? &map_v : &map_k, h * 64, kv_head,
-                     (int)(rk.first + key), bar);
-        }
-        if (clear) {  // the last tile only
-          wait(bar, 0, late);
-          for (int h = 0; h < kHalves; ++h)
-            for (uint32_t x = (uint32_t)own * 8 + lane; x < kKeys * 8; x += 32)
-              reinterpret_cast<uint4*>(sh.kv[st] + h * kBox)[x] = make_uint4(0, 0, 0, 0);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) bar_arrive(full);
+    } else if (warp == kSoftmaxWarps + 1) {
+      // ---- products
+      constexpr uint32_t kScores = product(kBf16, false, kKeys), kSums = product(kBf16, true, kDim);
+      const bool leader = elect();
+      const uint64_t q0 = operand(smem_addr(sh.q[0]), 16), k0 = operand(smem_addr(sh.kv[0]), 16),
+                     v0 = operand(smem_addr(sh.kv[0]), kBox);
+      constexpr uint32_t kTile = kRows * kDim * 2 >> 4;  // of operands' addresses
+      auto scores = [&](uint32_t t, uint32_t st) {       // S_t from the ring's place st
+        if (leader) {
+#pragma unroll
+          for (int x = 0; x < kDim / 16; ++x) {
+            const uint32_t off = (x / 4 * kBox + x % 4 * 32) >> 4;
+            mma_smem(kS + t * 128, q0 + t * kTile + off, k0 + st * kTile + off, kScores, x > 0);
+          }
+          commit(smem_addr(&sh.s_full[t]));
         }
         __syncwarp();
-      }
-    }
-   } else if (warp == kSoftmaxWarps + 1) {
-    // ---- products
-    if (lane == 0 && steps) {
-      constexpr uint32_t kScores = product(kBf16, false, kKeys), kSums = product(kBf16, true, kDim);
-      auto scores = [&](uint32_t t, uint32_t i) {  // S_t from the ring's i-th tile
-        const uint32_t q = smem_addr(sh.q[t]), k = smem_addr(sh.kv[i % kRing]);
-#pragma unroll
-        for (int x = 0; x < kDim / 16; ++x) {
-          const uint32_t off = x / 4 * kBox + x % 4 * 32;
-          mma_smem(s_at(t), operand(q + off, 16), operand(k + off, 16), kScores, x > 0);
-        }
-        commit(smem_addr(&sh.s_full[t]));
       };
-      auto sums = [&](uint32_t t, uint32_t i, bool add) {
-        const uint32_t v = smem_addr(sh.kv[i % kRing]);
+      auto sums = [&](uint32_t t, uint32_t st, uint32_t half, bool add) {
+        if (leader) {
 #pragma unroll
-        for (int x = 0; x < kKeys / 16; ++x)
-          mma_tmem(o_at(t), s_at(t) + x * 8, operand(v + x * 2048, kBox), kSums, add || x > 0);
+          for (uint32_t x = 0; x < kKeys / 32; ++x) {
+            const uint32_t step = half * (kKeys / 32) + x;
+            mma_tmem(kO + t * kDim, kS + t * 128 + step * 8, v0 + st * kTile + step * (2048 >> 4),
+                     kSums, add || step > 0);
+          }
+        }
+        __syncwarp();
+      };
+      auto signal = [&](uint64_t* bar) {
+        if (leader) commit(smem_addr(bar));
+        __syncwarp();
       };
       auto arrived = [&](uint32_t i) {
         wait(smem_addr(&sh.kv_full[i % kRing]), (i / kRing) & 1, late);
       };
-      wait(smem_addr(&sh.q_full), 0, late);
-      arrived(0);
-      after_sync();
-      for (uint32_t t = 0; t < 2; ++t)
-        if (t ? steps1 : steps0) scores(t, 0);
-      if (steps > 1) commit(smem_addr(&sh.kv_empty[0]));
-      for (uint32_t j = 0; j < steps && !*late; ++j) {
-        arrived(2 * j + 1);
-        if (j + 1 < steps) arrived(2 * j + 2);
-        for (uint32_t t = 0; t < 2; ++t) {
-          const uint32_t n = t ? steps1 : steps0;
-          if (j >= n) continue;
-          wait(smem_addr(&sh.p_full[t]), j & 1, late);
-          after_sync();
-          sums(t, 2 * j + 1, j > 0);
-          if (j + 1 < n) scores(t, 2 * j + 2);
-          else commit(smem_addr(&sh.o_full[t]));
-        }
-        // (nothing is signalled after the last products, which the softmax warps wait for)
-        if (j + 1 < steps) {
-          commit(smem_addr(&sh.kv_empty[(2 * j + 1) % kRing]));
-          commit(smem_addr(&sh.kv_empty[(2 * j + 2) % kRing]));
+      uint32_t i = 0, with_q = 0, done0 = 0, done1 = 0;  // tiles of the ring, items, steps
+      while (true) {
+        const Item x = items.next(sh, late);
+        if (x.valid < 0) break;
+        const uint32_t n0 = x.steps[0], n1 = x.steps[1], steps = max(n0, n1);
+        if (steps == 0) continue;
+        wait(smem_addr(&sh.q_full), with_q++ & 1, late);
+        arrived(i);
+        after_sync();
+        if (n0) scores(0, i % kRing);
+        if (n1) scores(1, i % kRing);
+        signal(&sh.kv_empty[i % kRing]);
+        if (steps == 1) signal(&sh.q_empty);
+        for (uint32_t j = 0; j < steps && !*late; ++j) {
+          const uint32_t v = (i + 1) % kRing, k = (i + 2) % kRing;
+          const bool more = j + 1 < steps;
+          arrived(i + 1);
+          if (more) arrived(i + 2);
+#pragma unroll
+          for (uint32_t t = 0; t < 2; ++t) {
+            const uint32_t n = t ? n1 : n0;
+            if (j < n) {
+              const uint32_t parity = (t ? done1++ : done0++) & 1;
+              wait(smem_addr(&sh.p_full[t][0]), parity, late);
+              after_sync();
+              sums(t, v, 0, j > 0);
+              wait(smem_addr(&sh.p_full[t][1]), parity, late);
+              after_sync();
+              sums(t, v, 1, true);
+              if (j + 1 < n) scores(t, k);
+              else signal(&sh.o_full[t]);
+            }
+          }
+          signal(&sh.kv_empty[v]);
+          if (more) signal(&sh.kv_empty[k]);
+          if (j + 2 == steps) signal(&sh.q_empty);
+          i += 2;
         }
       }
+      // the last signals have to reach a block that is still there
+      if (i >= 1) wait(smem_addr(&sh.kv_empty[(i - 1) % kRing]), ((i - 1) / kRing) & 1, late);
+    } else if (warp == kSoftmaxWarps + 2) {
+      // ---- plan: the block's own item, then those of blocks that have not started, which it
+      // takes over one by one
+      for (uint32_t i = blockIdx.x * 32 + lane; i < a.n_seqs; i += gridDim.x * 32)
+        if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
+          flag_status(a.status, NETKV_DEV_ERANGE);
+      uint32_t n = blockIdx.x;
+      for (uint32_t i = 0;; ++i) {
+        const bool end = n == ~0u || *late;
+        if (!end && lane == 0) {
+          bar_expect(smem_addr(&sh.claimed), 16);
+          asm volatile(
+              "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 "
+              "[%0], [%1];" ::"r"(smem_addr(&sh.claim)),
+              "r"(smem_addr(&sh.claimed))
+              : "memory");
+        }
+        Item x = {};
+        x.valid = -1;
+        if (!end) x = item_at(a, n);
+        if (i >= 2) wait(smem_addr(&sh.item_empty[i % 2]), (i / 2 - 1) & 1, late);
+        if (lane == 0) {
+          sh.item[i % 2] = x;
+          bar_arrive(smem_addr(&sh.item_full[i % 2]));
+        }
+        if (end) break;
+        wait(smem_addr(&sh.claimed), i & 1, late);
+        uint32_t got, first;
+        asm volatile(
+            "{\n\t.reg .b128 c;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+            "ld.shared.b128 c, [%2];\n\t"
+            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, c;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+            "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, c;\n\t}"
+            : "=r"(got), "=r"(first)
+            : "r"(smem_addr(&sh.claim))
+            : "memory");
+        n = got ? first : ~0u;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
     }
-   }
   } else {
     // ---- softmax: a thread has a row of its tile
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const uint32_t t = warp / 4, row = tid % 128, lanes = (warp % 4) * 32 << 16;
-    const Tile x = tile_of(t);
-    const int64_t visible = min((int64_t)rk.count, x.sees + (int64_t)row);  // keys of this row
-    float m = -INFINITY, l = 0.f;
-    for (uint32_t j = 0; j < x.steps; ++j) {
-      float s[kKeys];
-      wait(smem_addr(&sh.s_full[t]), j & 1, late);
-      after_sync();
+    const uint32_t s_at = kS + t * 128 + lanes, o_at = kO + t * kDim + lanes;
+    uint32_t taken = 0, finished = 0;  // steps, and items with any
+    while (true) {
+      const Item x = items.next(sh, late);
+      if (x.valid < 0) break;
+      if (x.valid == 0) continue;
+      const Tile y = tile_of(a, x, t);
+      const uint32_t steps = t ? x.steps[1] : x.steps[0];
+      // keys of this row
+      const int64_t visible =
+          min((int64_t)x.k_count, (int64_t)x.k_count - x.q_count + y.row + row + 1);
+      float m = -INFINITY, l = 0.f;
+      for (uint32_t j = 0; j < steps; ++j, ++taken) {
+        float s[kKeys];
+        wait(smem_addr(&sh.s_full[t]), taken & 1, late);
+        after_sync();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_load(s_at(t) + lanes + i * 32, s + i * 32);
-      tmem_loaded();
-      const int64_t rest = visible - (int64_t)j * kKeys;
-      const int seen = (int)max((int64_t)0, min((int64_t)kKeys, rest));
-      if (__any_sync(~0u, seen < kKeys)) {
+        for (int i = 0; i < 4; ++i) tmem_load(s_at + i * 32, s + i * 32);
+        tmem_loaded();
+        const int64_t rest = visible - (int64_t)j * kKeys;
+        const int seen = (int)max((int64_t)0, min((int64_t)kKeys, rest));
+        if (__any_sync(~0u, seen < kKeys)) {
 #pragma unroll
-        for (int i = 0; i < kKeys; ++i)
-          if (i >= seen) s[i] = -INFINITY;
-      }
-      float tops[4] = {m, s[0], s[1], s[2]};
-#pragma unroll
-      for (int i = 3; i + 1 < kKeys; i += 2) tops[i / 2 % 4] = fmaxf(tops[i / 2 % 4], fmaxf(s[i], s[i + 1]));
-      const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], fmaxf(tops[3], s[kKeys - 1])));
-      const bool follow = (top - m) * a.scale2 > kLag;  // also the first maximum
-      if (__any_sync(~0u, follow)) {
-        float to = 1.f;
-        if (follow) {
-          to = m == -INFINITY ? 0.f : ex2((m - top) * a.scale2);
-          m = top;
+          for (int i = 0; i < kKeys; ++i)
+            if (i >= seen) s[i] = -INFINITY;
         }
-        __syncwarp();
-        l *= to;
-        if (j) {  // S_t is complete, and so is P_t V before it
+        float tops[4] = {m, s[0], s[1], s[2]};
 #pragma unroll
-          for (int i = 0; i < kDim / 32; ++i) {
-            float o[32];
-            tmem_load(o_at(t) + lanes + i * 32, o);
-            tmem_loaded();
+        for (int i = 3; i + 1 < kKeys; i += 2)
+          tops[i / 2 % 4] = fmaxf(tops[i / 2 % 4], fmaxf(s[i], s[i + 1]));
+        const float top =
+            fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], fmaxf(tops[3], s[kKeys - 1])));
+        const bool follow = (top - m) * a.scale2 > kLag;  // also the first maximum
+        if (__any_sync(~0u, follow)) {
+          float to = 1.f;
+          if (follow) {
+            to = m == -INFINITY ? 0.f : ex2((m - top) * a.scale2);
+            m = top;
+          }
+          __syncwarp();
+          l *= to;
+          if (j) {  // S_t is complete, and so is P_t V before it
 #pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] *= to;
-            tmem_store(o_at(t) + lanes + i * 32, reinterpret_cast<const uint32_t*>(o));
+            for (int i = 0; i < kDim / 16; ++i) {
+              float o[16];
+              tmem_load16(o_at + i * 16, o);
+              tmem_loaded();
+#pragma unroll
+              for (int z = 0; z < 16; ++z) o[z] *= to;
+              tmem_store16(o_at + i * 16, reinterpret_cast<const uint32_t*>(o));
+            }
           }
         }
-      }
-      const float base = m == -INFINITY ? 0.f : -m * a.scale2;
-      const uint64_t scale_2 = pair(a.scale2, a.scale2), base_2 = pair(base, base);
-      uint64_t sums_2[2] = {0, 0};
+        const float base = m == -INFINITY ? 0.f : -m * a.scale2;
+        const uint64_t scale_2 = pair(a.scale2, a.scale2), base_2 = pair(base, base);
+        uint64_t sums_2[2] = {0, 0};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t p[32];
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          float u, w;
-          split(fma2(pair(s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1]), scale_2, base_2), &u, &w);
-          u = ex2(u);
-          w = ex2(w);
-          sums_2[i & 1] = add2(sums_2[i & 1], pair(u, w));
-          p[i] = pack16<kBf16>(u, w);
+          for (int i = 0; i < 32; ++i) {
+            float u, w;
+            split(fma2(pair(s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1]), scale_2, base_2), &u, &w);
+            u = ex2(u);
+            w = ex2(w);
+            sums_2[i & 1] = add2(sums_2[i & 1], pair(u, w));
+            p[i] = pack16<kBf16>(u, w);
+          }
+          tmem_store(s_at + h * 32, p);
+          tmem_stored();
+          before_sync();
+          bar_arrive(smem_addr(&sh.p_full[t][h]));
         }
-        tmem_store(s_at(t) + lanes + h * 32, p);
+        float u, w;
+        split(add2(sums_2[0], sums_2[1]), &u, &w);
+        l += u + w;
       }
-      float u, w;
-      split(add2(sums_2[0], sums_2[1]), &u, &w);
-      l += u + w;
-      tmem_stored();
-      before_sync();
-      bar_arrive(smem_addr(&sh.p_full[t]));
-    }
-    // ---- the row's output
-    const bool mine = row < x.rows;
-    const uint64_t at = rq.first + x.row + row;
-    if (x.steps) {
-      wait(smem_addr(&sh.o_full[t]), 0, late);
-      after_sync();
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+      // ---- the rows' outputs, through shared memory so that whole lines are written: 64
+      // values of a warp's 32 rows at a time, 16 bytes of row r in place (c ^ r) of 8
+      if (steps) {
+        wait(smem_addr(&sh.o_full[t]), finished++ & 1, late);
+        after_sync();
+      }
+      const bool any = steps && l != 0.f;
+      const float inv = any ? 1.f / l : 0.f;
+      uint4* stage = reinterpret_cast<uint4*>(sh.out[warp]);
+      const uint32_t row0 = (warp % 4) * 32;
+      unsigned char* dst = a.out + ((x.q_first + y.row + row0) * a.out_stride + (uint64_t)y.head * kDim) * 2;
 #pragma unroll
-    for (int i = 0; i < kDim / 32; ++i) {
-      float o[32];
+      for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float o[32];
+          if (steps) {
+            tmem_load(o_at + h * 64 + i * 32, o);
+            tmem_loaded();
+          }
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              w[q] = any ? pack16<kBf16>(o[z * 8 + q * 2] * inv, o[z * 8 + q * 2 + 1] * inv) : 0u;
+            stage[lane * 8 + ((i * 4 + z) ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t r = i * 4 + lane / 8, c = lane % 8;
+          if (row0 + r < y.rows)
+            *reinterpret_cast<uint4*>(dst + (r * a.out_stride + h * 64 + c * 8) * 2) =
+                stage[r * 8 + (c ^ (r & 7))];
+        }
+        __syncwarp();
+      }
+      if (row < y.rows && a.lse)
+        a.lse[(x.q_first + y.row + row) * a.heads + y.head] =
+            l == 0.f ? -INFINITY : m * a.scale2 * kLn2 + logf(l);
       __syncwarp();
-      if (x.steps) {
-        tmem_load(o_at(t) + lanes + i * 32, o);
-        tmem_loaded();
-      }
-      if (mine) {
-        uint4* dst = reinterpret_cast<uint4*>(
-            a.out + (at * a.out_stride + (uint64_t)x.head * kDim + i * 32) * 2);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          uint32_t w[4];
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            w[z] = x.steps && l != 0.f ? pack16<kBf16>(o[y * 8 + z * 2] * inv, o[y * 8 + z * 2 + 1] * inv) : 0u;
-          dst[y] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
+      before_sync();
     }
-    if (mine && a.lse)
-      a.lse[at * a.heads + x.head] = l == 0.f ? -INFINITY : m * a.scale2 * kLn2 + logf(l);
-    before_sync();
   }
   __syncthreads();
   if (warp == 0) {
@@ -486,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
     after_sync();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem) : "memory");
     if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
   }
 }
