@@ -36,7 +36,8 @@ struct PromptArgs {
   uint64_t q_rows, k_rows;
   uint32_t heads, group, n_seqs;
   uint32_t head_pairs;  // 1: a block's tiles are two heads; 0: two row blocks of a head
-  uint32_t tiles;       // row tiles (pairs of them) that the grid has
+  uint32_t tiles;       // row blocks that the grid has
+  uint32_t ordered;     // 1: row blocks by their key tiles, the most first
   float scale2;         // scale * log2(e)
   float* lse;
   int* status;
@@ -248,7 +249,7 @@ struct Shared {
   alignas(128) unsigned char out[kSoftmaxWarps][32 * 128];
   alignas(8) uint64_t q_full, q_empty, kv_full[kStages<kDim>], kv_empty[kStages<kDim>], landed;
   uint64_t s_full[2], p_full[2][2], o_full[2];  // p: the two halves of the keys
-  uint64_t item_full[2], item_empty[2], claimed;
+  uint64_t item_full[2], item_empty[2], begun, claimed;
   alignas(16) uint4 claim;
   Item item[2];
   uint32_t tmem;
@@ -268,13 +269,70 @@ __device__ __forceinline__ Tile tile_of(const PromptArgs& a, const Item& x, uint
   return y;
 }
 
-// The grid's n-th item.  The last row blocks come first: they see the most keys.
+// The n-th row block of all sequences: (sequence, block), sequence n_seqs where there is none.
+// In the plain order the last blocks of a sequence, which see the most keys, come first.  In the
+// ordered one the blocks come by their key tiles over all sequences, so that blocks of the grid
+// that take one item after another end together: the number of row blocks with at least s key
+// tiles is known for each sequence, and a search over s finds where the n-th stands.
+__device__ __forceinline__ Found row_block(const PromptArgs& a, uint32_t n, uint32_t block_rows) {
+  if (!a.ordered)
+    return find_unit(a.n_seqs, a.tiles - 1 - n, [&](uint32_t i) {
+      return (uint32_t)((row_range(a.q_off, i, a.q_rows).count + block_rows - 1) / block_rows);
+    });
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t q[4], k[4], most = 0, all = 0;  // lane l has sequences 4 l .. 4 l + 3 of up to 128
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t i = lane * 4 + j;
+    q[j] = i < a.n_seqs ? (uint32_t)row_range(a.q_off, i, a.q_rows).count : 0;
+    k[j] = i < a.n_seqs ? (uint32_t)row_range(a.k_off, i, a.k_rows).count : 0;
+    if (q[j]) most = max(most, (k[j] + kKeys - 1) / kKeys);
+    all += (q[j] + block_rows - 1) / block_rows;
+  }
+  // row blocks of q rows and k keys with at least s key tiles
+  auto least = [&](uint32_t q, uint32_t k, uint32_t s) -> uint32_t {
+    const uint32_t blocks = (q + block_rows - 1) / block_rows;
+    if (s == 0) return blocks;
+    // rows up to a block's end that make it see key 128 (s - 1)
+    const int64_t rows = (int64_t)(s - 1) * kKeys + 1 - k + q;
+    if (rows > (int64_t)q) return 0;
+    return rows <= 0 ? blocks : blocks + 1 - (uint32_t)((rows + block_rows - 1) / block_rows);
+  };
+  most = __reduce_max_sync(~0u, most);
+  all = __reduce_add_sync(~0u, all);
+  if (n >= all) return {a.n_seqs, 0};
+  uint32_t lo = 0, hi = most + 1;  // more than n blocks have lo key tiles, not so hi
+  while (hi - lo > 1) {
+    const uint32_t s = (lo + hi) / 2;
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c += least(q[j], k[j], s);
+    if (__reduce_add_sync(~0u, c) > n) lo = s;
+    else hi = s;
+  }
+  uint32_t above[4], sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum += above[j] = least(q[j], k[j], hi);
+  n -= __reduce_add_sync(~0u, sum);
+  const Found f = find_unit(a.n_seqs, n, [&](uint32_t i) {
+    const uint32_t j = i % 4;  // the lane's own sequences
+    const uint32_t qi = j == 0 ? q[0] : j == 1 ? q[1] : j == 2 ? q[2] : q[3];
+    const uint32_t ki = j == 0 ? k[0] : j == 1 ? k[1] : j == 2 ? k[2] : k[3];
+    return least(qi, ki, lo) - least(qi, ki, hi);
+  });
+  if (f.seq >= a.n_seqs) return f;
+  const uint32_t at = f.seq % 4, from = f.seq / 4;
+  const uint32_t qs = __shfl_sync(~0u, at == 0 ? q[0] : at == 1 ? q[1] : at == 2 ? q[2] : q[3], from);
+  const uint32_t ks =
+      __shfl_sync(~0u, at == 0 ? above[0] : at == 1 ? above[1] : at == 2 ? above[2] : above[3], from);
+  return {f.seq, (qs + block_rows - 1) / block_rows - 1 - ks - f.unit};
+}
+
+// The grid's n-th item.
 __device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n) {
   const uint32_t columns = a.head_pairs ? a.heads / 2 : a.heads;
   const uint32_t block_rows = a.head_pairs ? kRows : 2 * kRows;
-  const Found f = find_unit(a.n_seqs, a.tiles - 1 - n / columns, [&](uint32_t i) {
-    return (uint32_t)((row_range(a.q_off, i, a.q_rows).count + block_rows - 1) / block_rows);
-  });
+  const Found f = row_block(a, n / columns, block_rows);
   Item x = {};
   if (f.seq >= a.n_seqs) return x;
   const RowRange q = row_range(a.q_off, f.seq, a.q_rows), k = row_range(a.k_off, f.seq, a.k_rows);
@@ -333,6 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(smem_addr(&sh.q_empty), 1);
       bar_init(smem_addr(&sh.landed), 1);
       bar_init(smem_addr(&sh.claimed), 1);
+      bar_init(smem_addr(&sh.begun), 1);
       for (uint32_t i = 0; i < kRing; ++i) {
         bar_init(smem_addr(&sh.kv_full[i]), 1);
         bar_init(smem_addr(&sh.kv_empty[i]), 1);
@@ -448,6 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (true) {
         const Item x = items.next(sh, late);
         if (x.valid < 0) break;
+        if (leader) bar_arrive(smem_addr(&sh.begun));
+        __syncwarp();
         const uint32_t n0 = x.steps[0], n1 = x.steps[1], steps = max(n0, n1);
         if (steps == 0) continue;
         wait(smem_addr(&sh.q_full), with_q++ & 1, late);
@@ -491,40 +552,45 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (uint32_t i = blockIdx.x * 32 + lane; i < a.n_seqs; i += gridDim.x * 32)
         if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
           flag_status(a.status, NETKV_DEV_ERANGE);
+      // An item is claimed once the products of the one before begin, not earlier: what a block
+      // holds in advance, another that is ready cannot take.
       uint32_t n = blockIdx.x;
       for (uint32_t i = 0;; ++i) {
-        const bool end = n == ~0u || *late;
-        if (!end && lane == 0) {
-          bar_expect(smem_addr(&sh.claimed), 16);
+        if (i) {
+          wait(smem_addr(&sh.begun), (i - 1) & 1, late);
+          if (lane == 0) {
+            bar_expect(smem_addr(&sh.claimed), 16);
+            asm volatile(
+                "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes."
+                "b128 [%0], [%1];" ::"r"(smem_addr(&sh.claim)),
+                "r"(smem_addr(&sh.claimed))
+                : "memory");
+          }
+          wait(smem_addr(&sh.claimed), (i - 1) & 1, late);
+          uint32_t got, first;
           asm volatile(
-              "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 "
-              "[%0], [%1];" ::"r"(smem_addr(&sh.claim)),
-              "r"(smem_addr(&sh.claimed))
+              "{\n\t.reg .b128 c;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
+              "ld.shared.b128 c, [%2];\n\t"
+              "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, c;\n\t"
+              "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+              "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, c;"
+              "\n\t}"
+              : "=r"(got), "=r"(first)
+              : "r"(smem_addr(&sh.claim))
               : "memory");
+          n = got && !*late ? first : ~0u;
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
         }
         Item x = {};
         x.valid = -1;
-        if (!end) x = item_at(a, n);
+        if (n != ~0u) x = item_at(a, n);
         if (i >= 2) wait(smem_addr(&sh.item_empty[i % 2]), (i / 2 - 1) & 1, late);
         if (lane == 0) {
           sh.item[i % 2] = x;
           bar_arrive(smem_addr(&sh.item_full[i % 2]));
         }
-        if (end) break;
-        wait(smem_addr(&sh.claimed), i & 1, late);
-        uint32_t got, first;
-        asm volatile(
-            "{\n\t.reg .b128 c;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
-            "ld.shared.b128 c, [%2];\n\t"
-            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, c;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
-            "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, y, z, w}, c;\n\t}"
-            : "=r"(got), "=r"(first)
-            : "r"(smem_addr(&sh.claim))
-            : "memory");
-        n = got ? first : ~0u;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
+        if (n == ~0u) break;
       }
     }
   } else {
@@ -738,6 +804,12 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
   const uint64_t tiles = q_rows / block_rows + n_seqs, grid = tiles * (a.head_pairs ? heads / 2 : heads);
   if (grid >> 31) return NETKV_EINVAL;
   a.tiles = (uint32_t)tiles;
+  // One sequence alone is in order as it is, and where every item has an SM the order does not
+  // matter; more than 128 sequences would take the search longer than their blocks last.
+  int dev = 0, sms = 0;
+  NETKV_CUDA_TRY(cudaGetDevice(&dev));
+  NETKV_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  a.ordered = n_seqs > 1 && n_seqs <= 128 && grid > (uint64_t)sms;
   if (!encoder()) return NETKV_ECUDA;
   const bool bf = dtype == NETKV_BF16;
   CUtensorMap q, k, v;
