@@ -68,6 +68,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ uint32_t smem_addr(const void* p) {
   return (uint32_t)__cvta_generic_to_shared(p);
 }
@@ -606,8 +611,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Tile y = tile_of(a, x, t);
       const uint32_t steps = t ? x.steps[1] : x.steps[0];
       // keys of this row
-      const int64_t visible =
-          min((int64_t)x.k_count, (int64_t)x.k_count - x.q_count + y.row + row + 1);
+      const int visible =
+          (int)min((int64_t)x.k_count, (int64_t)x.k_count - x.q_count + y.row + row + 1);
       float m = -INFINITY, l = 0.f;
       for (uint32_t j = 0; j < steps; ++j, ++taken) {
         float s[kKeys];
@@ -616,8 +621,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) tmem_load(s_at + i * 32, s + i * 32);
         tmem_loaded();
-        const int64_t rest = visible - (int64_t)j * kKeys;
-        const int seen = (int)max((int64_t)0, min((int64_t)kKeys, rest));
+        const int seen = visible - (int)(j * kKeys);
         if (__any_sync(~0u, seen < kKeys)) {
 #pragma unroll
           for (int i = 0; i < kKeys; ++i)
@@ -626,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         float tops[4] = {m, s[0], s[1], s[2]};
 #pragma unroll
         for (int i = 3; i + 1 < kKeys; i += 2)
-          tops[i / 2 % 4] = fmaxf(tops[i / 2 % 4], fmaxf(s[i], s[i + 1]));
+          tops[i / 2 % 4] = max3(tops[i / 2 % 4], s[i], s[i + 1]);
         const float top =
             fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], fmaxf(tops[3], s[kKeys - 1])));
         const bool follow = (top - m) * a.scale2 > kLag;  // also the first maximum
