@@ -172,28 +172,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   return y;
 }
 
-// Four codes to two pairs of fp16.  int8: u = code + 128 behind fp16's exponent of 1024 is
-// 1024 + u, from which 1152 leaves the code, all exact.
-template <bool kE4m3>
-__device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {
-  if (kE4m3) {
-    const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
-    const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    *lo = (uint32_t)x.x | (uint32_t)x.y << 16;
-    *hi = (uint32_t)y.x | (uint32_t)y.y << 16;
-  } else {
-    const uint32_t u = w ^ 0x80808080u, p = __byte_perm(u, 0x64646464u, 0x4140),
-                   q = __byte_perm(u, 0x64646464u, 0x4342);
-    const uint32_t k1152 = 0x64806480u;
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&p),
-                              *reinterpret_cast<const __half2*>(&k1152));
-    const __half2 y = __hsub2(*reinterpret_cast<const __half2*>(&q),
-                              *reinterpret_cast<const __half2*>(&k1152));
-    *lo = *reinterpret_cast<const uint32_t*>(&x);
-    *hi = *reinterpret_cast<const uint32_t*>(&y);
-  }
-}
-
 template <int kDim, int kTiles>
 struct Shared {
   static constexpr int kHeads = kTiles * 8;

@@ -27,12 +27,6 @@ __device__ __forceinline__ Unit unit_of(uint32_t n_seqs, uint32_t kv_heads, Coun
   return {f.seq, f.unit, (w % per) / 2, (w & 1) != 0};
 }
 
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int d = 16; d; d /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
-  return x;
-}
-
 struct StoreArgs {
   KvArgs kv;
   const unsigned char* k;
@@ -87,63 +81,74 @@ __global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constan
 
   const uint32_t col = (lane % kLanes) * 8, row0 = lane / kLanes;
   const uint64_t pos0 = block * kBlockTokens;
-  const bool merges = pos0 < start;  // the block has tokens from earlier calls
+  // rows [lo, hi) of the block are new, those before lo are from earlier calls
+  const uint32_t lo = start > pos0 ? (uint32_t)(start - pos0) : 0;
+  const uint32_t hi = (uint32_t)min((uint64_t)kBlockTokens, start + r.count - pos0);
+  const bool all = hi - lo == kBlockTokens;
+  const unsigned char* from =
+      src + ((int64_t)(r.first + pos0 - start + row0) * (int64_t)stride + (int64_t)u.head * kDim + col) * 2;
   uint4 x[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const uint64_t pos = pos0 + row0 + i * kRows;
+    const uint32_t row = row0 + i * kRows;
     x[i] = make_uint4(0, 0, 0, 0);
-    if (pos >= start && pos < start + r.count)
-      x[i] = __ldcs(reinterpret_cast<const uint4*>(
-          src + ((r.first + (pos - start)) * stride + (uint64_t)u.head * kDim + col) * 2));
+    if (all || (row >= lo && row < hi)) x[i] = __ldcs(reinterpret_cast<const uint4*>(from));
+    from += kRows * stride * 2;
   }
-  const float was = merges ? *scale : 0.f;
-  float largest = 0.f;
-  bool odd = false;
+  const float was = lo ? *scale : 0.f;
+  // Magnitudes are in the order of their bits, two values a word.
+  constexpr uint32_t kInf = kBf16 ? 0x7f80 : 0x7c00;
+  auto top_bits = [&]() {
+    uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&x[i]);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 y = unpack16<kBf16>(w[j]);
-      // infinities and NaN have no code: they are held as zeros
-      if (!(fabsf(y.x) <= 3.4e38f)) w[j] &= 0xffff0000u, odd = true;
-      if (!(fabsf(y.y) <= 3.4e38f)) w[j] &= 0x0000ffffu, odd = true;
-      const float2 z = unpack16<kBf16>(w[j]);
-      largest = fmaxf(largest, fmaxf(fabsf(z.x), fabsf(z.y)));
+    for (int i = 0; i < kSteps; ++i) {
+      m = __vimax3_u16x2(m, x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu);
+      m = __vimax3_u16x2(m, x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu);
     }
+    return __reduce_max_sync(~0u, max(m & 0xffffu, m >> 16));
+  };
+  uint32_t top = top_bits();
+  if (top >= kInf) {  // infinities and NaN have no code: they are held as zeros
+    if (lane == 0) flag_status(a.status, NETKV_DEV_EDOMAIN);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(&x[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if ((w[j] & 0x7fffu) >= kInf) w[j] &= 0xffff0000u;
+        if ((w[j] >> 16 & 0x7fffu) >= kInf) w[j] &= 0x0000ffffu;
+      }
+    }
+    top = top_bits();
   }
-  if (odd) flag_status(a.status, NETKV_DEV_EDOMAIN);
-  largest = warp_max(largest);
+  const float largest = unpack16<kBf16>(top).x;
   const float fresh = largest < kSmallest ? 0.f : largest / (kE4m3 ? 448.f : 127.f);
   const float now = fmaxf(was, fresh);
   const float inv = now > 0.f ? 1.f / now : 0.f;
+  unsigned char* to = codes + row0 * kDim + col;
+  const bool grows = lo && now > was;
+  const float ratio = grows ? was / now : 0.f;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const uint32_t row = row0 + i * kRows;
-    const uint64_t pos = pos0 + row;
-    uint2* to = reinterpret_cast<uint2*>(codes + row * kDim + col);
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[i]);
-    if (pos >= start && pos < start + r.count) {
-      uint32_t c[4];
+    uint2* at = reinterpret_cast<uint2*>(to + i * kRows * kDim);
+    if (all || (row >= lo && row < hi)) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      float y[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 y = unpack16<kBf16>(w[j]);
-        c[j] = encode2<kE4m3>(y.x * inv, y.y * inv);
+        const float2 z = unpack16<kBf16>(w[j]);
+        y[2 * j] = z.x * inv;
+        y[2 * j + 1] = z.y * inv;
       }
-      *to = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
-    } else if (pos < start && now > was) {
+      *at = make_uint2(encode4<kE4m3>(y), encode4<kE4m3>(y + 4));
+    } else if (grows && row < lo) {
       // the block's scale grew: its earlier codes follow
-      const float ratio = was / now;
-      const uint2 old = *to;
-      const uint32_t q[4] = {old.x & 0xffff, old.x >> 16, old.y & 0xffff, old.y >> 16};
-      uint32_t c[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 y = decode2<kE4m3>(q[j]);
-        c[j] = encode2<kE4m3>(y.x * ratio, y.y * ratio);
-      }
-      *to = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+      const uint2 old = *at;
+      float y[8];
+      decode4<kE4m3>(old.x, ratio, y);
+      decode4<kE4m3>(old.y, ratio, y + 4);
+      *at = make_uint2(encode4<kE4m3>(y), encode4<kE4m3>(y + 4));
     }
   }
   if (lane == 0) *scale = now;
@@ -170,28 +175,30 @@ __global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant
   const float s = there ? (u.values ? a.kv.v_scale : a.kv.k_scale)[part] : 0.f;
   const uint32_t col = (lane % kLanes) * 8, row0 = lane / kLanes;
   const uint64_t pos0 = block * kBlockTokens;
+  const uint32_t lo = start > pos0 ? (uint32_t)(start - pos0) : 0;
+  const uint32_t hi = (uint32_t)min((uint64_t)kBlockTokens, start + r.count - pos0);
+  const bool all = hi - lo == kBlockTokens;
   uint2 x[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const uint64_t pos = pos0 + row0 + i * kRows;
+    const uint32_t row = row0 + i * kRows;
     x[i] = make_uint2(0, 0);
-    if (there && pos >= start && pos < start + r.count)
-      x[i] = *reinterpret_cast<const uint2*>(codes + (row0 + i * kRows) * kDim + col);
+    if (there && (all || (row >= lo && row < hi)))
+      x[i] = *reinterpret_cast<const uint2*>(codes + row * kDim + col);
   }
+  unsigned char* to =
+      dst + ((int64_t)(r.first + pos0 - start + row0) * (int64_t)stride + (int64_t)u.head * kDim + col) * 2;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const uint64_t pos = pos0 + row0 + i * kRows;
-    if (pos < start || pos >= start + r.count) continue;
-    const uint32_t q[4] = {x[i].x & 0xffff, x[i].x >> 16, x[i].y & 0xffff, x[i].y >> 16};
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 y = decode2<kE4m3>(q[j]);
-      w[j] = pack16<kBf16>(y.x * s, y.y * s);
+    const uint32_t row = row0 + i * kRows;
+    if (all || (row >= lo && row < hi)) {
+      float y[8];
+      decode4<kE4m3>(x[i].x, s, y);
+      decode4<kE4m3>(x[i].y, s, y + 4);
+      *reinterpret_cast<uint4*>(to) = make_uint4(pack16<kBf16>(y[0], y[1]), pack16<kBf16>(y[2], y[3]),
+                                                 pack16<kBf16>(y[4], y[5]), pack16<kBf16>(y[6], y[7]));
     }
-    *reinterpret_cast<uint4*>(
-        dst + ((r.first + (pos - start)) * stride + (uint64_t)u.head * kDim + col) * 2) =
-        make_uint4(w[0], w[1], w[2], w[3]);
+    to += kRows * stride * 2;
   }
 }
 

@@ -120,18 +120,47 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// Two codes (the low 16 bits) to floats; both formats are exact in fp16.
+// Four codes to two pairs of fp16.  int8: u = code + 128 behind fp16's exponent of 1024 is
+// 1024 + u, from which 1152 leaves the code, all exact.
 template <bool kE4m3>
-__device__ __forceinline__ float2 decode2(uint32_t x) {
+__device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {
   if (kE4m3) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffff), __NV_E4M3);
-    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+    const __half2_raw x = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
+    const __half2_raw y = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    *lo = (uint32_t)x.x | (uint32_t)x.y << 16;
+    *hi = (uint32_t)y.x | (uint32_t)y.y << 16;
+  } else {
+    const uint32_t u = w ^ 0x80808080u, p = __byte_perm(u, 0x64646464u, 0x4140),
+                   q = __byte_perm(u, 0x64646464u, 0x4342);
+    const uint32_t k1152 = 0x64806480u;
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&p),
+                              *reinterpret_cast<const __half2*>(&k1152));
+    const __half2 y = __hsub2(*reinterpret_cast<const __half2*>(&q),
+                              *reinterpret_cast<const __half2*>(&k1152));
+    *lo = *reinterpret_cast<const uint32_t*>(&x);
+    *hi = *reinterpret_cast<const uint32_t*>(&y);
   }
-  return make_float2((float)(signed char)(x & 0xff), (float)(signed char)((x >> 8) & 0xff));
 }
+
+// Four codes times a factor.
 template <bool kE4m3>
-__device__ __forceinline__ uint32_t encode2(float a, float b) {
-  if (kE4m3) return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-  const int x = max(-127, min(127, __float2int_rn(a))), y = max(-127, min(127, __float2int_rn(b)));
-  return (uint32_t)(x & 0xff) | (uint32_t)(y & 0xff) << 8;
+__device__ __forceinline__ void decode4(uint32_t w, float by, float* x) {
+  uint32_t lo, hi;
+  widen<kE4m3>(w, &lo, &hi);
+  const float2 a = unpack16<false>(lo), b = unpack16<false>(hi);
+  x[0] = a.x * by, x[1] = a.y * by, x[2] = b.x * by, x[3] = b.y * by;
+}
+
+// Four values over their scale, which are not above the format's largest by more than rounding,
+// to codes.  int8: 1.5 * 2^23 + x has rn(x) in its low bits, two's complement.
+template <bool kE4m3>
+__device__ __forceinline__ uint32_t encode4(const float* x) {
+  if constexpr (kE4m3)
+    return __nv_cvt_float2_to_fp8x2(make_float2(x[0], x[1]), __NV_SATFINITE, __NV_E4M3) |
+           (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2], x[3]), __NV_SATFINITE, __NV_E4M3)
+               << 16;
+  uint32_t c[4] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(__fadd_rn(x[i], 12582912.f));
+  return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
 }
