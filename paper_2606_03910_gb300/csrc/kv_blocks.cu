@@ -239,7 +239,8 @@ netkv_status blocks_call(const netkv_kv_pages* pages, uint32_t dtype, const void
 }
 
 // ------------------------------------------------------------------ eviction
-constexpr uint32_t kEvictThreads = 512;
+// One block of threads a sequence, a thread per eight neighbouring entries, 1,024 at most.
+constexpr uint32_t kEvictPer = 8, kEvictMost = 1024, kBins = 2048;
 
 // Weights in the order of unsigned keys; NaN above every number, the two zeros alike.
 __device__ __forceinline__ uint32_t weight_key(float x) {
@@ -262,10 +263,9 @@ struct EvictArgs {
   int* status;
 };
 
-// Exclusive sum over the block of two counts at once (16 bits would not hold a chunk's worth of
-// both, so two words); every thread gets its own sums and the totals.
+// Exclusive sums over the block of two counts; every thread gets its own and the totals.
 __device__ __forceinline__ uint2 block_scan(uint2 x, uint2* total, uint2* scratch) {
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, warps = blockDim.x / 32;
   uint2 y = x;
 #pragma unroll
   for (int d = 1; d < 32; d *= 2) {
@@ -275,105 +275,125 @@ __device__ __forceinline__ uint2 block_scan(uint2 x, uint2* total, uint2* scratc
   __syncthreads();  // scratch of an earlier call has been read
   if (lane == 31) scratch[warp] = y;
   __syncthreads();
-  uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
-#pragma unroll
-  for (uint32_t w = 0; w < kEvictThreads / 32; ++w) {
-    const uint2 s = scratch[w];
-    if (w < warp) before.x += s.x, before.y += s.y;
-    all.x += s.x, all.y += s.y;
-  }
-  *total = all;
+  const uint2 z = lane < warps ? scratch[lane] : make_uint2(0, 0);
+  const uint2 before = make_uint2(__reduce_add_sync(~0u, lane < warp ? z.x : 0),
+                                  __reduce_add_sync(~0u, lane < warp ? z.y : 0));
+  *total = make_uint2(__reduce_add_sync(~0u, z.x), __reduce_add_sync(~0u, z.y));
   return make_uint2(before.x + y.x - x.x, before.y + y.y - x.y);
 }
 
-// One block a sequence.  The evicted blocks are the `gone` smallest of the open ones by
-// (key, index): four passes of a byte each over the keys find the largest evicted key and how
-// many of its equals go, and one ordered pass packs what stays and what goes.
-__global__ void __launch_bounds__(kEvictThreads) evict_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint2 scratch[kEvictThreads / 32];
+// The evicted blocks are the `gone` smallest of the open ones by (key, index): three passes over
+// 11, 11 and 10 bits of the keys find the largest evicted key and how many of its equals go (11
+// bits spread positive weights of one magnitude over 8 bins, where bytes would meet in one),
+// and one pass in order packs what stays and what goes.  Rows of up to 8 entries a thread are
+// read once and stay in registers.  Bound by its round trips: the load, three histograms, a
+// scan; 8,192 entries are 64 KB.
+__global__ void __launch_bounds__(kEvictMost) evict_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint2 scratch[kEvictMost / 32];
   __shared__ uint32_t picked[2];
-  const uint32_t seq = blockIdx.x, tid = threadIdx.x;
+  const uint32_t seq = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
   const uint64_t row = (uint64_t)seq * a.width;
-  const uint32_t len = a.len[seq];
+  const uint32_t len = a.len[seq], budget = a.budget[seq];
   uint32_t n = len / kBlockTokens + (len % kBlockTokens != 0);
   if (n > a.width) {
     if (tid == 0) flag_status(a.status, NETKV_DEV_ERANGE);
     n = a.width;
   }
-  const uint64_t held = max((uint64_t)a.budget[seq], (uint64_t)a.sink + a.recent);
+  const uint64_t held = max((uint64_t)budget, (uint64_t)a.sink + a.recent);
   const uint32_t gone = n > held ? n - (uint32_t)held : 0;
   const uint32_t lo = gone ? a.sink : 0, hi = gone ? n - a.recent : 0;  // open: [lo, hi)
 
+  const uint32_t chunk = threads * kEvictPer, chunks = (n + chunk - 1) / chunk;
+  float mass[kEvictPer];
+  auto read = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t j = 0; j < kEvictPer; ++j) {
+      const uint32_t i = c * chunk + tid * kEvictPer + j;
+      mass[j] = i < n ? a.mass[row + i] : 0.f;
+    }
+  };
+  if (chunks) read(0);
   uint32_t prefix = 0, left = gone;  // of the keys that begin with prefix, `left` go
   if (gone) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (uint32_t i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+      for (uint32_t i = tid; i < kBins; i += threads) hist[i] = 0;
       __syncthreads();
-      for (uint32_t i = lo + tid; i < hi; i += kEvictThreads) {
-        const uint32_t key = weight_key(a.mass[row + i]);
-        if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))
-          atomicAdd(&hist[(key >> shift) & 255], 1u);
+      for (uint32_t c = 0; c < chunks; ++c) {
+        if (chunks > 1) read(c);
+#pragma unroll
+        for (uint32_t j = 0; j < kEvictPer; ++j) {
+          const uint32_t i = c * chunk + tid * kEvictPer + j, key = weight_key(mass[j]);
+          if (i >= lo && i < hi && (pass == 0 || key >> above == prefix >> above))
+            atomicAdd(&hist[(key >> shift) & (pass == 2 ? 1023 : 2047)], 1u);
+        }
       }
       __syncthreads();
-      if (tid < 32) {
-        uint32_t c[8], sum = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += c[j] = hist[tid * 8 + j];
-        uint32_t upto = sum;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-          const uint32_t x = __shfl_up_sync(~0u, upto, d);
-          if (tid >= (uint32_t)d) upto += x;
-        }
-        uint32_t before = upto - sum;
-        if (before < left && left <= upto) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (before < left && left <= before + c[j]) {
-              picked[0] = tid * 8 + j;
-              picked[1] = left - before;
-            }
-            before += c[j];
+      const uint32_t per = kBins / threads;  // 2 .. 16 bins a thread
+      uint32_t sum = 0;
+      for (uint32_t j = 0; j < per; ++j) sum += hist[tid * per + j];
+      uint2 total;
+      uint32_t before = block_scan(make_uint2(sum, 0), &total, scratch).x;
+      if (before < left && left <= before + sum)
+        for (uint32_t j = 0; j < per; ++j) {
+          const uint32_t x = hist[tid * per + j];
+          if (before < left && left <= before + x) {
+            picked[0] = tid * per + j;
+            picked[1] = left - before;
           }
+          before += x;
         }
-      }
       __syncthreads();
       prefix |= picked[0] << shift;
       left = picked[1];
     }
   }
-  uint32_t out = 0, equal = 0;  // evicted and equal to the last key so far
-  for (uint32_t base = 0; base < a.width; base += kEvictThreads) {
-    const uint32_t i = base + tid;
-    const bool in = i < n, open = i >= lo && i < hi;
-    const float m = in ? a.mass[row + i] : 0.f;
-    const int32_t page = in ? a.table[row + i] : -1;
-    const uint32_t key = open ? weight_key(m) : 0;
-    const bool same = open && key == prefix, less = open && key < prefix;
-    uint2 total;
-    const uint2 before = block_scan(make_uint2(less, same), &total, scratch);
-    const uint32_t same_before = equal + before.y;
-    // those of `equal` that went are the first `left` of them
-    const uint32_t gone_before = out + before.x + min(same_before, left);
-    if (in) {
-      if (less || (same && same_before < left)) {
-        a.freed[row + gone_before] = page;
-      } else {
-        a.table_out[row + i - gone_before] = page;
-        a.mass_out[row + i - gone_before] = m;
+  uint32_t out = 0, equal = 0;  // evicted and equal to the last key in earlier chunks
+  for (uint32_t c = 0; c < chunks; ++c) {
+    if (chunks > 1) read(c);
+    const uint32_t first = c * chunk + tid * kEvictPer;
+    int32_t page[kEvictPer];
+    uint32_t less = 0, same = 0;  // bits by entry
+#pragma unroll
+    for (uint32_t j = 0; j < kEvictPer; ++j) {
+      const uint32_t i = first + j, key = weight_key(mass[j]);
+      page[j] = i < n ? a.table[row + i] : -1;
+      if (i >= lo && i < hi) {
+        less |= (uint32_t)(key < prefix) << j;
+        same |= (uint32_t)(key == prefix) << j;
       }
+    }
+    uint2 total, before = block_scan(make_uint2(__popc(less), __popc(same)), &total, scratch);
+    before.x += out;
+    before.y += equal;
+#pragma unroll
+    for (uint32_t j = 0; j < kEvictPer; ++j) {
+      const uint32_t i = first + j;
+      // those equal that went are the first `left` of them
+      const uint32_t went = before.x + min(before.y, left);
+      const bool l = less >> j & 1, e = same >> j & 1;
+      if (i < n) {
+        if (l || (e && before.y < left)) {
+          a.freed[row + went] = page[j];
+        } else {
+          a.table_out[row + i - went] = page[j];
+          a.mass_out[row + i - went] = mass[j];
+        }
+      }
+      before.x += l;
+      before.y += e;
     }
     out += total.x;
     equal += total.y;
   }
   // the tails: entries past what stays and past what goes
-  for (uint32_t i = tid; i < a.width; i += kEvictThreads) {
-    if (i >= n - gone) a.table_out[row + i] = -1, a.mass_out[row + i] = 0.f;
-    if (i >= gone) a.freed[row + i] = -1;
-  }
+  for (uint32_t i = n - gone + tid; i < a.width; i += threads)
+    a.table_out[row + i] = -1, a.mass_out[row + i] = 0.f;
+  for (uint32_t i = gone + tid; i < a.width; i += threads) a.freed[row + i] = -1;
   if (tid == 0) {
-    a.len_out[seq] = (uint32_t)min((uint64_t)len, (uint64_t)n * kBlockTokens) - gone * kBlockTokens;
+    a.len_out[seq] =
+        (uint32_t)min((uint64_t)len, (uint64_t)n * kBlockTokens) - gone * kBlockTokens;
     a.n_freed[seq] = gone;
   }
 }
@@ -419,6 +439,8 @@ extern "C" netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table,
     return NETKV_EINVAL;
   const EvictArgs a = {d_table,     d_len,     d_mass,     d_budget, table_width, sink,    recent,
                        d_table_out, d_len_out, d_mass_out, d_freed,  d_n_freed,   d_status};
-  evict_kernel<<<n_seqs, kEvictThreads, 0, (cudaStream_t)stream>>>(a);
+  unsigned threads = 128;
+  while (threads < kEvictMost && (uint64_t)threads * kEvictPer < table_width) threads *= 2;
+  evict_kernel<<<n_seqs, threads, 0, (cudaStream_t)stream>>>(a);
   return netkv_launch_status();
 }
