@@ -240,7 +240,7 @@ netkv_status blocks_call(const netkv_kv_pages* pages, uint32_t dtype, const void
 
 // ------------------------------------------------------------------ eviction
 // One block of threads a sequence, a thread per eight neighbouring entries, 1,024 at most.
-constexpr uint32_t kEvictPer = 8, kEvictMost = 1024, kBins = 2048;
+constexpr uint32_t kEvictPer = 8, kEvictMost = 1024;
 
 // Weights in the order of unsigned keys; NaN above every number, the two zeros alike.
 __device__ __forceinline__ uint32_t weight_key(float x) {
@@ -282,19 +282,53 @@ __device__ __forceinline__ uint2 block_scan(uint2 x, uint2* total, uint2* scratc
   return make_uint2(before.x + y.x - x.x, before.y + y.y - x.y);
 }
 
+// One pass of the selection: 11 bits of the keys as 64 groups of 32 bins.
+struct Bins {
+  uint32_t group[64], bin[2048];
+};
+
+// The bin in which the left-th key lies, and how many of its keys are up to that one; found by
+// each warp for itself.
+__device__ __forceinline__ uint2 find_bin(const Bins& h, uint32_t left) {
+  const uint32_t lane = threadIdx.x & 31;
+  const uint32_t x = h.group[2 * lane], y = h.group[2 * lane + 1];
+  uint32_t upto = x + y;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const uint32_t z = __shfl_up_sync(~0u, upto, d);
+    if (lane >= (uint32_t)d) upto += z;
+  }
+  const int at = __ffs(__ballot_sync(~0u, left <= upto)) - 1;  // there is one
+  const uint32_t before = __shfl_sync(~0u, upto - x - y, at), first = __shfl_sync(~0u, x, at);
+  const bool second = left - before > first;
+  left -= before + (second ? first : 0);
+  const uint32_t group = 2 * at + second, mine = h.bin[group * 32 + lane];
+  upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const uint32_t z = __shfl_up_sync(~0u, upto, d);
+    if (lane >= (uint32_t)d) upto += z;
+  }
+  const int in = __ffs(__ballot_sync(~0u, left <= upto)) - 1;
+  return make_uint2(group * 32 + in, left - __shfl_sync(~0u, upto - mine, in));
+}
+
 // The evicted blocks are the `gone` smallest of the open ones by (key, index): three passes over
 // 11, 11 and 10 bits of the keys find the largest evicted key and how many of its equals go (11
 // bits spread positive weights of one magnitude over 8 bins, where bytes would meet in one),
-// and one pass in order packs what stays and what goes.  Rows of up to 8 entries a thread are
-// read once and stay in registers.  Bound by its round trips: the load, three histograms, a
-// scan; 8,192 entries are 64 KB.
+// and one pass in order packs what stays and what goes.  Bound by its round trips, one after
+// another: the lengths, the entries, three histograms, a scan, the writes; 8,192 entries are
+// 64 KB.  Rows of up to 8 entries a thread (kOne) are read once, stay in registers, and are packed
+// in shared memory, from which whole lines are written.
+template <bool kOne>
 __global__ void __launch_bounds__(kEvictMost) evict_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ uint32_t hist[kBins];
+  extern __shared__ uint32_t pack[];  // kOne: pages, then weights, of what stays; pages that went
+  __shared__ Bins bins[3];
   __shared__ uint2 scratch[kEvictMost / 32];
-  __shared__ uint32_t picked[2];
   const uint32_t seq = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
   const uint64_t row = (uint64_t)seq * a.width;
   const uint32_t len = a.len[seq], budget = a.budget[seq];
+  for (uint32_t i = tid; i < sizeof(bins) / 4; i += threads) reinterpret_cast<uint32_t*>(bins)[i] = 0;
   uint32_t n = len / kBlockTokens + (len % kBlockTokens != 0);
   if (n > a.width) {
     if (tid == 0) flag_status(a.status, NETKV_DEV_ERANGE);
@@ -304,61 +338,63 @@ __global__ void __launch_bounds__(kEvictMost) evict_kernel(const __grid_constant
   const uint32_t gone = n > held ? n - (uint32_t)held : 0;
   const uint32_t lo = gone ? a.sink : 0, hi = gone ? n - a.recent : 0;  // open: [lo, hi)
 
-  const uint32_t chunk = threads * kEvictPer, chunks = (n + chunk - 1) / chunk;
+  const uint32_t chunk = threads * kEvictPer, chunks = kOne ? 1 : (n + chunk - 1) / chunk;
   float mass[kEvictPer];
-  auto read = [&](uint32_t c) {
+  int32_t page[kEvictPer];
+  auto read_mass = [&](uint32_t c) {
 #pragma unroll
     for (uint32_t j = 0; j < kEvictPer; ++j) {
       const uint32_t i = c * chunk + tid * kEvictPer + j;
       mass[j] = i < n ? a.mass[row + i] : 0.f;
     }
   };
-  if (chunks) read(0);
+  auto read_pages = [&](uint32_t c) {
+#pragma unroll
+    for (uint32_t j = 0; j < kEvictPer; ++j) {
+      const uint32_t i = c * chunk + tid * kEvictPer + j;
+      page[j] = i < n ? a.table[row + i] : -1;
+    }
+  };
+  if (kOne) {
+    read_mass(0);
+    read_pages(0);
+  }
+  __syncthreads();
   uint32_t prefix = 0, left = gone;  // of the keys that begin with prefix, `left` go
   if (gone) {
+#pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
-      for (uint32_t i = tid; i < kBins; i += threads) hist[i] = 0;
-      __syncthreads();
+      constexpr int kShift[3] = {21, 10, 0};
+      const int shift = kShift[pass], above = pass == 0 ? 31 : kShift[pass - 1];
       for (uint32_t c = 0; c < chunks; ++c) {
-        if (chunks > 1) read(c);
+        if (!kOne) read_mass(c);
 #pragma unroll
         for (uint32_t j = 0; j < kEvictPer; ++j) {
           const uint32_t i = c * chunk + tid * kEvictPer + j, key = weight_key(mass[j]);
-          if (i >= lo && i < hi && (pass == 0 || key >> above == prefix >> above))
-            atomicAdd(&hist[(key >> shift) & (pass == 2 ? 1023 : 2047)], 1u);
+          if (i >= lo && i < hi && (pass == 0 || key >> above == prefix >> above)) {
+            const uint32_t b = (key >> shift) & (pass == 2 ? 1023 : 2047);
+            atomicAdd(&bins[pass].bin[b], 1u);
+            atomicAdd(&bins[pass].group[b / 32], 1u);
+          }
         }
       }
       __syncthreads();
-      const uint32_t per = kBins / threads;  // 2 .. 16 bins a thread
-      uint32_t sum = 0;
-      for (uint32_t j = 0; j < per; ++j) sum += hist[tid * per + j];
-      uint2 total;
-      uint32_t before = block_scan(make_uint2(sum, 0), &total, scratch).x;
-      if (before < left && left <= before + sum)
-        for (uint32_t j = 0; j < per; ++j) {
-          const uint32_t x = hist[tid * per + j];
-          if (before < left && left <= before + x) {
-            picked[0] = tid * per + j;
-            picked[1] = left - before;
-          }
-          before += x;
-        }
-      __syncthreads();
-      prefix |= picked[0] << shift;
-      left = picked[1];
+      const uint2 f = find_bin(bins[pass], left);
+      prefix |= f.x << shift;
+      left = f.y;
     }
   }
+  const uint32_t stay = n - gone;
   uint32_t out = 0, equal = 0;  // evicted and equal to the last key in earlier chunks
   for (uint32_t c = 0; c < chunks; ++c) {
-    if (chunks > 1) read(c);
-    const uint32_t first = c * chunk + tid * kEvictPer;
-    int32_t page[kEvictPer];
+    if (!kOne) {
+      read_mass(c);
+      read_pages(c);
+    }
     uint32_t less = 0, same = 0;  // bits by entry
 #pragma unroll
     for (uint32_t j = 0; j < kEvictPer; ++j) {
-      const uint32_t i = first + j, key = weight_key(mass[j]);
-      page[j] = i < n ? a.table[row + i] : -1;
+      const uint32_t i = c * chunk + tid * kEvictPer + j, key = weight_key(mass[j]);
       if (i >= lo && i < hi) {
         less |= (uint32_t)(key < prefix) << j;
         same |= (uint32_t)(key == prefix) << j;
@@ -369,12 +405,15 @@ __global__ void __launch_bounds__(kEvictMost) evict_kernel(const __grid_constant
     before.y += equal;
 #pragma unroll
     for (uint32_t j = 0; j < kEvictPer; ++j) {
-      const uint32_t i = first + j;
+      const uint32_t i = c * chunk + tid * kEvictPer + j;
       // those equal that went are the first `left` of them
       const uint32_t went = before.x + min(before.y, left);
-      const bool l = less >> j & 1, e = same >> j & 1;
+      const bool l = less >> j & 1, e = same >> j & 1, goes = l || (e && before.y < left);
       if (i < n) {
-        if (l || (e && before.y < left)) {
+        if (kOne) {
+          pack[goes ? stay + went : i - went] = (uint32_t)page[j];
+          if (!goes) pack[n + i - went] = __float_as_uint(mass[j]);
+        } else if (goes) {
           a.freed[row + went] = page[j];
         } else {
           a.table_out[row + i - went] = page[j];
@@ -387,10 +426,18 @@ __global__ void __launch_bounds__(kEvictMost) evict_kernel(const __grid_constant
     out += total.x;
     equal += total.y;
   }
-  // the tails: entries past what stays and past what goes
-  for (uint32_t i = n - gone + tid; i < a.width; i += threads)
-    a.table_out[row + i] = -1, a.mass_out[row + i] = 0.f;
-  for (uint32_t i = gone + tid; i < a.width; i += threads) a.freed[row + i] = -1;
+  if (kOne) {
+    __syncthreads();
+    for (uint32_t i = tid; i < a.width; i += threads) {
+      a.table_out[row + i] = i < stay ? (int32_t)pack[i] : -1;
+      a.mass_out[row + i] = i < stay ? __uint_as_float(pack[n + i]) : 0.f;
+      a.freed[row + i] = i < gone ? (int32_t)pack[stay + i] : -1;
+    }
+  } else {  // the tails: entries past what stays and past what goes
+    for (uint32_t i = stay + tid; i < a.width; i += threads)
+      a.table_out[row + i] = -1, a.mass_out[row + i] = 0.f;
+    for (uint32_t i = gone + tid; i < a.width; i += threads) a.freed[row + i] = -1;
+  }
   if (tid == 0) {
     a.len_out[seq] =
         (uint32_t)min((uint64_t)len, (uint64_t)n * kBlockTokens) - gone * kBlockTokens;
@@ -441,6 +488,11 @@ extern "C" netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table,
                        d_table_out, d_len_out, d_mass_out, d_freed,  d_n_freed,   d_status};
   unsigned threads = 128;
   while (threads < kEvictMost && (uint64_t)threads * kEvictPer < table_width) threads *= 2;
-  evict_kernel<<<n_seqs, threads, 0, (cudaStream_t)stream>>>(a);
+  if (table_width <= kEvictMost * kEvictPer) {
+    NETKV_CUDA_TRY(allow_shared<evict_kernel<true>>(kEvictMost * kEvictPer * 8));
+    evict_kernel<true><<<n_seqs, threads, table_width * 8, (cudaStream_t)stream>>>(a);
+  } else {
+    evict_kernel<false><<<n_seqs, threads, 0, (cudaStream_t)stream>>>(a);
+  }
   return netkv_launch_status();
 }

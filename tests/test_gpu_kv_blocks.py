@@ -328,6 +328,14 @@ def test_evict_ties_and_special_weights(netkv, kind):
     check_evict(netkv, [width * 16] * 3, width, [700, 20, 1299], 3, 5, mass.astype(np.float32))
 
 
+@pytest.mark.parametrize("width", [8192, 8193, 20001])
+def test_evict_long_tables(netkv, width):
+    """Rows at and past what one block of threads holds at a time."""
+    rng = np.random.default_rng(width)
+    mass = rng.choice(np.exp(rng.standard_normal(width // 3)), (3, width)).astype(np.float32)
+    check_evict(netkv, [width * 16, width * 16 - 9, 77], width, [width // 2, 30, 9], 4, 16, mass)
+
+
 def test_evict_refusals_and_long_lengths(netkv):
     t = ints(range(4)).view(1, 4)
     m = torch.ones((1, 4), device="cuda")
