@@ -151,6 +151,7 @@ class KvPages(C.Structure):
                          k.shape[0], k.shape[1], k.shape[3], _KV_FORMATS[fmt])
         self.tensors = (k, v, k_scale, v_scale)
         self.ref = C.byref(self)
+        self.heads_dim = (k.shape[1], k.shape[3])  # a field of a structure takes longer to read
 
 
 NETKV_BLOCK_TOKENS = 16
@@ -181,9 +182,15 @@ def _ptr(x) -> Optional[int]:
     return int(x.data_ptr())
 
 
+_torch = None
+
+
 def current_stream() -> Optional[int]:
     """torch's current CUDA stream, or None before CUDA is initialised."""
-    import torch
+    global _torch
+    if _torch is None:
+        import torch as _torch  # once: an import statement takes 0.3 us a call
+    torch = _torch
     if not torch.cuda.is_initialized():
         return None
     # the raw handle, without a Stream object around it (1.6 -> 0.4 us a call)
@@ -440,14 +447,18 @@ def _code(t) -> int:
 
 def _rows(t, heads: int, dim: int, code: Optional[int] = None):
     """(dtype code, address, row stride) of rows [rows, heads, dim]; a row is contiguous."""
-    c = _code(t)
-    if c != NETKV_BF16 and c != NETKV_F16:
+    c = _CODES.get(t.dtype)
+    if c is None:
+        c = _code(t)
+    if c > NETKV_BF16 or c < 0:
         raise TypeError(f"float16 or bfloat16 rows expected, got {t.dtype}")
     if code is not None and c != code:
         raise TypeError("tensors of one dtype expected")
     n, h, d = t.shape
     if h != heads or d != dim:
         raise ValueError(f"rows of {(heads, dim)} expected, got {(h, d)}")
+    if t.is_contiguous():
+        return c, t.data_ptr(), h * d
     s, sh, sd = t.stride()
     if (sd != 1 and d > 1) or (sh != d and h > 1):
         raise ValueError("a row's heads have to lie one after another")
@@ -458,7 +469,7 @@ def _ints(t, code: int, n: int) -> Optional[int]:
     """The address of a contiguous integer tensor of n entries."""
     if t is None:
         return None
-    if _code(t) != code:
+    if _CODES.get(t.dtype) != code and _code(t) != code:
         raise TypeError(f"{32 if code == _I32 else 64}-bit integers expected, got {t.dtype}")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"a contiguous tensor of {n} entries expected, got {tuple(t.shape)}")
@@ -476,34 +487,36 @@ def _plane(t, rows: int, width: int) -> Optional[int]:
     """The address of a contiguous fp32 tensor of that shape."""
     if t is None:
         return None
-    if _code(t) != _F32:
+    if _CODES.get(t.dtype) != _F32 and _code(t) != _F32:
         raise TypeError(f"float32 tensor expected, got {t.dtype}")
     if t.shape != (rows, width) or not t.is_contiguous():
         raise ValueError(f"a contiguous tensor of {(rows, width)} expected, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _kv_move(fn: str, pages: KvPages, k, v, off, start, table, status, stream) -> None:
-    heads, dim = pages.kv_heads, pages.head_dim
+def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, stream) -> None:
+    heads, dim = pages.heads_dim
     dt, kp, ks = _rows(k, heads, dim)
     _, vp, vs = _rows(v, heads, dim, dt)
-    rows = k.shape[0]
-    if v.shape[0] != rows:
+    rows = len(k)
+    if len(v) != rows:
         raise ValueError("as many rows of keys as of values expected")
-    n = off.numel() - 1
+    n = len(off) - 1
     tp, tw = _table(table, n)
-    _check(fn, getattr(_lib, fn)(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
-                                 _ints(start, _I32, n), tp, tw, _ptr(status), _stream(stream)))
+    code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
+                _ints(start, _I32, n), tp, tw, _ptr(status), _stream(stream))
+    if code:
+        raise NetKVError(fn, code)
 
 
 def netkv_kv_store(pages: KvPages, k, v, off, start, table, status=None, stream=None) -> None:
     """New tokens into 8-bit blocks: rows k, v [rows, kv_heads, dim]; see include/netkv.h."""
-    _kv_move("netkv_kv_store", pages, k, v, off, start, table, status, stream)
+    _kv_move("netkv_kv_store", _lib.netkv_kv_store, pages, k, v, off, start, table, status, stream)
 
 
 def netkv_kv_load(pages: KvPages, k, v, off, start, table, status=None, stream=None) -> None:
     """Tokens from 8-bit blocks into the rows k, v; see include/netkv.h."""
-    _kv_move("netkv_kv_load", pages, k, v, off, start, table, status, stream)
+    _kv_move("netkv_kv_load", _lib.netkv_kv_load, pages, k, v, off, start, table, status, stream)
 
 
 def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=None,
@@ -537,7 +550,7 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     """One query row a sequence over its blocks: q, out [n_seqs, heads, dim]; see
     include/netkv.h."""
     n, heads, dim = q.shape
-    dt, qp, qs = _rows(q, heads, pages.head_dim)
+    dt, qp, qs = _rows(q, heads, pages.heads_dim[1])
     _, op, os_ = _rows(out, heads, dim, dt)
     if out.shape[0] != n:
         raise ValueError("as many rows of out as of q expected")
