@@ -25,7 +25,10 @@ namespace {
 
 constexpr uint32_t kWarps = 4;
 constexpr uint32_t kThreads = kWarps * 32 + 32;  // and a warp for the loads
-constexpr uint32_t kCtas = 304;     // two blocks an SM on 152 SMs
+// Blocks of the grid: three an SM on 152 SMs, two where a second tile of heads takes the registers.
+template <int kTiles>
+constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
+constexpr uint32_t kMostCtas = 456;
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
 constexpr uint32_t kMinPages = 8;   // a block's run at least: two pages a warp
@@ -46,10 +49,11 @@ struct DecodeArgs {
   float* lse;
   const float* mass_in;
   float* mass_out;
-  float* part_o;    // [kCtas][2][kTiles * 8][kDim]
-  float* part_ml;   // [kCtas][2][kTiles * 8][2]
+  float* part_o;    // [ctas][2][kTiles * 8][kDim]
+  float* part_ml;   // [ctas][2][kTiles * 8][2]
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
+  uint32_t ctas;
   int* status;
 };
 
@@ -95,7 +99,7 @@ __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, uint32_t units) {
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
   r.total = sum * units;
-  r.ctas = (uint32_t)min((uint64_t)kCtas, max((uint64_t)1, r.total / kMinPages));
+  r.ctas = (uint32_t)min((uint64_t)a.ctas, max((uint64_t)1, r.total / kMinPages));
   return r;
 }
 
@@ -178,7 +182,7 @@ struct Shared {
   static constexpr uint32_t kRing = kStages<kDim>;
   static constexpr int kGroupFloats = 16 * kHeads + 8;  // of 16 dims; the 8 spread the banks
   alignas(128) unsigned char ring[kWarps][kRing][2][2][kBlockTokens * kDim];
-  float o[kWarps][kDim / 16 * kGroupFloats];
+  float o[kWarps / 2][kDim / 16 * kGroupFloats];
   float m[kWarps][kHeads], l[kWarps][kHeads];
   alignas(16) float2 scale[kWarps][kRing][2];  // of keys and values
   uint2 tokens[kWarps][kRing];                 // of each page; 0 where it is absent
@@ -308,7 +312,7 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
 }
 
 template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass>
-__global__ void __launch_bounds__(kThreads, 2) decode_kernel(const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   using Sh = Shared<kDim, kTiles>;
   Sh& sh = *reinterpret_cast<Sh*>(smem);
@@ -559,29 +563,56 @@ __global__ void __launch_bounds__(kThreads, 2) decode_kernel(const __grid_consta
           sh.m[warp][t * 8 + 2 * c + j] = m[t][j];
           sh.l[warp][t * 8 + 2 * c + j] = l[t][j];
         }
+      }
+    sync_warps();
+    // to one maximum; then two warps' sums through shared memory onto the other two's
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int h = t * 8 + 2 * c + j;
+        float top = sh.m[0][h];
+#pragma unroll
+        for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][h]);
+        const float by = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top) * v_unit;
 #pragma unroll
         for (int x = 0; x < kDim / 16; ++x)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t dim = r * (kDim / 8) + 2 * x + i;
-            sh.o[warp][dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + t * 8 + 2 * c + j] =
-                o[t][x][2 * i + j] * v_unit;
-          }
+          for (int i = 0; i < 2; ++i) o[t][x][2 * i + j] *= by;
       }
-    sync_warps();
+    auto place = [&](int t, int j, int x, int i) -> float& {
+      const uint32_t dim = r * (kDim / 8) + 2 * x + i;
+      return sh.o[warp % 2][dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + t * 8 + 2 * c + j];
+    };
+#pragma unroll
+    for (int half = 1; half >= 0; --half) {
+      if (warp / 2 == half) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int x = 0; x < kDim / 16; ++x)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                float& z = place(t, j, x, i);
+                z = half ? o[t][x][2 * i + j] : z + o[t][x][2 * i + j];
+              }
+      }
+      sync_warps();
+    }
     for (uint32_t x = tid; x < kHeads * kDim; x += kWarps * 32) {
       const uint32_t h = x / kDim, dim = x % kDim;
       if (head0 + h >= a.group) break;
       float top = sh.m[0][h];
 #pragma unroll
       for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][h]);
-      float sum = 0.f, all = 0.f;
+      float sum = 0.f;
 #pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w) {
-        const float y = sh.m[w][h] == -INFINITY ? 0.f : ex2(sh.m[w][h] - top);
-        sum += y * sh.l[w][h];
-        all += y * sh.o[w][dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + h];
-      }
+      for (uint32_t w = 0; w < kWarps; ++w)
+        sum += sh.m[w][h] == -INFINITY ? 0.f * sh.l[w][h] : ex2(sh.m[w][h] - top) * sh.l[w][h];
+      const uint32_t at = dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + h;
+      const float all = sh.o[0][at] + sh.o[1][at];
       const uint32_t head = kv_head * a.group + head0 + h;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -622,12 +653,12 @@ __global__ void __launch_bounds__(kThreads, 2) decode_kernel(const __grid_consta
 // Joins the segments that runs share: one block a (boundary between runs, head of the unit),
 // where the boundary is the first inside its segment.  The parts' weights first, then eight
 // groups of threads (a thread has four dims) over every eighth part: a long sequence alone on
-// the card has a part from each run, 304 for one unit.
+// the card has a part from each run, 456 for one unit.
 constexpr uint32_t kJoin = 256;
 template <int kDim, int kTiles, bool kBf16, bool kMass>
 __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int kHeads = kTiles * 8, kLanes = kDim / 4, kGroups = kJoin / kLanes;
-  __shared__ float weight[kCtas], reduce[kJoin / 32][2];
+  __shared__ float weight[kCtas<kTiles>], reduce[kJoin / 32][2];
   __shared__ float4 sums[kGroups][kLanes];
   const uint32_t units = a.kv.heads * a.chunks, tid = threadIdx.x, h = blockIdx.y;
   let_follow();
@@ -743,7 +774,7 @@ struct Workspace {
 Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, uint32_t width,
                     bool mass) {
   auto up = [](size_t x) { return (x + 127) / 128 * 128; };
-  const size_t rows = (size_t)kCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
+  const size_t rows = (size_t)kMostCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
   Workspace w;
   w.part_ml = up(rows * p->head_dim * 4);
   w.lse2 = w.part_ml + up(rows * 8);
@@ -802,6 +833,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         (float*)(w + ws.part_ml),
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
+                        per == 8 ? kCtas<1> : kCtas<2>,
                         d_status};
   const cudaStream_t s = (cudaStream_t)stream;
   auto go = [&](auto dim, auto tiles, auto bf, auto e4, auto mass) -> netkv_status {
@@ -810,10 +842,10 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     constexpr auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
     constexpr int bytes = (int)sizeof(Shared<kDim, kTiles>);
     NETKV_CUDA_TRY(allow_shared<kernel>(bytes));
-    kernel<<<kCtas, kThreads, bytes, s>>>(a);
+    kernel<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
     NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,
-                                    dim3(kCtas - 1, min(group, per)), kJoin, s, a));
+                                    dim3(kCtas<kTiles> - 1, min(group, per)), kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
