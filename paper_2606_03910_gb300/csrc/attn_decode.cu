@@ -31,11 +31,14 @@ constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
 constexpr uint32_t kMostCtas = 456;
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
-constexpr uint32_t kMinPages = 8;   // a block's run at least: two pages a warp
+constexpr uint32_t kEdge = 8;       // see Runs
+constexpr uint32_t kMinPages = 16;  // a block's run at least: a pair of pages a warp, and an edge
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
 // weights up to 2^8 are as exact in fp16 as those up to 1, and sums are fp32.
 constexpr float kLag = 8.f;
+
+struct Cut;
 
 struct DecodeArgs {
   KvArgs kv;
@@ -51,6 +54,7 @@ struct DecodeArgs {
   float* mass_out;
   float* part_o;    // [ctas][2][kTiles * 8][kDim]
   float* part_ml;   // [ctas][2][kTiles * 8][2]
+  Cut* cuts;        // [ctas - 1]
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
   uint32_t ctas;
@@ -84,53 +88,107 @@ __device__ __forceinline__ uint32_t tokens_of(const DecodeArgs& a, uint32_t seq)
   return (uint32_t)min((uint64_t)a.len[seq], (uint64_t)a.width * kBlockTokens);
 }
 
-// The runs: `total` pages over `ctas` blocks.
-struct Runs {
-  uint64_t total;
-  uint32_t ctas;
-  __device__ __forceinline__ uint64_t start(uint32_t c) const { return total * c / ctas; }
+__device__ __forceinline__ uint64_t div_floor(uint64_t x, uint64_t y) {
+  return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
+}
+
+// The pages of the first 128 sequences, lane l's 4 l .. 4 l + 3: read once a warp.
+struct Lens {
+  uint32_t n[4];
+  __device__ __forceinline__ explicit Lens(const DecodeArgs& a) {
+    const uint32_t i = (threadIdx.x & 31) * 4;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) n[j] = i + j < a.n_seqs ? pages_of(a, i + j) : 0;
+  }
 };
 
-__device__ __forceinline__ Runs runs_of(const DecodeArgs& a, uint32_t units) {
-  const uint32_t lane = threadIdx.x & 31;
+// The runs: equal parts of a line on which every segment (a sequence and a unit: a KV head and a
+// chunk of its query heads) takes kEdge places, what it costs to begin and end one in pages, and
+// one for each page.
+struct Runs {
+  uint64_t total, base;
+  uint32_t ctas, rest;
+  __device__ __forceinline__ uint64_t start(uint32_t c) const { return base * c + min(c, rest); }
+  // the first run that starts at `end` (up to total) or after it
+  __device__ __forceinline__ uint32_t until(uint64_t end) const {
+    const uint64_t longer = (base + 1) * rest;
+    return end <= longer ? (uint32_t)div_floor(end + base, base + 1)
+                         : rest + (uint32_t)div_floor(end - longer + base - 1, base);
+  }
+};
+
+__device__ __forceinline__ uint64_t places(uint32_t pages) { return pages ? pages + kEdge : 0; }
+
+__device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, uint32_t units) {
   uint64_t sum = 0;
-  for (uint32_t i = lane; i < a.n_seqs; i += 32) sum += pages_of(a, i);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum += places(lens.n[j]);
+  for (uint32_t i = 128 + (threadIdx.x & 31); i < a.n_seqs; i += 32) sum += places(pages_of(a, i));
 #pragma unroll
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
   r.total = sum * units;
   r.ctas = (uint32_t)min((uint64_t)a.ctas, max((uint64_t)1, r.total / kMinPages));
+  r.base = div_floor(r.total, r.ctas);
+  r.rest = (uint32_t)(r.total - r.base * r.ctas);
   return r;
 }
 
-// A segment: pages [first, first + count) of one (sequence, unit); a unit is a KV head and a
-// chunk of its query heads.
+// A segment and a run's part of it: pages [first, first + count) of a sequence's `pages`.
 struct Segment {
   uint32_t seq, unit, first, count, pages;
 };
 
-__device__ __forceinline__ Segment segment_at(const DecodeArgs& a, uint32_t units, uint64_t item) {
+// The segment at a place of the line, and how far into it the place is.
+__device__ __forceinline__ Segment segment_at(const DecodeArgs& a, const Lens& lens, uint32_t units,
+                                              uint64_t at, uint64_t* into) {
   const uint32_t lane = threadIdx.x & 31;
-  for (uint32_t base = 0; base < a.n_seqs; base += 32) {
-    const uint32_t i = base + lane, n = i < a.n_seqs ? pages_of(a, i) : 0;
-    const uint64_t mine = (uint64_t)n * units;
+  for (uint32_t from = 0; from < a.n_seqs; from += 128) {
+    uint32_t n[4];
+    uint64_t mine = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint32_t i = from + lane * 4 + j;
+      n[j] = from == 0 ? lens.n[j] : i < a.n_seqs ? pages_of(a, i) : 0;
+      mine += places(n[j]) * units;
+    }
     uint64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const uint64_t x = __shfl_up_sync(~0u, upto, d);
       if (lane >= (uint32_t)d) upto += x;
     }
-    const uint32_t hit = __ballot_sync(~0u, item < upto);
+    const uint32_t hit = __ballot_sync(~0u, at < upto);
     if (hit) {
-      const int at = __ffs(hit) - 1;
-      const uint64_t rest = __shfl_sync(~0u, item - (upto - mine), at);
-      const uint32_t pages = __shfl_sync(~0u, n, at);
-      return {base + at, (uint32_t)(rest / pages), (uint32_t)(rest % pages), 0, pages};
+      const int who = __ffs(hit) - 1;
+      uint64_t rest = at - (upto - mine);
+      uint32_t j = 0, pages = n[0];
+#pragma unroll
+      for (uint32_t q = 0; q < 3; ++q)
+        if (j == q && rest >= places(n[q]) * units) {
+          rest -= places(n[q]) * units;
+          j = q + 1;
+          pages = n[q + 1];
+        }
+      rest = __shfl_sync(~0u, rest, who);
+      pages = __shfl_sync(~0u, pages, who);
+      const uint32_t seq = __shfl_sync(~0u, from + lane * 4 + j, who);
+      const uint64_t unit = div_floor(rest, places(pages));
+      *into = rest - unit * places(pages);
+      return {seq, (uint32_t)unit, 0, 0, pages};
     }
-    item -= __shfl_sync(~0u, upto, 31);
+    at -= __shfl_sync(~0u, upto, 31);
   }
+  *into = 0;
   return {a.n_seqs, 0, 0, 0, 0};
 }
+
+// A boundary before a run, for the join: where it is inside a segment (parts > 0), that segment
+// has parts from the runs run0, run0 + 1, ...; of the first of them it is the second or a later
+// one (`second`) or the first; and `order` numbers the segment's boundaries.
+struct Cut {
+  uint32_t seq, unit, parts, run0, order, second;
+};
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) {
   return (uint32_t)__cvta_generic_to_shared(p);
@@ -193,27 +251,46 @@ struct Shared {
 // The segments of one run, in order.
 struct Walk {
   Segment s;
-  uint64_t left;  // pages from s on
-  __device__ __forceinline__ void start(const DecodeArgs& a, uint32_t units, const Runs& runs) {
+  uint64_t left;  // places from s on
+  __device__ __forceinline__ void take(uint64_t into) {
+    const uint64_t end = min(into + left, places(s.pages));
+    left -= end - into;
+    s.first = into > kEdge ? (uint32_t)(into - kEdge) : 0;
+    s.count = end > kEdge ? (uint32_t)(end - kEdge) - s.first : 0;
+  }
+  // s.count = 0: no (more) segments
+  __device__ __forceinline__ void start(const DecodeArgs& a, const Lens& lens, uint32_t units,
+                                        const Runs& runs, Cut* cut) {
+    s.count = 0;
+    cut->parts = 0;
+    if (blockIdx.x >= runs.ctas) return;
     const uint64_t first = runs.start(blockIdx.x);
     left = runs.start(blockIdx.x + 1) - first;
     if (left == 0) return;
-    s = segment_at(a, units, first);
-    s.count = (uint32_t)min((uint64_t)(s.pages - s.first), left);
+    uint64_t into;
+    s = segment_at(a, lens, units, first, &into);
+    if (blockIdx.x && into > kEdge) {
+      const uint64_t begin = first - into;
+      cut->seq = s.seq;
+      cut->unit = s.unit;
+      cut->run0 = runs.until(begin + kEdge + 1) - 1;
+      cut->parts = runs.until(begin + places(s.pages)) - cut->run0;
+      cut->order = blockIdx.x - cut->run0 - 1;
+      cut->second = runs.start(cut->run0) < begin;
+    }
+    take(into);
   }
   __device__ __forceinline__ void next(const DecodeArgs& a, uint32_t units) {
-    left -= s.count;
+    s.count = 0;
     if (left == 0) return;
-    s.first = 0;
     if (++s.unit == units) {
       s.unit = 0;
       do {
-        ++s.seq;
-        s.pages = s.seq < a.n_seqs ? pages_of(a, s.seq) : 1;
+        if (++s.seq >= a.n_seqs) return;  // lengths that changed under the call
+        s.pages = pages_of(a, s.seq);
       } while (s.pages == 0);
-      if (s.seq >= a.n_seqs) left = 0;  // lengths that changed under the call
     }
-    s.count = (uint32_t)min((uint64_t)s.pages, left);
+    take(0);
   }
 };
 
@@ -231,20 +308,21 @@ struct Batch {
 // so that a ring's place is filled as soon as it is free.
 template <int kDim, int kTiles>
 __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTiles>& sh,
-                                           uint32_t units, const Runs& runs) {
+                                           const Lens& lens, uint32_t units, const Runs& runs) {
   constexpr uint32_t kRing = kStages<kDim>, kPart = kBlockTokens * kDim;
   const uint32_t lane = threadIdx.x & 31;
   volatile int* late = &sh.late;
   Walk walk;
-  walk.start(a, units, runs);
+  Cut unused;
+  walk.start(a, lens, units, runs, &unused);
   uint32_t at = 0;  // pages of the present segment that batches have
   auto take = [&]() {
     Batch b = {0, 0, 0, -1, make_float2(0.f, 0.f)};
-    if (walk.left && at == walk.s.count) {
+    if (walk.s.count && at == walk.s.count) {
       walk.next(a, units);
       at = 0;
     }
-    if (walk.left == 0) return b;
+    if (walk.s.count == 0) return b;
     b.count = min(walk.s.count - at, 32u);
     b.kv_head = walk.s.unit / a.chunks;
     if (lane < b.count) {
@@ -330,16 +408,18 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid == 0) sh.late = 0;
-  const Runs runs = runs_of(a, units);
+  const Lens lens(a);
+  const Runs runs = runs_of(a, lens, units);
   __syncthreads();
   volatile int* late = &sh.late;
   if (warp == kWarps) {
-    if (blockIdx.x < runs.ctas) load_pages<kDim, kTiles>(a, sh, units, runs);
+    load_pages<kDim, kTiles>(a, sh, lens, units, runs);
     return;
   }
   Walk walk;
-  walk.left = 0;
-  if (blockIdx.x < runs.ctas) walk.start(a, units, runs);
+  Cut cut;
+  walk.start(a, lens, units, runs, &cut);
+  if (tid == 0 && blockIdx.x) a.cuts[blockIdx.x - 1] = cut;
 
   // Queries of a segment: thread (r, c) has head r of each tile, dims by 16 bytes of codes:
   // 64 h + 16 c + 4 i + 0..3 in step 4 h + i.  Read ahead of their segment.
@@ -356,10 +436,10 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
         raw[t][i] = h < a.group ? src[(i / 2) * 8 + c * 2 + i % 2] : make_uint4(0, 0, 0, 0);
     }
   };
-  if (walk.left) load_queries();
+  if (walk.s.count) load_queries();
   uint32_t taken = 0;  // pairs of all segments
   bool first_segment = true;
-  while (walk.left) {
+  while (walk.s.count) {
     const Segment seg = walk.s;
     const uint32_t kv_head = seg.unit / a.chunks, head0 = seg.unit % a.chunks * kHeads;
     const uint32_t all_pairs = (seg.count + 1) / 2;
@@ -552,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
     // ---- the warps' sums
     const bool whole = seg.count == seg.pages;
     walk.next(a, units);
-    if (walk.left) load_queries();
+    if (walk.s.count) load_queries();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -650,78 +730,68 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
   if (tid == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
 }
 
-// Joins the segments that runs share: one block a (boundary between runs, head of the unit),
-// where the boundary is the first inside its segment.  The parts' weights first, then eight
-// groups of threads (a thread has four dims) over every eighth part: a long sequence alone on
-// the card has a part from each run, 456 for one unit.
-constexpr uint32_t kJoin = 256;
+// Joins the segments that runs share: one block of threads a boundary.  The boundaries of a
+// segment share its heads; a head's parts are spread over the block's warps that have it (all 16
+// for one head: a long sequence alone on the card has 456 parts; two for each of eight where a
+// segment is cut once), a lane has kDim / 32 dims, and their sums are added in the warps' order.
+constexpr uint32_t kJoin = 512;
 template <int kDim, int kTiles, bool kBf16, bool kMass>
 __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ DecodeArgs a) {
-  constexpr int kHeads = kTiles * 8, kLanes = kDim / 4, kGroups = kJoin / kLanes;
-  __shared__ float weight[kCtas<kTiles>], reduce[kJoin / 32][2];
-  __shared__ float4 sums[kGroups][kLanes];
-  const uint32_t units = a.kv.heads * a.chunks, tid = threadIdx.x, h = blockIdx.y;
+  constexpr uint32_t kHeads = kTiles * 8, kJoinWarps = kJoin / 32, kPer = kDim / 32;
+  __shared__ float sums[kJoinWarps][kDim];
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   let_follow();
-  const Runs runs = runs_of(a, units);
-  const uint32_t cut = blockIdx.x + 1;
-  if (cut >= runs.ctas) return;
-  const Segment s = segment_at(a, units, runs.start(cut));
-  const uint64_t at = runs.start(cut) - s.first;  // the segment's first page
-  if (s.first == 0 || (cut > 1 && runs.start(cut - 1) > at)) return;
-  const uint32_t head0 = s.unit % a.chunks * kHeads;
-  if (head0 + h >= a.group) return;
-  const uint64_t end = at + s.pages;
-  // runs that start before the end, less those before cut - 1
-  const uint32_t parts =
-      (uint32_t)min((uint64_t)runs.ctas, (end * runs.ctas + runs.total - 1) / runs.total) - (cut - 1);
-  const uint32_t second = runs.start(cut - 1) < at;  // the segment is that run's last one
-  auto slot = [&](uint32_t i) {
-    return ((uint64_t)(cut - 1 + i) * 2 + (i == 0 ? second : 0)) * kHeads + h;
-  };
   follow();
-  float top = -INFINITY, sum = 0.f;
-  for (uint32_t i = tid; i < parts; i += kJoin) top = fmaxf(top, a.part_ml[slot(i) * 2]);
+  const Cut s = a.cuts[blockIdx.x];
+  const uint32_t joiners = min(s.parts - 1, kHeads);
+  if (s.parts == 0 || s.order >= joiners) return;
+  const uint32_t heads = (kHeads - s.order + joiners - 1) / joiners;  // of this block
+  uint32_t spread = 1;
+  while (spread < heads) spread *= 2;
+  const uint32_t each = kJoinWarps / spread;  // warps of a head
+  const uint32_t h = s.order + warp % spread * joiners, head0 = s.unit % a.chunks * kHeads;
+  const bool real = h < kHeads && head0 + h < a.group;
+  auto slot = [&](uint32_t i) {
+    return ((uint64_t)(s.run0 + i) * 2 + (i == 0 ? s.second : 0)) * kHeads + h;
+  };
+  float top = -INFINITY, sum = 0.f, o[kPer] = {};
+  if (real) {
+    for (uint32_t i = lane; i < s.parts; i += 32) top = fmaxf(top, a.part_ml[slot(i) * 2]);
 #pragma unroll
-  for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  if (tid % 32 == 0) reduce[tid / 32][0] = top;
-  __syncthreads();
-  top = reduce[0][0];
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    for (uint32_t i = lane; i < s.parts; i += 32) {
+      const float m = a.part_ml[slot(i) * 2], l = a.part_ml[slot(i) * 2 + 1];
+      // a part of NaN scores has no maximum, but its sum says so
+      sum += m == -INFINITY ? 0.f * l : ex2(m - top) * l;
+    }
 #pragma unroll
-  for (int w = 1; w < (int)kJoin / 32; ++w) top = fmaxf(top, reduce[w][0]);
-  for (uint32_t i = tid; i < parts; i += kJoin) {
-    const float m = a.part_ml[slot(i) * 2], l = a.part_ml[slot(i) * 2 + 1];
-    const float w = m == -INFINITY ? 0.f : ex2(m - top);
-    weight[i] = w;
-    // a part of NaN scores has no maximum, but its sum says so
-    sum += m == -INFINITY && l == l ? 0.f : w * l;
+    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+#pragma unroll 8
+    for (uint32_t i = warp / spread; i < s.parts; i += each) {
+      const float m = a.part_ml[slot(i) * 2], w = m == -INFINITY ? 0.f : ex2(m - top);
+      const float* x = a.part_o + slot(i) * kDim + lane * kPer;
+      if constexpr (kPer == 4) {
+        const float4 y = *reinterpret_cast<const float4*>(x);
+        o[0] += w * y.x, o[1] += w * y.y, o[2] += w * y.z, o[3] += w * y.w;
+      } else {
+        const float2 y = *reinterpret_cast<const float2*>(x);
+        o[0] += w * y.x, o[1] += w * y.y;
+      }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) sums[warp][lane * kPer + i] = o[i];
   }
-#pragma unroll
-  for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
-  if (tid % 32 == 0) reduce[tid / 32][1] = sum;
   __syncthreads();
-  sum = 0.f;
+  if (warp >= spread || !real) return;
+  for (uint32_t w = 1; w < each; ++w)
 #pragma unroll
-  for (int w = 0; w < (int)kJoin / 32; ++w) sum += reduce[w][1];
-  const uint32_t lane = tid % kLanes, group = tid / kLanes;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (uint32_t i = group; i < parts; i += kGroups) {
-    const float4 x = reinterpret_cast<const float4*>(a.part_o + slot(i) * kDim)[lane];
-    const float w = weight[i];
-    o.x += w * x.x, o.y += w * x.y, o.z += w * x.z, o.w += w * x.w;
-  }
-  sums[group][lane] = o;
-  __syncthreads();
-  if (group) return;
-#pragma unroll
-  for (int g = 1; g < kGroups; ++g) {
-    const float4 x = sums[g][lane];
-    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
-  }
+    for (uint32_t i = 0; i < kPer; ++i) o[i] += sums[warp + w * spread][lane * kPer + i];
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const uint32_t head = s.unit / a.chunks * a.group + head0 + h;
-  reinterpret_cast<uint2*>(a.out + (s.seq * a.out_stride + (uint64_t)head * kDim) * 2)[lane] =
-      make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
+  uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (s.seq * a.out_stride + (uint64_t)head * kDim) * 2);
+#pragma unroll
+  for (uint32_t i = 0; i < kPer; i += 2)
+    to[lane * (kPer / 2) + i / 2] = pack16<kBf16>(o[i] * inv, o[i + 1] * inv);
   if (lane == 0) {
     const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
     if (a.lse) a.lse[(uint64_t)s.seq * a.heads + head] = z * kLn2;
@@ -769,7 +839,7 @@ bool sizes_ok(const netkv_kv_pages* pages, uint32_t n_seqs, uint32_t heads, uint
 int tiles_of(uint32_t group) { return group <= 8 ? 1 : 2; }
 
 struct Workspace {
-  size_t part_ml, lse2, block2, total;  // part_o is at 0
+  size_t part_ml, cuts, lse2, block2, total;  // part_o is at 0
 };
 Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, uint32_t width,
                     bool mass) {
@@ -777,7 +847,8 @@ Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, ui
   const size_t rows = (size_t)kMostCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
   Workspace w;
   w.part_ml = up(rows * p->head_dim * 4);
-  w.lse2 = w.part_ml + up(rows * 8);
+  w.cuts = w.part_ml + up(rows * 8);
+  w.lse2 = w.cuts + up(kMostCtas * sizeof(Cut));
   w.block2 = w.lse2 + (mass ? up((size_t)n_seqs * heads * 4) : 0);
   w.total = w.block2 + (mass ? (size_t)n_seqs * width * heads * 4 : 0);
   return w;
@@ -831,6 +902,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         d_mass_out,
                         (float*)w,
                         (float*)(w + ws.part_ml),
+                        (Cut*)(w + ws.cuts),
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
                         per == 8 ? kCtas<1> : kCtas<2>,
@@ -845,7 +917,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     kernel<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
     NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,
-                                    dim3(kCtas<kTiles> - 1, min(group, per)), kJoin, s, a));
+                                    kCtas<kTiles> - 1, kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
