@@ -241,7 +241,7 @@ struct Shared {
   static constexpr int kGroupFloats = 16 * kHeads + 8;  // of 16 dims; the 8 spread the banks
   alignas(128) unsigned char ring[kWarps][kRing][2][2][kBlockTokens * kDim];
   float o[kWarps / 2][kDim / 16 * kGroupFloats];
-  float m[kWarps][kHeads], l[kWarps][kHeads];
+  float m[kWarps][kHeads], l[kWarps][kHeads], top[kHeads], sum[kHeads];
   alignas(16) float2 scale[kWarps][kRing][2];  // of keys and values
   uint2 tokens[kWarps][kRing];                 // of each page; 0 where it is absent
   alignas(8) uint64_t full[kWarps][kRing], empty[kWarps][kRing];
@@ -645,6 +645,16 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
         }
       }
     sync_warps();
+    if (tid < kHeads) {
+      float top = sh.m[0][tid], sum = 0.f;
+#pragma unroll
+      for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][tid]);
+#pragma unroll
+      for (uint32_t w = 0; w < kWarps; ++w)
+        sum += sh.m[w][tid] == -INFINITY ? 0.f * sh.l[w][tid] : ex2(sh.m[w][tid] - top) * sh.l[w][tid];
+      sh.top[tid] = top;
+      sh.sum[tid] = sum;
+    }
     // to one maximum; then two warps' sums through shared memory onto the other two's
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -684,13 +694,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
     for (uint32_t x = tid; x < kHeads * kDim; x += kWarps * 32) {
       const uint32_t h = x / kDim, dim = x % kDim;
       if (head0 + h >= a.group) break;
-      float top = sh.m[0][h];
-#pragma unroll
-      for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][h]);
-      float sum = 0.f;
-#pragma unroll
-      for (uint32_t w = 0; w < kWarps; ++w)
-        sum += sh.m[w][h] == -INFINITY ? 0.f * sh.l[w][h] : ex2(sh.m[w][h] - top) * sh.l[w][h];
+      const float top = sh.top[h], sum = sh.sum[h];
       const uint32_t at = dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + h;
       const float all = sh.o[0][at] + sh.o[1][at];
       const uint32_t head = kv_head * a.group + head0 + h;
@@ -756,26 +760,52 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ Dec
   };
   float top = -INFINITY, sum = 0.f, o[kPer] = {};
   if (real) {
-    for (uint32_t i = lane; i < s.parts; i += 32) top = fmaxf(top, a.part_ml[slot(i) * 2]);
+    // loads of several parts are under way at a time: each is a round trip to L2
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+    for (uint32_t i = 0; i < s.parts; i += 128) {
+      float2 x[4];
 #pragma unroll
-    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-    for (uint32_t i = lane; i < s.parts; i += 32) {
-      const float m = a.part_ml[slot(i) * 2], l = a.part_ml[slot(i) * 2 + 1];
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint32_t at = i + j * 32 + lane;
+        x[j] = at < s.parts ? ml[slot(at)] : make_float2(-INFINITY, 0.f);
+      }
+      float to = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), top);
+#pragma unroll
+      for (int d = 16; d; d /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, d));
+      sum = top == -INFINITY ? sum : sum * ex2(top - to);
       // a part of NaN scores has no maximum, but its sum says so
-      sum += m == -INFINITY ? 0.f * l : ex2(m - top) * l;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        sum += x[j].x == -INFINITY ? 0.f * x[j].y : ex2(x[j].x - to) * x[j].y;
+      top = to;
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
-#pragma unroll 8
-    for (uint32_t i = warp / spread; i < s.parts; i += each) {
-      const float m = a.part_ml[slot(i) * 2], w = m == -INFINITY ? 0.f : ex2(m - top);
-      const float* x = a.part_o + slot(i) * kDim + lane * kPer;
-      if constexpr (kPer == 4) {
-        const float4 y = *reinterpret_cast<const float4*>(x);
-        o[0] += w * y.x, o[1] += w * y.y, o[2] += w * y.z, o[3] += w * y.w;
-      } else {
-        const float2 y = *reinterpret_cast<const float2*>(x);
-        o[0] += w * y.x, o[1] += w * y.y;
+    for (uint32_t i = warp / spread; i < s.parts; i += 8 * each) {
+      float m[8], x[8][kPer];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        const uint32_t at = i + j * each;
+        const bool in = at < s.parts;
+        m[j] = in ? ml[slot(at)].x : -INFINITY;
+#pragma unroll
+        for (uint32_t q = 0; q < kPer; ++q) x[j][q] = 0.f;
+        if (in) {
+          const float* from = a.part_o + slot(at) * kDim + lane * kPer;
+          if constexpr (kPer == 4) {
+            const float4 y = *reinterpret_cast<const float4*>(from);
+            x[j][0] = y.x, x[j][1] = y.y, x[j][2] = y.z, x[j][3] = y.w;
+          } else {
+            const float2 y = *reinterpret_cast<const float2*>(from);
+            x[j][0] = y.x, x[j][1] = y.y;
+          }
+        }
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        const float w = m[j] == -INFINITY ? 0.f : ex2(m[j] - top);
+#pragma unroll
+        for (uint32_t q = 0; q < kPer; ++q) o[q] += w * x[j][q];
       }
     }
 #pragma unroll
@@ -799,18 +829,49 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ Dec
   }
 }
 
-// A block's weight over all heads, in the heads' order: one thread a block.
-__global__ void __launch_bounds__(128) mass_kernel(const __grid_constant__ DecodeArgs a) {
-  const uint32_t seq = blockIdx.x, pages = pages_of(a, seq);
+// A block's weight over all heads: its heads' parts are neighbours, a lane each (two or more
+// lanes' worth above 32 heads, several blocks a warp up to 16), added in one order.
+constexpr uint32_t kMassWarps = 8, kMassSteps = 8;
+__global__ void __launch_bounds__(kMassWarps * 32) mass_kernel(const __grid_constant__ DecodeArgs a) {
+  const uint32_t seq = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const uint32_t pages = pages_of(a, seq);
+  uint32_t lanes = 32;  // of a block
+  while (lanes / 2 >= a.heads) lanes /= 2;
+  const uint32_t per = 32 / lanes, head = lane % lanes;
   follow();
-  for (uint32_t block = blockIdx.y * 128 + threadIdx.x; block < pages; block += gridDim.y * 128) {
-    const uint64_t at = (uint64_t)seq * a.width + block;
-    float sum = 0.f;
-    for (uint32_t h = 0; h < a.heads; ++h) {
-      const float b = a.block2[at * a.heads + h];
-      if (b != -INFINITY) sum += ex2(b - a.lse2[(uint64_t)seq * a.heads + h]);
+  const float* lse2 = a.lse2 + (uint64_t)seq * a.heads;
+  float z[4];  // the first 128 heads'
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j) z[j] = head + j * 32 < a.heads ? lse2[head + j * 32] : 0.f;
+  for (uint32_t from = blockIdx.y * kMassWarps * kMassSteps * per; from < pages;
+       from += gridDim.y * kMassWarps * kMassSteps * per) {
+    float sum[kMassSteps] = {};
+#pragma unroll
+    for (uint32_t q = 0; q < kMassSteps; ++q) {
+      const uint32_t block = from + (q * kMassWarps + warp) * per + lane / lanes;
+      const float* part = a.block2 + ((uint64_t)seq * a.width + block) * a.heads;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint32_t h = head + j * 32;
+        if (block < pages && h < a.heads) {
+          const float b = part[h];
+          sum[q] += b == -INFINITY ? 0.f : ex2(b - z[j]);
+        }
+      }
+      for (uint32_t h = head + 128; h < a.heads && block < pages; h += 32) {
+        const float b = part[h];
+        sum[q] += b == -INFINITY ? 0.f : ex2(b - lse2[h]);
+      }
     }
-    a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum;
+#pragma unroll
+    for (uint32_t q = 0; q < kMassSteps; ++q) {
+      for (uint32_t d = lanes / 2; d; d /= 2) sum[q] += __shfl_xor_sync(~0u, sum[q], d);
+      const uint32_t block = from + (q * kMassWarps + warp) * per + lane / lanes;
+      if (head == 0 && block < pages) {
+        const uint64_t at = (uint64_t)seq * a.width + block;
+        a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum[q];
+      }
+    }
   }
 }
 
@@ -939,7 +1000,8 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                                    : widths(std::integral_constant<int, 2>());
   if (st != NETKV_OK) return st;
   if (d_mass_out)
-    NETKV_CUDA_TRY(launch_following(mass_kernel, dim3(n_seqs, min((table_width + 127) / 128, 1024u)),
-                                    128, s, a));
+    NETKV_CUDA_TRY(launch_following(
+        mass_kernel, dim3(n_seqs, min((table_width + kMassWarps * kMassSteps - 1) / (kMassWarps * kMassSteps), 1024u)),
+        kMassWarps * 32, s, a));
   return netkv_launch_status();
 }
