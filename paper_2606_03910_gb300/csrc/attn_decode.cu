@@ -28,7 +28,7 @@ constexpr uint32_t kThreads = kWarps * 32 + 32;  // and a warp for the loads
 // Blocks of the grid: three an SM on 152 SMs, two where a second tile of heads takes the registers.
 template <int kTiles>
 constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
-constexpr uint32_t kMostCtas = 456;
+constexpr uint32_t kOwnSegments = 456;  // see own_runs
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
 constexpr uint32_t kEdge = 8;       // see Runs
@@ -52,12 +52,12 @@ struct DecodeArgs {
   float* lse;
   const float* mass_in;
   float* mass_out;
-  float* part_o;    // [ctas][2][kTiles * 8][kDim]
-  float* part_ml;   // [ctas][2][kTiles * 8][2]
-  Cut* cuts;        // [ctas - 1]
+  float* part_o;    // [runs][2][kTiles * 8][kDim]
+  float* part_ml;   // [runs][2][kTiles * 8][2]
+  Cut* cuts;        // [runs - 1]
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
-  uint32_t ctas;
+  uint32_t most_runs;
   int* status;
 };
 
@@ -107,7 +107,7 @@ struct Lens {
 // one for each page.
 struct Runs {
   uint64_t total, base;
-  uint32_t ctas, rest;
+  uint32_t count, rest;
   __device__ __forceinline__ uint64_t start(uint32_t c) const { return base * c + min(c, rest); }
   // the first run that starts at `end` (up to total) or after it
   __device__ __forceinline__ uint32_t until(uint64_t end) const {
@@ -119,6 +119,7 @@ struct Runs {
 
 __device__ __forceinline__ uint64_t places(uint32_t pages) { return pages ? pages + kEdge : 0; }
 
+template <bool kOwn>
 __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, uint32_t units) {
   uint64_t sum = 0;
 #pragma unroll
@@ -128,9 +129,10 @@ __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, u
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
   r.total = sum * units;
-  r.ctas = (uint32_t)min((uint64_t)a.ctas, max((uint64_t)1, r.total / kMinPages));
-  r.base = div_floor(r.total, r.ctas);
-  r.rest = (uint32_t)(r.total - r.base * r.ctas);
+  // a warp's own run is long enough not to cut many short segments
+  r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / (kOwn ? 32 : kMinPages)));
+  r.base = div_floor(r.total, r.count);
+  r.rest = (uint32_t)(r.total - r.base * r.count);
   return r;
 }
 
@@ -260,22 +262,23 @@ struct Walk {
   }
   // s.count = 0: no (more) segments
   __device__ __forceinline__ void start(const DecodeArgs& a, const Lens& lens, uint32_t units,
-                                        const Runs& runs, Cut* cut) {
+                                        const Runs& runs, uint32_t run, Cut* cut) {
     s.count = 0;
+    left = 0;
     cut->parts = 0;
-    if (blockIdx.x >= runs.ctas) return;
-    const uint64_t first = runs.start(blockIdx.x);
-    left = runs.start(blockIdx.x + 1) - first;
+    if (run >= runs.count) return;
+    const uint64_t first = runs.start(run);
+    left = runs.start(run + 1) - first;
     if (left == 0) return;
     uint64_t into;
     s = segment_at(a, lens, units, first, &into);
-    if (blockIdx.x && into > kEdge) {
+    if (run && into > kEdge) {
       const uint64_t begin = first - into;
       cut->seq = s.seq;
       cut->unit = s.unit;
       cut->run0 = runs.until(begin + kEdge + 1) - 1;
       cut->parts = runs.until(begin + places(s.pages)) - cut->run0;
-      cut->order = blockIdx.x - cut->run0 - 1;
+      cut->order = run - cut->run0 - 1;
       cut->second = runs.start(cut->run0) < begin;
     }
     take(into);
@@ -294,8 +297,14 @@ struct Walk {
   }
 };
 
-// 32 pages on their way into the ring: lane j has page j, counted from the 2 * pair-th of a
-// segment's.
+// The run of a block's warp: the block's, or (kOwn) the warp's own.
+template <bool kOwn>
+__device__ __forceinline__ uint32_t run_of(uint32_t warp) {
+  return kOwn ? warp * gridDim.x + blockIdx.x : blockIdx.x;
+}
+
+// Pages on their way into the ring, a lane each: 32 of the block's segment, or (kOwn) 8 of each
+// warp's.
 struct Batch {
   uint32_t count;  // pages; 0: none left
   uint32_t kv_head, tokens;
@@ -303,18 +312,25 @@ struct Batch {
   float2 scale;
 };
 
-// The loading warp: pairs of neighbouring pages, one pair after another to the four warps.  The
-// table's entries are read two batches ahead and the scales one, over the ends of segments too,
-// so that a ring's place is filled as soon as it is free.
-template <int kDim, int kTiles>
+// The loading warp: pairs of neighbouring pages.  Of a block's run they go to the four warps in
+// turn; of the warps' own runs (kOwn), eight lanes serve a warp each.  The table's entries are
+// read two batches ahead and the scales one, over the ends of segments too, so that a ring's
+// place is filled as soon as it is free.
+template <int kDim, int kTiles, bool kOwn>
 __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTiles>& sh,
                                            const Lens& lens, uint32_t units, const Runs& runs) {
   constexpr uint32_t kRing = kStages<kDim>, kPart = kBlockTokens * kDim;
-  const uint32_t lane = threadIdx.x & 31;
+  constexpr uint32_t kLanes = kOwn ? 32 / kWarps : 32;  // of a batch
+  const uint32_t lane = threadIdx.x & 31, in = lane % kLanes;
   volatile int* late = &sh.late;
   Walk walk;
   Cut unused;
-  walk.start(a, lens, units, runs, &unused);
+#pragma unroll
+  for (uint32_t w = 0; w < (kOwn ? kWarps : 1); ++w) {
+    Walk x;
+    x.start(a, lens, units, runs, run_of<kOwn>(w), &unused);
+    if (w == lane / kLanes) walk = x;
+  }
   uint32_t at = 0;  // pages of the present segment that batches have
   auto take = [&]() {
     Batch b = {0, 0, 0, -1, make_float2(0.f, 0.f)};
@@ -323,10 +339,10 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
       at = 0;
     }
     if (walk.s.count == 0) return b;
-    b.count = min(walk.s.count - at, 32u);
+    b.count = min(walk.s.count - at, kLanes);
     b.kv_head = walk.s.unit / a.chunks;
-    if (lane < b.count) {
-      const uint32_t block = walk.s.first + at + lane;
+    if (in < b.count) {
+      const uint32_t block = walk.s.first + at + in;
       b.page = a.table[(uint64_t)walk.s.seq * a.width + block];
       b.tokens = min(tokens_of(a, walk.s.seq) - block * kBlockTokens, kBlockTokens);
     }
@@ -334,7 +350,7 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
     return b;
   };
   auto scales = [&](Batch& b) {
-    if (lane >= b.count) return;
+    if (in >= b.count) return;
     if (b.page < 0 || (uint32_t)b.page >= a.kv.n_pages) {
       flag_status(a.status, NETKV_DEV_ERANGE);
       b.page = -1;
@@ -344,20 +360,18 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
     const uint64_t part = (uint64_t)b.page * a.kv.heads + b.kv_head;
     b.scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
   };
-  uint32_t given[kWarps] = {};  // pairs that each warp was given
+  // the warp that a lane's pages go to, and the pairs that it was given
+  const uint32_t w = kOwn ? lane / kLanes : lane / 2 % kWarps, step = kOwn ? 1 : kWarps;
+  const uint32_t turn = in / 2 / step;  // of the batch's pairs for that warp
+  uint32_t given = 0;
   Batch b0 = take(), b1 = take();
   scales(b0);
   scales(b1);
-  while (b0.count) {
+  while (__any_sync(~0u, b0.count)) {
     const Batch b2 = take();
-    const uint32_t w = lane / 2 % kWarps, pairs = (b0.count + 1) / 2;
-    uint32_t n = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kWarps; ++i)
-      if (i == w) n = given[i];
-    n += lane / 2 / kWarps;
+    const uint32_t pairs = (b0.count + 1) / 2, n = given + turn;
     for (uint32_t q = 0; q < 32 / (2 * kWarps); ++q) {  // a pair for each warp
-      if (lane / (2 * kWarps) == q && lane / 2 < pairs) {
+      if (turn == q && in / 2 < pairs) {
         const uint32_t st = n % kRing, bar = smem_addr(&sh.full[w][st]);
         if (n >= kRing) wait(smem_addr(&sh.empty[w][st]), (n / kRing - 1) & 1, late);
         if (b0.page >= 0) {
@@ -381,15 +395,14 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
       }
       __syncwarp();
     }
-#pragma unroll
-    for (uint32_t i = 0; i < kWarps; ++i) given[i] += (pairs + kWarps - 1 - i) / kWarps;
+    given += kOwn ? pairs : (pairs + kWarps - 1 - w) / kWarps;
     b0 = b1;
     b1 = b2;
     scales(b1);
   }
 }
 
-template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass>
+template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass, bool kOwn>
 __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   using Sh = Shared<kDim, kTiles>;
@@ -409,17 +422,18 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
   }
   if (tid == 0) sh.late = 0;
   const Lens lens(a);
-  const Runs runs = runs_of(a, lens, units);
+  const Runs runs = runs_of<kOwn>(a, lens, units);
   __syncthreads();
   volatile int* late = &sh.late;
   if (warp == kWarps) {
-    load_pages<kDim, kTiles>(a, sh, lens, units, runs);
+    load_pages<kDim, kTiles, kOwn>(a, sh, lens, units, runs);
     return;
   }
   Walk walk;
   Cut cut;
-  walk.start(a, lens, units, runs, &cut);
-  if (tid == 0 && blockIdx.x) a.cuts[blockIdx.x - 1] = cut;
+  const uint32_t run = run_of<kOwn>(warp);
+  walk.start(a, lens, units, runs, run, &cut);
+  if (run && (kOwn ? lane : tid) == 0) a.cuts[run - 1] = cut;
 
   // Queries of a segment: thread (r, c) has head r of each tile, dims by 16 bytes of codes:
   // 64 h + 16 c + 4 i + 0..3 in step 4 h + i.  Read ahead of their segment.
@@ -443,7 +457,8 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
     const Segment seg = walk.s;
     const uint32_t kv_head = seg.unit / a.chunks, head0 = seg.unit % a.chunks * kHeads;
     const uint32_t all_pairs = (seg.count + 1) / 2;
-    const uint32_t pairs = all_pairs > warp ? (all_pairs - warp + kWarps - 1) / kWarps : 0;
+    const uint32_t pairs =
+        kOwn ? all_pairs : all_pairs > warp ? (all_pairs - warp + kWarps - 1) / kWarps : 0;
     uint32_t q[kTiles][kSteps][2];
     float f[kTiles][2];
 #pragma unroll
@@ -480,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
       const uint32_t st = taken % kRing;
       wait(smem_addr(&sh.full[warp][st]), (taken / kRing) & 1, late);
       ++taken;
-      const uint32_t at = 2 * (warp + kWarps * i), block = seg.first + at;
+      const uint32_t at = 2 * (kOwn ? i : warp + kWarps * i), block = seg.first + at;
       const uint2 nn = sh.tokens[warp][st];
       const uint32_t n[2] = {nn.x, nn.y};
       const bool full = n[0] + n[1] == 2 * kBlockTokens;
@@ -636,14 +651,59 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) l[t][j] += __shfl_xor_sync(~0u, l[t][j], d);
-        if (r == 0) {
+    const uint32_t slot = run * 2 + (first_segment ? 0 : 1);
+    first_segment = false;
+    if constexpr (kOwn) {  // a thread has kDim / 8 neighbouring dims of each of its heads
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t h = t * 8 + 2 * c + j;
+          if (head0 + h >= a.group) continue;
+          const uint32_t head = kv_head * a.group + head0 + h;
+          const float sum = l[t][j], top = m[t][j];
+          const float by = !whole ? v_unit : sum == 0.f ? 0.f : v_unit / sum;
+          float x[kDim / 8];
+#pragma unroll
+          for (int i = 0; i < kDim / 8; ++i) x[i] = o[t][i / 2][2 * (i & 1) + j] * by;
+          if (whole) {
+            uint4* to = reinterpret_cast<uint4*>(
+                a.out + (seg.seq * a.out_stride + (uint64_t)head * kDim + r * (kDim / 8)) * 2);
+#pragma unroll
+            for (int i = 0; i < kDim / 64; ++i)
+              to[i] = make_uint4(pack16<kBf16>(x[i * 8], x[i * 8 + 1]), pack16<kBf16>(x[i * 8 + 2], x[i * 8 + 3]),
+                                 pack16<kBf16>(x[i * 8 + 4], x[i * 8 + 5]), pack16<kBf16>(x[i * 8 + 6], x[i * 8 + 7]));
+            if (r == 0) {
+              const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
+              if (a.lse) a.lse[(uint64_t)seg.seq * a.heads + head] = z * kLn2;
+              if (kMass) a.lse2[(uint64_t)seg.seq * a.heads + head] = z;
+            }
+          } else {
+            float4* to = reinterpret_cast<float4*>(a.part_o + ((uint64_t)slot * kHeads + h) * kDim +
+                                                   r * (kDim / 8));
+#pragma unroll
+            for (int i = 0; i < kDim / 32; ++i)
+              to[i] = make_float4(x[i * 4], x[i * 4 + 1], x[i * 4 + 2], x[i * 4 + 3]);
+            if (r == 0) {
+              a.part_ml[(slot * kHeads + h) * 2] = top;
+              a.part_ml[(slot * kHeads + h) * 2 + 1] = sum;
+            }
+          }
+        }
+      continue;
+    }
+    if (r == 0) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
           sh.m[warp][t * 8 + 2 * c + j] = m[t][j];
           sh.l[warp][t * 8 + 2 * c + j] = l[t][j];
         }
-      }
+    }
     sync_warps();
     if (tid < kHeads) {
       float top = sh.m[0][tid], sum = 0.f;
@@ -709,7 +769,6 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
           if (kMass) a.lse2[(uint64_t)seg.seq * a.heads + head] = z;
         }
       } else {
-        const uint32_t slot = blockIdx.x * 2 + (first_segment ? 0 : 1);
         a.part_o[((uint64_t)slot * kHeads + h) * kDim + dim] = all;
         if (dim == 0) {
           a.part_ml[(slot * kHeads + h) * 2] = top;
@@ -717,7 +776,6 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
         }
       }
     }
-    first_segment = false;
     sync_warps();
   }
 
@@ -899,17 +957,27 @@ bool sizes_ok(const netkv_kv_pages* pages, uint32_t n_seqs, uint32_t heads, uint
 // registers and products, and a second chunk reads the pages again.
 int tiles_of(uint32_t group) { return group <= 8 ? 1 : 2; }
 
+// Batches with a segment for every block of the grid give each warp a run of its own: segments
+// then begin and end without the other warps.
+bool own_runs(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads) {
+  const uint32_t group = heads / p->kv_heads, per = tiles_of(group) * 8;
+  return (uint64_t)n_seqs * p->kv_heads * ((group + per - 1) / per) >= kOwnSegments;
+}
+
 struct Workspace {
+  uint32_t runs;
   size_t part_ml, cuts, lse2, block2, total;  // part_o is at 0
 };
 Workspace workspace(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads, uint32_t width,
                     bool mass) {
   auto up = [](size_t x) { return (x + 127) / 128 * 128; };
-  const size_t rows = (size_t)kMostCtas * 2 * tiles_of(heads / p->kv_heads) * 8;
+  const int tiles = tiles_of(heads / p->kv_heads);
   Workspace w;
+  w.runs = (tiles == 1 ? kCtas<1> : kCtas<2>) * (own_runs(p, n_seqs, heads) ? kWarps : 1);
+  const size_t rows = (size_t)w.runs * 2 * tiles * 8;
   w.part_ml = up(rows * p->head_dim * 4);
   w.cuts = w.part_ml + up(rows * 8);
-  w.lse2 = w.cuts + up(kMostCtas * sizeof(Cut));
+  w.lse2 = w.cuts + up(w.runs * sizeof(Cut));
   w.block2 = w.lse2 + (mass ? up((size_t)n_seqs * heads * 4) : 0);
   w.total = w.block2 + (mass ? (size_t)n_seqs * width * heads * 4 : 0);
   return w;
@@ -966,19 +1034,20 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         (Cut*)(w + ws.cuts),
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
-                        per == 8 ? kCtas<1> : kCtas<2>,
+                        ws.runs,
                         d_status};
   const cudaStream_t s = (cudaStream_t)stream;
+  const bool own = own_runs(pages, n_seqs, heads);
   auto go = [&](auto dim, auto tiles, auto bf, auto e4, auto mass) -> netkv_status {
     constexpr int kDim = decltype(dim)::value, kTiles = decltype(tiles)::value;
     constexpr bool kB = decltype(bf)::value, kE = decltype(e4)::value, kM = decltype(mass)::value;
-    constexpr auto kernel = decode_kernel<kDim, kTiles, kB, kE, kM>;
+    constexpr auto shared = decode_kernel<kDim, kTiles, kB, kE, kM, false>;
+    constexpr auto owned = decode_kernel<kDim, kTiles, kB, kE, kM, true>;
     constexpr int bytes = (int)sizeof(Shared<kDim, kTiles>);
-    NETKV_CUDA_TRY(allow_shared<kernel>(bytes));
-    kernel<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
+    NETKV_CUDA_TRY(own ? allow_shared<owned>(bytes) : allow_shared<shared>(bytes));
+    (own ? owned : shared)<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
-    NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>,
-                                    kCtas<kTiles> - 1, kJoin, s, a));
+    NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>, ws.runs - 1, kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
