@@ -130,7 +130,7 @@ __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, u
   Runs r;
   r.total = sum * units;
   // a warp's own run is long enough not to cut many short segments
-  r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / (kOwn ? 32 : kMinPages)));
+  r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / (kOwn ? 16 : kMinPages)));
   r.base = div_floor(r.total, r.count);
   r.rest = (uint32_t)(r.total - r.base * r.count);
   return r;
@@ -570,28 +570,32 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
         }
         uint32_t p[2][kTiles][2];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float w = vs[g] * v_inv;
+        for (int t = 0; t < kTiles; ++t) {
+          float sums[2][2];  // of a page's tokens r and r + 8
 #pragma unroll
-          for (int t = 0; t < kTiles; ++t) {
+          for (int g = 0; g < 2; ++g) {
+            const float w = vs[g] * v_inv;
             float x[4];
 #pragma unroll
             for (int z = 0; z < 4; ++z) x[z] = ex2(s[g][t][z] - m[t][z & 1]);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) l[t][j] += x[j] + x[j + 2];
-            if (kMass) {  // over the tokens: odd threads r take head 2 c + 1, even ones 2 c
-              const float sum0 = x[0] + x[2], sum1 = x[1] + x[3];
-              float sum = r & 1 ? sum1 : sum0;
-              sum += __shfl_xor_sync(~0u, r & 1 ? sum0 : sum1, 4);
-              sum += __shfl_xor_sync(~0u, sum, 8);
-              sum += __shfl_xor_sync(~0u, sum, 16);
-              const uint32_t h = head0 + t * 8 + 2 * c + r;
-              if (r < 2 && h < a.group && at + g < seg.count)
-                a.block2[((uint64_t)seg.seq * a.width + block + g) * a.heads +
-                         kv_head * a.group + h] = (r & 1 ? m[t][1] : m[t][0]) + lg2(sum);
-            }
+            for (int j = 0; j < 2; ++j) l[t][j] += sums[g][j] = x[j] + x[j + 2];
             p[g][t][0] = transpose8x8(pack16<false>(x[0] * w, x[1] * w));
             p[g][t][1] = transpose8x8(pack16<false>(x[2] * w, x[3] * w));
+          }
+          if (kMass) {  // over the tokens: a quarter of the threads r for each page and head
+            const bool page1 = r & 1, head1 = r & 2;
+            float y[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              y[j] = (page1 ? sums[1][j] : sums[0][j]) +
+                     __shfl_xor_sync(~0u, page1 ? sums[0][j] : sums[1][j], 4);
+            float sum = (head1 ? y[1] : y[0]) + __shfl_xor_sync(~0u, head1 ? y[0] : y[1], 8);
+            sum += __shfl_xor_sync(~0u, sum, 16);
+            const uint32_t h = head0 + t * 8 + 2 * c + (r >> 1), g = r & 1;
+            if (r < 4 && h < a.group && at + g < seg.count)
+              a.block2[((uint64_t)seg.seq * a.width + block + g) * a.heads + kv_head * a.group + h] =
+                  (head1 ? m[t][1] : m[t][0]) + lg2(sum);
           }
         }
         // values: tokens 2 c, 2 c + 1, 2 c + 8 and 2 c + 9, dims r * kDim / 8 on; zeros past
@@ -896,39 +900,36 @@ __global__ void __launch_bounds__(kMassWarps * 32) mass_kernel(const __grid_cons
   uint32_t lanes = 32;  // of a block
   while (lanes / 2 >= a.heads) lanes /= 2;
   const uint32_t per = 32 / lanes, head = lane % lanes;
+  if (blockIdx.y * kMassWarps * kMassSteps * per >= pages) return;
   follow();
-  const float* lse2 = a.lse2 + (uint64_t)seq * a.heads;
-  float z[4];  // the first 128 heads'
-#pragma unroll
-  for (uint32_t j = 0; j < 4; ++j) z[j] = head + j * 32 < a.heads ? lse2[head + j * 32] : 0.f;
   for (uint32_t from = blockIdx.y * kMassWarps * kMassSteps * per; from < pages;
        from += gridDim.y * kMassWarps * kMassSteps * per) {
-    float sum[kMassSteps] = {};
+    const uint32_t first = from + warp * per + lane / lanes;
+    float sum[kMassSteps] = {}, before[kMassSteps] = {};
+    if (a.mass_in && head == 0)
 #pragma unroll
-    for (uint32_t q = 0; q < kMassSteps; ++q) {
-      const uint32_t block = from + (q * kMassWarps + warp) * per + lane / lanes;
-      const float* part = a.block2 + ((uint64_t)seq * a.width + block) * a.heads;
+      for (uint32_t q = 0; q < kMassSteps; ++q) {
+        const uint32_t block = first + q * kMassWarps * per;
+        if (block < pages) before[q] = a.mass_in[(uint64_t)seq * a.width + block];
+      }
+    for (uint32_t h = head; h < a.heads; h += lanes) {
+      const float z = a.lse2[(uint64_t)seq * a.heads + h];
+      float b[kMassSteps];  // loaded together: each is a round trip to memory
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t h = head + j * 32;
-        if (block < pages && h < a.heads) {
-          const float b = part[h];
-          sum[q] += b == -INFINITY ? 0.f : ex2(b - z[j]);
-        }
+      for (uint32_t q = 0; q < kMassSteps; ++q) {
+        const uint32_t block = first + q * kMassWarps * per;
+        b[q] = -INFINITY;
+        if (block < pages) b[q] = a.block2[((uint64_t)seq * a.width + block) * a.heads + h];
       }
-      for (uint32_t h = head + 128; h < a.heads && block < pages; h += 32) {
-        const float b = part[h];
-        sum[q] += b == -INFINITY ? 0.f : ex2(b - lse2[h]);
-      }
+#pragma unroll
+      for (uint32_t q = 0; q < kMassSteps; ++q) sum[q] += b[q] == -INFINITY ? 0.f : ex2(b[q] - z);
     }
 #pragma unroll
     for (uint32_t q = 0; q < kMassSteps; ++q) {
       for (uint32_t d = lanes / 2; d; d /= 2) sum[q] += __shfl_xor_sync(~0u, sum[q], d);
-      const uint32_t block = from + (q * kMassWarps + warp) * per + lane / lanes;
-      if (head == 0 && block < pages) {
-        const uint64_t at = (uint64_t)seq * a.width + block;
-        a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum[q];
-      }
+      const uint32_t block = first + q * kMassWarps * per;
+      if (head == 0 && block < pages)
+        a.mass_out[(uint64_t)seq * a.width + block] = before[q] + sum[q];
     }
   }
 }
