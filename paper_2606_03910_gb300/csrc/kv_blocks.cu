@@ -85,15 +85,21 @@ __global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constan
   const uint32_t lo = start > pos0 ? (uint32_t)(start - pos0) : 0;
   const uint32_t hi = (uint32_t)min((uint64_t)kBlockTokens, start + r.count - pos0);
   const bool all = hi - lo == kBlockTokens;
+  // all loads at once: where a row is not a new one, the nearest that is, for nothing
   const unsigned char* from =
-      src + ((int64_t)(r.first + pos0 - start + row0) * (int64_t)stride + (int64_t)u.head * kDim + col) * 2;
+      src + ((r.first + (pos0 + lo - start)) * stride + (uint64_t)u.head * kDim + col) * 2;
   uint4 x[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const uint32_t row = row0 + i * kRows;
-    x[i] = make_uint4(0, 0, 0, 0);
-    if (all || (row >= lo && row < hi)) x[i] = __ldcs(reinterpret_cast<const uint4*>(from));
-    from += kRows * stride * 2;
+    const uint32_t row = min(max(row0 + i * kRows, lo), hi - 1);
+    x[i] = __ldcs(reinterpret_cast<const uint4*>(from + (row - lo) * stride * 2));
+  }
+  if (!all) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const uint32_t row = row0 + i * kRows;
+      if (row < lo || row >= hi) x[i] = make_uint4(0, 0, 0, 0);
+    }
   }
   const float was = lo ? *scale : 0.f;
   // Magnitudes are in the order of their bits, two values a word.
@@ -172,6 +178,7 @@ __global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant
   const uint64_t stride = u.values ? a.v_stride : a.k_stride;
   const uint64_t part = (uint64_t)(there ? page : 0) * a.kv.heads + u.head;
   const unsigned char* codes = (u.values ? a.kv.v : a.kv.k) + part * (kBlockTokens * kDim);
+  // an absent page's rows are zeros; page 0 is read in its place
   const float s = there ? (u.values ? a.kv.v_scale : a.kv.k_scale)[part] : 0.f;
   const uint32_t col = (lane % kLanes) * 8, row0 = lane / kLanes;
   const uint64_t pos0 = block * kBlockTokens;
@@ -182,9 +189,7 @@ __global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const uint32_t row = row0 + i * kRows;
-    x[i] = make_uint2(0, 0);
-    if (there && (all || (row >= lo && row < hi)))
-      x[i] = *reinterpret_cast<const uint2*>(codes + row * kDim + col);
+    x[i] = __ldcs(reinterpret_cast<const uint2*>(codes + row * kDim + col));
   }
   unsigned char* to =
       dst + ((int64_t)(r.first + pos0 - start + row0) * (int64_t)stride + (int64_t)u.head * kDim + col) * 2;
@@ -193,8 +198,8 @@ __global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant
     const uint32_t row = row0 + i * kRows;
     if (all || (row >= lo && row < hi)) {
       float y[8];
-      decode4<kE4m3>(x[i].x, s, y);
-      decode4<kE4m3>(x[i].y, s, y + 4);
+      decode4<kE4m3>(there ? x[i].x : 0u, s, y);
+      decode4<kE4m3>(there ? x[i].y : 0u, s, y + 4);
       *reinterpret_cast<uint4*>(to) = make_uint4(pack16<kBf16>(y[0], y[1]), pack16<kBf16>(y[2], y[3]),
                                                  pack16<kBf16>(y[4], y[5]), pack16<kBf16>(y[6], y[7]));
     }
