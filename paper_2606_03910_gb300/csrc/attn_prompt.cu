@@ -19,6 +19,7 @@
 namespace {
 
 constexpr int kRows = 128, kKeys = 128;  // of a tile
+constexpr uint32_t kFewItems = 6;         // items an SM, in halves, up to which they are split
 constexpr float kLag = 8.f;              // in powers of two
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kSoftmaxWarps = 8;
@@ -28,6 +29,10 @@ constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // and a warp for the loads,
 constexpr int kLaunchRegs = 168, kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
 
+// Two neighbouring row blocks of a head; two heads of a group; the even and the odd key tiles of
+// one row block.
+enum Mode : uint32_t { kRowPairs = 0, kHeadPairs = 1, kKeyHalves = 2 };
+
 struct PromptArgs {
   unsigned char* out;
   uint64_t out_stride;  // in values
@@ -35,7 +40,7 @@ struct PromptArgs {
   const uint64_t* k_off;
   uint64_t q_rows, k_rows;
   uint32_t heads, group, n_seqs;
-  uint32_t head_pairs;  // 1: a block's tiles are two heads; 0: two row blocks of a head
+  uint32_t mode;        // what a block's two tiles are
   uint32_t tiles;       // row blocks that the grid has
   uint32_t ordered;     // 1: row blocks by their key tiles, the most first
   float scale2;         // scale * log2(e)
@@ -226,6 +231,9 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
         "r"(at)
       : "memory");
 }
+__device__ __forceinline__ void sync_softmax() {
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+}
 __device__ __forceinline__ void tmem_loaded() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -257,6 +265,7 @@ struct Shared {
   uint64_t item_full[2], item_empty[2], begun, claimed;
   alignas(16) uint4 claim;
   Item item[2];
+  float half_m[kRows], half_l[kRows];  // kKeyHalves: the odd key tiles' maxima and sums
   uint32_t tmem;
   int late;
 };
@@ -268,8 +277,8 @@ struct Tile {
 };
 __device__ __forceinline__ Tile tile_of(const PromptArgs& a, const Item& x, uint32_t t) {
   Tile y;
-  y.head = a.head_pairs ? x.column * 2 + t : x.column;
-  y.row = (int32_t)(x.row + (a.head_pairs ? 0 : t * kRows));
+  y.head = a.mode == kHeadPairs ? x.column * 2 + t : x.column;
+  y.row = (int32_t)(x.row + (a.mode == kRowPairs ? t * kRows : 0));
   y.rows = (uint32_t)min(kRows, max(0, (int32_t)x.q_count - y.row));
   return y;
 }
@@ -335,8 +344,8 @@ __device__ __forceinline__ Found row_block(const PromptArgs& a, uint32_t n, uint
 
 // The grid's n-th item.
 __device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n) {
-  const uint32_t columns = a.head_pairs ? a.heads / 2 : a.heads;
-  const uint32_t block_rows = a.head_pairs ? kRows : 2 * kRows;
+  const uint32_t columns = a.mode == kHeadPairs ? a.heads / 2 : a.heads;
+  const uint32_t block_rows = a.mode == kRowPairs ? 2 * kRows : kRows;
   const Found f = row_block(a, n / columns, block_rows);
   Item x = {};
   if (f.seq >= a.n_seqs) return x;
@@ -354,6 +363,10 @@ __device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n) {
     // keys that the tile's last row sees
     const int64_t last = min((int64_t)x.k_count, (int64_t)x.k_count - x.q_count + y.row + y.rows);
     x.steps[t] = y.rows && last > 0 ? (uint32_t)((last + kKeys - 1) / kKeys) : 0;
+  }
+  if (a.mode == kKeyHalves) {
+    x.steps[1] = x.steps[0] / 2;
+    x.steps[0] -= x.steps[1];
   }
   return x;
 }
@@ -432,23 +445,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (x.valid < 0) break;
         const uint32_t steps = max(x.steps[0], x.steps[1]);
         if (steps == 0) continue;
-        const uint32_t kv_head = (a.head_pairs ? x.column * 2 : x.column) / a.group;
+        const uint32_t kv_head = (a.mode == kHeadPairs ? x.column * 2 : x.column) / a.group;
+        const uint32_t tiles = a.mode == kKeyHalves ? 1 : 2;  // of queries
         if (with_q) wait(smem_addr(&sh.q_empty), (with_q - 1) & 1, late);
         ++with_q;
         if (lane == 0) {
-          bar_expect(smem_addr(&sh.q_full), 2 * kRows * kDim * 2);
-          for (uint32_t t = 0; t < 2; ++t) {
+          bar_expect(smem_addr(&sh.q_full), tiles * kRows * kDim * 2);
+          for (uint32_t t = 0; t < tiles; ++t) {
             const Tile y = tile_of(a, x, t);
             for (int h = 0; h < kHalves; ++h)
               load_box(smem_addr(sh.q[t]) + h * kBox, &map_q, h * 64, y.head,
                        (int)(x.q_first + y.row), smem_addr(&sh.q_full));
           }
         }
-        for (uint32_t j = 0; j < 2 * steps && !*late; ++j, ++i) {
+        auto load = [&](uint32_t tile, bool values) {  // a key tile's keys or values
           const uint32_t st = i % kRing, full = smem_addr(&sh.kv_full[st]);
           if (i >= kRing) wait(smem_addr(&sh.kv_empty[st]), (i / kRing - 1) & 1, late);
-          const uint32_t key = j / 2 * kKeys;
-          const bool values = j & 1;
+          ++i;
+          const uint32_t key = tile * kKeys;
           // values past the sequence's end are another's and meet weights of 0: an infinity or a
           // NaN among them would not vanish, so the rows are cleared before they are handed on
           const uint32_t own = x.k_count - key;
@@ -470,6 +484,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) bar_arrive(full);
           }
           __syncwarp();
+        };
+        // in the order in which the products want them
+        if (a.mode == kKeyHalves) {
+          const uint32_t all = x.steps[0] + x.steps[1];
+          load(0, false);
+          if (all > 1) load(1, false);
+          for (uint32_t j = 0; j < all && !*late; ++j) {
+            load(j, true);
+            if (j + 2 < all) load(j + 2, false);
+          }
+        } else {
+          for (uint32_t j = 0; j < steps && !*late; ++j) {
+            load(j, false);
+            load(j, true);
+          }
         }
       }
     } else if (warp == kSoftmaxWarps + 1) {
@@ -479,12 +508,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t q0 = operand(smem_addr(sh.q[0]), 16), k0 = operand(smem_addr(sh.kv[0]), 16),
                      v0 = operand(smem_addr(sh.kv[0]), kBox);
       constexpr uint32_t kTile = kRows * kDim * 2 >> 4;  // of operands' addresses
-      auto scores = [&](uint32_t t, uint32_t st) {       // S_t from the ring's place st
+      auto scores = [&](uint32_t t, uint32_t st, uint32_t tq) {  // S_t from the ring's place st
         if (leader) {
 #pragma unroll
           for (int x = 0; x < kDim / 16; ++x) {
             const uint32_t off = (x / 4 * kBox + x % 4 * 32) >> 4;
-            mma_smem(kS + t * 128, q0 + t * kTile + off, k0 + st * kTile + off, kScores, x > 0);
+            mma_smem(kS + t * 128, q0 + tq * kTile + off, k0 + st * kTile + off, kScores, x > 0);
           }
           commit(smem_addr(&sh.s_full[t]));
         }
@@ -519,8 +548,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         wait(smem_addr(&sh.q_full), with_q++ & 1, late);
         arrived(i);
         after_sync();
-        if (n0) scores(0, i % kRing);
-        if (n1) scores(1, i % kRing);
+        auto take = [&](uint32_t t, uint32_t v, bool add) {  // P_t V from the ring's place v
+          const uint32_t parity = (t ? done1++ : done0++) & 1;
+          wait(smem_addr(&sh.p_full[t][0]), parity, late);
+          after_sync();
+          sums(t, v, 0, add);
+          wait(smem_addr(&sh.p_full[t][1]), parity, late);
+          after_sync();
+          sums(t, v, 1, true);
+        };
+        if (a.mode == kKeyHalves) {
+          const uint32_t all = n0 + n1;
+          scores(0, i % kRing, 0);
+          signal(&sh.kv_empty[i++ % kRing]);
+          if (all > 1) {
+            arrived(i);
+            after_sync();
+            scores(1, i % kRing, 0);
+            signal(&sh.kv_empty[i++ % kRing]);
+          }
+          for (uint32_t j = 0; j < all && !*late; j += 2) {
+#pragma unroll
+            for (uint32_t t = 0; t < 2; ++t) {
+              if (j + t >= all) continue;
+              arrived(i);
+              take(t, i % kRing, j > 0);
+              const bool more = j + t + 2 < all;
+              if (!more) signal(&sh.o_full[t]);
+              signal(&sh.kv_empty[i++ % kRing]);
+              if (more) {
+                arrived(i);
+                after_sync();
+                scores(t, i % kRing, 0);
+                signal(&sh.kv_empty[i++ % kRing]);
+              }
+            }
+          }
+          signal(&sh.q_empty);
+          continue;
+        }
+        if (n0) scores(0, i % kRing, 0);
+        if (n1) scores(1, i % kRing, 1);
         signal(&sh.kv_empty[i % kRing]);
         if (steps == 1) signal(&sh.q_empty);
         for (uint32_t j = 0; j < steps && !*late; ++j) {
@@ -532,14 +600,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (uint32_t t = 0; t < 2; ++t) {
             const uint32_t n = t ? n1 : n0;
             if (j < n) {
-              const uint32_t parity = (t ? done1++ : done0++) & 1;
-              wait(smem_addr(&sh.p_full[t][0]), parity, late);
-              after_sync();
-              sums(t, v, 0, j > 0);
-              wait(smem_addr(&sh.p_full[t][1]), parity, late);
-              after_sync();
-              sums(t, v, 1, true);
-              if (j + 1 < n) scores(t, k);
+              take(t, v, j > 0);
+              if (j + 1 < n) scores(t, k, t);
               else signal(&sh.o_full[t]);
             }
           }
@@ -550,6 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       // the last signals have to reach a block that is still there
+      if (with_q) wait(smem_addr(&sh.q_empty), (with_q - 1) & 1, late);
       if (i >= 1) wait(smem_addr(&sh.kv_empty[(i - 1) % kRing]), ((i - 1) / kRing) & 1, late);
     } else if (warp == kSoftmaxWarps + 2) {
       // ---- plan: the block's own item, then those of blocks that have not started, which it
@@ -621,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) tmem_load(s_at + i * 32, s + i * 32);
         tmem_loaded();
-        const int seen = visible - (int)(j * kKeys);
+        const int seen = visible - (int)((a.mode == kKeyHalves ? 2 * j + t : j) * kKeys);
         if (__any_sync(~0u, seen < kKeys)) {
 #pragma unroll
           for (int i = 0; i < kKeys; ++i)
@@ -684,13 +747,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         wait(smem_addr(&sh.o_full[t]), finished++ & 1, late);
         after_sync();
       }
-      const bool any = steps && l != 0.f;
-      const float inv = any ? 1.f / l : 0.f;
       uint4* stage = reinterpret_cast<uint4*>(sh.out[warp]);
       const uint32_t row0 = (warp % 4) * 32;
       unsigned char* dst = a.out + ((x.q_first + y.row + row0) * a.out_stride + (uint64_t)y.head * kDim) * 2;
+      const bool halves = a.mode == kKeyHalves;
+      float own = 1.f, other = 0.f;  // kKeyHalves: what brings the two sums to one maximum
+      float* part = reinterpret_cast<float*>(sh.out);  // and the odd tiles' sums, [64][kRows]
+      if (halves) {
+        if (t) {
+          sh.half_m[row] = m;
+          sh.half_l[row] = l;
+        }
+        sync_softmax();
+        const float m1 = sh.half_m[row], l1 = sh.half_l[row];
+        if (t == 0 && l1 != 0.f) {  // NaN too
+          const float top = fmaxf(m, m1);
+          own = ex2((m - top) * a.scale2);
+          other = m1 == -INFINITY ? l1 : ex2((m1 - top) * a.scale2);
+          l = l * own + l1 * other;
+          m = top;
+        }
+      }
+      const bool any = steps && l != 0.f;
+      const float inv = any ? 1.f / l : 0.f;
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
+        if (halves) {
+          if (h) sync_softmax();  // the half before has left shared memory
+          if (t && steps) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float o[32];
+              tmem_load(o_at + h * 64 + i * 32, o);
+              tmem_loaded();
+#pragma unroll
+              for (int z = 0; z < 32; ++z) part[(i * 32 + z) * kRows + row] = o[z];
+            }
+          }
+          sync_softmax();
+        }
+        uint4 packed[8];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float o[32];
@@ -698,15 +794,23 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_load(o_at + h * 64 + i * 32, o);
             tmem_loaded();
           }
+          if (halves && t == 0 && x.steps[1]) {
+#pragma unroll
+            for (int z = 0; z < 32; ++z) o[z] = o[z] * own + part[(i * 32 + z) * kRows + row] * other;
+          }
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             uint32_t w[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               w[q] = any ? pack16<kBf16>(o[z * 8 + q * 2] * inv, o[z * 8 + q * 2 + 1] * inv) : 0u;
-            stage[lane * 8 + ((i * 4 + z) ^ (lane & 7))] = make_uint4(w[0], w[1], w[2], w[3]);
+            packed[i * 4 + z] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
+        if (halves) sync_softmax();  // the odd tiles' sums have been read
+        if (halves && t) continue;
+#pragma unroll
+        for (int z = 0; z < 8; ++z) stage[lane * 8 + (z ^ (lane & 7))] = packed[z];
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -716,6 +820,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 stage[r * 8 + (c ^ (r & 7))];
         }
         __syncwarp();
+      }
+      if (halves) {
+        sync_softmax();
+        if (t) continue;
       }
       if (row < y.rows && a.lse)
         a.lse[(x.q_first + y.row + row) * a.heads + y.head] =
@@ -799,20 +907,27 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
   a.heads = heads;
   a.group = heads / kv_heads;
   a.n_seqs = n_seqs;
-  a.head_pairs = a.group % 2 == 0;
   a.scale2 = scale * kLog2e;
   a.lse = d_lse;
   a.status = d_status;
-  const uint64_t block_rows = a.head_pairs ? 128 : 256;
-  // a sequence ends at most one tile that it does not fill
-  const uint64_t tiles = q_rows / block_rows + n_seqs, grid = tiles * (a.head_pairs ? heads / 2 : heads);
+  int dev = 0, sms = 0;
+  NETKV_CUDA_TRY(cudaGetDevice(&dev));
+  NETKV_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  // A sequence ends at most one row block that it does not fill.
+  a.mode = a.group % 2 == 0 ? kHeadPairs : kRowPairs;
+  uint64_t block_rows = a.mode == kHeadPairs ? kRows : 2 * kRows;
+  uint64_t tiles = q_rows / block_rows + n_seqs, columns = a.mode == kHeadPairs ? heads / 2 : heads;
+  if (tiles * columns <= (uint64_t)sms * kFewItems / 2) {
+    a.mode = kKeyHalves;
+    block_rows = kRows;
+    tiles = q_rows / block_rows + n_seqs;
+    columns = heads;
+  }
+  const uint64_t grid = tiles * columns;
   if (grid >> 31) return NETKV_EINVAL;
   a.tiles = (uint32_t)tiles;
   // One sequence alone is in order as it is, and where every item has an SM the order does not
   // matter; more than 128 sequences would take the search longer than their blocks last.
-  int dev = 0, sms = 0;
-  NETKV_CUDA_TRY(cudaGetDevice(&dev));
-  NETKV_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   a.ordered = n_seqs > 1 && n_seqs <= 128 && grid > (uint64_t)sms;
   if (!encoder()) return NETKV_ECUDA;
   const bool bf = dtype == NETKV_BF16;
