@@ -494,6 +494,23 @@ def _plane(t, rows: int, width: int) -> Optional[int]:
     return t.data_ptr()
 
 
+_raw_stream = None
+
+
+def _on(t, stream):
+    """The stream of a call on t's device: the given one, else torch's current one there."""
+    d = t.get_device()
+    if d < 0:
+        raise TypeError(f"CUDA tensors expected, got one on {t.device}")
+    if stream is not None:
+        return _stream(stream)
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(d)
+
+
 def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, stream) -> None:
     heads, dim = pages.heads_dim
     dt, kp, ks = _rows(k, heads, dim)
@@ -504,7 +521,7 @@ def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, str
     n = len(off) - 1
     tp, tw = _table(table, n)
     code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
-                _ints(start, _I32, n), tp, tw, _ptr(status), _stream(stream))
+                _ints(start, _I32, n), tp, tw, _ptr(status), _on(k, stream))
     if code:
         raise NetKVError(fn, code)
 
@@ -535,7 +552,7 @@ def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=N
     _check("netkv_attn_prompt", _lib.netkv_attn_prompt(
         dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, _I64, n + 1),
         _ints(k_off, _I64, n + 1), q_rows, k_rows, dim ** -0.5 if scale is None else scale,
-        op, os_, _plane(lse, q_rows, heads), _ptr(status), _stream(stream)))
+        op, os_, _plane(lse, q_rows, heads), _ptr(status), _on(q, stream)))
 
 
 def netkv_attn_decode_workspace_size(pages: KvPages, n_seqs: int, heads: int, table_width: int,
@@ -555,12 +572,12 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     if out.shape[0] != n:
         raise ValueError("as many rows of out as of q expected")
     tp, tw = _table(table, n)
-    ws_bytes = 0 if workspace is None else _nbytes(workspace)
+    ws_bytes = 0 if workspace is None else workspace.nbytes
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
         pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n), tp, tw,
         dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads),
         _plane(mass_in, n, tw), _plane(mass_out, n, tw), _ptr(workspace), ws_bytes,
-        _ptr(status), _stream(stream)))
+        _ptr(status), _on(q, stream)))
 
 
 def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_out, length_out,
@@ -575,7 +592,7 @@ def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_ou
     _check("netkv_kv_evict", _lib.netkv_kv_evict(
         n, tp, _ints(length, _I32, n), _plane(mass, n, tw), tw, _ints(budget, _I32, n), int(sink),
         int(recent), to, _ints(length_out, _I32, n), _plane(mass_out, n, tw), fr,
-        _ints(n_freed, _I32, n), _ptr(status), _stream(stream)))
+        _ints(n_freed, _I32, n), _ptr(status), _on(table, stream)))
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:
