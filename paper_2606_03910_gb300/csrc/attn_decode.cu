@@ -28,7 +28,7 @@ constexpr uint32_t kThreads = kWarps * 32 + 32;  // and a warp for the loads
 // Blocks of the grid: three an SM on 152 SMs, two where a second tile of heads takes the registers.
 template <int kTiles>
 constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
-constexpr uint32_t kOwnSegments = 456;  // see own_runs
+constexpr uint32_t kUncutBlocks = 32;  // see uncut_runs
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
 constexpr uint32_t kEdge = 8;       // see Runs
@@ -58,6 +58,7 @@ struct DecodeArgs {
   float* lse2;      // [n_seqs][heads], in powers of two; with mass only
   float* block2;    // [n_seqs][width][heads]: log2 of a block's weight; with mass only
   uint32_t most_runs;
+  uint32_t uncut;   // 1: a segment is all its first run's
   int* status;
 };
 
@@ -254,7 +255,13 @@ struct Shared {
 struct Walk {
   Segment s;
   uint64_t left;  // places from s on
-  __device__ __forceinline__ void take(uint64_t into) {
+  __device__ __forceinline__ void take(const DecodeArgs& a, uint64_t into) {
+    if (a.uncut) {
+      left -= min(left, places(s.pages));
+      s.first = 0;
+      s.count = s.pages;
+      return;
+    }
     const uint64_t end = min(into + left, places(s.pages));
     left -= end - into;
     s.first = into > kEdge ? (uint32_t)(into - kEdge) : 0;
@@ -281,7 +288,13 @@ struct Walk {
       cut->order = run - cut->run0 - 1;
       cut->second = runs.start(cut->run0) < begin;
     }
-    take(into);
+    if (a.uncut && into) {  // the segment is an earlier run's
+      cut->parts = 0;
+      left -= min(left, places(s.pages) - into);
+      next(a, units);
+      return;
+    }
+    take(a, into);
   }
   __device__ __forceinline__ void next(const DecodeArgs& a, uint32_t units) {
     s.count = 0;
@@ -293,7 +306,7 @@ struct Walk {
         s.pages = pages_of(a, s.seq);
       } while (s.pages == 0);
     }
-    take(0);
+    take(a, 0);
   }
 };
 
@@ -958,12 +971,20 @@ bool sizes_ok(const netkv_kv_pages* pages, uint32_t n_seqs, uint32_t heads, uint
 // registers and products, and a second chunk reads the pages again.
 int tiles_of(uint32_t group) { return group <= 8 ? 1 : 2; }
 
-// Batches with a segment for every block of the grid give each warp a run of its own: segments
-// then begin and end without the other warps.
+// Batches with a segment for every warp of the grid give each warp a run of its own: segments
+// then begin and end without the other warps (1,000 sequences of about 100 tokens at 64 query
+// heads 153 -> 86 us).  With fewer, four warps are through a segment sooner than one.
 bool own_runs(const netkv_kv_pages* p, uint32_t n_seqs, uint32_t heads) {
-  const uint32_t group = heads / p->kv_heads, per = tiles_of(group) * 8;
-  return (uint64_t)n_seqs * p->kv_heads * ((group + per - 1) / per) >= kOwnSegments;
+  const uint32_t group = heads / p->kv_heads;
+  const int tiles = tiles_of(group);
+  return (uint64_t)n_seqs * p->kv_heads * ((group + tiles * 8 - 1) / (tiles * 8)) >=
+         (tiles == 1 ? kCtas<1> : kCtas<2>) * kWarps;
 }
+
+// Tables of up to 32 blocks: no segment is worth a join, whose launch and round trips take 5 us
+// (64 sequences of 500 tokens 18.8 -> 14.8 us).  At 64 blocks one of 1,000 tokens alone would
+// take 16.7 us instead of 14.7, and 300 of them 66 instead of 57, as runs get uneven.
+bool uncut_runs(uint32_t width) { return width <= kUncutBlocks; }
 
 struct Workspace {
   uint32_t runs;
@@ -1036,6 +1057,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
                         (float*)(w + ws.lse2),
                         (float*)(w + ws.block2),
                         ws.runs,
+                        uncut_runs(table_width),
                         d_status};
   const cudaStream_t s = (cudaStream_t)stream;
   const bool own = own_runs(pages, n_seqs, heads);
@@ -1048,7 +1070,8 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     NETKV_CUDA_TRY(own ? allow_shared<owned>(bytes) : allow_shared<shared>(bytes));
     (own ? owned : shared)<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
-    NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>, ws.runs - 1, kJoin, s, a));
+    if (!uncut_runs(table_width))
+      NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>, ws.runs - 1, kJoin, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {

@@ -129,6 +129,26 @@ def test_many_ragged_sequences(netkv, n):
     check(netkv, lengths, 3, 3, 128, torch.bfloat16, "e4m3", seed=n, same=True)
 
 
+@pytest.mark.parametrize("n,heads,kv_heads", [(6, 16, 2), (40, 8, 8), (700, 6, 3), (300, 60, 5)])
+@pytest.mark.parametrize("width", [1, 31, 32, 33])
+def test_short_tables(netkv, n, heads, kv_heads, width):
+    """Tables at and next to the width up to which no segment is shared between runs."""
+    rng = np.random.default_rng(width + n)
+    lengths = np.where(rng.random(n) < 0.1, 0, rng.integers(1, width * 16 + 1, n)).tolist()
+    lengths[0] = width * 16
+    check(netkv, lengths, heads, kv_heads, 64, torch.bfloat16, "int8", seed=n, width=width)
+
+
+@pytest.mark.parametrize("n,heads,kv_heads", [(620, 36, 3), (1900, 2, 1)])
+@pytest.mark.parametrize("mass", [False, True])
+def test_a_run_for_each_warp(netkv, n, heads, kv_heads, mass):
+    """Enough segments that warps have runs of their own, which cut some of them."""
+    rng = np.random.default_rng(n)
+    lengths = np.exp(rng.normal(3.5, 1.5, n)).astype(int).clip(0, 4000)
+    lengths[5] = 4000
+    check(netkv, lengths.tolist(), heads, kv_heads, 128, torch.float16, "e4m3", seed=n, mass=mass)
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_sharp_scores_and_spread_scales(netkv, fmt):
     """One token takes nearly all of a row's weight; scales of blocks orders apart."""
