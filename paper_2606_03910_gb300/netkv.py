@@ -515,10 +515,10 @@ def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, str
     heads, dim = pages.heads_dim
     dt, kp, ks = _rows(k, heads, dim)
     _, vp, vs = _rows(v, heads, dim, dt)
-    rows = len(k)
-    if len(v) != rows:
+    rows = k.shape[0]
+    if v.shape[0] != rows:
         raise ValueError("as many rows of keys as of values expected")
-    n = len(off) - 1
+    n = off.numel() - 1
     tp, tw = _table(table, n)
     code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
                 _ints(start, _I32, n), tp, tw, _ptr(status), _on(k, stream))
