@@ -2,15 +2,21 @@
 // block has drawn.
 //
 // Bound: the codes are read once, 2 kDim bytes a token and KV head, and everything else is
-// small, so the kernel streams pages and its arithmetic has to fit in their shadow.
+// small, so the kernel streams pages and its arithmetic has to fit in their shadow: about 330
+// instructions a warp and page of 4 KB, which take 45 % of the issue slots.  160 sequences of
+// 5,500 tokens with 64 query heads on 8 KV heads of 128, int8: 309 us, 5.8 TB/s; 64 of 13,000
+// with 16 on 2 and block weights: 94 us, 4.6 TB/s; two of 131,072, e4m3: 43 us, 3.1 TB/s (of
+// which 20 are the bytes and 10 the join and both ends); one of 512: 10.5 us on the device.
 //
-// Split: the work is the list of all pages, (sequence, KV head, block) in order, and every block
-// of the grid takes an equal run of it, so ragged batches and single long sequences spread over
-// the card alike.  A run holds whole (sequence, head) segments, which are finished at once, and
-// at most two that other blocks share, whose sums go to the workspace for the join.  Within a
-// segment the four warps take every fourth page; each has a ring of pages in flight, filled by
-// bulk copies (a page's part for a head is 16 kDim contiguous bytes) and refilled for the next
-// segment before the present one is summed up.
+// Split: the work is the list of all pages, (sequence, KV head, block) in order, cut into equal
+// runs, so that ragged batches and single long sequences spread over the card alike.  A run is
+// a block's (four warps take a segment's pairs of pages in turn) or, where there are segments for
+// every warp, a warp's.  It holds whole (sequence, head) segments, which are finished at once,
+// and at most two that other runs share, whose sums go to the workspace for the join.  A warp of
+// its own fills rings of pages by bulk copies (a page's part for a head is 16 kDim contiguous
+// bytes) over the ends of segments and ahead of their queries: with the copies issued by the
+// warps that use them, 160 sequences took 372 us.  Two pages a step make two chains of products
+// to interleave; three blocks an SM hide what is left (two: 363 us).
 //
 // Arithmetic: a page is 16 tokens and a KV head serves a group of query heads, so S^T = K q^T
 // and O^T = V^T P^T are products of 16 x 16 by 16 x 8: m16n8k16, with up to 8 (kTiles = 1) or
@@ -31,7 +37,7 @@ constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
 constexpr uint32_t kUncutBlocks = 32;  // see uncut_runs
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
-constexpr uint32_t kEdge = 8;       // see Runs
+constexpr uint32_t kEdge = 8;       // see Runs; at 0 runs of short segments end last (338 us for 309)
 constexpr uint32_t kMinPages = 16;  // a block's run at least: a pair of pages a warp, and an edge
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
@@ -416,7 +422,8 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
 }
 
 template <int kDim, int kTiles, bool kBf16, bool kE4m3, bool kMass, bool kOwn>
-__global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(const __grid_constant__ DecodeArgs a) {
+__global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
+    decode_kernel(const __grid_constant__ DecodeArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   using Sh = Shared<kDim, kTiles>;
   Sh& sh = *reinterpret_cast<Sh*>(smem);
@@ -457,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
     for (int t = 0; t < kTiles; ++t) {
       const uint32_t h = head0 + t * 8 + r;
       const uint4* src = reinterpret_cast<const uint4*>(
-          a.q + (walk.s.seq * a.q_stride + ((uint64_t)kv_head * a.group + min(h, a.group - 1)) * kDim) * 2);
+          a.q + (walk.s.seq * a.q_stride +
+                 ((uint64_t)kv_head * a.group + min(h, a.group - 1)) * kDim) * 2);
 #pragma unroll
       for (int i = 0; i < kDim / 32; ++i)
         raw[t][i] = h < a.group ? src[(i / 2) * 8 + c * 2 + i % 2] : make_uint4(0, 0, 0, 0);
@@ -691,8 +699,10 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
                 a.out + (seg.seq * a.out_stride + (uint64_t)head * kDim + r * (kDim / 8)) * 2);
 #pragma unroll
             for (int i = 0; i < kDim / 64; ++i)
-              to[i] = make_uint4(pack16<kBf16>(x[i * 8], x[i * 8 + 1]), pack16<kBf16>(x[i * 8 + 2], x[i * 8 + 3]),
-                                 pack16<kBf16>(x[i * 8 + 4], x[i * 8 + 5]), pack16<kBf16>(x[i * 8 + 6], x[i * 8 + 7]));
+              to[i] = make_uint4(pack16<kBf16>(x[i * 8], x[i * 8 + 1]),
+                                 pack16<kBf16>(x[i * 8 + 2], x[i * 8 + 3]),
+                                 pack16<kBf16>(x[i * 8 + 4], x[i * 8 + 5]),
+                                 pack16<kBf16>(x[i * 8 + 6], x[i * 8 + 7]));
             if (r == 0) {
               const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
               if (a.lse) a.lse[(uint64_t)seg.seq * a.heads + head] = z * kLn2;
@@ -728,7 +738,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2) decode_kernel(c
       for (uint32_t w = 1; w < kWarps; ++w) top = fmaxf(top, sh.m[w][tid]);
 #pragma unroll
       for (uint32_t w = 0; w < kWarps; ++w)
-        sum += sh.m[w][tid] == -INFINITY ? 0.f * sh.l[w][tid] : ex2(sh.m[w][tid] - top) * sh.l[w][tid];
+        sum += (sh.m[w][tid] == -INFINITY ? 0.f : ex2(sh.m[w][tid] - top)) * sh.l[w][tid];
       sh.top[tid] = top;
       sh.sum[tid] = sum;
     }
@@ -893,7 +903,8 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ Dec
     for (uint32_t i = 0; i < kPer; ++i) o[i] += sums[warp + w * spread][lane * kPer + i];
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const uint32_t head = s.unit / a.chunks * a.group + head0 + h;
-  uint32_t* to = reinterpret_cast<uint32_t*>(a.out + (s.seq * a.out_stride + (uint64_t)head * kDim) * 2);
+  uint32_t* to =
+      reinterpret_cast<uint32_t*>(a.out + (s.seq * a.out_stride + (uint64_t)head * kDim) * 2);
 #pragma unroll
   for (uint32_t i = 0; i < kPer; i += 2)
     to[lane * (kPer / 2) + i / 2] = pack16<kBf16>(o[i] * inv, o[i + 1] * inv);
@@ -1094,7 +1105,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
   if (st != NETKV_OK) return st;
   if (d_mass_out)
     NETKV_CUDA_TRY(launch_following(
-        mass_kernel, dim3(n_seqs, min((table_width + kMassWarps * kMassSteps - 1) / (kMassWarps * kMassSteps), 1024u)),
+        mass_kernel, dim3(n_seqs, min((table_width - 1) / (kMassWarps * kMassSteps) + 1, 1024u)),
         kMassWarps * 32, s, a));
   return netkv_launch_status();
 }

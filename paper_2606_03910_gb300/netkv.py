@@ -25,7 +25,8 @@ _lib = C.CDLL(LIB_PATH)
 
 NETKV_OK, NETKV_EINVAL, NETKV_ENOMEM, NETKV_ECUDA, NETKV_ELIMIT = 0, 1, 2, 3, 4
 NETKV_PREFIX_MATCH_STATIC_MAX_R = 524288
-NETKV_DEV_EDOMAIN, NETKV_DEV_EFULL, NETKV_DEV_ERANGE, NETKV_DEV_ETIMEOUT = 1, 2, 4, 8
+NETKV_DEV_EDOMAIN, NETKV_DEV_EFULL, NETKV_DEV_ERANGE = 1, 2, 4
+NETKV_DEV_ETIMEOUT = 8
 _NAMES = {1: "NETKV_EINVAL", 2: "NETKV_ENOMEM", 3: "NETKV_ECUDA",
           4: "NETKV_ELIMIT (more requests than the fixed scratch of netkv_prefix_match_static holds)"}
 
