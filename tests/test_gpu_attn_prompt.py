@@ -112,6 +112,43 @@ def test_many_short_prompts(netkv):
     check(netkv, lq, lk, 2, 2, 64, torch.bfloat16, lead=2)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv_heads", [(64, 8), (63, 9)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_items_than_the_card_takes_at_once(netkv, dtype, heads, kv_heads, dim):
+    """Even and odd groups, enough row blocks that blocks of the grid take several: ordered by
+    their keys, with prefixes, empty rows and empty sequences among them."""
+    lq = [300, 1, 0, 700, 128, 257, 40, 900, 129, 5]
+    lk = [300, 500, 20, 1100, 100, 257, 0, 900, 1000, 5]
+    pick = sorted({0, 1, heads // kv_heads - 1, heads // 2, heads - 2, heads - 1})
+    check(netkv, lq, lk, heads, kv_heads, dim, dtype, seed=dim + heads, pad=8, lead=2,
+          only_heads=pick, rows=60)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(16, 2), (15, 3)])
+def test_more_sequences_than_are_ordered(netkv, heads, kv_heads):
+    """More than 128 sequences, each with a few row blocks or less."""
+    rng = np.random.default_rng(heads)
+    lq = rng.integers(0, 300, 150).tolist()
+    lk = [a + int(b) for a, b in zip(lq, rng.integers(0, 200, 150))]
+    check(netkv, lq, lk, heads, kv_heads, 64, torch.bfloat16, only_heads=[0, heads - 1], rows=20)
+
+
+def test_one_long_prompt_of_many_items(netkv):
+    check(netkv, [20000], [20000], 16, 2, 128, torch.bfloat16, rows=40, only_heads=[0, 7, 8, 15])
+    check(netkv, [16000], [20000], 15, 5, 128, torch.float16, rows=40, only_heads=[0, 3, 14])
+
+
+def test_no_keys_at_all(netkv):
+    """Rows without any key row in the call: zeros and -inf."""
+    q = torch.randn((300, 4, 128)).bfloat16().cuda()
+    k = torch.empty((0, 2, 128), dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(q, 5.0), torch.full((300, 4), 5.0, device="cuda")
+    netkv.netkv_attn_prompt(q, k, k, offsets([300]), offsets([0]), out, lse=lse)
+    torch.cuda.synchronize()
+    assert (out == 0).all() and (lse == -math.inf).all()
+
+
 def test_long_prompts(netkv):
     check(netkv, [9000, 2500], [9000, 4000], 4, 1, 128, torch.bfloat16, rows=40)
     check(netkv, [40000], [40000], 2, 1, 64, torch.float16, rows=40)
