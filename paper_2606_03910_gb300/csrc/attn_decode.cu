@@ -99,16 +99,6 @@ __device__ __forceinline__ uint64_t div_floor(uint64_t x, uint64_t y) {
   return (x | y) >> 32 ? x / y : (uint32_t)x / (uint32_t)y;
 }
 
-// The pages of the first 128 sequences, lane l's 4 l .. 4 l + 3: read once a warp.
-struct Lens {
-  uint32_t n[4];
-  __device__ __forceinline__ explicit Lens(const DecodeArgs& a) {
-    const uint32_t i = (threadIdx.x & 31) * 4;
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) n[j] = i + j < a.n_seqs ? pages_of(a, i + j) : 0;
-  }
-};
-
 // The runs: equal parts of a line on which every segment (a sequence and a unit: a KV head and a
 // chunk of its query heads) takes kEdge places, what it costs to begin and end one in pages, and
 // one for each page.
@@ -126,16 +116,48 @@ struct Runs {
 
 __device__ __forceinline__ uint64_t places(uint32_t pages) { return pages ? pages + kEdge : 0; }
 
+// The sequences in chunks of 128, lane l's 4 l .. 4 l + 3 of one: the pages of the first chunk,
+// and of chunk c (of the first 32) its places, in lane c.  Read once a warp.
+struct Lens {
+  uint32_t n[4];
+  uint64_t chunk, total;
+  static __device__ __forceinline__ uint64_t read(const DecodeArgs& a, uint32_t from, uint32_t* n) {
+    const uint32_t i = from + (threadIdx.x & 31) * 4;
+    uint64_t sum = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      n[j] = i + j < a.n_seqs ? pages_of(a, i + j) : 0;
+      sum += places(n[j]);
+    }
+    return sum;
+  }
+  static __device__ __forceinline__ uint64_t all(uint64_t x) {
+#pragma unroll
+    for (int d = 16; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
+    return x;
+  }
+  __device__ __forceinline__ explicit Lens(const DecodeArgs& a) {
+    const uint32_t lane = threadIdx.x & 31;
+    total = all(read(a, 0, n));
+    chunk = lane == 0 ? total : 0;
+#pragma unroll 4
+    for (uint32_t c = 1; c < min((a.n_seqs + 127) / 128, 32u); ++c) {
+      uint32_t m[4];
+      const uint64_t sum = all(read(a, c * 128, m));
+      if (lane == c) chunk = sum;
+      total += sum;
+    }
+    for (uint32_t from = 32 * 128; from < a.n_seqs; from += 128) {
+      uint32_t m[4];
+      total += all(read(a, from, m));
+    }
+  }
+};
+
 template <bool kOwn>
 __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, uint32_t units) {
-  uint64_t sum = 0;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) sum += places(lens.n[j]);
-  for (uint32_t i = 128 + (threadIdx.x & 31); i < a.n_seqs; i += 32) sum += places(pages_of(a, i));
-#pragma unroll
-  for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   Runs r;
-  r.total = sum * units;
+  r.total = lens.total * units;
   // a warp's own run is long enough not to cut many short segments
   r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / (kOwn ? 16 : kMinPages)));
   r.base = div_floor(r.total, r.count);
@@ -152,15 +174,31 @@ struct Segment {
 __device__ __forceinline__ Segment segment_at(const DecodeArgs& a, const Lens& lens, uint32_t units,
                                               uint64_t at, uint64_t* into) {
   const uint32_t lane = threadIdx.x & 31;
-  for (uint32_t from = 0; from < a.n_seqs; from += 128) {
+  uint32_t from = 0;
+  if (a.n_seqs > 128) {  // the chunk first
+    uint64_t upto = lens.chunk * units;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint64_t x = __shfl_up_sync(~0u, upto, d);
+      if (lane >= (uint32_t)d) upto += x;
+    }
+    const uint32_t hit = __ballot_sync(~0u, at < upto);
+    const uint32_t c = hit ? __ffs(hit) - 1 : 32;
+    const uint64_t before = __shfl_sync(~0u, upto, c ? c - 1 : 0);
+    at -= c ? before : 0;
+    from = c * 128;
+  }
+  for (; from < a.n_seqs; from += 128) {
     uint32_t n[4];
     uint64_t mine = 0;
+    if (from == 0) {
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-      const uint32_t i = from + lane * 4 + j;
-      n[j] = from == 0 ? lens.n[j] : i < a.n_seqs ? pages_of(a, i) : 0;
-      mine += places(n[j]) * units;
+      for (uint32_t j = 0; j < 4; ++j) n[j] = lens.n[j];
+    } else {
+      Lens::read(a, from, n);
     }
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) mine += places(n[j]) * units;
     uint64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {

@@ -261,3 +261,12 @@ def test_refusals(netkv):
     torch.cuda.synchronize()
     assert netkv.netkv_attn_decode_workspace_size(pages, 1, 3, 1) == 0
     go(q=q[:0], out=out[:0], length=length[:0], table=table[:0])
+
+
+@pytest.mark.parametrize("n", [4097, 4500])
+def test_thousands_of_sequences(netkv, n):
+    """More sequences than a warp keeps sums of chunks for, some without tokens."""
+    rng = np.random.default_rng(n)
+    lengths = np.where(rng.random(n) < 0.3, 0, rng.integers(1, 60, n))
+    lengths[[0, n // 2, n - 1]] = 700
+    check(netkv, lengths.tolist(), 2, 1, 64, torch.float16, "int8", seed=n, width=44)
