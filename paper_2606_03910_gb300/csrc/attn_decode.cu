@@ -288,7 +288,8 @@ struct Shared {
   static constexpr int kGroupFloats = 16 * kHeads + 8;  // of 16 dims; the 8 spread the banks
   alignas(128) unsigned char ring[kWarps][kRing][2][2][kBlockTokens * kDim];
   float o[kWarps / 2][kDim / 16 * kGroupFloats];
-  float m[kWarps][kHeads], l[kWarps][kHeads], top[kHeads], sum[kHeads];
+  float m[kWarps][kHeads], l[kWarps][kHeads];
+  float by[kHeads];  // what a head's sums are multiplied by
   alignas(16) float2 scale[kWarps][kRing][2];  // of keys and values
   uint2 tokens[kWarps][kRing];                 // of each page; 0 where it is absent
   alignas(8) uint64_t full[kWarps][kRing], empty[kWarps][kRing];
@@ -777,8 +778,15 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
 #pragma unroll
       for (uint32_t w = 0; w < kWarps; ++w)
         sum += (sh.m[w][tid] == -INFINITY ? 0.f : ex2(sh.m[w][tid] - top)) * sh.l[w][tid];
-      sh.top[tid] = top;
-      sh.sum[tid] = sum;
+      sh.by[tid] = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+      if (head0 + tid < a.group) {
+        const uint64_t at = (uint64_t)seg.seq * a.heads + kv_head * a.group + head0 + tid;
+        const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
+        if (whole && a.lse) a.lse[at] = z * kLn2;
+        if (whole && kMass) a.lse2[at] = z;
+        if (!whole)
+          reinterpret_cast<float2*>(a.part_ml)[slot * kHeads + tid] = make_float2(top, sum);
+      }
     }
     // to one maximum; then two warps' sums through shared memory onto the other two's
 #pragma unroll
@@ -816,30 +824,21 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
       }
       sync_warps();
     }
-    for (uint32_t x = tid; x < kHeads * kDim; x += kWarps * 32) {
-      const uint32_t h = x / kDim, dim = x % kDim;
-      if (head0 + h >= a.group) break;
-      const float top = sh.top[h], sum = sh.sum[h];
+#pragma unroll
+    for (uint32_t i = 0; i < kHeads * kDim / 2 / (kWarps * 32); ++i) {  // two dims a thread
+      const uint32_t x = 2 * (i * kWarps * 32 + tid), h = x / kDim, dim = x % kDim;
       const uint32_t at = dim / 16 * Sh::kGroupFloats + dim % 16 * kHeads + h;
-      const float all = sh.o[0][at] + sh.o[1][at];
+      const float by = sh.by[h];
+      const float y0 = (sh.o[0][at] + sh.o[1][at]) * by;
+      const float y1 = (sh.o[0][at + kHeads] + sh.o[1][at + kHeads]) * by;
+      if (head0 + h >= a.group) continue;
       const uint32_t head = kv_head * a.group + head0 + h;
-      if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const uint32_t y = pack16<kBf16>(all * inv, 0.f);
-        reinterpret_cast<uint16_t*>(a.out)[seg.seq * a.out_stride + (uint64_t)head * kDim + dim] =
-            (uint16_t)y;
-        if (dim == 0) {
-          const float z = sum == 0.f ? -INFINITY : top + log2f(sum);
-          if (a.lse) a.lse[(uint64_t)seg.seq * a.heads + head] = z * kLn2;
-          if (kMass) a.lse2[(uint64_t)seg.seq * a.heads + head] = z;
-        }
-      } else {
-        a.part_o[((uint64_t)slot * kHeads + h) * kDim + dim] = all;
-        if (dim == 0) {
-          a.part_ml[(slot * kHeads + h) * 2] = top;
-          a.part_ml[(slot * kHeads + h) * 2 + 1] = sum;
-        }
-      }
+      if (whole)
+        *reinterpret_cast<uint32_t*>(
+            a.out + (seg.seq * a.out_stride + (uint64_t)head * kDim + dim) * 2) = pack16<kBf16>(y0, y1);
+      else
+        *reinterpret_cast<float2*>(a.part_o + ((uint64_t)slot * kHeads + h) * kDim + dim) =
+            make_float2(y0, y1);
     }
     sync_warps();
   }
