@@ -857,13 +857,18 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
 }
 
 // Joins the segments that runs share: one block of threads a boundary.  The boundaries of a
-// segment share its heads; a head's parts are spread over the block's warps that have it (all 16
-// for one head: a long sequence alone on the card has 456 parts; two for each of eight where a
-// segment is cut once), a lane has kDim / 32 dims, and their sums are added in the warps' order.
-constexpr uint32_t kJoin = 512;
-template <int kDim, int kTiles, bool kBf16, bool kMass>
-__global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ DecodeArgs a) {
-  constexpr uint32_t kHeads = kTiles * 8, kJoinWarps = kJoin / 32, kPer = kDim / 32;
+// segment share its heads; a head's parts are spread over the block's warps that have it (all 8
+// for one head: a long sequence alone on the card has 456 parts; one for each of eight heads where
+// a segment is cut once), a lane has kDim / 32 dims, and their sums are added in the warps' order.
+// A warp reads kBatch parts at a time: 8 where segments are few and long; 2 with a run for each
+// warp, whose boundaries are many and need the SMs' registers for other blocks (at 8, 300
+// sequences of 1,000 tokens at 64 query heads took 148 us instead of 134).
+template <int kTiles>
+constexpr uint32_t kJoin = kTiles == 1 ? 256 : 512;  // a warp for each head of a tile, at least
+template <int kDim, int kTiles, bool kBf16, bool kMass, bool kOwn>
+__global__ void __launch_bounds__(kJoin<kTiles>) join_kernel(const __grid_constant__ DecodeArgs a) {
+  constexpr int kBatch = kOwn ? 2 : 8;
+  constexpr uint32_t kHeads = kTiles * 8, kJoinWarps = kJoin<kTiles> / 32, kPer = kDim / 32;
   __shared__ float sums[kJoinWarps][kDim];
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   let_follow();
@@ -882,31 +887,13 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ Dec
   };
   float top = -INFINITY, sum = 0.f, o[kPer] = {};
   if (real) {
-    // loads of several parts are under way at a time: each is a round trip to L2
+    // loads of several parts are under way at a time, the first sums before the maxima they
+    // wait for: each is a round trip to L2
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
-    for (uint32_t i = 0; i < s.parts; i += 128) {
-      float2 x[4];
+    float m[kBatch], x[kBatch][kPer];
+    auto read = [&](uint32_t i) {
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        const uint32_t at = i + j * 32 + lane;
-        x[j] = at < s.parts ? ml[slot(at)] : make_float2(-INFINITY, 0.f);
-      }
-      float to = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), top);
-#pragma unroll
-      for (int d = 16; d; d /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, d));
-      sum = top == -INFINITY ? sum : sum * ex2(top - to);
-      // a part of NaN scores has no maximum, but its sum says so
-#pragma unroll
-      for (uint32_t j = 0; j < 4; ++j)
-        sum += x[j].x == -INFINITY ? 0.f * x[j].y : ex2(x[j].x - to) * x[j].y;
-      top = to;
-    }
-#pragma unroll
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
-    for (uint32_t i = warp / spread; i < s.parts; i += 8 * each) {
-      float m[8], x[8][kPer];
-#pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
+      for (int j = 0; j < kBatch; ++j) {
         const uint32_t at = i + j * each;
         const bool in = at < s.parts;
         m[j] = in ? ml[slot(at)].x : -INFINITY;
@@ -923,12 +910,38 @@ __global__ void __launch_bounds__(kJoin) join_kernel(const __grid_constant__ Dec
           }
         }
       }
+    };
+    uint32_t next = warp / spread;
+    read(next);
+    for (uint32_t i = 0; i < s.parts; i += 128) {
+      float2 z[4];
 #pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
+      for (uint32_t j = 0; j < 4; ++j) {
+        const uint32_t at = i + j * 32 + lane;
+        z[j] = at < s.parts ? ml[slot(at)] : make_float2(-INFINITY, 0.f);
+      }
+      float to = fmaxf(fmaxf(fmaxf(z[0].x, z[1].x), fmaxf(z[2].x, z[3].x)), top);
+#pragma unroll
+      for (int d = 16; d; d /= 2) to = fmaxf(to, __shfl_xor_sync(~0u, to, d));
+      sum = top == -INFINITY ? sum : sum * ex2(top - to);
+      // a part of NaN scores has no maximum, but its sum says so
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        sum += z[j].x == -INFINITY ? 0.f * z[j].y : ex2(z[j].x - to) * z[j].y;
+      top = to;
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    while (true) {
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
         const float w = m[j] == -INFINITY ? 0.f : ex2(m[j] - top);
 #pragma unroll
         for (uint32_t q = 0; q < kPer; ++q) o[q] += w * x[j][q];
       }
+      next += kBatch * each;
+      if (next >= s.parts) break;
+      read(next);
     }
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i) sums[warp][lane * kPer + i] = o[i];
@@ -1119,7 +1132,9 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
     (own ? owned : shared)<<<kCtas<kTiles>, kThreads, bytes, s>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
     if (!uncut_runs(table_width))
-      NETKV_CUDA_TRY(launch_following(join_kernel<kDim, kTiles, kB, kM>, ws.runs - 1, kJoin, s, a));
+      NETKV_CUDA_TRY(launch_following(own ? join_kernel<kDim, kTiles, kB, kM, true>
+                                          : join_kernel<kDim, kTiles, kB, kM, false>,
+                                      ws.runs - 1, kJoin<kTiles>, s, a));
     return NETKV_OK;
   };
   auto with_mass = [&](auto dim, auto tiles, auto bf, auto e4) {
