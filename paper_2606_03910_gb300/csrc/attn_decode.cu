@@ -4,9 +4,9 @@
 // Bound: the codes are read once, 2 kDim bytes a token and KV head, and everything else is
 // small, so the kernel streams pages and its arithmetic has to fit in their shadow: about 330
 // instructions a warp and page of 4 KB, which take 45 % of the issue slots.  160 sequences of
-// 5,500 tokens with 64 query heads on 8 KV heads of 128, int8: 309 us, 5.8 TB/s; 64 of 13,000
-// with 16 on 2 and block weights: 94 us, 4.6 TB/s; two of 131,072, e4m3: 43 us, 3.1 TB/s (of
-// which 20 are the bytes and 10 the join and both ends); one of 512: 10.5 us on the device.
+// 5,500 tokens with 64 query heads on 8 KV heads of 128, int8: 300 us, 6.0 TB/s; 64 of 13,000
+// with 16 on 2 and block weights: 91 us, 4.8 TB/s; two of 131,072, e4m3: 39 us, 3.4 TB/s (of
+// which 20 are the bytes and 10 the join and both ends); one of 512: 10 us.
 //
 // Split: the work is the list of all pages, (sequence, KV head, block) in order, cut into equal
 // runs, so that ragged batches and single long sequences spread over the card alike.  A run is
@@ -37,7 +37,7 @@ constexpr uint32_t kCtas = kTiles == 1 ? 456 : 304;
 constexpr uint32_t kUncutBlocks = 32;  // see uncut_runs
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
-constexpr uint32_t kEdge = 8;       // see Runs; at 0 runs of short segments end last (338 us for 309)
+constexpr uint32_t kEdge = 8;       // see Runs; at 0 runs of short segments end last (338 us for 308)
 constexpr uint32_t kMinPages = 16;  // a block's run at least: a pair of pages a warp, and an edge
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
