@@ -144,6 +144,10 @@ def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
     """Slot `slot` of src into the empty slot `to` of dst, block by block; the bytes moved."""
     if dst.tokens[to]:
         raise ValueError(f"slot {to} is in use")
+    # codes are copied as they are, page by page
+    kind = lambda pool: (tuple(pool.pages.tensors[0].shape[1:]), pool.pages.tensors[0].dtype)  # noqa: E731
+    if kind(src) != kind(dst):
+        raise ValueError(f"pools of one shape and format expected, got {kind(src)} and {kind(dst)}")
     n = src.tokens[slot]
     counts = [0] * dst.slots
     counts[to] = n
