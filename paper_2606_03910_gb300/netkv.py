@@ -146,6 +146,8 @@ class KvPages(C.Structure):
         for t in (k, v, k_scale, v_scale):
             if not t.is_contiguous():
                 raise ValueError("KV pages and scales are contiguous")
+            if t.get_device() != k.get_device():
+                raise ValueError("KV pages and scales of one device expected")
         _f32(k_scale)
         _f32(v_scale)
         super().__init__(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
@@ -153,6 +155,7 @@ class KvPages(C.Structure):
         self.tensors = (k, v, k_scale, v_scale)
         self.ref = C.byref(self)
         self.heads_dim = (k.shape[1], k.shape[3])  # a field of a structure takes longer to read
+        self.device, self.get_device = k.device, k.get_device
 
 
 NETKV_BLOCK_TOKENS = 16
@@ -495,21 +498,25 @@ def _plane(t, rows: int, width: int) -> Optional[int]:
     return t.data_ptr()
 
 
-_raw_stream = None
+_raw_stream = _current_device = None
 
 
-def _on(t, stream):
-    """The stream of a call on t's device: the given one, else torch's current one there."""
-    d = t.get_device()
-    if d < 0:
-        raise TypeError(f"CUDA tensors expected, got one on {t.device}")
-    if stream is not None:
-        return _stream(stream)
-    global _raw_stream
+def _on(stream, first, *others):
+    """The stream of a call whose tensors are all on the current CUDA device, where its kernels
+    run: the given one, else torch's current one.  None and addresses are not looked at."""
+    global _raw_stream, _current_device
     if _raw_stream is None:
         import torch
-        _raw_stream = torch._C._cuda_getCurrentRawStream
-    return _raw_stream(d)
+        _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    d = first.get_device()
+    if d < 0:
+        raise TypeError(f"CUDA tensors expected, got one on {first.device}")
+    if d != _current_device():
+        raise ValueError(f"tensors on CUDA device {d}, but the current one is {_current_device()}")
+    for t in others:
+        if t is not None and t.__class__ is not int and t.get_device() != d:
+            raise ValueError(f"tensors on CUDA device {d} expected, got one on {t.device}")
+    return _raw_stream(d) if stream is None else _stream(stream)
 
 
 def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, stream) -> None:
@@ -522,7 +529,8 @@ def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, str
     n = off.numel() - 1
     tp, tw = _table(table, n)
     code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
-                _ints(start, _I32, n), tp, tw, _ptr(status), _on(k, stream))
+                _ints(start, _I32, n), tp, tw, _ptr(status),
+                _on(stream, k, v, off, start, table, status, pages))
     if code:
         raise NetKVError(fn, code)
 
@@ -553,7 +561,8 @@ def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=N
     _check("netkv_attn_prompt", _lib.netkv_attn_prompt(
         dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, _I64, n + 1),
         _ints(k_off, _I64, n + 1), q_rows, k_rows, dim ** -0.5 if scale is None else scale,
-        op, os_, _plane(lse, q_rows, heads), _ptr(status), _on(q, stream)))
+        op, os_, _plane(lse, q_rows, heads), _ptr(status),
+        _on(stream, q, k, v, q_off, k_off, out, lse, status)))
 
 
 def netkv_attn_decode_workspace_size(pages: KvPages, n_seqs: int, heads: int, table_width: int,
@@ -578,7 +587,8 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
         pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n), tp, tw,
         dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads),
         _plane(mass_in, n, tw), _plane(mass_out, n, tw), _ptr(workspace), ws_bytes,
-        _ptr(status), _on(q, stream)))
+        _ptr(status), _on(stream, q, length, table, out, lse, mass_in, mass_out, workspace, status,
+                          pages)))
 
 
 def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_out, length_out,
@@ -593,7 +603,9 @@ def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_ou
     _check("netkv_kv_evict", _lib.netkv_kv_evict(
         n, tp, _ints(length, _I32, n), _plane(mass, n, tw), tw, _ints(budget, _I32, n), int(sink),
         int(recent), to, _ints(length_out, _I32, n), _plane(mass_out, n, tw), fr,
-        _ints(n_freed, _I32, n), _ptr(status), _on(table, stream)))
+        _ints(n_freed, _I32, n), _ptr(status),
+        _on(stream, table, length, mass, budget, table_out, length_out, mass_out, freed, n_freed,
+            status)))
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:
