@@ -583,6 +583,8 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
         raise ValueError("as many rows of out as of q expected")
     tp, tw = _table(table, n)
     ws_bytes = 0 if workspace is None else workspace.nbytes
+    if ws_bytes and not workspace.is_contiguous():
+        raise ValueError("a contiguous workspace expected")
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
         pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n), tp, tw,
         dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads),

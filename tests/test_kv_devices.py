@@ -116,3 +116,15 @@ def test_addresses_and_absent_arguments(kv):
     a.update(status=None, start=None)
     netkv.netkv_kv_store(pages(netkv, 0), **a)
     assert len(calls) == 2
+
+
+def test_a_workspace_that_is_not_as_large_as_it_says(kv):
+    """Elements that lie on one another or apart: their number is not the buffer's size."""
+    netkv, calls = kv
+    one = torch.zeros(1, dtype=torch.uint8)
+    for bad in (one.expand(1 << 10), torch.zeros(1 << 11, dtype=torch.uint8)[::2]):
+        a = {k: on(t, 0) for k, t in ARGS["netkv_attn_decode"].items()}
+        a.update(workspace=on(bad, 0))
+        with pytest.raises(ValueError):
+            netkv.netkv_attn_decode(pages(netkv, 0), **a)
+    assert not calls
