@@ -34,6 +34,11 @@ constexpr int kRows = 128, kKeys = 128;  // of a tile
 // 4,096 tokens takes 58 us, 67 without; at 6 ten ragged ones would take 89 instead of 67.
 constexpr uint32_t kFewItems = 6;
 constexpr float kLag = 8.f;              // in powers of two
+// Where the weight of the running maximum stands, in powers of two.  fp16 ends at 2^16, so weights
+// up to 2^kLag have room for 2^7, and are exact to 2^-11 down to 2^-21 of the largest one, 0 below
+// 2^-32; at 1, keys 2^-25 below a sink of small values would leave the output and not its sum.
+template <bool kBf16>
+constexpr float kUp = kBf16 ? 0.f : 7.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // and a warp for the loads, one for the products
@@ -730,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        const float base = m == -INFINITY ? 0.f : -m * a.scale2;
+        const float base = m == -INFINITY ? 0.f : fmaf(-m, a.scale2, kUp<kBf16>);
         const uint64_t scale_2 = pair(a.scale2, a.scale2), base_2 = pair(base, base);
         uint64_t sums_2[2] = {0, 0};
 #pragma unroll
@@ -841,7 +846,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (row < y.rows && a.lse)
         a.lse[(x.q_first + y.row + row) * a.heads + y.head] =
-            l == 0.f ? -INFINITY : m * a.scale2 * kLn2 + logf(l);
+            l == 0.f ? -INFINITY : logf(l) - fmaf(-m, a.scale2, kUp<kBf16>) * kLn2;
       __syncwarp();
       before_sync();
     }
