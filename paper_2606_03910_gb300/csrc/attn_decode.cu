@@ -43,6 +43,11 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
 // weights up to 2^8 are as exact in fp16 as those up to 1, and sums are fp32.
 constexpr float kLag = 8.f;
+// Weights go into the second product times their value scale over a unit that is above all value
+// scales so far (at most twice the largest), and times 2^kUp: up to 2^(kLag + kUp), below fp16's
+// 2^16.  They are exact to 2^-11 down to 2^-20 of the largest one, 0 below 2^-31; without the
+// factor, keys 2^-24 below a sink of small values would leave the output and not its sum.
+constexpr uint32_t kUp = 7;
 
 struct Cut;
 
@@ -549,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
     float o[kTiles][kDim / 16][4] = {}, m[kTiles][2], l[kTiles][2] = {};
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) m[t][0] = m[t][1] = -INFINITY;
-    float v_unit = 0.f, v_inv = 0.f;  // a power of two that the value scales are taken by
+    float v_unit = 0.f, v_inv = 0.f;  // a power of two that the sums are in, 1 over it
 
     for (uint32_t i = 0; i < pairs; ++i) {
       const uint32_t st = taken % kRing;
@@ -616,9 +621,9 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
               for (int z = 0; z < 4; ++z) o[t][j][z] *= to[z & 1];
           }
         }
-        if (fmaxf(vs[0], vs[1]) > v_unit) {  // the whole warp
-          const uint32_t e = min(max(__float_as_uint(fmaxf(vs[0], vs[1])) >> 23, 2u), 252u);
-          const float unit = __uint_as_float((e + 1) << 23), shrink = v_unit / unit;
+        if (fmaxf(vs[0], vs[1]) > v_unit * (1 << kUp)) {  // the whole warp
+          const uint32_t e = min(max(__float_as_uint(fmaxf(vs[0], vs[1])) >> 23, kUp + 2), 254u);
+          const float unit = __uint_as_float((e + 1 - kUp) << 23), shrink = v_unit / unit;
 #pragma unroll
           for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -626,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
 #pragma unroll
               for (int z = 0; z < 4; ++z) o[t][j][z] *= shrink;
           v_unit = unit;
-          v_inv = __uint_as_float((253 - e) << 23);
+          v_inv = __uint_as_float((253 + kUp - e) << 23);
         }
         uint32_t p[2][kTiles][2];
 #pragma unroll

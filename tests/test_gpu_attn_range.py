@@ -5,7 +5,8 @@ An attention sink is the usual case: one key takes nearly all of a row's weight,
 small, and the output is what the many other keys add.  A weight that goes into the second product
 in fp16 is rounded to 2^-11 of itself, or by 2^-25 of fp16's unit where it is subnormal.  The
 largest weight of a row may stand at 2^7 at least (weights are at most 2^8 above it, and fp16 ends
-at 2^16), so that is 2^-32 of the largest weight, or of the row's sum, for each key.
+at 2^16), so that is 2^-32 of the largest weight, or of the row's sum, for each key (decode: times up
+to 2 for the unit of the value scales).
 """
 import math
 
@@ -78,3 +79,94 @@ def test_long_prompts_to_a_narrow_bound(netkv, n, dim, heads, kv_heads):
         o, _, _, weight, size = plain.attention(q[at, h].double(), k[:, hk].double(),
                                                 v[:, hk].double(), dim ** -0.5, see)
         plain.close_out(out[at, h], o, weight, size, dim, q.dtype, plain.U[q.dtype], n * FLOOR * 6.0)
+
+
+def paged(k, v, fmt):
+    """Rows k, v [n, heads, dim] float32 as blocks: codes, scales, the values that they stand for
+    (float64, on the CPU) and the table of one sequence."""
+    n, heads, dim = k.shape
+    blocks = -(-n // 16)
+    got, values = [], []
+    for x in (k, v):
+        x = torch.cat([x, torch.zeros((blocks * 16 - n, heads, dim))])
+        x = x.view(blocks, 16, heads, dim).transpose(1, 2).contiguous()
+        scale = x.abs().amax((2, 3)).clamp_min(2.0 ** -100) / plain.TOP[fmt]
+        codes = (x / scale[..., None, None]).clamp(-plain.TOP[fmt], plain.TOP[fmt])
+        codes = codes.round().to(torch.int8) if fmt == "int8" else codes.to(torch.float8_e4m3fn)
+        got += [codes.cuda(), scale.cuda()]
+        values.append((codes.float().double() * scale.double()[..., None, None]).transpose(1, 2)
+                      .reshape(blocks * 16, heads, dim)[:n])
+    return (got[0], got[2], got[1], got[3]), values, ints(range(blocks)).view(1, blocks)
+
+
+def decode(netkv, q, tensors, table, n, scale, mass=True):
+    """One sequence's output, lse and block weights."""
+    heads = q.shape[1]
+    pages = netkv.KvPages(*tensors)
+    size = netkv.netkv_attn_decode_workspace_size(pages, 1, heads, table.shape[1], mass)
+    ws = torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((1, heads), device="cuda")
+    m = torch.zeros(table.shape, device="cuda") if mass else None
+    netkv.netkv_attn_decode(pages, q, ints([n]), table, out, lse=lse, mass_out=m, scale=scale,
+                            workspace=ws)
+    torch.cuda.synchronize()
+    return out[0].cpu(), lse[0].cpu(), None if m is None else m[0].cpu().double()
+
+
+def check_decode(netkv, q, k, v, fmt, scale=1.0):
+    """q [heads, dim] of its type, one KV head."""
+    n, dim = len(k), q.shape[1]
+    tensors, (kk, vv), table = paged(k, v, fmt)
+    out, lse, mass = decode(netkv, q[None].cuda(), tensors, table, n, scale)
+    see = torch.ones((len(q), n), dtype=torch.bool)
+    o, z, p, weight, size = plain.attention(q.double(), kk[:, 0], vv[:, 0], scale, see)
+    # a weight's unit goes by the largest value that a block of the call can hold, and is a power
+    # of two up to twice above
+    slack = n * 2 * FLOOR * float(tensors[3].max()) * plain.TOP[fmt]
+    plain.close_out(out, o, weight, size, dim, q.dtype, 2.0 ** -11, slack)
+    plain.close_lse(lse, z, size, dim)
+    drawn = torch.cat([p.sum(0), torch.zeros(-n % 16, dtype=torch.float64)]).view(-1, 16).sum(1)
+    tol = (2 * plain.score_error(size, dim) + 2.0 ** -18) * drawn + 1e-30
+    assert ((mass - drawn).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("gap,sink", [(10, 0), (22, 5), (24, 0), (26, 0), (24, 130000)])
+@pytest.mark.parametrize("n,heads,dim", [(500, 8, 64), (131072, 8, 128), (131072, 12, 64)])
+def test_decode_sinks(netkv, dtype, fmt, gap, sink, n, heads, dim):
+    """A sink 2^gap above the other keys, with values of 0, in a block whose other values are as
+    everywhere."""
+    sink = min(sink, n - 1)
+    g = torch.Generator().manual_seed(gap)
+    q = (0.05 * torch.randn((heads, dim), generator=g))
+    k = torch.randn((n, 1, dim), generator=g)
+    v = 0.5 + torch.rand((n, 1, dim), generator=g)
+    q[:, 0], k[..., 0] = 1.0, 0.0
+    k[sink], v[sink] = 0.0, 0.0
+    k[sink, :, 0] = gap * math.log(2)
+    check_decode(netkv, q.to(dtype), k, v, fmt)
+
+
+@pytest.mark.parametrize("n", [40000, 70000])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_long_decodes_to_a_narrow_bound(netkv, fmt, n):
+    """Near-uniform scores over many keys, where outputs are small themselves."""
+    g = torch.Generator().manual_seed(n)
+    q = torch.randn((8, 128), generator=g).half()
+    k, v = torch.randn((n, 1, 128), generator=g), torch.randn((n, 1, 128), generator=g)
+    check_decode(netkv, q, k, v, fmt, scale=128 ** -0.5)
+
+
+@pytest.mark.parametrize("spread", [4, 12])
+def test_decode_value_scales_far_apart(netkv, spread):
+    """Blocks whose values are 2^spread below another's: that one's scale sets the unit."""
+    g = torch.Generator().manual_seed(spread)
+    n, dim = 4000, 64
+    q = torch.randn((8, dim), generator=g).bfloat16()
+    k, v = torch.randn((n, 1, dim), generator=g), torch.rand((n, 1, dim), generator=g)
+    v[16:] *= 2.0 ** -spread
+    k[:16, :, :] = 0.0
+    q[:, 0], k[:, :, 0] = 1.0, 0.0
+    k[:16, :, 0] = -20 * math.log(2)  # and the large values have little weight
+    check_decode(netkv, q, k, v, "int8")
