@@ -22,9 +22,10 @@
 // and O^T = V^T P^T are products of 16 x 16 by 16 x 8: m16n8k16, with up to 8 (kTiles = 1) or
 // 16 heads (2) side by side.  A tcgen05 product would be 128 rows high, of which the group
 // fills 8.  Both code types are exact in fp16, so codes go into the products as they are and
-// the scales are applied to scores and weights in fp32.  A row of queries is brought to [1, 2)
-// by a power of two, which loses nothing of bf16's 8 bits.  The order of the inner dimension is
-// free in a product: a thread's operands are the bytes that lie together, 16 at a load.
+// the scales are applied to scores and weights in fp32.  A row of bf16 queries is brought to
+// [2^14, 2^15) by a power of two, the top of fp16's range that sums of fp32 leave room for: channels
+// down to 2^-31 of the largest keep all of bf16's 8 bits.  The order of the inner dimension is free
+// in a product: a thread's operands are the bytes that lie together, 16 at a load.
 #include "kv_common.cuh"
 
 namespace {
@@ -529,27 +530,35 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const uint32_t* w = reinterpret_cast<const uint32_t*>(raw[t]);
-      float largest = 0.f;
+      if constexpr (kBf16) {
+        float largest = 0.f;
 #pragma unroll
-      for (int i = 0; i < kDim / 8; ++i) {
-        const float2 x = unpack16<kBf16>(w[i]);
-        largest = fmaxf(largest, fmaxf(fabsf(x.x), fabsf(x.y)));
-      }
-      largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 1));
-      largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 2));
-      uint32_t e = __float_as_uint(largest) >> 23;
-      if (e < 2 || e > 252) e = 127;
-      const float inv = __uint_as_float((254 - e) << 23);
-      const float up = __uint_as_float(e << 23) * a.scale2;
-      f[t][0] = __shfl_sync(~0u, up, 8 * c);
-      f[t][1] = __shfl_sync(~0u, up, 8 * c + 4);
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 x = unpack16<kBf16>(w[i * 2 + j]);
-          q[t][i][j] = pack16<false>(x.x * inv, x.y * inv);
+        for (int i = 0; i < kDim / 8; ++i) {
+          const float2 x = unpack16<kBf16>(w[i]);
+          largest = fmaxf(largest, fmaxf(fabsf(x.x), fabsf(x.y)));
         }
+        largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 1));
+        largest = fmaxf(largest, __shfl_xor_sync(~0u, largest, 2));
+        // 2^14 over the largest value's power of two, and the reverse; both are normal numbers
+        const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);
+        const float inv = __uint_as_float((254 + 14 - e) << 23);
+        const float up = __uint_as_float((e - 14) << 23) * a.scale2;
+        f[t][0] = __shfl_sync(~0u, up, 8 * c);
+        f[t][1] = __shfl_sync(~0u, up, 8 * c + 4);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float2 x = unpack16<kBf16>(w[i * 2 + j]);
+            q[t][i][j] = pack16<false>(x.x * inv, x.y * inv);
+          }
+      } else {
+        f[t][0] = f[t][1] = a.scale2;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) q[t][i][j] = w[i * 2 + j];
+      }
     }
     float o[kTiles][kDim / 16][4] = {}, m[kTiles][2], l[kTiles][2] = {};
 #pragma unroll

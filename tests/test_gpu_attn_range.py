@@ -170,3 +170,34 @@ def test_decode_value_scales_far_apart(netkv, spread):
     q[:, 0], k[:, :, 0] = 1.0, 0.0
     k[:16, :, 0] = -20 * math.log(2)  # and the large values have little weight
     check_decode(netkv, q, k, v, "int8")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("heads", [8, 16])
+@pytest.mark.parametrize("dtype,large,small", [(torch.float16, 300.0, 0.003),
+                                               (torch.float16, 60000.0, 0.01),
+                                               (torch.bfloat16, 300.0, 0.003),
+                                               (torch.bfloat16, 1.0, 2.0 ** -20),
+                                               (torch.bfloat16, 1000.0, 2.0 ** -12)])
+def test_decode_channels_of_a_query_far_apart(netkv, dtype, large, small, heads, fmt):
+    """One channel dominates the query and is 0 in the keys, as outlier channels are: the others
+    make the scores, to all bits that they have."""
+    g = torch.Generator().manual_seed(heads)
+    n, dim = 700, 64
+    q = small * torch.randn((heads, dim), generator=g)
+    k, v = torch.randn((n, 1, dim), generator=g) / small, torch.randn((n, 1, dim), generator=g)
+    q[:, 5], k[..., 5] = large, 0.0
+    check_decode(netkv, q.to(dtype), k, v, fmt, scale=0.5)
+
+
+@pytest.mark.parametrize("power", [127, 126, 100, -100, -118, -126])
+def test_decode_queries_at_the_ends_of_bf16(netkv, power):
+    """Queries as large and as small as bf16 holds, with keys that bring the scores back."""
+    g = torch.Generator().manual_seed(1)
+    n, dim = 100, 64
+    q = (1 + torch.rand((8, dim), generator=g)).mul(0.99).double() * torch.randn((8, dim), generator=g).sign()
+    q = torch.ldexp(q, torch.tensor(power)).to(torch.bfloat16)
+    assert torch.isfinite(q.float()).all() and (q != 0).all()
+    k = torch.ldexp(torch.randn((n, 1, dim), generator=g).double(), torch.tensor(-max(-90, min(90, power)))).float()
+    v = torch.randn((n, 1, dim), generator=g)
+    check_decode(netkv, q, k, v, "int8", scale=2.0 ** (max(-90, min(90, power)) - power) / 8)
