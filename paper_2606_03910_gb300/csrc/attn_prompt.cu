@@ -252,6 +252,17 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
 __device__ __forceinline__ void sync_softmax() {
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
+// Whether all softmax threads say yes.
+__device__ __forceinline__ bool all_softmax(bool yes) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "bar.red.and.pred p, 1, 256, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(all)
+      : "r"((uint32_t)yes)
+      : "memory");
+  return all != 0;
+}
 __device__ __forceinline__ void tmem_loaded() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -687,7 +698,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t taken = 0, finished = 0;  // steps, and items with any
     while (true) {
       const Item x = items.next(sh, late);
-      if (x.valid < 0) break;
+      // Where the two tiles' warps meet at barriers inside an item, none leaves without the others:
+      // after a wait has run out, some may have taken the item and some been told that there is none.
+      if (!(a.mode == kKeyHalves ? all_softmax(x.valid >= 0) : x.valid >= 0)) break;
       if (x.valid == 0) continue;
       const Tile y = tile_of(a, x, t);
       const uint32_t steps = t ? x.steps[1] : x.steps[0];
