@@ -646,9 +646,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kSoftmaxWarps + 2) {
       // ---- plan: the block's own item, then those of blocks that have not started, which it
       // takes over one by one
-      for (uint32_t i = blockIdx.x * 32 + lane; i < a.n_seqs; i += gridDim.x * 32)
-        if (row_range(a.q_off, i, a.q_rows).bad || row_range(a.k_off, i, a.k_rows).bad)
-          flag_status(a.status, NETKV_DEV_ERANGE);
       // An item is claimed once the products of the one before begin, not earlier: what a block
       // holds in advance, another that is ready cannot take.
       uint32_t n = blockIdx.x;
@@ -679,6 +676,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
+        // Every index of the grid is some block's to check offsets for, its own or one taken over:
+        // blocks whose items others take never start.
+        if (n != ~0u)
+          for (uint64_t j = (uint64_t)n * 32 + lane; j < a.n_seqs; j += (uint64_t)gridDim.x * 32)
+            if (row_range(a.q_off, (uint32_t)j, a.q_rows).bad ||
+                row_range(a.k_off, (uint32_t)j, a.k_rows).bad)
+              flag_status(a.status, NETKV_DEV_ERANGE);
         Item x = {};
         x.valid = -1;
         if (n != ~0u) x = item_at(a, n);

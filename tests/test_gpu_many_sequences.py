@@ -1,0 +1,46 @@
+"""Calls with thousands of sequences."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_kv_blocks import ints  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+
+
+@pytest.fixture
+def netkv():
+    from paper_2606_03910_gb300 import netkv
+    return netkv
+
+
+@pytest.mark.parametrize("n,at", [(9000, 8990), (9000, 5000), (9000, 100), (20000, 19999)])
+@pytest.mark.parametrize("which", ["q", "k"])
+def test_bad_prompt_offsets_far_back(netkv, n, at, which):
+    """One bad pair among thousands of sequences, most of them empty: flagged, every time."""
+    rng = np.random.default_rng(n)
+    count = (rng.random(n) < 0.2).astype(np.int64)
+    count[at - 1:at + 1] = 1
+    off = np.concatenate([[0], np.cumsum(count)])
+    rows = int(off[-1])
+    bad = off.copy()
+    bad[at] += 2 if at + 1 < n else rows  # the next pair decreases, or this one passes the rows
+    q = torch.ones((rows, 2, 64), dtype=torch.float16, device="cuda")
+    k = torch.ones((rows, 1, 64), dtype=torch.float16, device="cuda")
+    good, wrong = ints(off.tolist(), torch.int64), ints(bad.tolist(), torch.int64)
+    for k_off, q_off, want in ((good, good, 0),
+                               (wrong if which == "k" else good, wrong if which == "q" else good,
+                                netkv.NETKV_DEV_ERANGE)):
+        for _ in range(3):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            netkv.netkv_attn_prompt(q, k, k, q_off, k_off, torch.empty_like(q), status=status)
+            torch.cuda.synchronize()
+            assert int(status.item()) == want
