@@ -988,7 +988,9 @@ __global__ void __launch_bounds__(kMassWarps * 32) mass_kernel(const __grid_cons
   uint32_t lanes = 32;  // of a block
   while (lanes / 2 >= a.heads) lanes /= 2;
   const uint32_t per = 32 / lanes, head = lane % lanes;
-  if (blockIdx.y * kMassWarps * kMassSteps * per >= pages) return;
+  // a sequence's first block waits without work too: were all blocks done before the kernels ahead,
+  // so would be the call
+  if (blockIdx.y && blockIdx.y * kMassWarps * kMassSteps * per >= pages) return;
   follow();
   for (uint32_t from = blockIdx.y * kMassWarps * kMassSteps * per; from < pages;
        from += gridDim.y * kMassWarps * kMassSteps * per) {

@@ -44,3 +44,23 @@ def test_bad_prompt_offsets_far_back(netkv, n, at, which):
             netkv.netkv_attn_prompt(q, k, k, q_off, k_off, torch.empty_like(q), status=status)
             torch.cuda.synchronize()
             assert int(status.item()) == want
+
+
+def test_what_follows_a_batch_without_tokens(netkv):
+    """Rows and lse of empty sequences are there for whatever comes next in the stream, block
+    weights or not."""
+    n, heads, dim = 30000, 16, 128
+    k, s = torch.zeros((2, 2, 16, dim), dtype=torch.int8, device="cuda"), torch.ones((2, 2), device="cuda")
+    pages = netkv.KvPages(k, k.clone(), s, s.clone())
+    q = torch.ones((n, heads, dim), dtype=torch.bfloat16, device="cuda")
+    length, table = ints([0] * n), torch.zeros((n, 40), dtype=torch.int32, device="cuda")
+    for mass in (None, torch.ones((n, 40), device="cuda")):
+        ws = torch.empty(netkv.netkv_attn_decode_workspace_size(pages, n, heads, 40, mass is not None),
+                         dtype=torch.uint8, device="cuda")
+        out, lse = torch.full_like(q, 5.0), torch.full((n, heads), 5.0, device="cuda")
+        torch.cuda.synchronize()
+        netkv.netkv_attn_decode(pages, q, length, table, out, lse=lse, mass_out=mass, workspace=ws)
+        seen, seen_lse = out.clone(), lse.clone()
+        torch.cuda.synchronize()
+        assert not seen.any() and bool((seen_lse == -float("inf")).all())
+        assert mass is None or bool((mass == 1).all())
