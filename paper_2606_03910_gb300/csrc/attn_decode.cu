@@ -258,16 +258,27 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   return done != 0;
 }
 
-// Waits for a phase of a barrier, a second at most (a hundredth once that has run out for a
-// thread of the block).
-__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
+// Waits for a phase of a barrier, a second at most.  Once that has run out for a thread of the
+// block, which says so, nobody waits any longer and the block runs to its end.
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late,
+                                     int* status) {
   if (try_wait(bar, parity)) return;
   const long long t0 = clock64();
-  while (!try_wait(bar, parity))
-    if (clock64() - t0 > (*late ? 20000000ll : 2000000000ll)) {
+  while (!try_wait(bar, parity)) {
+    if (*late) return;
+    if (clock64() - t0 > 2000000000ll) {
       *late = 1;
+      flag_status(status, NETKV_DEV_ETIMEOUT);
       return;
     }
+  }
+}
+// Before a warp ends: after a wait has run out, what is still in flight gets a moment to land.
+__device__ __forceinline__ void settle(volatile int* late) {
+  if (!*late) return;
+  const long long t0 = clock64();
+  while (clock64() - t0 < 20000000ll) {
+  }
 }
 __device__ __forceinline__ void sync_warps() {  // all but the loading one
   asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
@@ -431,31 +442,33 @@ __device__ __forceinline__ void load_pages(const DecodeArgs& a, Shared<kDim, kTi
   Batch b0 = take(), b1 = take();
   scales(b0);
   scales(b1);
-  while (__any_sync(~0u, b0.count)) {
+  while (__any_sync(~0u, b0.count && !*late)) {
     const Batch b2 = take();
     const uint32_t pairs = (b0.count + 1) / 2, n = given + turn;
     for (uint32_t q = 0; q < 32 / (2 * kWarps); ++q) {  // a pair for each warp
       if (turn == q && in / 2 < pairs) {
         const uint32_t st = n % kRing, bar = smem_addr(&sh.full[w][st]);
-        if (n >= kRing) wait(smem_addr(&sh.empty[w][st]), (n / kRing - 1) & 1, late);
-        if (b0.page >= 0) {
-          const uint64_t from = ((uint64_t)b0.page * a.kv.heads + b0.kv_head) * kPart;
-          asm volatile(
-              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-              "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][0])),
-              "l"(a.kv.k + from), "r"(kPart), "r"(bar)
-              : "memory");
-          asm volatile(
-              "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-              "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][1])),
-              "l"(a.kv.v + from), "r"(kPart), "r"(bar)
-              : "memory");
+        if (n >= kRing) wait(smem_addr(&sh.empty[w][st]), (n / kRing - 1) & 1, late, a.status);
+        if (!*late) {
+          if (b0.page >= 0) {
+            const uint64_t from = ((uint64_t)b0.page * a.kv.heads + b0.kv_head) * kPart;
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+                "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][0])),
+                "l"(a.kv.k + from), "r"(kPart), "r"(bar)
+                : "memory");
+            asm volatile(
+                "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+                "[%3];" ::"r"(smem_addr(sh.ring[w][st][lane & 1][1])),
+                "l"(a.kv.v + from), "r"(kPart), "r"(bar)
+                : "memory");
+          }
+          sh.scale[w][st][lane & 1] = b0.scale;
+          (&sh.tokens[w][st].x)[lane & 1] = b0.tokens;
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                       "r"(b0.page >= 0 ? 2 * kPart : 0)
+                       : "memory");
         }
-        sh.scale[w][st][lane & 1] = b0.scale;
-        (&sh.tokens[w][st].x)[lane & 1] = b0.tokens;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
-                     "r"(b0.page >= 0 ? 2 * kPart : 0)
-                     : "memory");
       }
       __syncwarp();
     }
@@ -492,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
   volatile int* late = &sh.late;
   if (warp == kWarps) {
     load_pages<kDim, kTiles, kOwn>(a, sh, lens, units, runs);
+    settle(late);
     return;
   }
   Walk walk;
@@ -567,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
 
     for (uint32_t i = 0; i < pairs; ++i) {
       const uint32_t st = taken % kRing;
-      wait(smem_addr(&sh.full[warp][st]), (taken / kRing) & 1, late);
+      wait(smem_addr(&sh.full[warp][st]), (taken / kRing) & 1, late, a.status);
       ++taken;
       const uint32_t at = 2 * (kOwn ? i : warp + kWarps * i), block = seg.first + at;
       const uint2 nn = sh.tokens[warp][st];
@@ -867,7 +881,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
     for (uint32_t h = tid; h < a.heads && a.lse; h += kWarps * 32)
       a.lse[(uint64_t)i * a.heads + h] = -INFINITY;
   }
-  if (tid == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
+  settle(late);
 }
 
 // Joins the segments that runs share: one block of threads a boundary.  The boundaries of a

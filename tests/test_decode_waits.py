@@ -26,3 +26,23 @@ def test_kernels_that_start_early_wait_before_they_end(kernel):
     assert len(before) == 2
     assert all(line.strip().startswith("if (blockIdx.y && ")
                for line in before[0].splitlines() if "return;" in line)
+
+
+def test_giving_up_is_said_and_copies_land():
+    """A wait that runs out sets the status itself: the thread that would say it for the block may
+    have ended.  Nobody waits after that, the loading warp starts no further copies (a ring's place may
+    still be in use, and a barrier takes no arrival before its turn), and the block stays until those
+    in flight have had time to land in its shared memory."""
+    wait = body("wait")
+    gives_up = wait[wait.index("*late = 1"):]
+    assert "flag_status(status, NETKV_DEV_ETIMEOUT)" in gives_up
+    assert re.search(r"if \(\*late\) return;", wait)
+    load = body("load_pages")
+    loop = load[load.index("while ("):]
+    assert "*late" in loop[:loop.index("{")]
+    issue = loop[loop.index("wait("):]
+    assert issue.index("if (!*late)") < issue.index("cp.async.bulk")
+    kernel = body("decode_kernel")
+    ends = [m.start() for m in re.finditer(r"return;", kernel)] + [len(kernel)]
+    for end in ends:
+        assert "settle(late);" in kernel[max(0, end - 60):end]
