@@ -148,14 +148,17 @@ class KvPages(C.Structure):
                 raise ValueError("KV pages and scales are contiguous")
             if t.get_device() != k.get_device():
                 raise ValueError("KV pages and scales of one device expected")
-        _f32(k_scale)
-        _f32(v_scale)
+        if not _ROWS:
+            _ask_torch()
+        for t in (k_scale, v_scale):
+            if t.dtype not in _F32:
+                raise TypeError(f"float32 tensor expected, got {t.dtype}")
         super().__init__(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
                          k.shape[0], k.shape[1], k.shape[3], _KV_FORMATS[fmt])
         self.tensors = (k, v, k_scale, v_scale)
         self.ref = C.byref(self)
         self.heads_dim = (k.shape[1], k.shape[3])  # a field of a structure takes longer to read
-        self.device, self.get_device = k.device, k.get_device
+        self.device, self.device_index = k.device, k.get_device()
 
 
 NETKV_BLOCK_TOKENS = 16
@@ -430,37 +433,49 @@ def netkv_copy_group_async(copies, stream=None) -> None:
 
 # ---- KV blocks: tensors carry their sizes, so these take them from the tensors and check that
 # they fit together; everything else is checked behind the entry points.
-def _f32(t) -> None:
-    if _code(t) != _F32:
-        raise TypeError(f"float32 tensor expected, got {t.dtype}")
+# What is asked of torch, once (a program without it may use the rest of the binding): the dtypes
+# of each kind, and who knows the current device and its stream.
+_ROWS, _F32, _I32, _I64 = {}, (), (), ()
+_raw_stream = _current_device = None
 
 
-_F32, _I32, _I64 = 100, 101, 102
-_NAMED = {"torch.float16": NETKV_F16, "torch.bfloat16": NETKV_BF16, "torch.float32": _F32,
-          "torch.int32": _I32, "torch.uint32": _I32, "torch.int64": _I64, "torch.uint64": _I64}
-_CODES = {}  # of the dtypes seen: a lookup by dtype is a fifth of one by its name
+def _ask_torch() -> None:
+    global _F32, _I32, _I64, _raw_stream, _current_device
+    import torch
+    _ROWS.update({torch.float16: NETKV_F16, torch.bfloat16: NETKV_BF16})
+    _F32, _I32, _I64 = (torch.float32,), (torch.int32, torch.uint32), (torch.int64, torch.uint64)
+    _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _code(t) -> int:
-    d = t.dtype
-    c = _CODES.get(d)
-    if c is None:
-        c = _CODES[d] = _NAMED.get(str(d), -1)
-    return c
+def _device(t) -> int:
+    """The device of a call's first tensor, which has to be the current one: its kernels run there.
+    The other tensors are compared with it one by one."""
+    if not _ROWS:
+        _ask_torch()
+    d = t.get_device()
+    if d < 0:
+        raise TypeError(f"CUDA tensors expected, got one on {t.device}")
+    if d != _current_device():
+        raise ValueError(f"tensors on CUDA device {d}, but the current one is {_current_device()}")
+    return d
 
 
-def _rows(t, heads: int, dim: int, code: Optional[int] = None):
+def _elsewhere(t, device: int) -> None:
+    raise ValueError(f"tensors on CUDA device {device} expected, got one on {t.device}")
+
+
+def _rows(t, heads: int, dim: int, device: int, code: Optional[int] = None):
     """(dtype code, address, row stride) of rows [rows, heads, dim]; a row is contiguous."""
-    c = _CODES.get(t.dtype)
+    c = _ROWS.get(t.dtype)
     if c is None:
-        c = _code(t)
-    if c > NETKV_BF16 or c < 0:
         raise TypeError(f"float16 or bfloat16 rows expected, got {t.dtype}")
     if code is not None and c != code:
         raise TypeError("tensors of one dtype expected")
     n, h, d = t.shape
     if h != heads or d != dim:
         raise ValueError(f"rows of {(heads, dim)} expected, got {(h, d)}")
+    if t.get_device() != device:
+        _elsewhere(t, device)
     if t.is_contiguous():
         return c, t.data_ptr(), h * d
     s, sh, sd = t.stride()
@@ -469,68 +484,68 @@ def _rows(t, heads: int, dim: int, code: Optional[int] = None):
     return c, t.data_ptr(), s if n > 1 else h * d
 
 
-def _ints(t, code: int, n: int) -> Optional[int]:
+def _ints(t, kind: tuple, n: int, device: int) -> Optional[int]:
     """The address of a contiguous integer tensor of n entries."""
     if t is None:
         return None
-    if _CODES.get(t.dtype) != code and _code(t) != code:
-        raise TypeError(f"{32 if code == _I32 else 64}-bit integers expected, got {t.dtype}")
+    if t.dtype not in kind:
+        raise TypeError(f"{32 if kind is _I32 else 64}-bit integers expected, got {t.dtype}")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"a contiguous tensor of {n} entries expected, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        _elsewhere(t, device)
     return t.data_ptr()
 
 
-def _table(t, n_seqs: int):
+def _table(t, n_seqs: int, device: int):
     shape = t.shape
     if len(shape) != 2 or shape[0] != n_seqs:
         raise ValueError(f"a block table of {n_seqs} rows expected, got {tuple(shape)}")
-    return _ints(t, _I32, n_seqs * shape[1]), shape[1]
+    width = shape[1]
+    return _ints(t, _I32, n_seqs * width, device), width
 
 
-def _plane(t, rows: int, width: int) -> Optional[int]:
+def _plane(t, rows: int, width: int, device: int) -> Optional[int]:
     """The address of a contiguous fp32 tensor of that shape."""
     if t is None:
         return None
-    if _CODES.get(t.dtype) != _F32 and _code(t) != _F32:
+    if t.dtype not in _F32:
         raise TypeError(f"float32 tensor expected, got {t.dtype}")
     if t.shape != (rows, width) or not t.is_contiguous():
         raise ValueError(f"a contiguous tensor of {(rows, width)} expected, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        _elsewhere(t, device)
     return t.data_ptr()
 
 
-_raw_stream = _current_device = None
+def _word(t, device: int) -> Optional[int]:
+    """The address of a status word: a tensor, an address, or None."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.get_device() != device:
+        _elsewhere(t, device)
+    return t.data_ptr()
 
 
-def _on(stream, first, *others):
-    """The stream of a call whose tensors are all on the current CUDA device, where its kernels
-    run: the given one, else torch's current one.  None and addresses are not looked at."""
-    global _raw_stream, _current_device
-    if _raw_stream is None:
-        import torch
-        _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-    d = first.get_device()
-    if d < 0:
-        raise TypeError(f"CUDA tensors expected, got one on {first.device}")
-    if d != _current_device():
-        raise ValueError(f"tensors on CUDA device {d}, but the current one is {_current_device()}")
-    for t in others:
-        if t is not None and t.__class__ is not int and t.get_device() != d:
-            raise ValueError(f"tensors on CUDA device {d} expected, got one on {t.device}")
-    return _raw_stream(d) if stream is None else _stream(stream)
+def _on_stream(device: int, stream) -> Optional[int]:
+    """The given stream, else torch's current one on the device."""
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 def _kv_move(fn: str, call, pages: KvPages, k, v, off, start, table, status, stream) -> None:
     heads, dim = pages.heads_dim
-    dt, kp, ks = _rows(k, heads, dim)
-    _, vp, vs = _rows(v, heads, dim, dt)
+    d = _device(k)
+    if pages.device_index != d:
+        _elsewhere(pages, d)
+    dt, kp, ks = _rows(k, heads, dim, d)
+    _, vp, vs = _rows(v, heads, dim, d, dt)
     rows = k.shape[0]
     if v.shape[0] != rows:
         raise ValueError("as many rows of keys as of values expected")
     n = off.numel() - 1
-    tp, tw = _table(table, n)
-    code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1), rows,
-                _ints(start, _I32, n), tp, tw, _ptr(status),
-                _on(stream, k, v, off, start, table, status, pages))
+    tp, tw = _table(table, n, d)
+    code = call(pages.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1, d), rows,
+                _ints(start, _I32, n, d), tp, tw, _word(status, d), _on_stream(d, stream))
     if code:
         raise NetKVError(fn, code)
 
@@ -551,18 +566,18 @@ def netkv_attn_prompt(q, k, v, q_off, k_off, out, lse=None, scale=None, status=N
     dim]; scale defaults to dim ** -0.5.  See include/netkv.h."""
     q_rows, heads, dim = q.shape
     k_rows, kv_heads, _ = k.shape
-    dt, qp, qs = _rows(q, heads, dim)
-    _, kp, ks = _rows(k, kv_heads, dim, dt)
-    _, vp, vs = _rows(v, kv_heads, dim, dt)
-    _, op, os_ = _rows(out, heads, dim, dt)
+    d = _device(q)
+    dt, qp, qs = _rows(q, heads, dim, d)
+    _, kp, ks = _rows(k, kv_heads, dim, d, dt)
+    _, vp, vs = _rows(v, kv_heads, dim, d, dt)
+    _, op, os_ = _rows(out, heads, dim, d, dt)
     if v.shape[0] != k_rows or out.shape[0] != q_rows:
         raise ValueError("as many rows of keys as of values, and of out as of q, expected")
     n = q_off.numel() - 1
     _check("netkv_attn_prompt", _lib.netkv_attn_prompt(
-        dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, _I64, n + 1),
-        _ints(k_off, _I64, n + 1), q_rows, k_rows, dim ** -0.5 if scale is None else scale,
-        op, os_, _plane(lse, q_rows, heads), _ptr(status),
-        _on(stream, q, k, v, q_off, k_off, out, lse, status)))
+        dt, qp, qs, kp, ks, vp, vs, heads, kv_heads, dim, n, _ints(q_off, _I64, n + 1, d),
+        _ints(k_off, _I64, n + 1, d), q_rows, k_rows, dim ** -0.5 if scale is None else scale,
+        op, os_, _plane(lse, q_rows, heads, d), _word(status, d), _on_stream(d, stream)))
 
 
 def netkv_attn_decode_workspace_size(pages: KvPages, n_seqs: int, heads: int, table_width: int,
@@ -577,37 +592,40 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     """One query row a sequence over its blocks: q, out [n_seqs, heads, dim]; see
     include/netkv.h."""
     n, heads, dim = q.shape
-    dt, qp, qs = _rows(q, heads, pages.heads_dim[1])
-    _, op, os_ = _rows(out, heads, dim, dt)
+    d = _device(q)
+    if pages.device_index != d:
+        _elsewhere(pages, d)
+    dt, qp, qs = _rows(q, heads, pages.heads_dim[1], d)
+    _, op, os_ = _rows(out, heads, dim, d, dt)
     if out.shape[0] != n:
         raise ValueError("as many rows of out as of q expected")
-    tp, tw = _table(table, n)
-    ws_bytes = 0 if workspace is None else workspace.nbytes
-    if ws_bytes and not workspace.is_contiguous():
-        raise ValueError("a contiguous workspace expected")
+    tp, tw = _table(table, n, d)
+    wp, ws_bytes = None, 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("a contiguous workspace expected")
+        wp, ws_bytes = _word(workspace, d), workspace.nbytes
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
-        pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n), tp, tw,
-        dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads),
-        _plane(mass_in, n, tw), _plane(mass_out, n, tw), _ptr(workspace), ws_bytes,
-        _ptr(status), _on(stream, q, length, table, out, lse, mass_in, mass_out, workspace, status,
-                          pages)))
+        pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n, d), tp, tw,
+        dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads, d),
+        _plane(mass_in, n, tw, d), _plane(mass_out, n, tw, d), wp, ws_bytes,
+        _word(status, d), _on_stream(d, stream)))
 
 
 def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_out, length_out,
                    mass_out, freed, n_freed, status=None, stream=None) -> None:
     """Block tables cut to a budget by accumulated attention weight; see include/netkv.h."""
     n = length.numel()
-    tp, tw = _table(table, n)
-    to, two = _table(table_out, n)
-    fr, twf = _table(freed, n)
+    d = _device(table)
+    tp, tw = _table(table, n, d)
+    to, two = _table(table_out, n, d)
+    fr, twf = _table(freed, n, d)
     if two != tw or twf != tw:
         raise ValueError("tables of one width expected")
     _check("netkv_kv_evict", _lib.netkv_kv_evict(
-        n, tp, _ints(length, _I32, n), _plane(mass, n, tw), tw, _ints(budget, _I32, n), int(sink),
-        int(recent), to, _ints(length_out, _I32, n), _plane(mass_out, n, tw), fr,
-        _ints(n_freed, _I32, n), _ptr(status),
-        _on(stream, table, length, mass, budget, table_out, length_out, mass_out, freed, n_freed,
-            status)))
+        n, tp, _ints(length, _I32, n, d), _plane(mass, n, tw, d), tw, _ints(budget, _I32, n, d),
+        int(sink), int(recent), to, _ints(length_out, _I32, n, d), _plane(mass_out, n, tw, d), fr,
+        _ints(n_freed, _I32, n, d), _word(status, d), _on_stream(d, stream)))
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:

@@ -25,12 +25,13 @@ def kv(monkeypatch):
     import __graft_entry__
     __graft_entry__.build()
     from paper_2606_03910_gb300 import netkv
+    netkv._ask_torch()
     calls = []
     for f in ("netkv_kv_store", "netkv_kv_load", "netkv_attn_prompt", "netkv_attn_decode",
               "netkv_kv_evict"):
         monkeypatch.setattr(netkv._lib, f, lambda *a: calls.append(a) or 0)
     monkeypatch.setattr(netkv, "_raw_stream", lambda d: 0)
-    monkeypatch.setattr(netkv, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(netkv, "_current_device", lambda: 0)
     return netkv, calls
 
 
