@@ -249,20 +249,6 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
         "r"(at)
       : "memory");
 }
-__device__ __forceinline__ void sync_softmax() {
-  asm volatile("bar.sync 1, 256;" ::: "memory");
-}
-// Whether all softmax threads say yes.
-__device__ __forceinline__ bool all_softmax(bool yes) {
-  uint32_t all;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "bar.red.and.pred p, 1, 256, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(all)
-      : "r"((uint32_t)yes)
-      : "memory");
-  return all != 0;
-}
 __device__ __forceinline__ void tmem_loaded() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
@@ -291,7 +277,7 @@ struct Shared {
   alignas(128) unsigned char out[kSoftmaxWarps][32 * 128];
   alignas(8) uint64_t q_full, q_empty, kv_full[kStages<kDim>], kv_empty[kStages<kDim>], landed;
   uint64_t s_full[2], p_full[2][2], o_full[2];  // p: the two halves of the keys
-  uint64_t item_full[2], item_empty[2], begun, claimed;
+  uint64_t item_full[2], item_empty[2], begun, claimed, met;
   alignas(16) uint4 claim;
   Item item[2];
   float half_m[kRows], half_l[kRows];  // kKeyHalves: the odd key tiles' maxima and sums
@@ -439,6 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(smem_addr(&sh.landed), 1);
       bar_init(smem_addr(&sh.claimed), 1);
       bar_init(smem_addr(&sh.begun), 1);
+      bar_init(smem_addr(&sh.met), kSoftmaxWarps);
       for (uint32_t i = 0; i < kRing; ++i) {
         bar_init(smem_addr(&sh.kv_full[i]), 1);
         bar_init(smem_addr(&sh.kv_empty[i]), 1);
@@ -700,11 +687,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t = warp / 4, row = tid % 128, lanes = (warp % 4) * 32 << 16;
     const uint32_t s_at = kS + t * 128 + lanes, o_at = kO + t * kDim + lanes;
     uint32_t taken = 0, finished = 0;  // steps, and items with any
+    // kKeyHalves: the two tiles' warps meet inside an item.  The wait ends like every other: after
+    // one has run out, some may have taken the item and some been told that there is none.
+    uint32_t meetings = 0;
+    auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&sh.met));
+      wait(smem_addr(&sh.met), meetings++ & 1, late);
+      __syncwarp();
+    };
     while (true) {
       const Item x = items.next(sh, late);
-      // Where the two tiles' warps meet at barriers inside an item, none leaves without the others:
-      // after a wait has run out, some may have taken the item and some been told that there is none.
-      if (!(a.mode == kKeyHalves ? all_softmax(x.valid >= 0) : x.valid >= 0)) break;
+      if (x.valid < 0) break;
       if (x.valid == 0) continue;
       const Tile y = tile_of(a, x, t);
       const uint32_t steps = t ? x.steps[1] : x.steps[0];
@@ -794,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           sh.half_m[row] = m;
           sh.half_l[row] = l;
         }
-        sync_softmax();
+        meet();
         const float m1 = sh.half_m[row], l1 = sh.half_l[row];
         if (t == 0 && l1 != 0.f) {  // NaN too
           const float top = fmaxf(m, m1);
@@ -809,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
         if (halves) {
-          if (h) sync_softmax();  // the half before has left shared memory
+          if (h) meet();  // the half before has left shared memory
           if (t && steps) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -820,7 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int z = 0; z < 32; ++z) part[(i * 32 + z) * kRows + row] = o[z];
             }
           }
-          sync_softmax();
+          meet();
         }
         uint4 packed[8];
 #pragma unroll
@@ -843,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             packed[i * 4 + z] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
-        if (halves) sync_softmax();  // the odd tiles' sums have been read
+        if (halves) meet();  // the odd tiles' sums have been read
         if (halves && t) continue;
 #pragma unroll
         for (int z = 0; z < 8; ++z) stage[lane * 8 + (z ^ (lane & 7))] = packed[z];
@@ -858,7 +852,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       }
       if (halves) {
-        sync_softmax();
+        meet();
         if (t) continue;
       }
       if (row < y.rows && a.lse)

@@ -17,17 +17,14 @@ def softmax_branch():
     return text[at:text.index("using Encode")]
 
 
-def test_softmax_warps_leave_together():
-    """The softmax warps meet at barriers inside an item.  After a wait has run out each warp is told
-    "no more items" whenever it asks, so whether to take an item is a vote of them all, and no
-    warp leaves the loop, or skips the item, before it."""
-    body = softmax_branch()
-    taken = body.index("items.next(")
-    vote = body.index("all_softmax(")
-    assert taken < vote < body.index("break;") and vote < body.index("continue;")
-    # every barrier of the branch stands behind the vote
-    assert body.index("sync_softmax(") > vote
-    # and the vote is a barrier of all eight warps
-    text = source()
-    vote = text[text.index("bool all_softmax("):]
-    assert "bar.red.and.pred p, 1, 256, " in vote[:vote.index("\n}\n")]
+def test_softmax_warps_meet_for_a_limited_time():
+    """The softmax warps meet inside an item.  After a wait has run out each warp is told "no more
+    items" whenever it asks, so some may be in an item and some have left: where they meet is a
+    wait with a limit like the others, not a barrier of a number of threads."""
+    text, body = source(), softmax_branch()
+    assert not re.search(r"bar(rier)?\.(cta\.)?(sync|red)", text)
+    meet = body[body.index("auto meet ="):]
+    assert "wait(smem_addr(&sh.met), " in meet[:meet.index("};")]
+    # only where every warp of the block ends do they all come together
+    assert text.count("__syncthreads()") == 2
+    assert text.index("__syncthreads()", text.index("__syncthreads()") + 1) > text.index("meet();")
