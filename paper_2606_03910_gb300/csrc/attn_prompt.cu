@@ -40,6 +40,11 @@ constexpr float kLag = 8.f;              // in powers of two
 template <bool kBf16>
 constexpr float kUp = kBf16 ? 0.f : 7.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Limits of waits in clocks: two seconds for what is at most a few steps away.  What may be a whole
+// item away (the next item, or a tile's scores where it has no rows in the item before) has ten times
+// what the steps of the longest one take; that others wait for the steps of that item ends it too.
+constexpr long long kPatience = 4000000000, kStepClocks = 20000;
+constexpr long long kItemPatience = kPatience + ((1ll << 31) / kKeys) * kStepClocks;
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = (kSoftmaxWarps + 4) * 32;  // and a warp for the loads, one for the products
 // Registers: the launch has kThreads * kLaunchRegs, of which the softmax warps, that hold a row
@@ -120,14 +125,15 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return done != 0;
 }
-// Waits for a phase, two seconds' clocks at most; once one thread of the block has given up,
-// nobody waits any longer and the block runs to its end.
+// Waits for a phase, kPatience clocks at most; once one thread of the block has given up, nobody
+// waits any longer and the block runs to its end.
+template <long long kLimit = kPatience>
 __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
   if (try_wait(bar, parity)) return;
   const long long t0 = clock64();
   while (!try_wait(bar, parity)) {
     if (*late) return;
-    if (clock64() - t0 > 4000000000ll) {
+    if (clock64() - t0 > kLimit) {
       *late = 1;
       return;
     }
@@ -392,7 +398,7 @@ struct Items {
   template <class Sh>
   __device__ __forceinline__ Item next(Sh& sh, volatile int* late) {
     const uint32_t at = n % 2;
-    wait(smem_addr(&sh.item_full[at]), n / 2 & 1, late);
+    wait<kItemPatience>(smem_addr(&sh.item_full[at]), n / 2 & 1, late);
     const Item x = sh.item[at];
     ++n;
     __syncwarp();
@@ -638,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n = blockIdx.x;
       for (uint32_t i = 0;; ++i) {
         if (i) {
-          wait(smem_addr(&sh.begun), (i - 1) & 1, late);
+          wait<kItemPatience>(smem_addr(&sh.begun), (i - 1) & 1, late);
           if (lane == 0) {
             bar_expect(smem_addr(&sh.claimed), 16);
             asm volatile(
@@ -708,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m = -INFINITY, l = 0.f;
       for (uint32_t j = 0; j < steps; ++j, ++taken) {
         float s[kKeys];
-        wait(smem_addr(&sh.s_full[t]), taken & 1, late);
+        wait<kItemPatience>(smem_addr(&sh.s_full[t]), taken & 1, late);
         after_sync();
 #pragma unroll
         for (int i = 0; i < 4; ++i) tmem_load(s_at + i * 32, s + i * 32);

@@ -28,3 +28,17 @@ def test_softmax_warps_meet_for_a_limited_time():
     # only where every warp of the block ends do they all come together
     assert text.count("__syncthreads()") == 2
     assert text.index("__syncthreads()", text.index("__syncthreads()") + 1) > text.index("meet();")
+
+
+def test_what_is_an_item_away_is_waited_for():
+    """The planning warp waits through a whole item, and so do warps of a tile without rows beside a
+    long one, for its next item and that one's scores.  2^31 - 1 keys are 2^24 steps of about 2,100
+    clocks, so two seconds would end calls that are only long."""
+    text = source()
+    clocks = int(re.search(r"kStepClocks = (\d+)", text).group(1))
+    assert clocks >= 20000
+    assert "kItemPatience = kPatience + ((1ll << 31) / kKeys) * kStepClocks" in text
+    for bar in ("item_full[at]", "begun", "s_full[t]"):
+        waits = [text[m.start() - 20:m.start()] for m in re.finditer(re.escape(f"(smem_addr(&sh.{bar})"), text)]
+        waits = [w for w in waits if re.search(r"wait(<\w+>)?$", w)]
+        assert waits and all(w.endswith("wait<kItemPatience>") for w in waits), bar
