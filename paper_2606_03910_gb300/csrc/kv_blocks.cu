@@ -20,17 +20,18 @@ constexpr float kSmallest = 7.8886091e-31f;  // 2^-100: blocks below are held as
 
 // A unit is one block of one KV head, its keys or its values, taken by one warp: 16 rows of
 // kDim 16-bit values.  A lane has 8 neighbouring values of a row, kDim / 8 lanes a row.
-struct Unit {
-  uint32_t seq, block, head;
+// Up to kSearched sequences a warp finds its block by counting (find_unit), 128 sequences a step, so
+// that ragged batches spread evenly.  Of more, a sequence has `parts` warps for a head's keys, as many
+// as an average one has blocks, which take its blocks in turn: with each warp counting, a call's time
+// would grow with the square of its sequences.  Ragged rows of 2 heads stored: 300 sequences 47 us by
+// counting and 61 in turn, 600 125 and 100, 4,096 2,860 and 590; a token each: 300 8.6 and 7.1, 4,096
+// 248 and 17, 262,144 407 ms by counting.
+constexpr uint32_t kSearched = 512;
+struct Units {
+  uint32_t seq, block, step, end;  // blocks block, block + step, ... below end
+  uint32_t head;
   bool values;
 };
-
-template <class Count>
-__device__ __forceinline__ Unit unit_of(uint32_t n_seqs, uint32_t kv_heads, Count count) {
-  const uint32_t w = blockIdx.x * kWarps + threadIdx.x / 32, per = 2 * kv_heads;
-  const Found f = find_unit(n_seqs, w / per, count);
-  return {f.seq, f.unit, (w % per) / 2, (w & 1) != 0};
-}
 
 struct StoreArgs {
   KvArgs kv;
@@ -41,6 +42,7 @@ struct StoreArgs {
   const uint32_t* start;
   const int32_t* table;
   uint32_t n_seqs, width;
+  uint32_t parts;  // kMany: warps of a sequence for a head's keys
   int* status;
 };
 
@@ -50,6 +52,19 @@ __device__ __forceinline__ uint32_t touched(const StoreArgs& a, uint32_t i) {
   if (n == 0) return 0;
   const uint64_t end = min((s + n + kBlockTokens - 1) / kBlockTokens, (uint64_t)a.width);
   return end > s / kBlockTokens ? (uint32_t)(end - s / kBlockTokens) : 0;
+}
+
+template <bool kMany>
+__device__ __forceinline__ Units units_of(const StoreArgs& a) {
+  const uint32_t w = blockIdx.x * kWarps + threadIdx.x / 32, per = 2 * a.kv.heads;
+  const uint32_t head = (w % per) / 2, n = w / per;
+  const bool values = (w & 1) != 0;
+  if (kMany) {
+    const uint32_t seq = n / a.parts;
+    return {seq, n % a.parts, a.parts, seq < a.n_seqs ? touched(a, seq) : 0, head, values};
+  }
+  const Found f = find_unit(a.n_seqs, n, [&](uint32_t i) { return touched(a, i); });
+  return {f.seq, f.unit, 1, f.unit + 1, head, values};
 }
 
 // Bad offsets or a table that is too short, said once a sequence.
@@ -64,15 +79,12 @@ __device__ __forceinline__ void check_ranges(const StoreArgs& a) {
 }
 
 template <int kDim, bool kBf16, bool kE4m3>
-__global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constant__ StoreArgs a) {
+__device__ __forceinline__ void store_block(const StoreArgs& a, const Units& u, uint32_t at) {
   constexpr int kLanes = kDim / 8, kRows = 32 / kLanes, kSteps = kBlockTokens / kRows;
-  check_ranges(a);
-  const Unit u = unit_of(a.n_seqs, a.kv.heads, [&](uint32_t i) { return touched(a, i); });
-  if (u.seq >= a.n_seqs) return;
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t start = a.start ? a.start[u.seq] : 0;
   const RowRange r = row_range(a.off, u.seq, a.rows);
-  const uint64_t block = start / kBlockTokens + u.block;
+  const uint64_t block = start / kBlockTokens + at;
   const int32_t page = a.table[(uint64_t)u.seq * a.width + block];
   if (page < 0 || (uint32_t)page >= a.kv.n_pages) {
     if (lane == 0) flag_status(a.status, NETKV_DEV_ERANGE);
@@ -165,17 +177,26 @@ __global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constan
   if (lane == 0) *scale = now;
 }
 
+template <int kDim, bool kBf16, bool kE4m3, bool kMany>
+__global__ void __launch_bounds__(kWarps * 32) store_kernel(const __grid_constant__ StoreArgs a) {
+  check_ranges(a);
+  const Units u = units_of<kMany>(a);
+  if (u.seq >= a.n_seqs) return;
+  if constexpr (kMany) {
+    for (uint32_t at = u.block; at < u.end; at += u.step) store_block<kDim, kBf16, kE4m3>(a, u, at);
+  } else {
+    store_block<kDim, kBf16, kE4m3>(a, u, u.block);
+  }
+}
+
 // Rows from blocks: the reverse walk, its output rows through StoreArgs' k and v.
 template <int kDim, bool kBf16, bool kE4m3>
-__global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant__ StoreArgs a) {
+__device__ __forceinline__ void load_block(const StoreArgs& a, const Units& u, uint32_t at) {
   constexpr int kLanes = kDim / 8, kRows = 32 / kLanes, kSteps = kBlockTokens / kRows;
-  check_ranges(a);
-  const Unit u = unit_of(a.n_seqs, a.kv.heads, [&](uint32_t i) { return touched(a, i); });
-  if (u.seq >= a.n_seqs) return;
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t start = a.start ? a.start[u.seq] : 0;
   const RowRange r = row_range(a.off, u.seq, a.rows);
-  const uint64_t block = start / kBlockTokens + u.block;
+  const uint64_t block = start / kBlockTokens + at;
   const int32_t page = a.table[(uint64_t)u.seq * a.width + block];
   const bool there = page >= 0 && (uint32_t)page < a.kv.n_pages;
   if (!there && lane == 0) flag_status(a.status, NETKV_DEV_ERANGE);
@@ -214,7 +235,20 @@ __global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant
   }
 }
 
-// Units of a call: at most one block a sequence more than its rows fill, at either end.
+template <int kDim, bool kBf16, bool kE4m3, bool kMany>
+__global__ void __launch_bounds__(kWarps * 32) load_kernel(const __grid_constant__ StoreArgs a) {
+  check_ranges(a);
+  const Units u = units_of<kMany>(a);
+  if (u.seq >= a.n_seqs) return;
+  if constexpr (kMany) {
+    for (uint32_t at = u.block; at < u.end; at += u.step) load_block<kDim, kBf16, kE4m3>(a, u, at);
+  } else {
+    load_block<kDim, kBf16, kE4m3>(a, u, u.block);
+  }
+}
+
+// Units of a call: at most one block a sequence more than its rows fill, at either end; of many
+// sequences, the average's blocks and one for each.
 template <bool kStore>
 netkv_status blocks_call(const netkv_kv_pages* pages, uint32_t dtype, const void* d_k,
                          uint64_t k_stride, const void* d_v, uint64_t v_stride, uint32_t n_seqs,
@@ -229,24 +263,37 @@ netkv_status blocks_call(const netkv_kv_pages* pages, uint32_t dtype, const void
       !aligned_to(d_status, 4) || width == 0 || width >= (1u << 28) || rows >> 31 ||
       n_seqs >> 24)
     return NETKV_EINVAL;
-  const uint64_t units = (rows / kBlockTokens + 2ull * n_seqs) * 2 * pages->kv_heads;
+  const uint32_t parts =
+      n_seqs > kSearched ? (uint32_t)(rows / ((uint64_t)kBlockTokens * n_seqs)) + 1 : 0;
+  const uint64_t units =
+      (parts ? (uint64_t)parts * n_seqs : rows / kBlockTokens + 2ull * n_seqs) * 2 * pages->kv_heads;
   const uint64_t grid = (units + kWarps - 1) / kWarps;
   if (units >> 32 || grid >> 31) return NETKV_EINVAL;
   const StoreArgs a = {kv_args(pages), (const unsigned char*)d_k, (const unsigned char*)d_v,
-                       k_stride, v_stride, rows, d_off, d_start, d_table, n_seqs, width, d_status};
+                       k_stride, v_stride, rows, d_off, d_start, d_table, n_seqs, width, parts,
+                       d_status};
   const bool bf = dtype == NETKV_BF16, e4 = pages->format == NETKV_KV_E4M3;
   auto go = [&](auto kernel) {
     kernel<<<(unsigned)grid, kWarps * 32, 0, (cudaStream_t)stream>>>(a);
   };
-  auto pick = [&](auto dim) {
+  auto pick = [&](auto dim, auto many) {
     constexpr int kDim = decltype(dim)::value;
-    if (bf && e4) go(kStore ? store_kernel<kDim, true, true> : load_kernel<kDim, true, true>);
-    else if (bf) go(kStore ? store_kernel<kDim, true, false> : load_kernel<kDim, true, false>);
-    else if (e4) go(kStore ? store_kernel<kDim, false, true> : load_kernel<kDim, false, true>);
-    else go(kStore ? store_kernel<kDim, false, false> : load_kernel<kDim, false, false>);
+    constexpr bool kMany = decltype(many)::value;
+    if (bf && e4)
+      go(kStore ? store_kernel<kDim, true, true, kMany> : load_kernel<kDim, true, true, kMany>);
+    else if (bf)
+      go(kStore ? store_kernel<kDim, true, false, kMany> : load_kernel<kDim, true, false, kMany>);
+    else if (e4)
+      go(kStore ? store_kernel<kDim, false, true, kMany> : load_kernel<kDim, false, true, kMany>);
+    else
+      go(kStore ? store_kernel<kDim, false, false, kMany> : load_kernel<kDim, false, false, kMany>);
   };
-  if (pages->head_dim == 64) pick(std::integral_constant<int, 64>());
-  else pick(std::integral_constant<int, 128>());
+  auto widths = [&](auto many) {
+    if (pages->head_dim == 64) pick(std::integral_constant<int, 64>(), many);
+    else pick(std::integral_constant<int, 128>(), many);
+  };
+  if (parts) widths(std::true_type());
+  else widths(std::false_type());
   return netkv_launch_status();
 }
 

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_kv_blocks import ints  # noqa: E402
+from tests.test_gpu_kv_blocks import check_store, ints, offsets, pool, tables  # noqa: E402
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -64,3 +64,86 @@ def test_what_follows_a_batch_without_tokens(netkv):
         torch.cuda.synchronize()
         assert not seen.any() and bool((seen_lse == -float("inf")).all())
         assert mass is None or bool((mass == 1).all())
+
+
+def milliseconds(f):
+    """GPU time of the second of two calls."""
+    f()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    f()
+    b.record()
+    torch.cuda.synchronize()
+    return a.elapsed_time(b)
+
+
+@pytest.mark.parametrize("n", [512, 513, 2500])
+@pytest.mark.parametrize("fmt,dim", [("int8", 64), ("e4m3", 128)])
+def test_store_of_thousands(netkv, n, fmt, dim):
+    """Rows into blocks of many sequences, some without rows and some far longer than the average."""
+    rng = np.random.default_rng(n)
+    held = rng.integers(0, 40, n).tolist()
+    new = (rng.integers(0, 2, n) * rng.integers(1, 20, n)).tolist()
+    new[0], new[n // 2], new[n - 1] = 900, 0, 300
+    assert check_store(netkv, held, new, 1, dim, fmt, torch.bfloat16, seed=n)[2] == 0
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 3), (128, 1)])
+def test_load_of_thousands(netkv, dim, heads):
+    """One call for all sequences gives what calls for 500 at a time give."""
+    rng = np.random.default_rng(dim)
+    n = 2000
+    start, count = rng.integers(0, 40, n), rng.integers(0, 2, n) * rng.integers(1, 60, n)
+    count[7], count[n - 1] = 1500, 600
+    blocks = (-(-(start + count) // 16)).tolist()
+    pages = netkv.KvPages(*pool(sum(blocks) + 2, heads, dim, "int8", 7))
+    table = tables(blocks, max(blocks), sum(blocks) + 2, 7)
+    got, want = (torch.full((2, int(count.sum()), heads, dim), 9.0, dtype=torch.float16, device="cuda")
+                 for _ in range(2))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    netkv.netkv_kv_load(pages, got[0], got[1], offsets(count), ints(start.tolist()), table, status=status)
+    at = 0
+    for i in range(0, n, 500):
+        rows = int(count[i:i + 500].sum())
+        netkv.netkv_kv_load(pages, want[0, at:at + rows], want[1, at:at + rows], offsets(count[i:i + 500]),
+                            ints(start[i:i + 500].tolist()), table[i:i + 500], status=status)
+        at += rows
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and int(status) == 0
+
+
+def test_bad_rows_among_thousands(netkv):
+    """Pages, offsets and tables out of range in a long batch: flagged, the others stored."""
+    n = 3000
+    rows = torch.ones((n, 1, 64), dtype=torch.float16, device="cuda")
+    off = np.arange(n + 1)
+    off[1000] = n + 5          # pair 999 passes the rows, pair 1000 decreases
+    table = np.arange(n).reshape(n, 1)
+    table[2000] = n            # no such page
+    start = np.zeros(n, np.int64)
+    start[2500] = 16           # past the table
+    k, s = torch.zeros((n, 1, 16, 64), dtype=torch.int8, device="cuda"), torch.zeros((n, 1), device="cuda")
+    pages = netkv.KvPages(k, k.clone(), s, s.clone())
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    netkv.netkv_kv_store(pages, rows, rows, ints(off.tolist(), torch.int64), ints(start.tolist()),
+                         ints(table.ravel().tolist()).view(n, 1), status=status)
+    torch.cuda.synchronize()
+    assert int(status) == netkv.NETKV_DEV_ERANGE
+    written = set(torch.nonzero(s[:, 0]).ravel().tolist())
+    assert written == set(range(n)) - {999, 1000, 2000, 2500}
+    assert (k[list(written)][:, :, 0] == 127).all() and (k[:, :, 1:] == 0).all()
+
+
+def test_time_of_a_token_for_each_of_many(netkv):
+    """A warp that looks for its block among all sequences makes the call quadratic: the limit of
+    2^24 - 1 sequences would take minutes."""
+    n = 1 << 18
+    rows = torch.ones((n, 1, 64), dtype=torch.float16, device="cuda")
+    k, s = torch.zeros((n, 1, 16, 64), dtype=torch.int8, device="cuda"), torch.zeros((n, 1), device="cuda")
+    pages = netkv.KvPages(k, k.clone(), s, s.clone())
+    off = torch.arange(n + 1, device="cuda")
+    table = torch.arange(n, dtype=torch.int32, device="cuda").view(n, 1)
+    back = torch.zeros((2,) + rows.shape, dtype=rows.dtype, device="cuda")
+    assert milliseconds(lambda: netkv.netkv_kv_store(pages, rows, rows, off, None, table)) < 10
+    assert milliseconds(lambda: netkv.netkv_kv_load(pages, back[0], back[1], off, None, table)) < 10
+    assert torch.equal(back[0], rows) and torch.equal(back[1], rows)
