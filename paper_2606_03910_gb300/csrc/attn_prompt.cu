@@ -140,6 +140,13 @@ __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int
   }
 }
 
+// Whether a thread of the block has, by the whole warp: its threads go the same way.  (The warp that
+// issues products ends its item without asking, a vote a step cost 1 % of ten ragged prompts: its waits
+// are over at once, and each of its signals is a phase's only one.)
+__device__ __forceinline__ bool given_up(volatile int* late) {
+  return __any_sync(~0u, *late);
+}
+
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
                                          uint32_t bar) {
   asm volatile(
@@ -403,7 +410,7 @@ struct Items {
     ++n;
     __syncwarp();
     if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.item_empty[at]));
-    if (*late) return Item{0, 0, 0, 0, 0, 0, {0, 0}, -1};
+    if (given_up(late)) return Item{0, 0, 0, 0, 0, 0, {0, 0}, -1};
     return x;
   }
 };
@@ -512,12 +519,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t all = x.steps[0] + x.steps[1];
           load(0, false);
           if (all > 1) load(1, false);
-          for (uint32_t j = 0; j < all && !*late; ++j) {
+          for (uint32_t j = 0; j < all && !given_up(late); ++j) {
             load(j, true);
             if (j + 2 < all) load(j + 2, false);
           }
         } else {
-          for (uint32_t j = 0; j < steps && !*late; ++j) {
+          for (uint32_t j = 0; j < steps && !given_up(late); ++j) {
             load(j, false);
             load(j, true);
           }
@@ -589,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             scores(1, i % kRing, 0);
             signal(&sh.kv_empty[i++ % kRing]);
           }
-          for (uint32_t j = 0; j < all && !*late; j += 2) {
+          for (uint32_t j = 0; j < all; j += 2) {
 #pragma unroll
             for (uint32_t t = 0; t < 2; ++t) {
               if (j + t >= all) continue;
@@ -613,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (n1) scores(1, i % kRing, 1);
         signal(&sh.kv_empty[i % kRing]);
         if (steps == 1) signal(&sh.q_empty);
-        for (uint32_t j = 0; j < steps && !*late; ++j) {
+        for (uint32_t j = 0; j < steps; ++j) {
           const uint32_t v = (i + 1) % kRing, k = (i + 2) % kRing;
           const bool more = j + 1 < steps;
           arrived(i + 1);
@@ -665,7 +672,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               : "=r"(got), "=r"(first)
               : "r"(smem_addr(&sh.claim))
               : "memory");
-          n = got && !*late ? first : ~0u;
+          const bool gone = given_up(late);
+          n = got && !gone ? first : ~0u;
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }

@@ -42,3 +42,16 @@ def test_what_is_an_item_away_is_waited_for():
         waits = [text[m.start() - 20:m.start()] for m in re.finditer(re.escape(f"(smem_addr(&sh.{bar})"), text)]
         waits = [w for w in waits if re.search(r"wait(<\w+>)?$", w)]
         assert waits and all(w.endswith("wait<kItemPatience>") for w in waits), bar
+
+
+def test_a_warp_decides_as_one():
+    """Whether somebody has given up is read by each thread at its own time.  Threads of a warp that
+    went different ways on it would wait for one another for ever, at the warp's barriers, shuffles
+    and TMEM accesses: only the wait itself, and the end of the block, look at it thread by thread."""
+    text = source()
+    kernel = text[text.index("struct Items {"):]
+    alone = [line.strip() for line in kernel.splitlines() if "*late" in line and "volatile int*" not in line]
+    assert alone == ["if (*late) {", "if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);"]
+    given_up = text[text.index("bool given_up("):]
+    assert "__any_sync(~0u, *late)" in given_up[:given_up.index("\n}\n")]
+    assert kernel.count("given_up(late)") == 4  # the next item, the loads of either kind, the plan
