@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t tiles = a.mode == kKeyHalves ? 1 : 2;  // of queries
         if (with_q) wait(smem_addr(&sh.q_empty), (with_q - 1) & 1, late);
         ++with_q;
-        if (lane == 0) {
+        bool gone = given_up(late);  // no copy into a place that may be in use
+        if (lane == 0 && !gone) {
           bar_expect(smem_addr(&sh.q_full), tiles * kRows * kDim * 2);
           for (uint32_t t = 0; t < tiles; ++t) {
             const Tile y = tile_of(a, x, t);
@@ -490,6 +491,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto load = [&](uint32_t tile, bool values) {  // a key tile's keys or values
           const uint32_t st = i % kRing, full = smem_addr(&sh.kv_full[st]);
           if (i >= kRing) wait(smem_addr(&sh.kv_empty[st]), (i / kRing - 1) & 1, late);
+          gone = given_up(late);
+          if (gone) return;
           ++i;
           const uint32_t key = tile * kKeys;
           // values past the sequence's end are another's and meet weights of 0: an infinity or a
@@ -519,12 +522,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t all = x.steps[0] + x.steps[1];
           load(0, false);
           if (all > 1) load(1, false);
-          for (uint32_t j = 0; j < all && !given_up(late); ++j) {
+          for (uint32_t j = 0; j < all && !gone; ++j) {
             load(j, true);
             if (j + 2 < all) load(j + 2, false);
           }
         } else {
-          for (uint32_t j = 0; j < steps && !given_up(late); ++j) {
+          for (uint32_t j = 0; j < steps && !gone; ++j) {
             load(j, false);
             load(j, true);
           }

@@ -54,4 +54,15 @@ def test_a_warp_decides_as_one():
     assert alone == ["if (*late) {", "if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);"]
     given_up = text[text.index("bool given_up("):]
     assert "__any_sync(~0u, *late)" in given_up[:given_up.index("\n}\n")]
-    assert kernel.count("given_up(late)") == 4  # the next item, the loads of either kind, the plan
+    assert kernel.count("given_up(late)") == 4  # the next item, queries, keys and values, the plan
+
+
+def test_no_loads_after_a_wait_has_run_out():
+    """A ring's place may still be in use then, and its barrier takes no arrival before its turn: every
+    load is behind a look at the flag that comes after the wait for its place."""
+    text = source()
+    load = text[text.index("items.next(sh, late)", text.index("uint32_t i = 0, cleared = 0")):]
+    load = load[:load.index("warp == kSoftmaxWarps + 1")]
+    for empty, expect in (("q_empty", "bar_expect(smem_addr(&sh.q_full)"), ("kv_empty[st]", "bar_expect(bar,")):
+        wait = load.index(f"wait(smem_addr(&sh.{empty})")
+        assert "given_up(late)" in load[wait:load.index(expect, wait)]
