@@ -33,6 +33,12 @@ constexpr int kRows = 128, kKeys = 128;  // of a tile
 // Items an SM, in halves, up to which a row block's key tiles go to two tiles: at 3 a prompt of
 // 4,096 tokens takes 58 us, 67 without; at 6 ten ragged ones would take 89 instead of 67.
 constexpr uint32_t kFewItems = 6;
+// Sequences up to which an item's row block is found by counting through them; above, a sequence and
+// column has indices of the grid of its own, as many as the average has row blocks, which take its
+// row blocks in turn: with each item counting, a call's time grows with the square of the sequences.
+// 7 heads on 1 of 128: ragged prompts, 600 1,000 us by counting and 1,260 in turn, 1,024 1,460 and
+// 1,550, 4,096 8,130 and 6,530; up to 200 rows each, 1,024 372 and 289, 4,096 2,730 and 1,130.
+constexpr uint32_t kSearched = 1024;
 constexpr float kLag = 8.f;              // in powers of two
 // Where the weight of the running maximum stands, in powers of two.  fp16 ends at 2^16, so weights
 // up to 2^kLag have room for 2^7, and are exact to 2^-11 down to 2^-21 of the largest one, 0 below
@@ -66,6 +72,7 @@ struct PromptArgs {
   uint32_t mode;        // what a block's two tiles are
   uint32_t tiles;       // row blocks that the grid has
   uint32_t ordered;     // 1: row blocks by their key tiles, the most first
+  uint32_t parts;       // many sequences: indices of the grid for each one and column; else 0
   float scale2;         // scale * log2(e)
   float* lse;
   int* status;
@@ -370,11 +377,22 @@ __device__ __forceinline__ Found row_block(const PromptArgs& a, uint32_t n, uint
   return {f.seq, (qs + block_rows - 1) / block_rows - 1 - ks - f.unit};
 }
 
-// The grid's n-th item.
-__device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n) {
+// The grid's n-th item.  Of many sequences (a.parts) an index of the grid has every parts-th row block
+// of a sequence, the last ones first: the one of turn `turn`, and whether there is another.
+__device__ __forceinline__ Item item_at(const PromptArgs& a, uint32_t n, uint32_t turn, bool* more) {
   const uint32_t columns = a.mode == kHeadPairs ? a.heads / 2 : a.heads;
   const uint32_t block_rows = a.mode == kRowPairs ? 2 * kRows : kRows;
-  const Found f = row_block(a, n / columns, block_rows);
+  Found f = {a.n_seqs, 0};
+  *more = false;
+  if (a.parts) {
+    const uint32_t seq = n / columns / a.parts, unit = n / columns % a.parts + turn * a.parts;
+    const uint32_t blocks =
+        (uint32_t)((row_range(a.q_off, seq, a.q_rows).count + block_rows - 1) / block_rows);
+    if (unit < blocks) f = {seq, blocks - 1 - unit};
+    *more = unit + a.parts < blocks;
+  } else {
+    f = row_block(a, n / columns, block_rows);
+  }
   Item x = {};
   if (f.seq >= a.n_seqs) return x;
   const RowRange q = row_range(a.q_off, f.seq, a.q_rows), k = row_range(a.k_off, f.seq, a.k_rows);
@@ -651,10 +669,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       // takes over one by one
       // An item is claimed once the products of the one before begin, not earlier: what a block
       // holds in advance, another that is ready cannot take.
-      uint32_t n = blockIdx.x;
+      uint32_t n = blockIdx.x, claims = 0, turn = 0;
+      bool more = false;
       for (uint32_t i = 0;; ++i) {
-        if (i) {
-          wait<kItemPatience>(smem_addr(&sh.begun), (i - 1) & 1, late);
+        if (i) wait<kItemPatience>(smem_addr(&sh.begun), (i - 1) & 1, late);
+        turn = more ? turn + 1 : 0;
+        if (more) {
+          if (given_up(late)) n = ~0u;
+        } else if (i) {
           if (lane == 0) {
             bar_expect(smem_addr(&sh.claimed), 16);
             asm volatile(
@@ -663,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 "r"(smem_addr(&sh.claimed))
                 : "memory");
           }
-          wait(smem_addr(&sh.claimed), (i - 1) & 1, late);
+          wait(smem_addr(&sh.claimed), claims++ & 1, late);
           uint32_t got, first;
           asm volatile(
               "{\n\t.reg .b128 c;\n\t.reg .pred p;\n\t.reg .b32 y, z, w;\n\t"
@@ -682,14 +704,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         // Every index of the grid is some block's to check offsets for, its own or one taken over:
         // blocks whose items others take never start.
-        if (n != ~0u)
+        if (n != ~0u && turn == 0)
           for (uint64_t j = (uint64_t)n * 32 + lane; j < a.n_seqs; j += (uint64_t)gridDim.x * 32)
             if (row_range(a.q_off, (uint32_t)j, a.q_rows).bad ||
                 row_range(a.k_off, (uint32_t)j, a.k_rows).bad)
               flag_status(a.status, NETKV_DEV_ERANGE);
         Item x = {};
         x.valid = -1;
-        if (n != ~0u) x = item_at(a, n);
+        if (n != ~0u) x = item_at(a, n, turn, &more);
         if (i >= 2) wait(smem_addr(&sh.item_empty[i % 2]), (i / 2 - 1) & 1, late);
         if (lane == 0) {
           sh.item[i % 2] = x;
@@ -969,6 +991,10 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
     block_rows = kRows;
     tiles = q_rows / block_rows + n_seqs;
     columns = heads;
+  }
+  if (n_seqs > kSearched) {
+    a.parts = (uint32_t)(q_rows / (block_rows * n_seqs)) + 1;
+    tiles = (uint64_t)n_seqs * a.parts;
   }
   const uint64_t grid = tiles * columns;
   if (grid >> 31) return NETKV_EINVAL;

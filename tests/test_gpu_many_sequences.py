@@ -147,3 +147,45 @@ def test_time_of_a_token_for_each_of_many(netkv):
     assert milliseconds(lambda: netkv.netkv_kv_store(pages, rows, rows, off, None, table)) < 10
     assert milliseconds(lambda: netkv.netkv_kv_load(pages, back[0], back[1], off, None, table)) < 10
     assert torch.equal(back[0], rows) and torch.equal(back[1], rows)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (3, 1, 128)])
+@pytest.mark.parametrize("n", [1024, 1025, 2000])
+def test_prompts_of_thousands(netkv, n, heads, kv_heads, dim):
+    """Many prompts with prefixes, some without rows and some of several row blocks, with rows that
+    see no key among them: as calls for a hundred at a time give them."""
+    rng = np.random.default_rng(n)
+    lq = rng.integers(0, 2, n) * rng.integers(1, 40, n)
+    lq[[3, n // 2, n - 1]] = 1500, 700, 900
+    lk = np.maximum(lq + rng.integers(-5, 100, n), 0)
+    q, k, v = (torch.randn((int(r.sum()), h, dim), device="cuda").half()
+               for r, h in ((lq, heads), (lk, kv_heads), (lk, kv_heads)))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def call(a, b, out, lse):
+        i, j = int(lq[:a].sum()), int(lk[:a].sum())
+        x, y = i + int(lq[a:b].sum()), j + int(lk[a:b].sum())
+        netkv.netkv_attn_prompt(q[i:x], k[j:y], v[j:y], offsets(lq[a:b]), offsets(lk[a:b]), out[i:x],
+                                lse=lse[i:x], status=status)
+
+    got, want = torch.full_like(q, 5.0), torch.full_like(q, 5.0)
+    lse, want_lse = (torch.full((len(q), heads), 5.0, device="cuda") for _ in range(2))
+    call(0, n, got, lse)
+    for a in range(0, n, 100):
+        call(a, min(n, a + 100), want, want_lse)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    # the two may take a row's keys in another order; outputs are sums of weights of at most 1
+    finite = want_lse > -float("inf")
+    assert torch.equal(finite, lse > -float("inf")) and bool((got[~finite] == 0).all())
+    assert (lse - want_lse)[finite].abs().max() < 1e-5 * (1 + want_lse[finite].abs().max())
+    assert (got.float() - want.float()).abs().max() < 4 * 2.0 ** -11 * v.float().abs().max()
+
+
+def test_time_of_a_row_for_each_of_many_prompts(netkv):
+    n = 1 << 16
+    q = torch.ones((n, 1, 64), dtype=torch.float16, device="cuda")
+    k = q.clone()
+    off, out = torch.arange(n + 1, device="cuda"), torch.empty_like(q)
+    assert milliseconds(lambda: netkv.netkv_attn_prompt(q, k, k, off, off, out)) < 20
+    assert torch.equal(out, k)

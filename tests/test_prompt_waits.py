@@ -54,7 +54,7 @@ def test_a_warp_decides_as_one():
     assert alone == ["if (*late) {", "if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);"]
     given_up = text[text.index("bool given_up("):]
     assert "__any_sync(~0u, *late)" in given_up[:given_up.index("\n}\n")]
-    assert kernel.count("given_up(late)") == 4  # the next item, queries, keys and values, the plan
+    assert kernel.count("given_up(late)") == 5  # the next item, queries, keys and values, twice the plan
 
 
 def test_no_loads_after_a_wait_has_run_out():
