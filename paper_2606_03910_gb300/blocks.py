@@ -67,9 +67,23 @@ class BlockPool:
             off.append(off[-1] + c)
         return self._dev(off, torch.int64)
 
+    def _counts(self, counts: Sequence[int], *rows: torch.Tensor) -> List[int]:
+        """counts as integers: one a slot, none below 0, not more in all than any of the rows."""
+        out = [int(c) for c in counts]
+        if len(out) != self.slots or any(c < 0 or c != d for c, d in zip(out, counts)):
+            raise ValueError(f"{self.slots} counts of 0 or more expected, got {list(counts)}")
+        if any(sum(out) > len(x) for x in rows):
+            raise ValueError(f"{sum(out)} rows expected, got {[len(x) for x in rows]}")
+        return out
+
     def reserve(self, counts: Sequence[int]) -> None:
         """Pages for counts[i] more tokens of each slot; nothing changes where they do not fit."""
-        need = [blocks_of(t + c) - len(p) for t, c, p in zip(self.tokens, counts, self.page_of)]
+        self._take(self._counts(counts))
+
+    def _take(self, counts: List[int]) -> List[int]:
+        """reserve(); how many pages each slot was given."""
+        need = [max(0, blocks_of(t + c) - len(p))
+                for t, c, p in zip(self.tokens, counts, self.page_of)]
         if sum(need) > len(self.free):
             raise MemoryError(f"{sum(need)} pages needed, {len(self.free)} free")
         if any(blocks_of(t + c) > self.table.shape[1] for t, c in zip(self.tokens, counts)):
@@ -85,17 +99,30 @@ class BlockPool:
             at = self._dev(at, torch.int64)
             self.table.view(-1)[at] = self._dev(pages)
             self.mass.view(-1)[at] = 0.0
+        return need
+
+    def _give_back(self, taken: List[int]) -> None:
+        for pages, n in zip(reversed(self.page_of), reversed(taken)):
+            for _ in range(n):
+                self.free.append(pages.pop())
 
     def append(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int]) -> None:
-        """Rows k, v [sum(counts), kv_heads, dim]: counts[i] new tokens of slot i each."""
-        self.reserve(counts)
-        netkv.netkv_kv_store(self.pages, k, v, self._offsets(counts), self.length, self.table,
-                             status=self.status)
+        """Rows k, v [sum(counts), kv_heads, dim]: counts[i] new tokens of slot i each.  Nothing
+        changes where a call is refused."""
+        counts = self._counts(counts, k, v)
+        taken = self._take(counts)
+        try:
+            netkv.netkv_kv_store(self.pages, k, v, self._offsets(counts), self.length, self.table,
+                                 status=self.status)
+        except Exception:
+            self._give_back(taken)
+            raise
         self.tokens = [t + c for t, c in zip(self.tokens, counts)]
         self.length += self._dev(counts)
 
     def read(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int]) -> None:
         """The first counts[i] tokens of each slot into the rows k, v."""
+        counts = self._counts(counts, k, v)
         if any(c > t for c, t in zip(counts, self.tokens)):
             raise ValueError("more tokens asked for than a slot holds")
         netkv.netkv_kv_load(self.pages, k, v, self._offsets(counts), None, self.table,

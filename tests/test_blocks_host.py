@@ -31,3 +31,48 @@ def test_move_between_unlike_pools(blocks, other):
     with pytest.raises(ValueError):
         blocks.move(src, 0, dst, 1)
     assert state(dst) == before
+
+
+def rows(n, heads=2, dim=64):
+    return torch.zeros((n, heads, dim), dtype=torch.float16)
+
+
+def test_a_refused_append_changes_nothing(blocks):
+    """Whatever the call behind it refuses (here: tensors of the host), the pool's pages are as before."""
+    pool = make(blocks)
+    pool.reserve([20, 0, 1])
+    before = state(pool)
+    for counts in ([30, 5, 0], [0, 0, 40]):
+        with pytest.raises(TypeError):
+            pool.append(rows(sum(counts)), rows(sum(counts)), counts)
+        now = state(pool)
+        assert now[:3] == before[:3] and sorted(now[0] + sum(now[1], [])) == list(range(12))
+        assert [row[:len(p)] for row, p in zip(now[3], now[1])] == now[1]
+
+
+@pytest.mark.parametrize("counts", [[16], [16, 16, 16, 16], [-1, 16, 16], [16, 16, 17], [1.5, 0, 0]])
+def test_counts_that_do_not_fit(blocks, counts):
+    """One count a slot, none below 0, and rows for all of them."""
+    pool = make(blocks)
+    before = state(pool)
+    for call in (lambda: pool.append(rows(48), rows(48), counts),
+                 lambda: pool.append(rows(64), rows(48), counts),
+                 lambda: pool.read(rows(48), rows(48), counts)):
+        with pytest.raises(ValueError):
+            call()
+        assert state(pool) == before
+    if sum(counts) != 49:
+        with pytest.raises(ValueError):
+            pool.reserve(counts)
+    assert state(pool) == before
+
+
+def test_reserve_when_one_slot_has_more_than_it_needs(blocks):
+    """Pages that a slot holds in advance are not another's."""
+    pool = make(blocks)
+    pool.reserve([80, 0, 0])
+    with pytest.raises(MemoryError):
+        pool.reserve([0, 80, 80])
+    assert len(pool.free) == 7 and [len(p) for p in pool.page_of] == [5, 0, 0]
+    pool.reserve([16, 80, 32])
+    assert len(pool.free) == 0 and [len(p) for p in pool.page_of] == [5, 5, 2]

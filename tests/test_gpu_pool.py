@@ -1,0 +1,34 @@
+"""The block pool on a GPU: what it keeps in step with the blocks."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_blocks import check_attend, make, rows  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import __graft_entry__
+    __graft_entry__.build()
+
+
+def test_appends_after_refused_ones():
+    """Another type of values, fewer rows than counts, a strided row: refused, and what follows is as
+    if it had not been asked."""
+    pool = make(pages=12)
+    pool.append(rows(20), rows(20, seed=1), [10, 0, 10])
+    free, held = list(pool.free), [list(p) for p in pool.page_of]
+    for k, v, counts, error in ((rows(60), rows(60).bfloat16(), [20, 20, 20], TypeError),
+                                (rows(59), rows(59), [20, 20, 20], ValueError),
+                                (rows(60, dim=32), rows(60, dim=32), [20, 20, 20], ValueError),
+                                (rows(60).transpose(0, 1).contiguous().transpose(0, 1), rows(60),
+                                 [20, 20, 20], ValueError)):
+        with pytest.raises(error):
+            pool.append(k, v, counts)
+        assert pool.free == free and pool.page_of == held and pool.tokens == [10, 0, 10]
+    pool.append(rows(64, seed=2), rows(64, seed=3), [20, 30, 14])
+    check_attend(pool, rows(3, heads=6, seed=4), pool.mass.clone())
+    assert int(pool.status) == 0
