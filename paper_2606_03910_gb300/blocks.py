@@ -168,7 +168,8 @@ class BlockPool:
 
 
 def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
-    """Slot `slot` of src into the empty slot `to` of dst, block by block; the bytes moved."""
+    """Slot `slot` of src into the empty slot `to` of dst, block by block, with the weight that each
+    block has drawn; the bytes of blocks moved.  The slot of src stays as it is until release()."""
     if dst.tokens[to]:
         raise ValueError(f"slot {to} is in use")
     # codes are copied as they are, page by page
@@ -190,6 +191,8 @@ def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
     for i in (2, 3):
         dst.pages.tensors[i][b] = src.pages.tensors[i][a]
         total += len(src.page_of[slot]) * src.pages.tensors[i][0].numel() * 4
+    blocks = blocks_of(n)
+    dst.mass[to, :blocks] = src.mass[slot, :blocks]
     dst.tokens[to] = n
     dst.length[to] = n
     return total + len(copies) * one

@@ -32,3 +32,25 @@ def test_appends_after_refused_ones():
     pool.append(rows(64, seed=2), rows(64, seed=3), [20, 30, 14])
     check_attend(pool, rows(3, heads=6, seed=4), pool.mass.clone())
     assert int(pool.status) == 0
+
+
+def test_a_moved_sequence_keeps_its_weights():
+    """The weight that each block has drawn goes with it: eviction after a move takes the blocks that
+    it would have taken before."""
+    from paper_2606_03910_gb300.blocks import move
+    pool = make(slots=1, width=20)
+    pool.append(rows(200), rows(200, seed=1), [200])
+    pool.attend(rows(1, heads=6, seed=2) * 4)
+    torch.cuda.synchronize()
+    drawn = pool.mass[0, :13].clone()
+    assert float(drawn.max()) > 2 * float(drawn.min()) > 0
+    there = make(slots=2, width=16)
+    there.append(rows(30), rows(30), [30, 0])
+    move(pool, 0, there, 1)
+    assert torch.equal(there.mass[1, :13], drawn) and (there.mass[1, 13:] == 0).all()
+    held, order = list(pool.page_of[0]), list(there.page_of[1])
+    gone = pool.evict([6], sink=1, recent=1)[0]
+    assert [held.index(p) for p in gone] == \
+        [order.index(p) for p in there.evict([2, 6], sink=1, recent=1)[1]]
+    assert gone != held[1:8]  # not the oldest, as equal weights would have it
+
