@@ -179,20 +179,22 @@ def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
     n = src.tokens[slot]
     counts = [0] * dst.slots
     counts[to] = n
-    dst.reserve(counts)
+    taken = dst._take(counts)
+    # either slot may hold pages beyond its tokens
+    blocks = blocks_of(n)
+    here, there = src.page_of[slot][:blocks], dst.page_of[to][:blocks]
     one = src.pages.tensors[0][0].numel()
-    copies, total = [], 0
-    for a, b in zip(src.page_of[slot], dst.page_of[to]):
-        for i in (0, 1):
-            copies.append((dst.pages.tensors[i][b], src.pages.tensors[i][a], one))
-    netkv.netkv_copy_group_async(copies)
+    try:
+        netkv.netkv_copy_group_async([(dst.pages.tensors[i][b], src.pages.tensors[i][a], one)
+                                      for a, b in zip(here, there) for i in (0, 1)])
+    except Exception:
+        dst._give_back(taken)
+        raise
     # scales are kv_heads floats a page, less than a copy's 16 bytes for some shapes
-    a, b = src._dev(src.page_of[slot], torch.int64), dst._dev(dst.page_of[to], torch.int64)
+    a, b = src._dev(here, torch.int64), dst._dev(there, torch.int64)
     for i in (2, 3):
         dst.pages.tensors[i][b] = src.pages.tensors[i][a]
-        total += len(src.page_of[slot]) * src.pages.tensors[i][0].numel() * 4
-    blocks = blocks_of(n)
     dst.mass[to, :blocks] = src.mass[slot, :blocks]
     dst.tokens[to] = n
     dst.length[to] = n
-    return total + len(copies) * one
+    return 2 * blocks * (one + src.pages.tensors[2][0].numel() * 4)

@@ -76,3 +76,24 @@ def test_reserve_when_one_slot_has_more_than_it_needs(blocks):
     assert len(pool.free) == 7 and [len(p) for p in pool.page_of] == [5, 0, 0]
     pool.reserve([16, 80, 32])
     assert len(pool.free) == 0 and [len(p) for p in pool.page_of] == [5, 5, 2]
+
+
+def test_move_of_a_slot_with_pages_in_advance(blocks, monkeypatch):
+    """Pages that a slot holds beyond its tokens are neither copied nor counted, on either side, and a
+    move that fails leaves the destination's pages as they were."""
+    src, dst = make(blocks), make(blocks)
+    src.reserve([60, 0, 0])
+    src.tokens[0] = 20
+    dst.reserve([0, 70, 0])
+    copies = []
+    monkeypatch.setattr(blocks.netkv, "netkv_copy_group_async", copies.extend)
+    assert blocks.move(src, 0, dst, 1) == 2 * 2 * 2 * (16 * 64 + 4)
+    assert len(copies) == 4 and dst.tokens == [0, 20, 0] and len(dst.page_of[1]) == 5
+
+    def fail(copies):
+        raise RuntimeError
+    monkeypatch.setattr(blocks.netkv, "netkv_copy_group_async", fail)
+    before = state(dst)
+    with pytest.raises(RuntimeError):
+        blocks.move(src, 0, dst, 2)
+    assert state(dst)[:3] == before[:3]

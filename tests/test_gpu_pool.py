@@ -54,3 +54,24 @@ def test_a_moved_sequence_keeps_its_weights():
         [order.index(p) for p in there.evict([2, 6], sink=1, recent=1)[1]]
     assert gone != held[1:8]  # not the oldest, as equal weights would have it
 
+
+def test_a_move_of_a_slot_with_pages_in_advance():
+    """Pages that either slot holds beyond its tokens are neither copied nor in the way."""
+    from paper_2606_03910_gb300.blocks import move
+    pool, there = make(slots=2), make(slots=2)
+    pool.append(rows(20), rows(20, seed=1), [20, 0])
+    pool.reserve([100, 0])
+    there.reserve([0, 60])
+    moved = move(pool, 0, there, 1)
+    assert moved == 2 * 2 * 2 * (16 * 64 + 4) and there.tokens == [0, 20]
+    check_same_tokens(pool, 0, there, 1)
+
+
+def check_same_tokens(a, i, b, j):
+    """Two slots' tokens, value for value."""
+    n = a.tokens[i]
+    assert b.tokens[j] == n and int(b.length[j]) == n
+    got = [torch.zeros((n, 2, 64), dtype=torch.float16, device="cuda") for _ in range(4)]
+    a.read(got[0], got[1], [n if s == i else 0 for s in range(a.slots)])
+    b.read(got[2], got[3], [n if s == j else 0 for s in range(b.slots)])
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3]) and got[0].any()
