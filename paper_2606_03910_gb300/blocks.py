@@ -59,7 +59,10 @@ class BlockPool:
         return len(self.tokens)
 
     def _dev(self, x, dtype=torch.int32):
-        return torch.tensor(list(x), dtype=dtype, device=self.table.device)
+        """A list on the device, sent from pinned memory: a copy from elsewhere waits for the stream."""
+        cuda = self.table.device.type == "cuda"
+        t = torch.tensor(list(x), dtype=dtype, pin_memory=cuda)
+        return t.to(self.table.device, non_blocking=True)
 
     def _offsets(self, counts: Sequence[int]):
         off = [0]
@@ -98,7 +101,7 @@ class BlockPool:
         if at:
             at = self._dev(at, torch.int64)
             self.table.view(-1)[at] = self._dev(pages)
-            self.mass.view(-1)[at] = 0.0
+            self.mass.view(-1).index_fill_(0, at, 0.0)
         return need
 
     def _give_back(self, taken: List[int]) -> None:
@@ -163,8 +166,8 @@ class BlockPool:
         self.free.extend(self.page_of[slot])
         self.page_of[slot] = []
         self.tokens[slot] = 0
-        self.table[slot] = -1
-        self.length[slot] = 0
+        self.table[slot].fill_(-1)
+        self.length[slot].fill_(0)
 
 
 def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
@@ -196,5 +199,5 @@ def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
         dst.pages.tensors[i][b] = src.pages.tensors[i][a]
     dst.mass[to, :blocks] = src.mass[slot, :blocks]
     dst.tokens[to] = n
-    dst.length[to] = n
+    dst.length[to].fill_(n)
     return 2 * blocks * (one + src.pages.tensors[2][0].numel() * 4)

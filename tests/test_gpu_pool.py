@@ -75,3 +75,27 @@ def check_same_tokens(a, i, b, j):
     a.read(got[0], got[1], [n if s == i else 0 for s in range(a.slots)])
     b.read(got[2], got[3], [n if s == j else 0 for s in range(b.slots)])
     assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3]) and got[0].any()
+
+
+def test_only_eviction_waits_for_the_device():
+    """Every call but evict() only enqueues work: what the host sends is staged, and nothing asks the
+    device for an answer."""
+    from paper_2606_03910_gb300.blocks import move
+    pool, there = make(), make()
+    k, v, q = rows(90), rows(90, seed=1), rows(3, heads=6, seed=2)
+    pool.append(k[:3], v[:3], [1, 1, 1])
+    torch.cuda.synchronize()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        pool.append(k, v, [40, 50, 0])
+        pool.append(k[:3], v[:3], [1, 1, 1])
+        pool.attend(q)
+        pool.read(k, v, [40, 50, 0])
+        move(pool, 1, there, 2)
+        pool.release(1)
+        pool.reserve([0, 100, 0])
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    torch.cuda.synchronize()
+    check_attend(pool, q, pool.mass.clone())
+    check_attend(there, q, there.mass.clone())
