@@ -564,7 +564,8 @@ netkv_status netkv_kv_load(const netkv_kv_pages* pages, uint32_t dtype, void* d_
  *     out = sum_j softmax_j(scale * q_r . k_j) v_j,   lse = log sum_j exp(scale * q_r . k_j)
  * A row that sees no key (Lk < Lq) gives 0 and -inf.  Products are of 16-bit values with fp32
  * sums; the softmax is in fp32; its weights are rounded to the inputs' type for the second
- * product.  d_lse [q_rows][heads] fp32 or NULL.  Rows outside every sequence are not written.
+ * product (fp16: to 2^-11 of themselves down to 2^-21 of the row's largest, 0 below 2^-32 of it).
+ * d_lse [q_rows][heads] fp32 or NULL.  Rows outside every sequence are not written.
  * Values of a sequence's own v have to be finite: an infinity or NaN may reach rows that do
  * not see it.  What lies outside the sequence reaches nothing.  scale is finite and > 0.
  * At most 2^31 - 1 rows of either kind and 2^24 - 1 sequences. */
@@ -585,6 +586,10 @@ size_t netkv_attn_decode_workspace_size(const netkv_kv_pages* pages, uint32_t n_
  * [0, d_len[i]) of sequence i.
  *     out = sum_t softmax_t(scale * q . k_t) v_t,  lse as for netkv_attn_prompt
  * A sequence without tokens gives 0 and -inf.  A length past the table sets ERANGE and is cut.
+ * Codes go into the products as they are, queries as fp16 (bf16 rows times a power of two: channels
+ * down to 2^-31 of a row's largest keep their bits), and so do the softmax weights times the blocks'
+ * value scales (to 2^-11 of themselves down to 2^-20 of the largest, 0 below 2^-31 of it); sums,
+ * lse and block weights are fp32.
  *   d_lse       [n_seqs][heads] fp32 or NULL
  *   d_mass_in, d_mass_out  [n_seqs][table_width] fp32 or NULL (both or d_mass_in only NULL):
  *               mass_out[i][j] = mass_in[i][j] + the softmax weights of block j's tokens,

@@ -4,9 +4,9 @@
 // Bound: the codes are read once, 2 kDim bytes a token and KV head, and everything else is
 // small, so the kernel streams pages and its arithmetic has to fit in their shadow: about 330
 // instructions a warp and page of 4 KB, which take 45 % of the issue slots.  160 sequences of
-// 5,500 tokens with 64 query heads on 8 KV heads of 128, int8: 300 us, 6.0 TB/s; 64 of 13,000
-// with 16 on 2 and block weights: 91 us, 4.8 TB/s; two of 131,072, e4m3: 39 us, 3.4 TB/s (of
-// which 20 are the bytes and 10 the join and both ends); one of 512: 10 us.
+// 5,500 tokens with 64 query heads on 8 KV heads of 128, int8: 291 us, 6.2 TB/s (bf16 queries 298);
+// 64 of 13,000 with 16 on 2 and block weights: 90 us, 4.8 TB/s; two of 131,072, e4m3: 40 us, 3.4 TB/s
+// (of which 20 are the bytes and 10 the join and both ends); one of 512: 10 us.
 //
 // Split: the work is the list of all pages, (sequence, KV head, block) in order, cut into equal
 // runs, so that ragged batches and single long sequences spread over the card alike.  A run is
@@ -39,7 +39,8 @@ constexpr uint32_t kUncutBlocks = 32;  // see uncut_runs
 template <int kDim>
 constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16 KB
 constexpr uint32_t kEdge = 8;       // see Runs; at 0 runs of short segments end last (338 us for 308)
-constexpr uint32_t kMinPages = 16;  // a block's run at least: a pair of pages a warp, and an edge
+constexpr uint32_t kMinPages = 16;  // places of a run at least: a pair of pages for each of a block's
+                                    // warps and an edge; a warp's own then cuts few short segments
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
 // weights up to 2^8 are as exact in fp16 as those up to 1, and sums are fp32.
@@ -160,12 +161,10 @@ struct Lens {
   }
 };
 
-template <bool kOwn>
 __device__ __forceinline__ Runs runs_of(const DecodeArgs& a, const Lens& lens, uint32_t units) {
   Runs r;
   r.total = lens.total * units;
-  // a warp's own run is long enough not to cut many short segments
-  r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / (kOwn ? 16 : kMinPages)));
+  r.count = (uint32_t)min((uint64_t)a.most_runs, max((uint64_t)1, r.total / kMinPages));
   r.base = div_floor(r.total, r.count);
   r.rest = (uint32_t)(r.total - r.base * r.count);
   return r;
@@ -500,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, kTiles == 1 ? 3 : 2)
   }
   if (tid == 0) sh.late = 0;
   const Lens lens(a);
-  const Runs runs = runs_of<kOwn>(a, lens, units);
+  const Runs runs = runs_of(a, lens, units);
   __syncthreads();
   volatile int* late = &sh.late;
   if (warp == kWarps) {

@@ -3,8 +3,8 @@
 // Bound: 4 kDim flops a visible (query, key) pair on the tensor cores, 1,024 clocks for 128 x 128
 // pairs at 128 wide; the exponentials, 512 clocks at 32 a clock and SM, come next and bind at 64
 // wide.  One prompt of 32,768 tokens, 16 heads of 128: 2.57 ms, 1,710 TFLOP/s; ten ragged ones of
-// 10,740 tokens in all: 67 us, 1,030; six behind cached prefixes, 8 heads of 64: 40 us, 600 (its
-// longest row block sees 41 key tiles, one after another); one of 512: 10 us on the device.
+// 10,740 tokens in all: 68 us, 1,010; six behind cached prefixes, 8 heads of 64: 41 us, 590 (the
+// longest row block's 41 key tiles are 21 steps in a row); one of 512: 10 us on the device.
 //
 // A block takes two tiles of 128 query rows that read the same keys: two heads of a group where
 // the group is even, else two neighbouring row blocks of one head.  Where items are few it takes
@@ -18,8 +18,9 @@
 // on which their product can begin.  The products of one issuing thread complete in order, so S_t
 // of the next keys may follow P_t V at once.  The issuing warp stays together and elects that
 // thread: operands of a divergent thread go through vector registers, 70 clocks a product.
-// The running maximum is left behind until a score passes it by 2^8 (kLag): weights of up to
-// 2^8 are as exact, and the output is then rescaled only a few times a row.
+// One pass over the keys carries a row's maximum and sum (Milakov and Gimelshein, 2018).  The maximum
+// is left behind until a score passes it by 2^8 (kLag): weights of up to 2^8 are as exact, and the
+// output is then rescaled only a few times a row.
 // Loads, products and softmax run on from one item to the next.  The grid has a block for each
 // item; a running block takes over items of blocks that have not started (cluster launch control),
 // one ahead, so that they end together (ten ragged prompts 82 -> 65 us with the order by steps).

@@ -7,7 +7,7 @@
 // is kept to 2^-8 or 2^-4.
 //
 // Storing and loading are bound by HBM: 223,000 rows of 8 heads of 128 in 235 us (5.8 TB/s) and
-// back in 208 (6.6 TB/s), one warp a block and head with all of its loads under way at once.
+// back in 207 (6.6 TB/s), one warp a block and head with all of its loads under way at once.
 // With the loads behind a branch each, the way back took 277 us; with conversions one value at a
 // time, the way there 476.
 #include "kv_common.cuh"

@@ -128,6 +128,26 @@ _lib.netkv_schedule_streams_evolving.argtypes = [_P, _U32, _P, _U32, _P, _P, _P,
                                                  _P, _P, _P, _P, _P, _P, _P]
 _lib.netkv_copy_async.argtypes = [_P, _P, C.c_size_t, _P]
 _lib.netkv_copy_group_async.argtypes = [_P, _U32, _P]
+NETKV_BLOCK_TOKENS = 16
+NETKV_F16, NETKV_BF16 = 0, 1
+NETKV_KV_INT8, NETKV_KV_E4M3 = 0, 1
+_KV_FORMATS = {"int8": NETKV_KV_INT8, "float8_e4m3fn": NETKV_KV_E4M3}
+_lib.netkv_kv_store.argtypes = [_P, _U32, _P, _U64, _P, _U64, _U32, _P, _U64, _P, _P, _U32, _P, _P]
+_lib.netkv_kv_load.argtypes = _lib.netkv_kv_store.argtypes
+_lib.netkv_attn_prompt.argtypes = [_U32, _P, _U64, _P, _U64, _P, _U64, _U32, _U32, _U32, _U32, _P,
+                                   _P, _U64, _U64, C.c_float, _P, _U64, _P, _P, _P]
+_lib.netkv_attn_decode_workspace_size.argtypes = [_P, _U32, _U32, _U32, C.c_int]
+_lib.netkv_attn_decode_workspace_size.restype = C.c_size_t
+_lib.netkv_attn_decode.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _P, _P, _U32, C.c_float, _P,
+                                   _U64, _P, _P, _P, _P, C.c_size_t, _P, _P]
+_lib.netkv_kv_evict.argtypes = [_U32, _P, _P, _P, _U32, _P, _U32, _U32, _P, _P, _P, _P, _P, _P, _P]
+for _f in EXPORTS:
+    if _f not in ("netkv_version", "netkv_prefix_match_workspace_size", "netkv_cache_index_bytes",
+                  "netkv_schedule_workspace_size", "netkv_schedule_inflight_workspace_size",
+                  "netkv_lru_state_bytes", "netkv_attn_decode_workspace_size"):
+        getattr(_lib, _f).restype = C.c_int
+
+
 class KvPages(C.Structure):
     """netkv_kv_pages over four tensors, which it keeps: codes [n_pages, kv_heads, 16, dim] of
     torch.int8 or torch.float8_e4m3fn, and fp32 scales [n_pages, kv_heads]."""
@@ -159,26 +179,6 @@ class KvPages(C.Structure):
         self.ref = C.byref(self)
         self.heads_dim = (k.shape[1], k.shape[3])  # a field of a structure takes longer to read
         self.device, self.device_index = k.device, k.get_device()
-
-
-NETKV_BLOCK_TOKENS = 16
-NETKV_F16, NETKV_BF16 = 0, 1
-NETKV_KV_INT8, NETKV_KV_E4M3 = 0, 1
-_KV_FORMATS = {"int8": NETKV_KV_INT8, "float8_e4m3fn": NETKV_KV_E4M3}
-_lib.netkv_kv_store.argtypes = [_P, _U32, _P, _U64, _P, _U64, _U32, _P, _U64, _P, _P, _U32, _P, _P]
-_lib.netkv_kv_load.argtypes = _lib.netkv_kv_store.argtypes
-_lib.netkv_attn_prompt.argtypes = [_U32, _P, _U64, _P, _U64, _P, _U64, _U32, _U32, _U32, _U32, _P,
-                                   _P, _U64, _U64, C.c_float, _P, _U64, _P, _P, _P]
-_lib.netkv_attn_decode_workspace_size.argtypes = [_P, _U32, _U32, _U32, C.c_int]
-_lib.netkv_attn_decode_workspace_size.restype = C.c_size_t
-_lib.netkv_attn_decode.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _P, _P, _U32, C.c_float, _P,
-                                   _U64, _P, _P, _P, _P, C.c_size_t, _P, _P]
-_lib.netkv_kv_evict.argtypes = [_U32, _P, _P, _P, _U32, _P, _U32, _U32, _P, _P, _P, _P, _P, _P, _P]
-for _f in EXPORTS:
-    if _f not in ("netkv_version", "netkv_prefix_match_workspace_size", "netkv_cache_index_bytes",
-                  "netkv_schedule_workspace_size", "netkv_schedule_inflight_workspace_size",
-                  "netkv_lru_state_bytes", "netkv_attn_decode_workspace_size"):
-        getattr(_lib, _f).restype = C.c_int
 
 
 def _ptr(x) -> Optional[int]:
@@ -432,7 +432,9 @@ def netkv_copy_group_async(copies, stream=None) -> None:
 
 
 # ---- KV blocks: tensors carry their sizes, so these take them from the tensors and check that
-# they fit together; everything else is checked behind the entry points.
+# they fit together and are all on the current CUDA device, on which the kernels run; everything else
+# is checked behind the entry points.
+
 # What is asked of torch, once (a program without it may use the rest of the binding): the dtypes
 # of each kind, and who knows the current device and its stream.
 _ROWS, _F32, _I32, _I64 = {}, (), (), ()
