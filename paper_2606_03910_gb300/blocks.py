@@ -98,11 +98,15 @@ class BlockPool:
                 at.append(s * self.table.shape[1] + len(self.page_of[s]))
                 pages.append(page)
                 self.page_of[s].append(page)
+        self._enter(at, pages)
+        return need
+
+    def _enter(self, at: List[int], pages: List[int]) -> None:
+        """Pages into the table's entries, which have drawn nothing yet."""
         if at:
             at = self._dev(at, torch.int64)
             self.table.view(-1)[at] = self._dev(pages)
             self.mass.view(-1).index_fill_(0, at, 0.0)
-        return need
 
     def _give_back(self, taken: List[int]) -> None:
         for pages, n in zip(reversed(self.page_of), reversed(taken)):
@@ -154,11 +158,16 @@ class BlockPool:
         self._spare = (self.table, self.length, self.mass, freed, n_freed)
         self.table, self.length, self.mass = table, length, mass
         gone = [row[:n] for row, n in zip(freed.tolist(), n_freed.tolist())]
+        at, ahead = [], []  # pages for tokens to come, which the call does not know of
         for s, pages in enumerate(gone):
             out = set(pages)
             self.page_of[s] = [p for p in self.page_of[s] if p not in out]
             self.tokens[s] -= BLOCK * len(pages)
             self.free.extend(pages)
+            used = blocks_of(self.tokens[s])
+            at.extend(s * self.table.shape[1] + i for i in range(used, len(self.page_of[s])))
+            ahead.extend(self.page_of[s][used:])
+        self._enter(at, ahead)
         return gone
 
     def release(self, slot: int) -> None:

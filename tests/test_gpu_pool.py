@@ -67,6 +67,23 @@ def test_a_move_of_a_slot_with_pages_in_advance():
     check_same_tokens(pool, 0, there, 1)
 
 
+def test_pages_in_advance_outlive_an_eviction():
+    """A slot that holds pages for tokens to come still has them in its table after blocks before
+    them have gone."""
+    pool = make(pages=40, width=16)
+    pool.append(rows(170), rows(170, seed=1), [100, 0, 70])
+    pool.reserve([60, 40, 0])
+    held = [list(p) for p in pool.page_of]
+    gone = pool.evict([3, 3, 3], sink=1, recent=1)
+    assert [len(x) for x in gone] == [4, 0, 2]
+    for s in range(3):
+        assert pool.page_of[s] == [p for p in held[s] if p not in gone[s]]
+        assert pool.table[s, :len(pool.page_of[s])].tolist() == pool.page_of[s]
+    pool.append(rows(110, seed=2), rows(110, seed=3), [60, 40, 10])
+    check_attend(pool, rows(3, heads=6, seed=4), pool.mass.clone())
+    assert int(pool.status) == 0
+
+
 def check_same_tokens(a, i, b, j):
     """Two slots' tokens, value for value."""
     n = a.tokens[i]
