@@ -521,10 +521,11 @@ def _plane(t, rows: int, width: int, device: int) -> Optional[int]:
 
 
 def _word(t, device: int) -> Optional[int]:
-    """The address of a status word: a tensor, an address, or None."""
+    """The address of a status word: a tensor (in pinned host memory too, where a program may read it
+    without a copy), an address, or None."""
     if t is None or t.__class__ is int:
         return t
-    if t.get_device() != device:
+    if t.get_device() != device and not t.is_pinned():
         _elsewhere(t, device)
     return t.data_ptr()
 
@@ -606,7 +607,9 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     if workspace is not None:
         if not workspace.is_contiguous():
             raise ValueError("a contiguous workspace expected")
-        wp, ws_bytes = _word(workspace, d), workspace.nbytes
+        if workspace.get_device() != d:
+            _elsewhere(workspace, d)
+        wp, ws_bytes = workspace.data_ptr(), workspace.nbytes
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
         pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n, d), tp, tw,
         dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads, d),

@@ -70,3 +70,15 @@ def test_replay(width):
         torch.cuda.synchronize()
         assert int(status) == 0
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_status_in_pinned_memory():
+    """A status word that the host reads without a copy."""
+    from paper_2606_03910_gb300 import netkv
+    k, s = torch.zeros((1, 1, 16, 64), dtype=torch.int8, device="cuda"), torch.zeros((1, 1), device="cuda")
+    pages = netkv.KvPages(k, k.clone(), s, s.clone())
+    row = torch.full((1, 1, 64), float("inf"), dtype=torch.float16, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, pin_memory=True)
+    netkv.netkv_kv_store(pages, row, row, offsets([1]), None, ints([0]).view(1, 1), status=status)
+    torch.cuda.synchronize()
+    assert int(status) == netkv.NETKV_DEV_EDOMAIN

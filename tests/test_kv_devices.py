@@ -119,6 +119,19 @@ def test_addresses_and_absent_arguments(kv):
     assert len(calls) == 2
 
 
+def test_a_status_in_pinned_memory(kv, monkeypatch):
+    """The host may poll it: the kernels' atomics reach pinned memory."""
+    netkv, calls = kv
+    a = {k: on(t, 0) for k, t in ARGS["netkv_kv_store"].items()}
+    a.update(status=on(torch.zeros(1, dtype=I), -1))
+    monkeypatch.setattr(On, "is_pinned", lambda t: True, raising=False)
+    netkv.netkv_kv_store(pages(netkv, 0), **a)
+    assert len(calls) == 1
+    a.update(table=on(ARGS["netkv_kv_store"]["table"], -1))
+    with pytest.raises(ValueError):
+        netkv.netkv_kv_store(pages(netkv, 0), **a)
+
+
 def test_a_workspace_that_is_not_as_large_as_it_says(kv):
     """Elements that lie on one another or apart: their number is not the buffer's size."""
     netkv, calls = kv
