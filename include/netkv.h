@@ -622,6 +622,83 @@ netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table, const uint3
                             uint32_t* d_len_out, float* d_mass_out, int32_t* d_freed,
                             uint32_t* d_n_freed, int* d_status, netkv_stream_t stream);
 
+/* ------------------------------------------------------------------ new tokens of running sequences
+ * A running sequence gets its tokens in chunks: parts of a long prompt, one token a step, or a few
+ * drafted ones to verify.  A step of a layer is netkv_kv_append, which turns the chunk's queries and
+ * keys by their positions and puts keys and values behind what the blocks hold, and then
+ * netkv_attn_chunk over the blocks.  netkv_rotate turns rows that go elsewhere, as a prompt's to
+ * netkv_attn_prompt.
+ *
+ * Rotary positions.  Pair p of a head is its channels p and p + pairs (interleaved: 2p and 2p + 1);
+ * channels from 2 * pairs on are left as they are.  With the token's position t on the pair's axis
+ * and a = t * step[p] / 2^64 turns,
+ *     (x, y) -> (x cos a - y sin a, y cos a + x sin a)
+ * in fp32.  Several axes: time, height and width of a token of an image or a video, for example. */
+typedef struct {
+  uint64_t step[64];    /* of pair p: the part of a whole turn that a position is, times 2^64 */
+  uint8_t axis[64];     /* of pair p: the axis whose positions it goes by, < axes */
+  uint32_t pairs;       /* 8 .. head_dim / 2, a multiple of 8 */
+  uint32_t axes;        /* 1 .. 4 */
+  uint32_t interleaved; /* 0 or 1 */
+  uint32_t reserved;    /* set to 0 */
+} netkv_rotary;         /* 592 bytes; host memory, read during a call */
+
+/* Fills *rot (host only, no GPU): pair p turns by frequency[p] radians a position, 0 or more and
+ * below 2 pi.  sections [axes] pairs of each axis in order, pairs in all; NULL with one axis. */
+netkv_status netkv_rotary_set(netkv_rotary* rot, uint32_t pairs, const double* frequency,
+                              uint32_t axes, const uint32_t* sections, uint32_t interleaved);
+
+/* Rows of heads * head_dim values by their positions.  d_pos [axes][rows] int32, any sign (negated
+ * positions undo the rotation).  d_out may be d_x with the same stride, and may not overlap it
+ * otherwise.  At most 2^31 - 1 rows. */
+netkv_status netkv_rotate(const netkv_rotary* rot, uint32_t dtype, const void* d_x,
+                          uint64_t x_stride, uint32_t heads, uint32_t head_dim, uint64_t rows,
+                          const int32_t* d_pos, void* d_out, uint64_t out_stride,
+                          netkv_stream_t stream);
+
+/* netkv_kv_store of keys that are turned by their positions on the way, in fp32 without another
+ * rounding: a block's scale is that of the turned values, and infinities and NaN are those after
+ * the rotation.  Values are stored as they are.
+ *   d_pos    [axes][rows] int32, or NULL with one axis: tokens d_start[i], d_start[i] + 1, ... of
+ *            sequence i are at just those positions
+ *   d_q      the same tokens' queries, rows of heads * head_dim values, turned into d_q_out, which
+ *            may be d_q with the same stride; NULL for none.  Queries are turned where a token has
+ *            no place in the table too.  Rows outside every sequence are not written. */
+netkv_status netkv_kv_append(const netkv_kv_pages* pages, const netkv_rotary* rot, uint32_t dtype,
+                             const void* d_k, uint64_t k_stride, const void* d_v, uint64_t v_stride,
+                             uint32_t n_seqs, const uint64_t* d_off, uint64_t rows,
+                             const uint32_t* d_start, const int32_t* d_table, uint32_t table_width,
+                             const int32_t* d_pos, uint32_t heads, const void* d_q,
+                             uint64_t q_stride, void* d_q_out, uint64_t q_out_stride, int* d_status,
+                             netkv_stream_t stream);
+
+/* Workspace of netkv_attn_chunk, 16-byte aligned; 0 for sizes out of range. */
+size_t netkv_attn_chunk_workspace_size(const netkv_kv_pages* pages, uint64_t rows, uint32_t n_seqs,
+                                       uint32_t heads);
+
+/* Causal attention of each sequence's new tokens over its blocks, which hold them already.  Rows
+ * [d_off[i], d_off[i+1]) of d_q are the last Lq of sequence i's L = d_len[i] tokens; row r of them
+ * sees tokens t <= r + L - Lq:
+ *     out = sum_t softmax_t(scale * q_r . k_t) v_t,   lse = log sum_t exp(scale * q_r . k_t)
+ * A row that sees no token (L < Lq, or absent pages only) gives 0 and -inf.  A length past the table
+ * sets ERANGE and is cut, and so does a sequence with bad offsets, which has no rows.  Rows outside
+ * every sequence are not written.
+ * Codes go into the products as they are, queries as fp16 (bf16 rows times a power of two: channels
+ * down to 2^-31 of a row's largest keep their bits), and so do the softmax weights times the blocks'
+ * value scales (to 2^-11 of themselves down to 2^-20 of the largest, 0 below 2^-31 of it); sums and lse
+ * are fp32.  Scales are finite and 0 or more.
+ *   d_lse [rows][heads] fp32 or NULL
+ *   d_ws  caller-owned, netkv_attn_chunk_workspace_size bytes; needs no initial value; calls that
+ *         overlap on the GPU need distinct ones
+ * Codes past a sequence's last token reach nothing.  scale is finite and > 0.  At most 2^31 - 1 rows
+ * and 2^24 - 1 sequences. */
+netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t dtype, const void* d_q,
+                              uint64_t q_stride, uint32_t heads, uint32_t n_seqs,
+                              const uint64_t* d_off, uint64_t rows, const uint32_t* d_len,
+                              const int32_t* d_table, uint32_t table_width, float scale, void* d_out,
+                              uint64_t out_stride, float* d_lse, void* d_ws, size_t ws_bytes,
+                              int* d_status, netkv_stream_t stream);
+
 /* Library version, for the bindings' load check. */
 uint32_t netkv_version(void);
 

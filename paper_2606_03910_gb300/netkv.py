@@ -45,6 +45,8 @@ EXPORTS = ("netkv_topology_create", "netkv_topology_destroy", "netkv_topology_qu
            "netkv_copy_async", "netkv_copy_group_async",
            "netkv_kv_store", "netkv_kv_load", "netkv_attn_prompt",
            "netkv_attn_decode_workspace_size", "netkv_attn_decode", "netkv_kv_evict",
+           "netkv_rotary_set", "netkv_rotate", "netkv_kv_append",
+           "netkv_attn_chunk_workspace_size", "netkv_attn_chunk",
            "netkv_version")
 
 
@@ -141,10 +143,19 @@ _lib.netkv_attn_decode_workspace_size.restype = C.c_size_t
 _lib.netkv_attn_decode.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _P, _P, _U32, C.c_float, _P,
                                    _U64, _P, _P, _P, _P, C.c_size_t, _P, _P]
 _lib.netkv_kv_evict.argtypes = [_U32, _P, _P, _P, _U32, _P, _U32, _U32, _P, _P, _P, _P, _P, _P, _P]
+_lib.netkv_rotary_set.argtypes = [_P, _U32, C.POINTER(C.c_double), _U32, C.POINTER(C.c_uint32), _U32]
+_lib.netkv_rotate.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _U64, _P, _P, _U64, _P]
+_lib.netkv_kv_append.argtypes = [_P, _P, _U32, _P, _U64, _P, _U64, _U32, _P, _U64, _P, _P, _U32, _P,
+                                 _U32, _P, _U64, _P, _U64, _P, _P]
+_lib.netkv_attn_chunk_workspace_size.argtypes = [_P, _U64, _U32, _U32]
+_lib.netkv_attn_chunk_workspace_size.restype = C.c_size_t
+_lib.netkv_attn_chunk.argtypes = [_P, _U32, _P, _U64, _U32, _U32, _P, _U64, _P, _P, _U32, C.c_float,
+                                  _P, _U64, _P, _P, C.c_size_t, _P, _P]
 for _f in EXPORTS:
     if _f not in ("netkv_version", "netkv_prefix_match_workspace_size", "netkv_cache_index_bytes",
                   "netkv_schedule_workspace_size", "netkv_schedule_inflight_workspace_size",
-                  "netkv_lru_state_bytes", "netkv_attn_decode_workspace_size"):
+                  "netkv_lru_state_bytes", "netkv_attn_decode_workspace_size",
+                  "netkv_attn_chunk_workspace_size"):
         getattr(_lib, _f).restype = C.c_int
 
 
@@ -530,6 +541,17 @@ def _word(t, device: int) -> Optional[int]:
     return t.data_ptr()
 
 
+def _workspace(t, device: int):
+    """(address, bytes) of a call's workspace, or of none."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError("a contiguous workspace expected")
+    if t.get_device() != device:
+        _elsewhere(t, device)
+    return t.data_ptr(), t.nbytes
+
+
 def _on_stream(device: int, stream) -> Optional[int]:
     """The given stream, else torch's current one on the device."""
     return _raw_stream(device) if stream is None else _stream(stream)
@@ -603,13 +625,7 @@ def netkv_attn_decode(pages: KvPages, q, length, table, out, lse=None, mass_in=N
     if out.shape[0] != n:
         raise ValueError("as many rows of out as of q expected")
     tp, tw = _table(table, n, d)
-    wp, ws_bytes = None, 0
-    if workspace is not None:
-        if not workspace.is_contiguous():
-            raise ValueError("a contiguous workspace expected")
-        if workspace.get_device() != d:
-            _elsewhere(workspace, d)
-        wp, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    wp, ws_bytes = _workspace(workspace, d)
     _check("netkv_attn_decode", _lib.netkv_attn_decode(
         pages.ref, dt, qp, qs, heads, n, _ints(length, _I32, n, d), tp, tw,
         dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, n, heads, d),
@@ -631,6 +647,121 @@ def netkv_kv_evict(table, length, mass, budget, sink: int, recent: int, table_ou
         n, tp, _ints(length, _I32, n, d), _plane(mass, n, tw, d), tw, _ints(budget, _I32, n, d),
         int(sink), int(recent), to, _ints(length_out, _I32, n, d), _plane(mass_out, n, tw, d), fr,
         _ints(n_freed, _I32, n, d), _word(status, d), _on_stream(d, stream)))
+
+
+class Rotary(C.Structure):
+    """netkv_rotary: which channel pairs of a head are turned, and how fast.
+
+    ``pairs`` pairs of a head (half its dim, or fewer: the channels behind them are left as they
+    are) turn by ``frequencies`` radians a position, base ** (-p / pairs) by default.  ``sections``:
+    pairs of each position axis in order (one axis by default).  See include/netkv.h."""
+    _fields_ = [("step", C.c_uint64 * 64), ("axis", C.c_uint8 * 64), ("pairs", C.c_uint32),
+                ("axes", C.c_uint32), ("interleaved", C.c_uint32), ("reserved", C.c_uint32)]
+
+    def __init__(self, pairs: int, base: float = 10000.0, sections: Optional[Sequence[int]] = None,
+                 interleaved: bool = False, frequencies: Optional[Sequence[float]] = None):
+        super().__init__()
+        pairs = int(pairs)
+        if not 0 < pairs <= 64:
+            raise ValueError(f"1 to 64 pairs expected, got {pairs}")
+        f = [base ** (-p / pairs) for p in range(pairs)] if frequencies is None else \
+            [float(x) for x in frequencies]
+        sections = [pairs] if sections is None else [int(n) for n in sections]
+        if len(f) != pairs or sum(sections) != pairs or min(sections, default=-1) < 0:
+            raise ValueError(f"{pairs} frequencies, and sections of {pairs} pairs in all, expected")
+        _check("netkv_rotary_set", _lib.netkv_rotary_set(
+            C.byref(self), pairs, (C.c_double * pairs)(*f), len(sections),
+            (C.c_uint32 * len(sections))(*sections), int(bool(interleaved))))
+        self.ref = C.byref(self)
+
+
+def _positions(pos, rotary: Rotary, rows: int, device: int) -> Optional[int]:
+    """The address of the positions of each axis: [axes, rows], or [rows] with one axis."""
+    if pos is None:
+        return None
+    shape = tuple(pos.shape)
+    if shape != (rotary.axes, rows) and not (rotary.axes == 1 and shape == (rows,)):
+        raise ValueError(f"positions of {(rotary.axes, rows)} expected, got {shape}")
+    if pos.dtype not in _I32[:1]:
+        raise TypeError(f"int32 positions expected, got {pos.dtype}")
+    return _ints(pos, _I32, rotary.axes * rows, device)
+
+
+def netkv_rotate(rotary: Rotary, x, pos, out, stream=None) -> None:
+    """Rows x [rows, heads, dim] turned by their positions [axes, rows] into out, which may be x; see
+    include/netkv.h."""
+    rows, heads, dim = x.shape
+    d = _device(x)
+    dt, xp, xs = _rows(x, heads, dim, d)
+    _, op, os_ = _rows(out, heads, dim, d, dt)
+    if out.shape[0] != rows:
+        raise ValueError("as many rows of out as of x expected")
+    if pos is None:
+        raise ValueError("positions expected")
+    code = _lib.netkv_rotate(rotary.ref, dt, xp, xs, heads, dim, rows,
+                             _positions(pos, rotary, rows, d), op, os_, _on_stream(d, stream))
+    if code:
+        raise NetKVError("netkv_rotate", code)
+
+
+def netkv_kv_append(pages: KvPages, k, v, off, start, table, rotary: Rotary, pos=None, q=None,
+                    q_out=None, status=None, stream=None) -> None:
+    """New tokens into 8-bit blocks, keys turned by their positions on the way, and the tokens'
+    queries q [rows, heads, dim] turned into q_out; see include/netkv.h."""
+    kv_heads, dim = pages.heads_dim
+    d = _device(k)
+    if pages.device_index != d:
+        _elsewhere(pages, d)
+    dt, kp, ks = _rows(k, kv_heads, dim, d)
+    _, vp, vs = _rows(v, kv_heads, dim, d, dt)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
+        raise ValueError("as many rows of keys as of values expected")
+    heads, qp, qs, op, os_ = 0, None, 0, None, 0
+    if (q is None) != (q_out is None):
+        raise ValueError("queries and a place for them expected, or neither")
+    if q is not None:
+        heads = q.shape[1]
+        _, qp, qs = _rows(q, heads, dim, d, dt)
+        _, op, os_ = _rows(q_out, heads, dim, d, dt)
+        if q.shape[0] != rows or q_out.shape[0] != rows:
+            raise ValueError("as many rows of queries as of keys expected")
+    n = off.numel() - 1
+    tp, tw = _table(table, n, d)
+    code = _lib.netkv_kv_append(
+        pages.ref, rotary.ref, dt, kp, ks, vp, vs, n, _ints(off, _I64, n + 1, d), rows,
+        _ints(start, _I32, n, d), tp, tw, _positions(pos, rotary, rows, d), heads, qp, qs, op, os_,
+        _word(status, d), _on_stream(d, stream))
+    if code:
+        raise NetKVError("netkv_kv_append", code)
+
+
+def netkv_attn_chunk_workspace_size(pages: KvPages, rows: int, n_seqs: int, heads: int) -> int:
+    """Bytes of the workspace; see include/netkv.h."""
+    return int(_lib.netkv_attn_chunk_workspace_size(pages.ref, int(rows), int(n_seqs), int(heads)))
+
+
+def netkv_attn_chunk(pages: KvPages, q, off, length, table, out, lse=None, scale=None,
+                     workspace=None, status=None, stream=None) -> None:
+    """Causal attention of each sequence's new tokens, the rows q [rows, heads, dim] that off numbers,
+    over its blocks, which hold length[i] tokens with these; see include/netkv.h."""
+    rows, heads, dim = q.shape
+    d = _device(q)
+    if pages.device_index != d:
+        _elsewhere(pages, d)
+    dt, qp, qs = _rows(q, heads, pages.heads_dim[1], d)
+    _, op, os_ = _rows(out, heads, dim, d, dt)
+    if out.shape[0] != rows:
+        raise ValueError("as many rows of out as of q expected")
+    n = off.numel() - 1
+    tp, tw = _table(table, n, d)
+    wp, ws_bytes = _workspace(workspace, d)
+    code = _lib.netkv_attn_chunk(
+        pages.ref, dt, qp, qs, heads, n, _ints(off, _I64, n + 1, d), rows, _ints(length, _I32, n, d),
+        tp, tw, dim ** -0.5 if scale is None else scale, op, os_, _plane(lse, rows, heads, d), wp,
+        ws_bytes, _word(status, d), _on_stream(d, stream))
+    if code:
+        raise NetKVError("netkv_attn_chunk", code)
 
 
 def make_weights(w: np.ndarray, theta: float, cap_tokens: int, bytes_per_token: int) -> np.ndarray:
