@@ -1,11 +1,64 @@
-// Causal attention of each sequence's new tokens over its 8-bit KV blocks, in its simplest kernel: a
-// warp has a row and head, and goes through the tokens that the row sees one by one.
-#include "kv_common.cuh"
+// Causal attention of each sequence's new tokens over its 8-bit KV blocks.
+//
+// A KV head serves `group` query heads, so a sequence's new tokens are tokens * group rows for it,
+// token by token, and a row block is 256 of them: two tiles of 128 rows that read the same keys.  Where
+// a row block has 128 rows or fewer, both tiles are the same rows, and take the even and the odd key
+// tiles.  Keys come 128 at a time: eight blocks of 16 tokens.
+//
+// Bound: with 256 rows the tensor cores, 2,048 clocks a key tile at 128 wide for both products; with
+// 128 or fewer HBM, 32 KB of codes a key tile, 1,400 clocks of an SM's share.
+//
+// Split: a line on which every row block has places for the keys that it sees and for its beginning
+// and end is cut into equal runs, one a block of threads, so that single long sequences, ragged
+// batches and long chunks spread over the card alike.  Row blocks that runs share are joined by a
+// second kernel from fp32 sums in the workspace.
+//
+// Roles of a block's warps: one plans (the run's items), one reads table entries and scales ahead and
+// prefetches the pages' codes to L2, four turn codes into fp16 tiles in shared memory, one issues the
+// products, eight take the softmax.
+//
+// Arithmetic: both code types are exact in fp16, so codes go into the products as they are, and the
+// blocks' scales are applied to scores and weights in fp32.  A row of bf16 queries is brought to
+// [2^14, 2^15) by a power of two.  S = Q K^T and O += P V are tcgen05 products with fp32 sums in TMEM;
+// P takes S's place as fp16.  One pass over the keys carries a row's maximum and sum (Milakov and
+// Gimelshein, 2018).
+#include "tensor.cuh"
 
 namespace {
 
-constexpr uint32_t kWarps = 8, kParts = 64;
+constexpr uint32_t kRows = 128, kKeys = 128;  // of a tile
+constexpr uint32_t kTileBlocks = kKeys / kBlockTokens;
+constexpr uint32_t kCtas = 152;  // blocks of the grid, one an SM: they hold all of TMEM
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The running maximum follows the scores once one is above it by this (in powers of two).
+constexpr float kLag = 8.f;
+// Weights go into the second product times their value scale over a unit that is above all value
+// scales so far (at most twice the largest), and times 2^kUp: up to 2^(kLag + kUp), below fp16's
+// 2^16.  They are exact to 2^-11 down to 2^-20 of the largest one, 0 below 2^-31.
+constexpr float kUp = 7.f;
+// Places on the line: a key of a row block with two tiles of rows, of one with one tile, and the
+// beginning and end of a row block.
+constexpr uint64_t kPairKey = 8, kOneKey = 5, kEdge = 1536;
+constexpr uint64_t kLeast = 1280;  // places of a run at least
+// Scores that may be above this (in powers of two) are rounded before the maximum is taken from them,
+// as where some are hidden: a product that is not is off the rounded maximum by 2^-24 of itself.
+constexpr float kFar = 1048576.f;
+// Limits of waits in clocks: two seconds for what is at most a few steps away; what may be a whole
+// item away has ten times what the steps of the longest one take.
+constexpr long long kPatience = 4000000000, kStepClocks = 20000;
+constexpr long long kItemPatience = kPatience + ((1ll << 32) / kKeys) * kStepClocks;
+constexpr uint32_t kSoftmaxWarps = 8, kLoadWarps = 4;
+constexpr uint32_t kThreads = (kSoftmaxWarps + kLoadWarps + 4) * 32;
+constexpr uint32_t kProducts = 12, kPlan = 13, kPages = 14;  // warps, after the softmax's and the loads'
+// Registers: the launch has kThreads * kLaunchRegs, which the warps share out.
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 168, kLoadRegs = 104, kOtherRegs = 72;
+static_assert(256 * kSoftmaxRegs + 128 * kLoadRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs,
+              "register split");
+template <int kDim>
+constexpr uint32_t kStages = kDim == 128 ? 4 : 8;  // tiles in the ring, 32 or 16 KB each
+constexpr uint32_t kBatchTiles = 4, kBatches = 3;  // table entries and scales read ahead
+
+struct Cut;
 
 struct ChunkArgs {
   KvArgs kv;
@@ -16,61 +69,948 @@ struct ChunkArgs {
   const uint32_t* len;
   const int32_t* table;
   uint32_t heads, group, n_seqs, width;
-  float scale;
+  float scale2;  // scale * log2(e)
   float* lse;
+  float* part_o;   // [kCtas][2][kDim / 4][slot_rows][4]
+  float2* part_ml; // [kCtas][2][slot_rows]: a row's maximum and sum
+  Cut* cuts;       // [kCtas]
+  uint32_t slot_rows;
   int* status;
 };
 
-template <int kDim, bool kBf16, bool kE4m3>
-__global__ void __launch_bounds__(kWarps * 32) chunk_kernel(const __grid_constant__ ChunkArgs a) {
-  constexpr int kPer = kDim / 32;  // values of a lane
-  const uint32_t lane = threadIdx.x & 31;
-  for (uint32_t seq = blockIdx.x; seq < a.n_seqs; seq += gridDim.x) {
-    const RowRange r = row_range(a.off, seq, a.rows);
-    const uint64_t most = (uint64_t)a.width * kBlockTokens;
-    const uint64_t tokens = min((uint64_t)a.len[seq], most);
-    if (threadIdx.x == 0 && blockIdx.y == 0 && (r.bad || a.len[seq] > most))
-      flag_status(a.status, NETKV_DEV_ERANGE);
-    for (uint64_t u = blockIdx.y * kWarps + threadIdx.x / 32; u < r.count * a.heads;
-         u += gridDim.y * kWarps) {
-      const uint64_t row = u / a.heads;
-      const uint32_t head = (uint32_t)(u % a.heads), kv_head = head / a.group;
-      const int64_t sees = min((int64_t)tokens, (int64_t)(row + 1 + tokens) - (int64_t)r.count);
-      float q[kPer], o[kPer] = {}, m = -INFINITY, l = 0.f;
-      const uint16_t* from = reinterpret_cast<const uint16_t*>(a.q) +
-                             (r.first + row) * a.q_stride + (uint64_t)head * kDim + lane * kPer;
-      for (int i = 0; i < kPer; ++i) q[i] = unpack16<kBf16>(from[i]).x;
-      for (int64_t t = 0; t < sees; ++t) {
-        const int32_t page = a.table[(uint64_t)seq * a.width + t / kBlockTokens];
-        if (page < 0 || (uint32_t)page >= a.kv.n_pages) {
-          flag_status(a.status, NETKV_DEV_ERANGE);
-          continue;
-        }
-        const uint64_t part = (uint64_t)page * a.kv.heads + kv_head;
-        const uint64_t at = (part * kBlockTokens + t % kBlockTokens) * kDim + lane * kPer;
-        float k[4], v[4], s = 0.f;
-        const uint32_t wk = kPer == 4 ? *reinterpret_cast<const uint32_t*>(a.kv.k + at)
-                                      : *reinterpret_cast<const uint16_t*>(a.kv.k + at);
-        const uint32_t wv = kPer == 4 ? *reinterpret_cast<const uint32_t*>(a.kv.v + at)
-                                      : *reinterpret_cast<const uint16_t*>(a.kv.v + at);
-        decode4<kE4m3>(wk, a.kv.k_scale[part], k);
-        decode4<kE4m3>(wv, a.kv.v_scale[part], v);
-        for (int i = 0; i < kPer; ++i) s += q[i] * k[i];
-        for (int d = 16; d; d /= 2) s += __shfl_xor_sync(~0u, s, d);
-        s *= a.scale;
-        const float top = fmaxf(m, s), to = m == -INFINITY ? 0.f : exp2f((m - top) * kLog2e);
-        const float p = exp2f((s - top) * kLog2e);
-        l = l * to + p;
-        for (int i = 0; i < kPer; ++i) o[i] = o[i] * to + p * v[i];
-        m = top;
-      }
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      uint16_t* to = reinterpret_cast<uint16_t*>(a.out) + (r.first + row) * a.out_stride +
-                     (uint64_t)head * kDim + lane * kPer;
-      for (int i = 0; i < kPer; ++i) to[i] = (uint16_t)pack16<kBf16>(o[i] * inv, 0.f);
-      if (a.lse && lane == 0)
-        a.lse[(r.first + row) * a.heads + head] = l == 0.f ? -INFINITY : m + log2f(l) * kLn2;
+// A wait of a limited time; once one has run out for a thread of the block, nobody waits any longer
+// and the block runs to its end.
+template <long long kLimit = kPatience>
+__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
+  if (try_wait(bar, parity)) return;
+  const long long t0 = clock64();
+  while (!try_wait(bar, parity)) {
+    if (*late) return;
+    if (clock64() - t0 > kLimit) {
+      *late = 1;
+      return;
     }
+  }
+}
+// Whether a thread of the block has given up, by the whole warp: its threads go the same way.
+__device__ __forceinline__ bool given_up(volatile int* late) { return __any_sync(~0u, *late); }
+
+// ---- the line
+// A sequence of the call: its rows and tokens.
+struct Seq {
+  uint64_t first, new_tokens;
+  uint32_t tokens;
+};
+__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, uint32_t i) {
+  const RowRange r = row_range(a.off, i, a.rows);
+  return {r.first, r.count,
+          (uint32_t)min((uint64_t)a.len[i], (uint64_t)a.width * kBlockTokens)};
+}
+// Row blocks of a sequence and KV head, and the places that they take: block b has kEdge and the keys
+// that its last row sees, up to roundings by the group's size; the last one all the sequence's keys.
+struct Shape {
+  uint64_t blocks, before;  // keys before the new tokens
+  uint64_t group, last;     // places of the last row block
+  __device__ __forceinline__ Shape(const Seq& s, uint32_t g) {
+    const uint64_t rows = s.new_tokens * g;
+    group = g;
+    blocks = (rows + 2 * kRows - 1) / (2 * kRows);
+    before = s.tokens > s.new_tokens ? s.tokens - s.new_tokens : 0;
+    const uint64_t rest = rows - (blocks ? blocks - 1 : 0) * (2 * kRows);
+    last = blocks ? kEdge + s.tokens * (rest > kRows ? kPairKey : kOneKey) : 0;
+  }
+  // places before block b < blocks
+  __device__ __forceinline__ uint64_t upto(uint64_t b) const {
+    return b * kEdge + kPairKey * (b * before + kRows * b * (b + 1) / group);
+  }
+  __device__ __forceinline__ uint64_t all() const { return blocks ? upto(blocks - 1) + last : 0; }
+  __device__ __forceinline__ uint64_t of(uint64_t b) const {
+    return b + 1 == blocks ? last : upto(b + 1) - upto(b);
+  }
+};
+
+// Equal parts of the line.
+struct Runs {
+  uint64_t total, base;
+  uint32_t count, rest;
+  __device__ __forceinline__ explicit Runs(uint64_t t) {
+    total = t;
+    count = (uint32_t)max((uint64_t)1, min((uint64_t)kCtas, t / kLeast));
+    base = t / count;
+    rest = (uint32_t)(t - base * count);
+  }
+  __device__ __forceinline__ uint64_t start(uint32_t c) const { return base * c + min(c, rest); }
+  // the run that has place p < total
+  __device__ __forceinline__ uint32_t at(uint64_t p) const {
+    const uint64_t longer = (base + 1) * rest;
+    return p < longer ? (uint32_t)(p / (base + 1)) : rest + (uint32_t)((p - longer) / base);
+  }
+};
+
+// What a block works on: key tiles [first, first + steps) of a row block.
+struct Item {
+  uint64_t row;       // of queries: the row block's first token
+  int64_t sees;       // tokens that the first token sees; each later one sees one more
+  uint32_t seq, kv_head;
+  uint32_t lead;      // heads of the first token that are another row block's
+  uint32_t rows;      // 1 .. 256
+  uint32_t tokens;    // of the sequence
+  uint32_t first, steps;
+  int32_t slot;       // of the workspace; -1: the row block is all this item's
+  int32_t valid;      // 0: no more items
+};
+
+// A run's beginning inside a row block, for the join: it has parts of the runs run0, run0 + 1, ...; of
+// run0 it is the first row block (second = 0) or a later one; `order` numbers its cuts.
+struct Cut {
+  uint64_t row;
+  uint32_t kv_head, lead, rows;
+  uint32_t parts, run0, second, order;
+};
+
+// A block's eight pages and scales for each of a batch of key tiles.
+struct Batch {
+  int32_t page[kBatchTiles * kTileBlocks];  // -1: absent
+  alignas(16) float k_scale[kBatchTiles * kTileBlocks], v_scale[kBatchTiles * kTileBlocks];
+  uint32_t absent;  // a bit each
+};
+
+template <int kDim>
+struct Shared {
+  alignas(1024) unsigned char q[2][kRows * kDim * 2];
+  alignas(1024) unsigned char kv[kStages<kDim>][kKeys * kDim * 2];
+  alignas(16) Batch batch[kBatches];
+  alignas(8) uint64_t q_full[2], kv_full[kStages<kDim>], kv_empty[kStages<kDim>];
+  uint64_t s_full[2], p_full[2][2], o_full[2];  // p: the two halves of the keys
+  uint64_t item_full[2], item_empty[2], batch_full[kBatches], batch_empty[kBatches], met;
+  Item item[2];
+  float stat[2][3][kRows];  // one tile of rows: both tiles' maxima, sums and units
+  uint64_t sums[kThreads / 32];
+  uint32_t tmem;
+  int late;
+};
+
+// The items of a block, as its warps read them: two places, filled by the planning warp.
+struct Items {
+  uint32_t n = 0;
+  template <class Sh>
+  __device__ __forceinline__ Item next(Sh& sh, volatile int* late) {
+    const uint32_t at = n % 2;
+    wait<kItemPatience>(smem_addr(&sh.item_full[at]), n / 2 & 1, late);
+    Item x = sh.item[at];
+    ++n;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.item_empty[at]));
+    if (given_up(late)) x.valid = 0;
+    return x;
+  }
+};
+
+// A warp's view of the batches: those it has seen filled, and those it has given back.
+struct Batches {
+  uint32_t seen = 0, given = 0, base = 0;
+  template <class Sh>
+  __device__ __forceinline__ void see(Sh& sh, uint32_t upto, volatile int* late) {
+    for (; seen < upto; ++seen)
+      wait(smem_addr(&sh.batch_full[seen % kBatches]), seen / kBatches & 1, late);
+  }
+  template <class Sh>
+  __device__ __forceinline__ const Batch& get(Sh& sh, uint32_t tile, volatile int* late) {
+    see(sh, base + tile / kBatchTiles + 1, late);
+    return sh.batch[(base + tile / kBatchTiles) % kBatches];
+  }
+  // back to the pages' warp: what comes before tile `next` of n
+  template <class Sh>
+  __device__ __forceinline__ void give(Sh& sh, uint32_t next, uint32_t n, volatile int* late) {
+    const uint32_t upto = base + (next < n ? next / kBatchTiles : (n + kBatchTiles - 1) / kBatchTiles);
+    if (given == upto) return;
+    see(sh, upto, late);
+    __syncwarp();
+    for (; given < upto; ++given)
+      if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.batch_empty[given % kBatches]));
+  }
+  __device__ __forceinline__ void end(uint32_t n) { base += (n + kBatchTiles - 1) / kBatchTiles; }
+};
+
+__device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
+  return (uint64_t)__shfl_sync(~0u, (uint32_t)(x >> 32), from) << 32 |
+         __shfl_sync(~0u, (uint32_t)x, from);
+}
+
+// ---- the planning warp: the run's items one after another
+template <class Sh>
+__device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, volatile int* late) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint64_t total = 0;
+  for (uint32_t w = 0; w < kThreads / 32; ++w) total += sh.sums[w];
+  const Runs runs(total);
+  const uint32_t run = blockIdx.x;
+  uint64_t at = total ? runs.start(min(run, runs.count)) : 0;
+  const uint64_t end = total && run < runs.count ? runs.start(run + 1) : at;
+  if (lane == 0) a.cuts[run].parts = 0;
+  // a window of 32 sequences, a lane each
+  uint32_t base = 0, seq = 0;
+  Seq mine = {0, 0, 0};
+  auto window = [&](uint32_t from) {
+    base = from;
+    mine = from + lane < a.n_seqs ? seq_of(a, from + lane) : Seq{0, 0, 0};
+  };
+  auto pick = [&](uint32_t i) -> Seq {
+    const int j = (int)(i - base);
+    return {shfl64(mine.first, j), shfl64(mine.new_tokens, j), __shfl_sync(~0u, mine.tokens, j)};
+  };
+  uint32_t n = 0;
+  auto publish = [&](const Item& x) {
+    if (n >= 2) wait<kItemPatience>(smem_addr(&sh.item_empty[n % 2]), (n / 2 - 1) & 1, late);
+    if (lane == 0) {
+      sh.item[n % 2] = x;
+      bar_arrive(smem_addr(&sh.item_full[n % 2]));
+    }
+    __syncwarp();
+    ++n;
+  };
+  Item x = {};
+  // the sequence that has place `at`
+  uint64_t before = 0, into = 0;
+  bool found = false;
+  if (at < end) {
+    for (uint32_t from = 0; from < a.n_seqs; from += 32) {
+      window(from);
+      const uint64_t c = Shape(mine, a.group).all() * a.kv.heads;
+      uint64_t upto = c;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint64_t y = (uint64_t)__shfl_up_sync(~0u, (uint32_t)(upto >> 32), d) << 32 |
+                           __shfl_up_sync(~0u, (uint32_t)upto, d);
+        if (lane >= (uint32_t)d) upto += y;
+      }
+      const uint32_t hit = __ballot_sync(~0u, at < before + upto);
+      if (hit) {
+        const int who = __ffs(hit) - 1;
+        seq = from + who;
+        into = at - before - shfl64(upto - c, who);
+        found = true;
+        break;
+      }
+      before += shfl64(upto, 31);
+    }
+  }
+  if (found) {  // (not with lengths that change under the call)
+    Seq s = pick(seq);
+    Shape shape(s, a.group);
+    uint32_t kv_head = 0;
+    uint64_t b = 0;
+    {
+      const uint64_t all = shape.all();
+      kv_head = (uint32_t)(into / all);
+      into -= kv_head * all;
+      b = shape.blocks - 1;
+      if (into < shape.upto(b)) {
+        uint64_t lo = 0, hi = b;  // upto(lo) <= into < upto(hi)
+        while (hi - lo > 1) {
+          const uint64_t mid = (lo + hi) / 2;
+          if (shape.upto(mid) <= into) lo = mid;
+          else hi = mid;
+        }
+        b = lo;
+      }
+      into -= shape.upto(b);
+    }
+    bool first = true;
+    while (at < end && !given_up(late)) {
+      const uint64_t places = shape.of(b), upto = min(places, into + (end - at));
+      const uint64_t row0 = b * (2 * kRows);
+      x.rows = (uint32_t)min((uint64_t)(2 * kRows), s.new_tokens * a.group - row0);
+      x.lead = (uint32_t)(row0 % a.group);
+      const uint64_t token = row0 / a.group;
+      x.row = s.first + token;
+      x.sees = (int64_t)s.tokens - (int64_t)s.new_tokens + (int64_t)token + 1;
+      x.seq = seq;
+      x.kv_head = kv_head;
+      x.tokens = s.tokens;
+      const int64_t most = x.sees + (x.lead + x.rows - 1) / a.group;  // of the last row
+      const uint64_t tiles = most > 0 ? ((uint64_t)most + kKeys - 1) / kKeys : 0;
+      auto step = [&](uint64_t p) {
+        return p <= kEdge || places <= kEdge ? p == places ? tiles : 0
+                                             : (p - kEdge) * tiles / (places - kEdge);
+      };
+      x.first = (uint32_t)step(into);
+      x.steps = (uint32_t)step(upto) - x.first;
+      const bool whole = into == 0 && upto == places;
+      x.slot = whole ? -1 : (int32_t)(run * 2 + (first ? 0 : 1));
+      x.valid = 1;
+      if (into && lane == 0) {
+        const uint64_t begin = at - into;
+        const uint32_t run0 = runs.at(begin);
+        a.cuts[run] = {x.row, kv_head, x.lead, x.rows, runs.at(begin + places - 1) - run0 + 1, run0,
+                       runs.start(run0) < begin, run - run0 - 1};
+      }
+      publish(x);
+      first = false;
+      at += upto - into;
+      into = 0;
+      if (++b < shape.blocks) continue;
+      b = 0;
+      if (++kv_head < a.kv.heads) continue;
+      kv_head = 0;
+      do {
+        if (++seq >= a.n_seqs) break;
+        if (seq >= base + 32) window(seq);
+        s = pick(seq);
+        shape = Shape(s, a.group);
+      } while (shape.blocks == 0);
+      if (seq >= a.n_seqs) break;
+    }
+  }
+  x.valid = 0;
+  publish(x);
+}
+
+// ---- the pages' warp: table entries and scales, a batch of key tiles at a time, a lane each block
+template <int kDim, class Sh>
+__device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, volatile int* late) {
+  const uint32_t lane = threadIdx.x & 31;
+  Items items;
+  uint32_t n = 0;
+  while (true) {
+    const Item x = items.next(sh, late);
+    if (!x.valid) break;
+    const uint32_t blocks = (x.tokens + kBlockTokens - 1) / kBlockTokens;
+    const uint32_t end = min((x.first + x.steps) * kTileBlocks, blocks);
+    auto entry = [&](uint32_t from) {
+      const uint32_t block = from + lane;
+      return block < end ? a.table[(uint64_t)x.seq * a.width + block] : -1;
+    };
+    uint32_t from = x.first * kTileBlocks;
+    int32_t next = entry(from);
+    for (uint32_t i = 0; i < (x.steps + kBatchTiles - 1) / kBatchTiles; ++i, ++n) {
+      int32_t page = next;
+      const bool in = from + lane < end;
+      next = entry(from + 32);
+      const bool there = page >= 0 && (uint32_t)page < a.kv.n_pages;
+      if (in && !there) flag_status(a.status, NETKV_DEV_ERANGE);
+      float2 scale = make_float2(0.f, 0.f);
+      if (there) {
+        const uint64_t part = (uint64_t)page * a.kv.heads + x.kv_head;
+        const uint64_t at = part * (kBlockTokens * kDim);
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.k + at),
+                     "n"(kBlockTokens * kDim)
+                     : "memory");
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.v + at),
+                     "n"(kBlockTokens * kDim)
+                     : "memory");
+        scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
+      } else {
+        page = -1;
+      }
+      Batch& to = sh.batch[n % kBatches];
+      if (n >= kBatches)
+        wait(smem_addr(&sh.batch_empty[n % kBatches]), (n / kBatches - 1) & 1, late);
+      to.page[lane] = page;
+      to.k_scale[lane] = scale.x;
+      to.v_scale[lane] = scale.y;
+      const uint32_t absent = __ballot_sync(~0u, !there);
+      if (lane == 0) to.absent = absent;
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&sh.batch_full[n % kBatches]));
+      if (given_up(late)) break;
+      from += 32;
+    }
+  }
+}
+
+// ---- the loading warps: codes of two of a key tile's blocks each, to fp16 in the ring.  A lane has 16
+// codes of a row at a time, 4 lanes 64 of them, so that 8 lanes' stores of 16 bytes are in all banks.
+template <int kDim, bool kE4m3, class Sh>
+__device__ __forceinline__ void load_tiles(const ChunkArgs& a, Sh& sh, volatile int* late) {
+  constexpr uint32_t kRing = kStages<kDim>, kLoads = 2 * kDim / 32, kBox = kKeys * 128;
+  constexpr uint32_t kHalves = kDim / 64;
+  const uint32_t lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftmaxWarps;
+  Items items;
+  Batches batches;
+  uint32_t n = 0;  // tiles of the ring
+  while (true) {
+    const Item x = items.next(sh, late);
+    if (!x.valid) break;
+    const bool one = x.rows <= kRows;
+    // the n-th piece in the order in which the products want them: of two tiles of rows K 0, V 0, K 1,
+    // V 1, ...; of one K 0, K 1, V 0, K 2, V 1, ...
+    const uint32_t pieces = 2 * x.steps;
+    auto tile_of = [&](uint32_t p, bool* values) -> uint32_t {
+      if (!one) {
+        *values = p & 1;
+        return p / 2;
+      }
+      if (p == 0 || p + 1 == pieces) {
+        *values = p != 0;
+        return p ? x.steps - 1 : 0;
+      }
+      *values = !(p & 1);
+      return p & 1 ? (p + 1) / 2 : p / 2 - 1;
+    };
+    uint4 c[2][kLoads];
+    auto load = [&](uint32_t p, uint4* to) {
+      bool values;
+      const uint32_t tile = tile_of(p, &values);
+      const Batch& batch = batches.get(sh, tile, late);
+      const uint32_t block = tile % kBatchTiles * kTileBlocks + 2 * w;
+      const unsigned char* codes = values ? a.kv.v : a.kv.k;
+      const uint32_t key0 = (x.first + tile) * kKeys + w * 32;
+#pragma unroll
+      for (uint32_t z = 0; z < 2; ++z) {
+        const int32_t page = batch.page[block + z];
+        const unsigned char* from =
+            codes + ((uint64_t)max(page, 0) * a.kv.heads + x.kv_head) * (kBlockTokens * kDim);
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads / 2; ++i) {
+          const uint32_t row = i / kHalves * 8 + lane / 4, half = i % kHalves;
+          // past the sequence's end are others' codes, and weights of 0 would not hide a NaN
+          const bool in = page >= 0 && key0 + z * kBlockTokens + row < x.tokens;
+          to[z * (kLoads / 2) + i] =
+              in ? __ldcg(reinterpret_cast<const uint4*>(from + row * kDim + half * 64 + lane % 4 * 16))
+                 : make_uint4(0, 0, 0, 0);
+        }
+      }
+      if (values) batches.give(sh, tile + 1, x.steps, late);
+    };
+    auto store = [&](const uint4* from) {
+      const uint32_t st = n % kRing;
+      if (n >= kRing) wait(smem_addr(&sh.kv_empty[st]), (n / kRing - 1) & 1, late);
+      ++n;
+      if (given_up(late)) return;
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t y = i % (kLoads / 2);
+        const uint32_t row = w * 32 + i / (kLoads / 2) * kBlockTokens + y / kHalves * 8 + lane / 4;
+        unsigned char* to = sh.kv[st] + y % kHalves * kBox + row * 128;
+        uint32_t h[8];
+        widen<kE4m3>(from[i].x, &h[0], &h[1]);
+        widen<kE4m3>(from[i].y, &h[2], &h[3]);
+        widen<kE4m3>(from[i].z, &h[4], &h[5]);
+        widen<kE4m3>(from[i].w, &h[6], &h[7]);
+        const uint32_t at = lane % 4 * 2;
+        *reinterpret_cast<uint4*>(to + ((at ^ (row & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(to + (((at + 1) ^ (row & 7)) * 16)) = make_uint4(h[4], h[5], h[6], h[7]);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&sh.kv_full[st]));
+    };
+    // a piece's loads are under way while the one before is stored
+    if (pieces) load(0, c[0]);
+    for (uint32_t p = 0; p < pieces && !given_up(late); p += 2) {
+      load(p + 1, c[1]);
+      store(c[0]);
+      if (p + 2 < pieces) load(p + 2, c[0]);
+      store(c[1]);
+    }
+    batches.end(x.steps);
+  }
+}
+
+// ---- the products
+template <int kDim, class Sh>
+__device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
+  constexpr uint32_t kRing = kStages<kDim>, kBox = 128 * 128, kS = 0, kO = 256;
+  constexpr uint32_t kScores = product(false, false, kKeys), kSums = product(false, true, kDim);
+  constexpr uint32_t kTile = kRows * kDim * 2 >> 4;  // of operands' addresses
+  const bool leader = elect();
+  const uint64_t q0 = operand(smem_addr(sh.q[0]), 16), k0 = operand(smem_addr(sh.kv[0]), 16),
+                 v0 = operand(smem_addr(sh.kv[0]), kBox);
+  auto scores = [&](uint32_t t, uint32_t st) {  // S_t from the ring's place st
+    if (leader) {
+#pragma unroll
+      for (int x = 0; x < kDim / 16; ++x) {
+        const uint32_t off = (x / 4 * kBox + x % 4 * 32) >> 4;
+        mma_smem(kS + t * 128, q0 + t * kTile + off, k0 + st * kTile + off, kScores, x > 0);
+      }
+      commit(smem_addr(&sh.s_full[t]));
+    }
+    __syncwarp();
+  };
+  auto sums = [&](uint32_t t, uint32_t st, uint32_t half, bool add) {
+    if (leader) {
+#pragma unroll
+      for (uint32_t x = 0; x < kKeys / 32; ++x)
+        mma_tmem(kO + t * kDim, kS + t * 128 + half * 64 + x * 8,
+                 v0 + st * kTile + (half * (kKeys / 32) + x) * (2048 >> 4), kSums, add || x > 0);
+    }
+    __syncwarp();
+  };
+  auto signal = [&](uint64_t* bar) {
+    if (leader) commit(smem_addr(bar));
+    __syncwarp();
+  };
+  uint32_t i = 0, with_q = 0, done0 = 0, done1 = 0;  // tiles of the ring, items, steps
+  auto arrived = [&](uint32_t n) {
+    wait(smem_addr(&sh.kv_full[n % kRing]), (n / kRing) & 1, late);
+    after_sync();
+  };
+  auto take = [&](uint32_t t, uint32_t v, bool add) {  // P_t V from the ring's place v
+    const uint32_t parity = (t ? done1++ : done0++) & 1;
+    wait(smem_addr(&sh.p_full[t][1]), parity, late);
+    after_sync();
+    sums(t, v, 1, add);
+    wait(smem_addr(&sh.p_full[t][0]), parity, late);
+    after_sync();
+    sums(t, v, 0, true);
+  };
+  Items items;
+  while (true) {
+    const Item x = items.next(sh, late);
+    if (!x.valid) break;
+    if (x.steps == 0) continue;
+    const uint32_t n = x.steps;
+    wait(smem_addr(&sh.q_full[0]), with_q & 1, late);
+    wait(smem_addr(&sh.q_full[1]), with_q & 1, late);
+    ++with_q;
+    after_sync();
+    arrived(i);
+    scores(0, i % kRing);
+    if (x.rows <= kRows) {  // the even and the odd key tiles of one tile of rows
+      signal(&sh.kv_empty[i++ % kRing]);
+      if (n > 1) {
+        arrived(i);
+        scores(1, i % kRing);
+        signal(&sh.kv_empty[i++ % kRing]);
+      }
+      for (uint32_t j = 0; j < n; j += 2) {
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t) {
+          if (j + t >= n) continue;
+          arrived(i);
+          take(t, i % kRing, j > 0);
+          const bool more = j + t + 2 < n;
+          if (!more) signal(&sh.o_full[t]);
+          signal(&sh.kv_empty[i++ % kRing]);
+          if (more) {
+            arrived(i);
+            scores(t, i % kRing);
+            signal(&sh.kv_empty[i++ % kRing]);
+          }
+        }
+      }
+      continue;
+    }
+    scores(1, i % kRing);
+    signal(&sh.kv_empty[i++ % kRing]);
+    for (uint32_t j = 0; j < n; ++j) {
+      const uint32_t v = i++ % kRing, k = i % kRing;
+      const bool more = j + 1 < n;
+      arrived(i - 1);
+      if (more) arrived(i);
+#pragma unroll
+      for (uint32_t t = 0; t < 2; ++t) {
+        take(t, v, j > 0);
+        if (more) scores(t, k);
+        else signal(&sh.o_full[t]);
+      }
+      signal(&sh.kv_empty[v]);
+      if (more) {
+        signal(&sh.kv_empty[k]);
+        ++i;
+      }
+    }
+  }
+  // the last signals have to reach a block that is still there
+  if (i >= 1) wait(smem_addr(&sh.kv_empty[(i - 1) % kRing]), ((i - 1) / kRing) & 1, late);
+  if (i >= 2) wait(smem_addr(&sh.kv_empty[(i - 2) % kRing]), ((i - 2) / kRing) & 1, late);
+}
+
+// ---- softmax: a thread has a row of its tile
+template <int kDim, bool kBf16, bool kE4m3, class Sh>
+__device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int* late) {
+  constexpr uint32_t kS = 0, kO = 256, kBox = 128 * 128;
+  constexpr float kTop = kE4m3 ? 448.f : 128.f;  // of the codes
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid / 32, 0);
+  const uint32_t t = warp / 4, row = tid % kRows, lanes = (warp % 4) * 32 << 16;
+  const uint32_t s_at = kS + t * 128 + lanes, o_at = kO + t * kDim + lanes;
+  Items items;
+  Batches batches;
+  uint32_t taken = 0, finished0 = 0, finished1 = 0, meetings = 0;  // steps; items of each tile; meetings
+  auto meet = [&]() {
+    __syncwarp();
+    if (lane == 0) bar_arrive(smem_addr(&sh.met));
+    wait(smem_addr(&sh.met), meetings++ & 1, late);
+    __syncwarp();
+  };
+  while (true) {
+    const Item x = items.next(sh, late);
+    if (!x.valid) break;
+    const bool one = x.rows <= kRows;
+    const uint32_t mine = (one ? 0 : t * kRows) + row;  // the thread's row of the row block
+    const bool real = mine < x.rows;
+    const bool busy = __any_sync(~0u, real);
+    const uint32_t token = (x.lead + mine) / a.group, head = x.kv_head * a.group + (x.lead + mine) % a.group;
+    float by = 0.f;  // what brings a sum of products to a score in powers of two, but for the scales
+    float reach = 0.f;  // no score is above this times the scales
+    if (x.steps) {
+      // the row's queries as fp16, 16 bytes of row r in place (c ^ r) of 8
+      if (busy) {
+        const uint4* from = reinterpret_cast<const uint4*>(
+            a.q + ((x.row + token) * a.q_stride + (uint64_t)head * kDim) * 2);
+        uint4 v[kDim / 8];
+#pragma unroll
+        for (int i = 0; i < kDim / 8; ++i) v[i] = real ? __ldcs(from + i) : make_uint4(0, 0, 0, 0);
+        by = a.scale2;
+        float largest = 0.f;
+#pragma unroll
+        for (int i = 0; i < kDim / 8; ++i) {
+          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = unpack16<kBf16>(w[j]);
+            largest = max3(largest, fabsf(y.x), fabsf(y.y));
+          }
+        }
+        // (rows of infinities are not others' concern)
+        reach = largest <= 3.4028235e38f ? largest * by * (kDim * kTop) : 0.f;
+        if constexpr (kBf16) {
+          // 2^14 over the largest value's power of two, and the reverse; both are normal numbers
+          const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);
+          const float inv = __uint_as_float((254 + 14 - e) << 23);
+          by *= __uint_as_float((e - 14) << 23);
+#pragma unroll
+          for (int i = 0; i < kDim / 8; ++i) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 y = unpack16<true>(w[j]);
+              w[j] = pack16<false>(y.x * inv, y.y * inv);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kDim / 8; ++i)
+          *reinterpret_cast<uint4*>(sh.q[t] + i / 8 * kBox + row * 128 + ((i % 8) ^ (row & 7)) * 16) = v[i];
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(smem_addr(&sh.q_full[t]));
+    }
+    // tokens that this row sees
+    const int64_t sees = real ? x.sees + token : x.tokens;
+    const uint32_t stride = one ? 2 : 1, own0 = one ? t : 0;
+    float m = -INFINITY, l = 0.f;
+    uint32_t unit = 1;  // the exponent of what value scales are taken over
+    bool any = false;
+    for (uint32_t j = own0; j < x.steps; j += stride) {
+      wait(smem_addr(&sh.s_full[t]), taken++ & 1, late);
+      after_sync();
+      if (busy) {
+        const Batch& batch = batches.get(sh, j, late);
+        const uint32_t b0 = j % kBatchTiles * kTileBlocks;
+        float k[kTileBlocks], v[kTileBlocks];
+        *reinterpret_cast<float4*>(k) = *reinterpret_cast<const float4*>(batch.k_scale + b0);
+        *reinterpret_cast<float4*>(k + 4) = *reinterpret_cast<const float4*>(batch.k_scale + b0 + 4);
+        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(batch.v_scale + b0);
+        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(batch.v_scale + b0 + 4);
+        const uint32_t absent = batch.absent >> b0 & 0xff;
+        const int seen = (int)max((int64_t)0, min((int64_t)kKeys, sees - (int64_t)(x.first + j) * kKeys));
+        float most = 0.f, most_k = 0.f;
+#pragma unroll
+        for (uint32_t b = 0; b < kTileBlocks; b += 2) {
+          most_k = max3(most_k, k[b], k[b + 1]);
+          most = max3(most, v[b], v[b + 1]);
+        }
+        const bool masked = __any_sync(~0u, seen < (int)kKeys || reach * most_k > kFar) || absent;
+#pragma unroll
+        for (uint32_t b = 0; b < kTileBlocks; ++b) k[b] *= by;
+        float s[64];
+        float f[kTileBlocks];  // what scores are multiplied by, where fetch() has not done so
+#pragma unroll
+        for (uint32_t b = 0; b < kTileBlocks; ++b) f[b] = masked ? 1.f : k[b];
+        auto fetch = [&](uint32_t h) {  // the scores of half the keys
+          tmem_load(s_at + h * 64, s);
+          tmem_load(s_at + h * 64 + 32, s + 32);
+          tmem_loaded();
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i) {
+              const int key = (int)h * 64 + i;
+              s[i] = key < seen && !(absent >> (key / 16) & 1) ? s[i] * k[key / 16] : -INFINITY;
+            }
+          }
+        };
+        float top = m;
+        auto tops = [&](uint32_t h) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            float y = s[b * 16];
+#pragma unroll
+            for (int i = 1; i + 1 < 16; i += 2) y = max3(y, s[b * 16 + i], s[b * 16 + i + 1]);
+            y = fmaxf(y, s[b * 16 + 15]);
+            top = fmaxf(top, y * f[h * 4 + b]);
+          }
+        };
+        fetch(0);
+        tops(0);
+        fetch(1);
+        tops(1);
+        const uint32_t above = min((__float_as_uint(most) >> 23 & 0xff) + 1, 253u);
+        const bool grown = above > unit;  // alike for all rows
+        const bool follow = top - m > kLag;  // also the first maximum
+        if (grown || __any_sync(~0u, follow)) {
+          float to = 1.f;
+          if (follow) {
+            to = m == -INFINITY ? 0.f : ex2(m - top);
+            m = top;
+          }
+          __syncwarp();
+          l *= to;
+          if (grown) {
+            to *= any ? __uint_as_float(127 + unit > above ? (127 + unit - above) << 23 : 0) : 0.f;
+            unit = above;
+          }
+          if (any) {  // S_t is complete, and so is P_t V before it
+#pragma unroll
+            for (int i = 0; i < kDim / 16; ++i) {
+              float o[16];
+              tmem_load16(o_at + i * 16, o);
+              tmem_loaded();
+#pragma unroll
+              for (int z = 0; z < 16; ++z) o[z] *= to;
+              tmem_store16(o_at + i * 16, reinterpret_cast<const uint32_t*>(o));
+            }
+          }
+        }
+        any = true;
+        const float base = m == -INFINITY ? 0.f : kUp - m;
+        const float over = __uint_as_float((254 - unit) << 23);
+        const uint64_t base_2 = pair(base, base);
+        uint64_t sums_2[2] = {0, 0};
+        auto weigh = [&](uint32_t h) {
+          uint32_t p[32];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const float g = v[h * 4 + b] * over;
+            const uint64_t f_2 = pair(f[h * 4 + b], f[h * 4 + b]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float u, w;
+              split(fma2(pair(s[b * 16 + 2 * i], s[b * 16 + 2 * i + 1]), f_2, base_2), &u, &w);
+              u = ex2(u);
+              w = ex2(w);
+              sums_2[i & 1] = add2(sums_2[i & 1], pair(u, w));
+              p[b * 8 + i] = pack16<false>(u * g, w * g);
+            }
+          }
+          tmem_store(s_at + h * 64, p);
+          tmem_stored();
+          before_sync();
+          bar_arrive(smem_addr(&sh.p_full[t][h]));
+        };
+        weigh(1);
+        fetch(0);
+        weigh(0);
+        float u, w;
+        split(add2(sums_2[0], sums_2[1]), &u, &w);
+        l += u + w;
+      } else {
+        before_sync();
+        bar_arrive(smem_addr(&sh.p_full[t][1]));
+        bar_arrive(smem_addr(&sh.p_full[t][0]));
+      }
+      batches.give(sh, j + stride, x.steps, late);
+      if (given_up(late)) break;
+    }
+    batches.give(sh, x.steps, x.steps, late);
+    batches.end(x.steps);
+
+    // ---- the row's output, or its part
+    const float made = __uint_as_float(unit << 23);
+    float w0 = 1.f, w1 = 0.f;  // what the two tiles' sums are multiplied by
+    if (one) {
+      const bool has0 = x.steps > 0, has1 = x.steps > 1;
+      if (t == 0 && has0) wait(smem_addr(&sh.o_full[0]), finished0 & 1, late);
+      if (t == 1 && has1) wait(smem_addr(&sh.o_full[1]), finished1 & 1, late);
+      finished0 += has0;
+      finished1 += has1;
+      sh.stat[t][0][row] = m;
+      sh.stat[t][1][row] = l;
+      sh.stat[t][2][row] = made;
+      meet();
+      after_sync();
+      const float m0 = sh.stat[0][0][row], m1 = sh.stat[1][0][row];
+      m = fmaxf(m0, m1);
+      w0 = m0 == -INFINITY ? 0.f : ex2(m0 - m);
+      w1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
+      // (a tile of NaN scores has no maximum, but its sum says so)
+      l = w0 * sh.stat[0][1][row] + w1 * sh.stat[1][1][row];
+      w0 *= sh.stat[0][2][row];
+      w1 *= sh.stat[1][2][row];
+    } else if (x.steps) {
+      wait(smem_addr(&sh.o_full[t]), (t ? finished1 : finished0) & 1, late);
+      ++finished0;
+      ++finished1;
+      after_sync();
+      w0 = made;
+    }
+    if (busy) {
+      const float inv = l == 0.f || x.slot >= 0 ? 1.f : 1.f / l;
+      const bool none = l == 0.f;  // NaN is not
+      w0 *= inv;
+      w1 *= inv;
+      // of one tile of rows each tile's warps write half the columns
+      constexpr int kCols = 16;
+      const uint32_t c0 = one ? t * (kDim / 2) : 0, c1 = one ? c0 + kDim / 2 : kDim;
+      for (uint32_t c = c0; c < c1; c += kCols) {
+        float o[kCols] = {}, y[kCols];
+        if (x.steps) {
+          tmem_load16(kO + lanes + (one ? 0 : t * kDim) + c, o);
+          tmem_loaded();
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) o[i] = none ? 0.f : o[i] * w0;
+        }
+        if (one && x.steps > 1) {
+          tmem_load16(kO + lanes + kDim + c, y);
+          tmem_loaded();
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) o[i] += none ? 0.f : y[i] * w1;
+        }
+        if (!real) {
+        } else if (x.slot >= 0) {
+          float4* to = reinterpret_cast<float4*>(a.part_o) +
+                       ((uint64_t)x.slot * (kDim / 4) + c / 4) * a.slot_rows + mine;
+#pragma unroll
+          for (int i = 0; i < kCols / 4; ++i)
+            to[i * a.slot_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+          uint4* to = reinterpret_cast<uint4*>(
+              a.out + ((x.row + token) * a.out_stride + (uint64_t)head * kDim + c) * 2);
+#pragma unroll
+          for (int i = 0; i < kCols / 8; ++i)
+            to[i] = make_uint4(pack16<kBf16>(o[8 * i], o[8 * i + 1]), pack16<kBf16>(o[8 * i + 2], o[8 * i + 3]),
+                               pack16<kBf16>(o[8 * i + 4], o[8 * i + 5]),
+                               pack16<kBf16>(o[8 * i + 6], o[8 * i + 7]));
+        }
+        __syncwarp();
+      }
+      if (real && !(one && t)) {
+        if (x.slot >= 0)
+          a.part_ml[(uint64_t)x.slot * a.slot_rows + mine] = make_float2(m, l);
+        else if (a.lse)
+          a.lse[(x.row + token) * a.heads + head] = none ? -INFINITY : (m - kUp) * kLn2 + logf(l);
+      }
+      __syncwarp();
+    }
+    before_sync();
+    if (one) meet();  // both tiles' sums have been read
+  }
+}
+
+template <int kDim, bool kBf16, bool kE4m3>
+__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  Shared<kDim>& sh = *reinterpret_cast<Shared<kDim>*>(smem);
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid / 32, 0);
+  volatile int* late = &sh.late;
+  if (warp == 0) {
+    if (lane == 0) {
+      sh.late = 0;
+      for (uint32_t i = 0; i < kStages<kDim>; ++i) {
+        bar_init(smem_addr(&sh.kv_full[i]), kLoadWarps);
+        bar_init(smem_addr(&sh.kv_empty[i]), 1);
+      }
+      for (uint32_t i = 0; i < kBatches; ++i) {
+        bar_init(smem_addr(&sh.batch_full[i]), 1);
+        bar_init(smem_addr(&sh.batch_empty[i]), kSoftmaxWarps + kLoadWarps);
+      }
+      for (int t = 0; t < 2; ++t) {
+        bar_init(smem_addr(&sh.q_full[t]), kRows);
+        bar_init(smem_addr(&sh.s_full[t]), 1);
+        bar_init(smem_addr(&sh.p_full[t][0]), kRows);
+        bar_init(smem_addr(&sh.p_full[t][1]), kRows);
+        bar_init(smem_addr(&sh.o_full[t]), 1);
+        bar_init(smem_addr(&sh.item_full[t]), 1);
+        bar_init(smem_addr(&sh.item_empty[t]), kSoftmaxWarps + kLoadWarps + 2);
+      }
+      bar_init(smem_addr(&sh.met), kSoftmaxWarps);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+                     smem_addr(&sh.tmem))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    before_sync();
+  }
+  // the line's length, and what is wrong with the sequences, said by the first block
+  uint64_t sum = 0;
+  for (uint32_t i = tid; i < a.n_seqs; i += kThreads) {
+    sum += Shape(seq_of(a, i), a.group).all();
+    if (blockIdx.x == 0 && (row_range(a.off, i, a.rows).bad ||
+                            a.len[i] > (uint64_t)a.width * kBlockTokens))
+      flag_status(a.status, NETKV_DEV_ERANGE);
+  }
+  sum *= a.kv.heads;
+#pragma unroll
+  for (int d = 16; d; d /= 2)
+    sum += (uint64_t)__shfl_xor_sync(~0u, (uint32_t)(sum >> 32), d) << 32 |
+           __shfl_xor_sync(~0u, (uint32_t)sum, d);
+  if (lane == 0) sh.sums[warp] = sum;
+  __syncthreads();
+  after_sync();
+  if (warp >= kProducts) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kProducts) multiply<kDim>(sh, late);
+    else if (warp == kPlan) plan(a, sh, late);
+    else if (warp == kPages) read_pages<kDim>(a, sh, late);
+  } else if (warp >= kSoftmaxWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
+    load_tiles<kDim, kE4m3>(a, sh, late);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    softmax<kDim, kBf16, kE4m3>(a, sh, late);
+  }
+  __syncthreads();
+  if (warp == 0) {
+    if (*late) {  // what is still in flight gets a moment to end
+      const long long t0 = clock64();
+      while (clock64() - t0 < 20000000ll) {
+      }
+    }
+    __syncwarp();
+    after_sync();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem) : "memory");
+    if (lane == 0 && *late) flag_status(a.status, NETKV_DEV_ETIMEOUT);
+  }
+}
+
+// Joins the row blocks that runs share: a run's beginning inside one has blocks of threads for a share
+// of its rows, a thread each row and 4 columns.
+constexpr uint32_t kJoinThreads = 256, kJoinShares = 8;
+template <int kDim, bool kBf16>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ ChunkArgs a) {
+  const Cut c = a.cuts[blockIdx.x + 1];
+  if (c.parts == 0) return;
+  const uint32_t shares = (c.parts - 1) * kJoinShares;
+  auto slot = [&](uint32_t i) { return (c.run0 + i) * 2 + (i == 0 ? c.second : 0); };
+  for (uint32_t u = (c.order * kJoinShares + blockIdx.y) * kJoinThreads + threadIdx.x;
+       u < c.rows * (kDim / 4); u += shares * kJoinThreads) {
+    const uint32_t row = u % c.rows, col = u / c.rows;
+    float top = -INFINITY;
+    for (uint32_t i = 0; i < c.parts; ++i)
+      top = fmaxf(top, a.part_ml[(uint64_t)slot(i) * a.slot_rows + row].x);
+    float sum = 0.f, o[4] = {};
+    for (uint32_t i = 0; i < c.parts; ++i) {
+      const float2 ml = a.part_ml[(uint64_t)slot(i) * a.slot_rows + row];
+      const float w = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+      sum += w * ml.y;
+      if (ml.y == 0.f) continue;
+      const float4 y = reinterpret_cast<const float4*>(
+          a.part_o)[((uint64_t)slot(i) * (kDim / 4) + col) * a.slot_rows + row];
+      o[0] += w * y.x;
+      o[1] += w * y.y;
+      o[2] += w * y.z;
+      o[3] += w * y.w;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const uint64_t to = c.row + (c.lead + row) / a.group;
+    const uint32_t head = c.kv_head * a.group + (c.lead + row) % a.group;
+    *reinterpret_cast<uint2*>(a.out + (to * a.out_stride + (uint64_t)head * kDim + col * 4) * 2) =
+        make_uint2(pack16<kBf16>(o[0] * inv, o[1] * inv), pack16<kBf16>(o[2] * inv, o[3] * inv));
+    if (col == 0 && a.lse)
+      a.lse[to * a.heads + head] = sum == 0.f ? -INFINITY : (top - kUp) * kLn2 + logf(sum);
   }
 }
 
@@ -79,11 +1019,26 @@ bool sizes_ok(const netkv_kv_pages* pages, uint64_t rows, uint32_t n_seqs, uint3
          !(n_seqs >> 24) && !(rows >> 31);
 }
 
+struct Workspace {
+  uint32_t slot_rows;
+  size_t part_ml, cuts, total;  // part_o is at 0
+};
+Workspace workspace(const netkv_kv_pages* p, uint64_t rows, uint32_t heads) {
+  auto up = [](size_t x) { return (x + 127) / 128 * 128; };
+  Workspace w;
+  // rows of a row block at most, in whole lines
+  w.slot_rows = (uint32_t)up(min((uint64_t)(2 * kRows), max((uint64_t)1, rows * (heads / p->kv_heads))) * 16) / 16;
+  w.part_ml = up((size_t)kCtas * 2 * w.slot_rows * p->head_dim * 4);
+  w.cuts = w.part_ml + up((size_t)kCtas * 2 * w.slot_rows * sizeof(float2));
+  w.total = w.cuts + up(kCtas * sizeof(Cut));
+  return w;
+}
+
 }  // namespace
 
 extern "C" size_t netkv_attn_chunk_workspace_size(const netkv_kv_pages* pages, uint64_t rows,
                                                   uint32_t n_seqs, uint32_t heads) {
-  return sizes_ok(pages, rows, n_seqs, heads) ? 128 : 0;
+  return sizes_ok(pages, rows, n_seqs, heads) ? workspace(pages, rows, heads).total : 0;
 }
 
 extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t dtype,
@@ -101,23 +1056,57 @@ extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t d
   if (!rows_ok(d_q, q_stride, row) || !rows_ok(d_out, out_stride, row) || !d_off || !d_len ||
       !d_table || !d_ws || !aligned_to(d_off, 8) || !aligned_to(d_len, 4) ||
       !aligned_to(d_table, 4) || !aligned_to(d_lse, 4) || !aligned_to(d_ws, 16) ||
-      !aligned_to(d_status, 4) ||
-      ws_bytes < netkv_attn_chunk_workspace_size(pages, rows, n_seqs, heads))
+      !aligned_to(d_status, 4))
     return NETKV_EINVAL;
-  const ChunkArgs a = {kv_args(pages), (const unsigned char*)d_q, (unsigned char*)d_out, q_stride,
-                       out_stride, rows, d_off, d_len, d_table, heads, heads / pages->kv_heads,
-                       n_seqs, table_width, scale, d_lse, d_status};
-  const dim3 grid(min(n_seqs, 1u << 20), kParts);
-  const bool bf = dtype == NETKV_BF16, e4 = pages->format == NETKV_KV_E4M3;
-  auto go = [&](auto kernel) { kernel<<<grid, kWarps * 32, 0, (cudaStream_t)stream>>>(a); };
-  auto types = [&](auto dim) {
+  const Workspace ws = workspace(pages, rows, heads);
+  if (ws_bytes < ws.total) return NETKV_EINVAL;
+  unsigned char* w = (unsigned char*)d_ws;
+  const ChunkArgs a = {kv_args(pages),
+                       (const unsigned char*)d_q,
+                       (unsigned char*)d_out,
+                       q_stride,
+                       out_stride,
+                       rows,
+                       d_off,
+                       d_len,
+                       d_table,
+                       heads,
+                       heads / pages->kv_heads,
+                       n_seqs,
+                       table_width,
+                       scale * kLog2e,
+                       d_lse,
+                       (float*)w,
+                       (float2*)(w + ws.part_ml),
+                       (Cut*)(w + ws.cuts),
+                       ws.slot_rows,
+                       d_status};
+  auto go = [&](auto dim, auto bf, auto e4) -> netkv_status {
     constexpr int kDim = decltype(dim)::value;
-    if (bf && e4) go(chunk_kernel<kDim, true, true>);
-    else if (bf) go(chunk_kernel<kDim, true, false>);
-    else if (e4) go(chunk_kernel<kDim, false, true>);
-    else go(chunk_kernel<kDim, false, false>);
+    constexpr bool kB = decltype(bf)::value, kE = decltype(e4)::value;
+    constexpr auto kernel = chunk_kernel<kDim, kB, kE>;
+    constexpr size_t bytes = sizeof(Shared<kDim>);
+    static_assert(bytes <= 227 * 1024, "shared memory");
+    // a launch with fewer registers than the warps share out would never end
+    static const int regs = [] {
+      cudaFuncAttributes has;
+      return cudaFuncGetAttributes(&has, kernel) == cudaSuccess ? has.numRegs : 0;
+    }();
+    if (regs < kLaunchRegs) return NETKV_ECUDA;
+    NETKV_CUDA_TRY(allow_shared<kernel>((int)bytes));
+    kernel<<<kCtas, kThreads, bytes, (cudaStream_t)stream>>>(a);
+    if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
+    join_kernel<kDim, kB>
+        <<<dim3(kCtas - 1, kJoinShares), kJoinThreads, 0, (cudaStream_t)stream>>>(a);
+    return netkv_launch_status();
   };
-  if (pages->head_dim == 64) types(std::integral_constant<int, 64>());
-  else types(std::integral_constant<int, 128>());
-  return netkv_launch_status();
+  auto types = [&](auto dim) {
+    const bool bf = dtype == NETKV_BF16, e4 = pages->format == NETKV_KV_E4M3;
+    if (bf && e4) return go(dim, std::true_type(), std::true_type());
+    if (bf) return go(dim, std::true_type(), std::false_type());
+    if (e4) return go(dim, std::false_type(), std::true_type());
+    return go(dim, std::false_type(), std::false_type());
+  };
+  return pages->head_dim == 64 ? types(std::integral_constant<int, 64>())
+                               : types(std::integral_constant<int, 128>());
 }
