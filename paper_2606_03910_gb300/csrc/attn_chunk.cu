@@ -14,8 +14,8 @@
 // second kernel from fp32 sums in the workspace.
 //
 // Roles of a block's warps: one plans (the run's items), one reads table entries and scales ahead and
-// prefetches the pages' codes to L2, four turn codes into fp16 tiles in shared memory, one issues the
-// products, eight take the softmax.
+// copies the keys' codes to shared memory, one the values', four widen them into fp16 tiles, one issues
+// the products, and eight take the softmax.
 //
 // Arithmetic: both code types are exact in fp16, so codes go into the products as they are, and the
 // blocks' scales are applied to scores and weights in fp32.  A row of bf16 queries is brought to
@@ -47,16 +47,20 @@ constexpr float kFar = 1048576.f;
 // item away has ten times what the steps of the longest one take.
 constexpr long long kPatience = 4000000000, kStepClocks = 20000;
 constexpr long long kItemPatience = kPatience + ((1ll << 32) / kKeys) * kStepClocks;
-constexpr uint32_t kSoftmaxWarps = 8, kLoadWarps = 4;
-constexpr uint32_t kThreads = (kSoftmaxWarps + kLoadWarps + 4) * 32;
-constexpr uint32_t kProducts = 12, kPlan = 13, kPages = 14;  // warps, after the softmax's and the loads'
+constexpr uint32_t kSoftmaxWarps = 8, kWidenWarps = 4;
+constexpr uint32_t kThreads = (kSoftmaxWarps + kWidenWarps + 4) * 32;
+constexpr uint32_t kProducts = 12, kPlan = 13, kPages = 14, kValues = 15;  // warps with one role each
 // Registers: the launch has kThreads * kLaunchRegs, which the warps share out.
-constexpr int kLaunchRegs = 128, kSoftmaxRegs = 168, kLoadRegs = 104, kOtherRegs = 72;
-static_assert(256 * kSoftmaxRegs + 128 * kLoadRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs,
+constexpr int kLaunchRegs = 128, kSoftmaxRegs = 200, kWidenRegs = 56, kOtherRegs = 56;
+static_assert(256 * kSoftmaxRegs + 128 * kWidenRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs,
               "register split");
 template <int kDim>
-constexpr uint32_t kStages = kDim == 128 ? 4 : 8;  // tiles in the ring, 32 or 16 KB each
-constexpr uint32_t kBatchTiles = 4, kBatches = 3;  // table entries and scales read ahead
+constexpr uint32_t kStages = kDim == 128 ? 3 : 6;  // fp16 tiles in the ring, 32 or 16 KB each
+// Key tiles whose codes are on their way or there, 32 or 16 KB each.
+template <int kDim>
+constexpr uint32_t kDeep = kDim == 128 ? 2 : 4;
+constexpr uint32_t kBatchTiles = 4, kBatches = 2;  // table entries and scales read ahead
+constexpr uint32_t kItems = 4;                     // items planned ahead
 
 struct Cut;
 
@@ -81,16 +85,17 @@ struct ChunkArgs {
 // A wait of a limited time; once one has run out for a thread of the block, nobody waits any longer
 // and the block runs to its end.
 template <long long kLimit = kPatience>
-__device__ __forceinline__ void wait(uint32_t bar, uint32_t parity, volatile int* late) {
-  if (try_wait(bar, parity)) return;
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* late) {
+  if (try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!try_wait(bar, parity)) {
-    if (*late) return;
+    if (*late) return false;
     if (clock64() - t0 > kLimit) {
       *late = 1;
-      return;
+      return false;
     }
   }
+  return true;
 }
 // Whether a thread of the block has given up, by the whole warp: its threads go the same way.
 __device__ __forceinline__ bool given_up(volatile int* late) { return __any_sync(~0u, *late); }
@@ -168,41 +173,59 @@ struct Cut {
   uint32_t parts, run0, second, order;
 };
 
-// A block's eight pages and scales for each of a batch of key tiles.
+// Pages and scales of a batch of key tiles' blocks.
 struct Batch {
   int32_t page[kBatchTiles * kTileBlocks];  // -1: absent
   alignas(16) float k_scale[kBatchTiles * kTileBlocks], v_scale[kBatchTiles * kTileBlocks];
-  uint32_t absent;  // a bit each
+  uint32_t absent;  // blocks without a page, or past the sequence's end; a bit each
 };
 
 template <int kDim>
 struct Shared {
   alignas(1024) unsigned char q[2][kRows * kDim * 2];
   alignas(1024) unsigned char kv[kStages<kDim>][kKeys * kDim * 2];
+  alignas(1024) unsigned char codes[2 * kDeep<kDim>][kKeys * kDim];  // keys', values'
   alignas(16) Batch batch[kBatches];
   alignas(8) uint64_t q_full[2], kv_full[kStages<kDim>], kv_empty[kStages<kDim>];
+  uint64_t codes_full[2 * kDeep<kDim>], codes_empty[2 * kDeep<kDim>];
   uint64_t s_full[2], p_full[2][2], o_full[2];  // p: the two halves of the keys
-  uint64_t item_full[2], item_empty[2], batch_full[kBatches], batch_empty[kBatches], met;
-  Item item[2];
-  float stat[2][3][kRows];  // one tile of rows: both tiles' maxima, sums and units
+  uint64_t item_full[kItems], item_empty[kItems], batch_full[kBatches], batch_empty[kBatches], met;
+  Item item[kItems];
   uint64_t sums[kThreads / 32];
   uint32_t tmem;
   int late;
 };
 
-// The items of a block, as its warps read them: two places, filled by the planning warp.
+// Places in shared memory, from the address of its beginning in a register: an address taken anew
+// costs three instructions.
+#define AT(x) (sb + (uint32_t)(reinterpret_cast<const char*>(&(sh.x)) - reinterpret_cast<const char*>(&sh)))
+
+// The items of a block, as its warps read them: places that the planning warp fills.
 struct Items {
   uint32_t n = 0;
   template <class Sh>
-  __device__ __forceinline__ Item next(Sh& sh, volatile int* late) {
-    const uint32_t at = n % 2;
-    wait<kItemPatience>(smem_addr(&sh.item_full[at]), n / 2 & 1, late);
+  __device__ __forceinline__ Item next(Sh& sh, uint32_t sb, volatile int* late) {
+    const uint32_t at = n % kItems;
+    wait<kItemPatience>(AT(item_full[at]), n / kItems & 1, late);
     Item x = sh.item[at];
     ++n;
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.item_empty[at]));
+    if ((threadIdx.x & 31) == 0) bar_arrive(AT(item_empty[at]));
     if (given_up(late)) x.valid = 0;
     return x;
+  }
+  // The item where it is, kept until done(); null: no more.
+  template <class Sh>
+  __device__ __forceinline__ const Item* see(Sh& sh, uint32_t sb, volatile int* late) {
+    wait<kItemPatience>(AT(item_full[n % kItems]), n / kItems & 1, late);
+    const Item* x = &sh.item[n % kItems];
+    return __any_sync(~0u, !x->valid) || given_up(late) ? nullptr : x;
+  }
+  template <class Sh>
+  __device__ __forceinline__ void done(Sh& sh, uint32_t sb) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(AT(item_empty[n % kItems]));
+    ++n;
   }
 };
 
@@ -210,24 +233,24 @@ struct Items {
 struct Batches {
   uint32_t seen = 0, given = 0, base = 0;
   template <class Sh>
-  __device__ __forceinline__ void see(Sh& sh, uint32_t upto, volatile int* late) {
+  __device__ __forceinline__ void see(Sh& sh, uint32_t sb, uint32_t upto, volatile int* late) {
     for (; seen < upto; ++seen)
-      wait(smem_addr(&sh.batch_full[seen % kBatches]), seen / kBatches & 1, late);
+      wait(AT(batch_full[seen % kBatches]), seen / kBatches & 1, late);
   }
   template <class Sh>
-  __device__ __forceinline__ const Batch& get(Sh& sh, uint32_t tile, volatile int* late) {
-    see(sh, base + tile / kBatchTiles + 1, late);
+  __device__ __forceinline__ const Batch& get(Sh& sh, uint32_t sb, uint32_t tile, volatile int* late) {
+    see(sh, sb, base + tile / kBatchTiles + 1, late);
     return sh.batch[(base + tile / kBatchTiles) % kBatches];
   }
   // back to the pages' warp: what comes before tile `next` of n
   template <class Sh>
-  __device__ __forceinline__ void give(Sh& sh, uint32_t next, uint32_t n, volatile int* late) {
+  __device__ __forceinline__ void give(Sh& sh, uint32_t sb, uint32_t next, uint32_t n, volatile int* late) {
     const uint32_t upto = base + (next < n ? next / kBatchTiles : (n + kBatchTiles - 1) / kBatchTiles);
     if (given == upto) return;
-    see(sh, upto, late);
+    see(sh, sb, upto, late);
     __syncwarp();
     for (; given < upto; ++given)
-      if ((threadIdx.x & 31) == 0) bar_arrive(smem_addr(&sh.batch_empty[given % kBatches]));
+      if ((threadIdx.x & 31) == 0) bar_arrive(AT(batch_empty[given % kBatches]));
   }
   __device__ __forceinline__ void end(uint32_t n) { base += (n + kBatchTiles - 1) / kBatchTiles; }
 };
@@ -239,7 +262,7 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
 
 // ---- the planning warp: the run's items one after another
 template <class Sh>
-__device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, volatile int* late) {
+__device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
   const uint32_t lane = threadIdx.x & 31;
   uint64_t total = 0;
   for (uint32_t w = 0; w < kThreads / 32; ++w) total += sh.sums[w];
@@ -261,10 +284,11 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, volatile int* l
   };
   uint32_t n = 0;
   auto publish = [&](const Item& x) {
-    if (n >= 2) wait<kItemPatience>(smem_addr(&sh.item_empty[n % 2]), (n / 2 - 1) & 1, late);
+    if (n >= kItems)
+      wait<kItemPatience>(AT(item_empty[n % kItems]), (n / kItems - 1) & 1, late);
     if (lane == 0) {
-      sh.item[n % 2] = x;
-      bar_arrive(smem_addr(&sh.item_full[n % 2]));
+      sh.item[n % kItems] = x;
+      bar_arrive(AT(item_full[n % kItems]));
     }
     __syncwarp();
     ++n;
@@ -366,157 +390,219 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, volatile int* l
   publish(x);
 }
 
-// ---- the pages' warp: table entries and scales, a batch of key tiles at a time, a lane each block
+__device__ __forceinline__ uint4 load_shared(uint32_t at) {
+  uint4 x;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+               : "r"(at)
+               : "memory");
+  return x;
+}
+__device__ __forceinline__ void store_shared(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
+}
+
+// A key tile's codes, keys' (z = 0) or values', into their place once the widening warps have left it:
+// a copy each block, by 8 lanes, and zeros for blocks without a page.  A copy takes its warp 80 clocks
+// to issue, so keys and values have a warp each.
+template <int kDim, uint32_t z, class Sh>
+__device__ __forceinline__ bool copy_tile(const ChunkArgs& a, Sh& sh, uint32_t sb, uint32_t tile, bool mine,
+                                          int32_t page, uint32_t kv_head, volatile int* late) {
+  constexpr uint32_t kPart = kBlockTokens * kDim, kRing = kDeep<kDim>;
+  const uint32_t lane = threadIdx.x & 31, st = tile % kRing + z * kRing, bar = AT(codes_full[st]);
+  const bool ok = tile < kRing || wait(AT(codes_empty[st]), (tile / kRing - 1) & 1, late);
+  if (!__all_sync(~0u, ok)) return false;
+  const uint32_t at = AT(codes[st]) + lane % kTileBlocks * kPart;
+  const uint32_t bytes = __popc(__ballot_sync(~0u, mine && page >= 0)) * kPart;
+  if (bytes < kTileBlocks * kPart) {
+    if (mine && page < 0)
+      for (uint32_t i = 0; i < kPart; i += 16) store_shared(at + i, 0, 0, 0, 0);
+    __syncwarp();
+  }
+  if (lane == 0) bar_expect(bar, bytes);
+  __syncwarp();
+  if (mine && page >= 0)
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+        "[%3];" ::"r"(at),
+        "l"((z ? a.kv.v : a.kv.k) + ((uint64_t)page * a.kv.heads + kv_head) * kPart), "r"(kPart), "r"(bar)
+        : "memory");
+  __syncwarp();
+  return true;
+}
+
+// ---- the pages' warp: table entries and scales, a batch of key tiles at a time, a lane each block, and
+// the keys' codes.  Entries are read two batches ahead and scales one, over the ends of items too.
 template <int kDim, class Sh>
-__device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, volatile int* late) {
+__device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
   const uint32_t lane = threadIdx.x & 31;
+  struct Next {
+    uint32_t tiles, kv_head;  // key tiles of the batch, 0: no more
+    int32_t page;
+    bool in;
+    float2 scale;
+  };
   Items items;
-  uint32_t n = 0;
-  while (true) {
-    const Item x = items.next(sh, late);
-    if (!x.valid) break;
-    const uint32_t blocks = (x.tokens + kBlockTokens - 1) / kBlockTokens;
-    const uint32_t end = min((x.first + x.steps) * kTileBlocks, blocks);
-    auto entry = [&](uint32_t from) {
-      const uint32_t block = from + lane;
-      return block < end ? a.table[(uint64_t)x.seq * a.width + block] : -1;
-    };
-    uint32_t from = x.first * kTileBlocks;
-    int32_t next = entry(from);
-    for (uint32_t i = 0; i < (x.steps + kBatchTiles - 1) / kBatchTiles; ++i, ++n) {
-      int32_t page = next;
-      const bool in = from + lane < end;
-      next = entry(from + 32);
-      const bool there = page >= 0 && (uint32_t)page < a.kv.n_pages;
-      if (in && !there) flag_status(a.status, NETKV_DEV_ERANGE);
-      float2 scale = make_float2(0.f, 0.f);
-      if (there) {
-        const uint64_t part = (uint64_t)page * a.kv.heads + x.kv_head;
-        const uint64_t at = part * (kBlockTokens * kDim);
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.k + at),
-                     "n"(kBlockTokens * kDim)
-                     : "memory");
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.v + at),
-                     "n"(kBlockTokens * kDim)
-                     : "memory");
-        scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
-      } else {
-        page = -1;
-      }
-      Batch& to = sh.batch[n % kBatches];
-      if (n >= kBatches)
-        wait(smem_addr(&sh.batch_empty[n % kBatches]), (n / kBatches - 1) & 1, late);
-      to.page[lane] = page;
-      to.k_scale[lane] = scale.x;
-      to.v_scale[lane] = scale.y;
-      const uint32_t absent = __ballot_sync(~0u, !there);
-      if (lane == 0) to.absent = absent;
-      __syncwarp();
-      if (lane == 0) bar_arrive(smem_addr(&sh.batch_full[n % kBatches]));
-      if (given_up(late)) break;
-      from += 32;
+  Item x = {};
+  uint32_t at = 0;  // key tiles of the item that batches have
+  bool over = false;
+  auto take = [&]() -> Next {
+    while (!over && at >= x.steps) {
+      x = items.next(sh, sb, late);
+      over = !x.valid;
+      at = 0;
     }
+    Next b = {0, x.kv_head, -1, false, make_float2(0.f, 0.f)};
+    if (over) return b;
+    b.tiles = min(kBatchTiles, x.steps - at);
+    const uint32_t block = (x.first + at) * kTileBlocks + lane;
+    b.in = lane < b.tiles * kTileBlocks && (uint64_t)block * kBlockTokens < x.tokens;
+    if (b.in) b.page = a.table[(uint64_t)x.seq * a.width + block];
+    at += b.tiles;
+    return b;
+  };
+  auto scales = [&](Next& b) {
+    if (!b.in) return;
+    if (b.page < 0 || (uint32_t)b.page >= a.kv.n_pages) {
+      flag_status(a.status, NETKV_DEV_ERANGE);
+      b.page = -1;
+      return;
+    }
+    const uint64_t part = (uint64_t)b.page * a.kv.heads + b.kv_head;
+    b.scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.k + part * (kBlockTokens * kDim)),
+                 "n"(kBlockTokens * kDim)
+                 : "memory");
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.v + part * (kBlockTokens * kDim)),
+                 "n"(kBlockTokens * kDim)
+                 : "memory");
+  };
+  uint32_t tile = 0;
+  Next b0 = take();
+  scales(b0);
+  Next b1 = take();
+  for (uint32_t n = 0; b0.tiles; ++n) {
+    scales(b1);
+    const Next b2 = take();
+    Batch& to = sh.batch[n % kBatches];
+    if (n >= kBatches) wait(AT(batch_empty[n % kBatches]), (n / kBatches - 1) & 1, late);
+    to.page[lane] = b0.page;
+    to.k_scale[lane] = b0.scale.x;
+    to.v_scale[lane] = b0.scale.y;
+    const uint32_t absent = __ballot_sync(~0u, b0.page < 0);
+    if (lane == 0) to.absent = absent;
+    __syncwarp();
+    if (lane == 0) bar_arrive(AT(batch_full[n % kBatches]));
+    for (uint32_t q = 0; q < b0.tiles; ++q)
+      if (!copy_tile<kDim, 0>(a, sh, sb, tile++, lane / kTileBlocks == q, b0.page, b0.kv_head, late))
+        return;
+    b0 = b1;
+    b1 = b2;
   }
 }
 
-// ---- the loading warps: codes of two of a key tile's blocks each, to fp16 in the ring.  A lane has 16
-// codes of a row at a time, 4 lanes 64 of them, so that 8 lanes' stores of 16 bytes are in all banks.
-template <int kDim, bool kE4m3, class Sh>
-__device__ __forceinline__ void load_tiles(const ChunkArgs& a, Sh& sh, volatile int* late) {
-  constexpr uint32_t kRing = kStages<kDim>, kLoads = 2 * kDim / 32, kBox = kKeys * 128;
-  constexpr uint32_t kHalves = kDim / 64;
-  const uint32_t lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftmaxWarps;
+// ---- the values' warp: their codes
+template <int kDim, class Sh>
+__device__ __forceinline__ void copy_values(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
+  const uint32_t lane = threadIdx.x & 31;
   Items items;
   Batches batches;
-  uint32_t n = 0;  // tiles of the ring
+  uint32_t count = 0;
   while (true) {
-    const Item x = items.next(sh, late);
+    const Item x = items.next(sh, sb, late);
     if (!x.valid) break;
-    const bool one = x.rows <= kRows;
-    // the n-th piece in the order in which the products want them: of two tiles of rows K 0, V 0, K 1,
-    // V 1, ...; of one K 0, K 1, V 0, K 2, V 1, ...
-    const uint32_t pieces = 2 * x.steps;
-    auto tile_of = [&](uint32_t p, bool* values) -> uint32_t {
-      if (!one) {
-        *values = p & 1;
-        return p / 2;
-      }
-      if (p == 0 || p + 1 == pieces) {
-        *values = p != 0;
-        return p ? x.steps - 1 : 0;
-      }
-      *values = !(p & 1);
-      return p & 1 ? (p + 1) / 2 : p / 2 - 1;
-    };
-    uint4 c[2][kLoads];
-    auto load = [&](uint32_t p, uint4* to) {
-      bool values;
-      const uint32_t tile = tile_of(p, &values);
-      const Batch& batch = batches.get(sh, tile, late);
-      const uint32_t block = tile % kBatchTiles * kTileBlocks + 2 * w;
-      const unsigned char* codes = values ? a.kv.v : a.kv.k;
-      const uint32_t key0 = (x.first + tile) * kKeys + w * 32;
-#pragma unroll
-      for (uint32_t z = 0; z < 2; ++z) {
-        const int32_t page = batch.page[block + z];
-        const unsigned char* from =
-            codes + ((uint64_t)max(page, 0) * a.kv.heads + x.kv_head) * (kBlockTokens * kDim);
-#pragma unroll
-        for (uint32_t i = 0; i < kLoads / 2; ++i) {
-          const uint32_t row = i / kHalves * 8 + lane / 4, half = i % kHalves;
-          // past the sequence's end are others' codes, and weights of 0 would not hide a NaN
-          const bool in = page >= 0 && key0 + z * kBlockTokens + row < x.tokens;
-          to[z * (kLoads / 2) + i] =
-              in ? __ldcg(reinterpret_cast<const uint4*>(from + row * kDim + half * 64 + lane % 4 * 16))
-                 : make_uint4(0, 0, 0, 0);
-        }
-      }
-      if (values) batches.give(sh, tile + 1, x.steps, late);
-    };
-    auto store = [&](const uint4* from) {
-      const uint32_t st = n % kRing;
-      if (n >= kRing) wait(smem_addr(&sh.kv_empty[st]), (n / kRing - 1) & 1, late);
-      ++n;
-      if (given_up(late)) return;
-#pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) {
-        const uint32_t y = i % (kLoads / 2);
-        const uint32_t row = w * 32 + i / (kLoads / 2) * kBlockTokens + y / kHalves * 8 + lane / 4;
-        unsigned char* to = sh.kv[st] + y % kHalves * kBox + row * 128;
-        uint32_t h[8];
-        widen<kE4m3>(from[i].x, &h[0], &h[1]);
-        widen<kE4m3>(from[i].y, &h[2], &h[3]);
-        widen<kE4m3>(from[i].z, &h[4], &h[5]);
-        widen<kE4m3>(from[i].w, &h[6], &h[7]);
-        const uint32_t at = lane % 4 * 2;
-        *reinterpret_cast<uint4*>(to + ((at ^ (row & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
-        *reinterpret_cast<uint4*>(to + (((at + 1) ^ (row & 7)) * 16)) = make_uint4(h[4], h[5], h[6], h[7]);
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) bar_arrive(smem_addr(&sh.kv_full[st]));
-    };
-    // a piece's loads are under way while the one before is stored
-    if (pieces) load(0, c[0]);
-    for (uint32_t p = 0; p < pieces && !given_up(late); p += 2) {
-      load(p + 1, c[1]);
-      store(c[0]);
-      if (p + 2 < pieces) load(p + 2, c[0]);
-      store(c[1]);
+    for (uint32_t from = 0; from < x.steps; from += kBatchTiles) {
+      const int32_t page = batches.get(sh, sb, from, late).page[lane];
+      batches.give(sh, sb, from + kBatchTiles, x.steps, late);
+      for (uint32_t q = 0; q < min(kBatchTiles, x.steps - from); ++q)
+        if (!copy_tile<kDim, 1>(a, sh, sb, count++, lane / kTileBlocks == q, page, x.kv_head, late))
+          return;
     }
     batches.end(x.steps);
   }
 }
 
+// ---- the widening warps: codes of two of a key tile's blocks each, to fp16 in the ring.  A lane has
+// 16 codes of a row at a time; 8 lanes have the halves of two rows such that their loads and their
+// stores of 16 bytes are in all banks.
+template <int kDim, bool kE4m3, class Sh>
+__device__ __forceinline__ void widen_tiles(Sh& sh, uint32_t sb, volatile int* late) {
+  constexpr uint32_t kRing = kStages<kDim>, kLoads = 2 * kDim / 32, kBox = kKeys * 128;
+  constexpr uint32_t kCodes = kDeep<kDim>, kTile = kKeys * kDim * 2;
+  const uint32_t lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftmaxWarps;
+  // A lane's load i: row 8 * (i / 2) + row0 of the warp's 32, half (i + odd) % 2 (of 64: row 8 i + row0)
+  const uint32_t row0 = kDim == 128 ? lane / 8 * 2 + lane / 4 % 2 : lane / 4;
+  const uint32_t odd = kDim == 128 ? lane / 4 % 2 : 0;
+  const uint32_t src0 = AT(codes[0]) + (w * 32 + row0) * kDim + lane % 4 * 16;
+  const uint32_t dst0 = AT(kv[0]) + (w * 32 + row0) * 128;
+  const uint32_t at0 = ((lane % 4 * 2) ^ (row0 & 7)) * 16, at1 = at0 ^ 16;
+  Items items;
+  uint32_t n = 0, tiles = 0;  // tiles of the ring; key tiles of the items before
+  while (true) {
+    const Item* item = items.see(sh, sb, late);
+    if (!item) break;
+    const uint32_t steps = item->steps, first = item->first, tokens = item->tokens;
+    // in the order in which the products want them: of two tiles of rows K 0, V 0, K 1, V 1, ...; of
+    // one K 0, K 1, V 0, K 2, V 1, ...
+    const uint32_t ahead = item->rows <= kRows ? 2 : 1;
+    items.done(sh, sb);
+#pragma unroll 1
+    for (uint32_t p = 0; p < 2 * (steps + ahead); ++p) {
+      const uint32_t z = p & 1 ? 0 : 1;  // values of an earlier tile, then keys
+      const uint32_t tile = p / 2 - (z ? ahead : 0);
+      if (tile >= steps) continue;
+      const uint32_t cs = (tiles + tile) % kCodes + z * kCodes, st = n % kRing;
+      wait(AT(codes_full[cs]), (tiles + tile) / kCodes & 1, late);
+      const uint32_t src = src0 + cs * (kKeys * kDim);
+      uint4 c[kLoads];
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i)
+        c[i] = load_shared(kDim == 128 ? src + (i % 2 ? 64 - odd * 64 : odd * 64) + i / 2 * 8 * kDim
+                                       : src + i * 8 * kDim);
+      // past the sequence's end are others' codes, and weights of 0 would not hide a NaN
+      if (tile + 1 == steps) {
+        const uint32_t key0 = (first + tile) * kKeys + w * 32;
+        const uint32_t own = key0 < tokens ? tokens - key0 : 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i)
+          if (row0 + (kDim == 128 ? i / 2 : i) * 8 >= own) c[i] = make_uint4(0, 0, 0, 0);
+      }
+      bool ok = n < kRing || wait(AT(kv_empty[st]), (n / kRing - 1) & 1, late);
+      ++n;
+      if (!__all_sync(~0u, ok)) break;
+      const uint32_t dst = dst0 + st * kTile, dst_even = dst + odd * kBox, dst_odd = dst + (kBox - odd * kBox);
+#pragma unroll
+      for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t to = kDim == 128 ? (i % 2 ? dst_odd : dst_even) + i / 2 * 1024 : dst + i * 1024;
+        uint32_t h[8];
+        widen<kE4m3>(c[i].x, &h[0], &h[1]);
+        widen<kE4m3>(c[i].y, &h[2], &h[3]);
+        widen<kE4m3>(c[i].z, &h[4], &h[5]);
+        widen<kE4m3>(c[i].w, &h[6], &h[7]);
+        store_shared(to + at0, h[0], h[1], h[2], h[3]);
+        store_shared(to + at1, h[4], h[5], h[6], h[7]);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        bar_arrive(AT(kv_full[st]));
+        bar_arrive(AT(codes_empty[cs]));
+      }
+    }
+    tiles += steps;
+  }
+}
+
 // ---- the products
 template <int kDim, class Sh>
-__device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
+__device__ __forceinline__ void multiply(Sh& sh, uint32_t sb, volatile int* late) {
   constexpr uint32_t kRing = kStages<kDim>, kBox = 128 * 128, kS = 0, kO = 256;
   constexpr uint32_t kScores = product(false, false, kKeys), kSums = product(false, true, kDim);
   constexpr uint32_t kTile = kRows * kDim * 2 >> 4;  // of operands' addresses
   const bool leader = elect();
-  const uint64_t q0 = operand(smem_addr(sh.q[0]), 16), k0 = operand(smem_addr(sh.kv[0]), 16),
-                 v0 = operand(smem_addr(sh.kv[0]), kBox);
+  const uint64_t q0 = operand(AT(q[0]), 16), k0 = operand(AT(kv[0]), 16),
+                 v0 = operand(AT(kv[0]), kBox);
   auto scores = [&](uint32_t t, uint32_t st) {  // S_t from the ring's place st
     if (leader) {
 #pragma unroll
@@ -524,55 +610,52 @@ __device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
         const uint32_t off = (x / 4 * kBox + x % 4 * 32) >> 4;
         mma_smem(kS + t * 128, q0 + t * kTile + off, k0 + st * kTile + off, kScores, x > 0);
       }
-      commit(smem_addr(&sh.s_full[t]));
+      commit(AT(s_full[t]));
     }
     __syncwarp();
   };
-  auto sums = [&](uint32_t t, uint32_t st, uint32_t half, bool add) {
-    if (leader) {
-#pragma unroll
-      for (uint32_t x = 0; x < kKeys / 32; ++x)
-        mma_tmem(kO + t * kDim, kS + t * 128 + half * 64 + x * 8,
-                 v0 + st * kTile + (half * (kKeys / 32) + x) * (2048 >> 4), kSums, add || x > 0);
-    }
-    __syncwarp();
-  };
-  auto signal = [&](uint64_t* bar) {
-    if (leader) commit(smem_addr(bar));
+  auto signal = [&](uint32_t bar) {
+    if (leader) commit(bar);
     __syncwarp();
   };
   uint32_t i = 0, with_q = 0, done0 = 0, done1 = 0;  // tiles of the ring, items, steps
   auto arrived = [&](uint32_t n) {
-    wait(smem_addr(&sh.kv_full[n % kRing]), (n / kRing) & 1, late);
+    wait(AT(kv_full[n % kRing]), (n / kRing) & 1, late);
     after_sync();
   };
   auto take = [&](uint32_t t, uint32_t v, bool add) {  // P_t V from the ring's place v
     const uint32_t parity = (t ? done1++ : done0++) & 1;
-    wait(smem_addr(&sh.p_full[t][1]), parity, late);
-    after_sync();
-    sums(t, v, 1, add);
-    wait(smem_addr(&sh.p_full[t][0]), parity, late);
-    after_sync();
-    sums(t, v, 0, true);
+#pragma unroll
+    for (uint32_t half = 0; half < 2; ++half) {
+      wait(AT(p_full[t][half]), parity, late);
+      after_sync();
+      if (leader) {
+#pragma unroll
+        for (uint32_t x = half * (kKeys / 32); x < (half + 1) * (kKeys / 32); ++x)
+          mma_tmem(kO + t * kDim, kS + t * 128 + x * 8, v0 + v * kTile + x * (2048 >> 4), kSums,
+                   add || x > 0);
+      }
+      __syncwarp();
+    }
   };
   Items items;
   while (true) {
-    const Item x = items.next(sh, late);
+    const Item x = items.next(sh, sb, late);
     if (!x.valid) break;
     if (x.steps == 0) continue;
     const uint32_t n = x.steps;
-    wait(smem_addr(&sh.q_full[0]), with_q & 1, late);
-    wait(smem_addr(&sh.q_full[1]), with_q & 1, late);
+    wait(AT(q_full[0]), with_q & 1, late);
+    wait(AT(q_full[1]), with_q & 1, late);
     ++with_q;
     after_sync();
     arrived(i);
     scores(0, i % kRing);
     if (x.rows <= kRows) {  // the even and the odd key tiles of one tile of rows
-      signal(&sh.kv_empty[i++ % kRing]);
+      signal(AT(kv_empty[i++ % kRing]));
       if (n > 1) {
         arrived(i);
         scores(1, i % kRing);
-        signal(&sh.kv_empty[i++ % kRing]);
+        signal(AT(kv_empty[i++ % kRing]));
       }
       for (uint32_t j = 0; j < n; j += 2) {
 #pragma unroll
@@ -581,19 +664,19 @@ __device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
           arrived(i);
           take(t, i % kRing, j > 0);
           const bool more = j + t + 2 < n;
-          if (!more) signal(&sh.o_full[t]);
-          signal(&sh.kv_empty[i++ % kRing]);
+          if (!more) signal(AT(o_full[t]));
+          signal(AT(kv_empty[i++ % kRing]));
           if (more) {
             arrived(i);
             scores(t, i % kRing);
-            signal(&sh.kv_empty[i++ % kRing]);
+            signal(AT(kv_empty[i++ % kRing]));
           }
         }
       }
       continue;
     }
     scores(1, i % kRing);
-    signal(&sh.kv_empty[i++ % kRing]);
+    signal(AT(kv_empty[i++ % kRing]));
     for (uint32_t j = 0; j < n; ++j) {
       const uint32_t v = i++ % kRing, k = i % kRing;
       const bool more = j + 1 < n;
@@ -603,11 +686,11 @@ __device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
       for (uint32_t t = 0; t < 2; ++t) {
         take(t, v, j > 0);
         if (more) scores(t, k);
-        else signal(&sh.o_full[t]);
+        else signal(AT(o_full[t]));
       }
-      signal(&sh.kv_empty[v]);
+      signal(AT(kv_empty[v]));
       if (more) {
-        signal(&sh.kv_empty[k]);
+        signal(AT(kv_empty[k]));
         ++i;
       }
     }
@@ -619,7 +702,7 @@ __device__ __forceinline__ void multiply(Sh& sh, volatile int* late) {
 
 // ---- softmax: a thread has a row of its tile
 template <int kDim, bool kBf16, bool kE4m3, class Sh>
-__device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int* late) {
+__device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
   constexpr uint32_t kS = 0, kO = 256, kBox = 128 * 128;
   constexpr float kTop = kE4m3 ? 448.f : 128.f;  // of the codes
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid / 32, 0);
@@ -630,23 +713,25 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int
   uint32_t taken = 0, finished0 = 0, finished1 = 0, meetings = 0;  // steps; items of each tile; meetings
   auto meet = [&]() {
     __syncwarp();
-    if (lane == 0) bar_arrive(smem_addr(&sh.met));
-    wait(smem_addr(&sh.met), meetings++ & 1, late);
+    if (lane == 0) bar_arrive(AT(met));
+    wait(AT(met), meetings++ & 1, late);
     __syncwarp();
   };
   while (true) {
-    const Item x = items.next(sh, late);
-    if (!x.valid) break;
+    const Item* item = items.see(sh, sb, late);
+    if (!item) break;
+    const Item& x = *item;  // read where it is used: registers are for scores
     const bool one = x.rows <= kRows;
     const uint32_t mine = (one ? 0 : t * kRows) + row;  // the thread's row of the row block
     const bool real = mine < x.rows;
     const bool busy = __any_sync(~0u, real);
-    const uint32_t token = (x.lead + mine) / a.group, head = x.kv_head * a.group + (x.lead + mine) % a.group;
     float by = 0.f;  // what brings a sum of products to a score in powers of two, but for the scales
     float reach = 0.f;  // no score is above this times the scales
     if (x.steps) {
       // the row's queries as fp16, 16 bytes of row r in place (c ^ r) of 8
       if (busy) {
+        const uint32_t token = (x.lead + mine) / a.group;
+        const uint32_t head = x.kv_head * a.group + (x.lead + mine) % a.group;
         const uint4* from = reinterpret_cast<const uint4*>(
             a.q + ((x.row + token) * a.q_stride + (uint64_t)head * kDim) * 2);
         uint4 v[kDim / 8];
@@ -685,67 +770,59 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int
           *reinterpret_cast<uint4*>(sh.q[t] + i / 8 * kBox + row * 128 + ((i % 8) ^ (row & 7)) * 16) = v[i];
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      bar_arrive(smem_addr(&sh.q_full[t]));
+      bar_arrive(AT(q_full[t]));
     }
-    // tokens that this row sees
-    const int64_t sees = real ? x.sees + token : x.tokens;
-    const uint32_t stride = one ? 2 : 1, own0 = one ? t : 0;
+    // tokens that this row sees: of its key tiles all of the first `full`, and `rest` of the next
+    const int64_t sees = (real ? x.sees + (x.lead + mine) / a.group : (int64_t)x.tokens) -
+                         (int64_t)x.first * kKeys;
+    const uint32_t full = sees < (int)kKeys ? 0 : (uint32_t)(sees / kKeys);
+    const int rest = (int)max((int64_t)0, sees - (int64_t)full * kKeys);
+    const uint32_t stride = one ? 2 : 1, own0 = one ? t : 0, steps = x.steps;
     float m = -INFINITY, l = 0.f;
     uint32_t unit = 1;  // the exponent of what value scales are taken over
     bool any = false;
-    for (uint32_t j = own0; j < x.steps; j += stride) {
-      wait(smem_addr(&sh.s_full[t]), taken++ & 1, late);
+    for (uint32_t j = own0; j < steps; j += stride) {
+      wait(AT(s_full[t]), taken++ & 1, late);
       after_sync();
       if (busy) {
-        const Batch& batch = batches.get(sh, j, late);
+        float s[kKeys];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_load(s_at + i * 32, s + i * 32);
+        const Batch& batch = batches.get(sh, sb, j, late);
         const uint32_t b0 = j % kBatchTiles * kTileBlocks;
-        float k[kTileBlocks], v[kTileBlocks];
+        float k[kTileBlocks];
         *reinterpret_cast<float4*>(k) = *reinterpret_cast<const float4*>(batch.k_scale + b0);
         *reinterpret_cast<float4*>(k + 4) = *reinterpret_cast<const float4*>(batch.k_scale + b0 + 4);
-        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(batch.v_scale + b0);
-        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(batch.v_scale + b0 + 4);
+        const float4* v = reinterpret_cast<const float4*>(batch.v_scale + b0);
         const uint32_t absent = batch.absent >> b0 & 0xff;
-        const int seen = (int)max((int64_t)0, min((int64_t)kKeys, sees - (int64_t)(x.first + j) * kKeys));
-        float most = 0.f, most_k = 0.f;
-#pragma unroll
-        for (uint32_t b = 0; b < kTileBlocks; b += 2) {
-          most_k = max3(most_k, k[b], k[b + 1]);
-          most = max3(most, v[b], v[b + 1]);
-        }
+        const int seen = j < full ? kKeys : j == full ? rest : 0;
+        const float most = max3(max3(v[0].x, v[0].y, v[0].z), max3(v[0].w, v[1].x, v[1].y),
+                                fmaxf(v[1].z, v[1].w));
+        const float most_k = max3(max3(k[0], k[1], k[2]), max3(k[3], k[4], k[5]), fmaxf(k[6], k[7]));
         const bool masked = __any_sync(~0u, seen < (int)kKeys || reach * most_k > kFar) || absent;
 #pragma unroll
         for (uint32_t b = 0; b < kTileBlocks; ++b) k[b] *= by;
-        float s[64];
-        float f[kTileBlocks];  // what scores are multiplied by, where fetch() has not done so
+        tmem_loaded();
+        if (masked) {
 #pragma unroll
-        for (uint32_t b = 0; b < kTileBlocks; ++b) f[b] = masked ? 1.f : k[b];
-        auto fetch = [&](uint32_t h) {  // the scores of half the keys
-          tmem_load(s_at + h * 64, s);
-          tmem_load(s_at + h * 64 + 32, s + 32);
-          tmem_loaded();
-          if (masked) {
+          for (int i = 0; i < (int)kKeys; ++i)
+            s[i] = i < seen && !(absent >> (i / 16) & 1) ? s[i] * k[i / 16] : -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 64; ++i) {
-              const int key = (int)h * 64 + i;
-              s[i] = key < seen && !(absent >> (key / 16) & 1) ? s[i] * k[key / 16] : -INFINITY;
-            }
-          }
-        };
+          for (uint32_t b = 0; b < kTileBlocks; ++b) k[b] = 1.f;
+        }
         float top = m;
-        auto tops = [&](uint32_t h) {
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            float y = s[b * 16];
+        for (uint32_t b = 0; b < kTileBlocks; ++b) {
+          const float* y = s + b * 16;
+          float u = max3(y[0], y[1], y[2]), w = max3(y[3], y[4], y[5]);
 #pragma unroll
-            for (int i = 1; i + 1 < 16; i += 2) y = max3(y, s[b * 16 + i], s[b * 16 + i + 1]);
-            y = fmaxf(y, s[b * 16 + 15]);
-            top = fmaxf(top, y * f[h * 4 + b]);
+          for (int i = 6; i + 3 < 16; i += 4) {
+            u = max3(u, y[i], y[i + 1]);
+            w = max3(w, y[i + 2], y[i + 3]);
           }
-        };
-        fetch(0);
-        tops(0);
-        fetch(1);
-        tops(1);
+          u = max3(u, y[14], y[15]);
+          top = fmaxf(top, fmaxf(u, w) * k[b]);
+        }
         const uint32_t above = min((__float_as_uint(most) >> 23 & 0xff) + 1, 253u);
         const bool grown = above > unit;  // alike for all rows
         const bool follow = top - m > kLag;  // also the first maximum
@@ -778,74 +855,81 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int
         const float over = __uint_as_float((254 - unit) << 23);
         const uint64_t base_2 = pair(base, base);
         uint64_t sums_2[2] = {0, 0};
-        auto weigh = [&](uint32_t h) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
           uint32_t p[32];
+          const float4 four = v[h];
+          const float scale[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            const float g = v[h * 4 + b] * over;
-            const uint64_t f_2 = pair(f[h * 4 + b], f[h * 4 + b]);
+            const float g = scale[b] * over, f = k[h * 4 + b];
+            const uint64_t f_2 = pair(f, f), g_2 = pair(g, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+              const float* y = s + h * 64 + b * 16 + 2 * i;
               float u, w;
-              split(fma2(pair(s[b * 16 + 2 * i], s[b * 16 + 2 * i + 1]), f_2, base_2), &u, &w);
-              u = ex2(u);
-              w = ex2(w);
-              sums_2[i & 1] = add2(sums_2[i & 1], pair(u, w));
-              p[b * 8 + i] = pack16<false>(u * g, w * g);
+              split(fma2(pair(y[0], y[1]), f_2, base_2), &u, &w);
+              const uint64_t e = pair(ex2(u), ex2(w));
+              sums_2[i & 1] = add2(sums_2[i & 1], e);
+              split(mul2(e, g_2), &u, &w);
+              p[b * 8 + i] = pack16<false>(u, w);
             }
           }
-          tmem_store(s_at + h * 64, p);
+          tmem_store(s_at + h * 32, p);
           tmem_stored();
           before_sync();
-          bar_arrive(smem_addr(&sh.p_full[t][h]));
-        };
-        weigh(1);
-        fetch(0);
-        weigh(0);
+          bar_arrive(AT(p_full[t][h]));
+        }
         float u, w;
         split(add2(sums_2[0], sums_2[1]), &u, &w);
         l += u + w;
       } else {
         before_sync();
-        bar_arrive(smem_addr(&sh.p_full[t][1]));
-        bar_arrive(smem_addr(&sh.p_full[t][0]));
+        bar_arrive(AT(p_full[t][0]));
+        bar_arrive(AT(p_full[t][1]));
       }
-      batches.give(sh, j + stride, x.steps, late);
-      if (given_up(late)) break;
+      batches.give(sh, sb, j + stride, steps, late);
     }
-    batches.give(sh, x.steps, x.steps, late);
-    batches.end(x.steps);
+    batches.give(sh, sb, steps, steps, late);
+    batches.end(steps);
 
     // ---- the row's output, or its part
     const float made = __uint_as_float(unit << 23);
     float w0 = 1.f, w1 = 0.f;  // what the two tiles' sums are multiplied by
     if (one) {
       const bool has0 = x.steps > 0, has1 = x.steps > 1;
-      if (t == 0 && has0) wait(smem_addr(&sh.o_full[0]), finished0 & 1, late);
-      if (t == 1 && has1) wait(smem_addr(&sh.o_full[1]), finished1 & 1, late);
+      if (t == 0 && has0) wait(AT(o_full[0]), finished0 & 1, late);
+      if (t == 1 && has1) wait(AT(o_full[1]), finished1 & 1, late);
       finished0 += has0;
       finished1 += has1;
-      sh.stat[t][0][row] = m;
-      sh.stat[t][1][row] = l;
-      sh.stat[t][2][row] = made;
+      // what a row's two threads have goes through their lane of TMEM, where the scores were
+      float own[4] = {m, l, made, 0.f}, other[4];
+      after_sync();
+      tmem_store4(s_at, reinterpret_cast<const uint32_t*>(own));
+      tmem_stored();
+      before_sync();
       meet();
       after_sync();
-      const float m0 = sh.stat[0][0][row], m1 = sh.stat[1][0][row];
+      tmem_load4(kS + (1 - t) * 128 + lanes, other);
+      tmem_loaded();
+      const float m0 = t ? other[0] : m, m1 = t ? m : other[0];
       m = fmaxf(m0, m1);
       w0 = m0 == -INFINITY ? 0.f : ex2(m0 - m);
       w1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
       // (a tile of NaN scores has no maximum, but its sum says so)
-      l = w0 * sh.stat[0][1][row] + w1 * sh.stat[1][1][row];
-      w0 *= sh.stat[0][2][row];
-      w1 *= sh.stat[1][2][row];
+      l = w0 * (t ? other[1] : l) + w1 * (t ? l : other[1]);
+      w0 *= t ? other[2] : made;
+      w1 *= t ? made : other[2];
     } else if (x.steps) {
-      wait(smem_addr(&sh.o_full[t]), (t ? finished1 : finished0) & 1, late);
+      wait(AT(o_full[t]), (t ? finished1 : finished0) & 1, late);
       ++finished0;
       ++finished1;
       after_sync();
       w0 = made;
     }
     if (busy) {
+      const uint32_t token = (x.lead + mine) / a.group;
+      const uint32_t head = x.kv_head * a.group + (x.lead + mine) % a.group;
       const float inv = l == 0.f || x.slot >= 0 ? 1.f : 1.f / l;
       const bool none = l == 0.f;  // NaN is not
       w0 *= inv;
@@ -853,19 +937,18 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int
       // of one tile of rows each tile's warps write half the columns
       constexpr int kCols = 16;
       const uint32_t c0 = one ? t * (kDim / 2) : 0, c1 = one ? c0 + kDim / 2 : kDim;
+#pragma unroll 1
       for (uint32_t c = c0; c < c1; c += kCols) {
         float o[kCols] = {}, y[kCols];
         if (x.steps) {
           tmem_load16(kO + lanes + (one ? 0 : t * kDim) + c, o);
+          if (one && x.steps > 1) tmem_load16(kO + lanes + kDim + c, y);
           tmem_loaded();
 #pragma unroll
-          for (int i = 0; i < kCols; ++i) o[i] = none ? 0.f : o[i] * w0;
-        }
-        if (one && x.steps > 1) {
-          tmem_load16(kO + lanes + kDim + c, y);
-          tmem_loaded();
-#pragma unroll
-          for (int i = 0; i < kCols; ++i) o[i] += none ? 0.f : y[i] * w1;
+          for (int i = 0; i < kCols; ++i) {
+            o[i] = none ? 0.f : o[i] * w0;
+            if (one && x.steps > 1) o[i] += none ? 0.f : y[i] * w1;
+          }
         }
         if (!real) {
         } else if (x.slot >= 0) {
@@ -895,6 +978,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, volatile int
     }
     before_sync();
     if (one) meet();  // both tiles' sums have been read
+    items.done(sh, sb);
   }
 }
 
@@ -908,12 +992,20 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     if (lane == 0) {
       sh.late = 0;
       for (uint32_t i = 0; i < kStages<kDim>; ++i) {
-        bar_init(smem_addr(&sh.kv_full[i]), kLoadWarps);
+        bar_init(smem_addr(&sh.kv_full[i]), kWidenWarps);
         bar_init(smem_addr(&sh.kv_empty[i]), 1);
+      }
+      for (uint32_t i = 0; i < 2 * kDeep<kDim>; ++i) {
+        bar_init(smem_addr(&sh.codes_full[i]), 1);
+        bar_init(smem_addr(&sh.codes_empty[i]), kWidenWarps);
       }
       for (uint32_t i = 0; i < kBatches; ++i) {
         bar_init(smem_addr(&sh.batch_full[i]), 1);
-        bar_init(smem_addr(&sh.batch_empty[i]), kSoftmaxWarps + kLoadWarps);
+        bar_init(smem_addr(&sh.batch_empty[i]), kSoftmaxWarps + 1);
+      }
+      for (uint32_t i = 0; i < kItems; ++i) {
+        bar_init(smem_addr(&sh.item_full[i]), 1);
+        bar_init(smem_addr(&sh.item_empty[i]), kSoftmaxWarps + kWidenWarps + 3);
       }
       for (int t = 0; t < 2; ++t) {
         bar_init(smem_addr(&sh.q_full[t]), kRows);
@@ -921,8 +1013,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
         bar_init(smem_addr(&sh.p_full[t][0]), kRows);
         bar_init(smem_addr(&sh.p_full[t][1]), kRows);
         bar_init(smem_addr(&sh.o_full[t]), 1);
-        bar_init(smem_addr(&sh.item_full[t]), 1);
-        bar_init(smem_addr(&sh.item_empty[t]), kSoftmaxWarps + kLoadWarps + 2);
       }
       bar_init(smem_addr(&sh.met), kSoftmaxWarps);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -950,17 +1040,20 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   if (lane == 0) sh.sums[warp] = sum;
   __syncthreads();
   after_sync();
+  uint32_t sb;
+  asm volatile("mov.u32 %0, %1;" : "=r"(sb) : "r"(smem_addr(&sh)));
   if (warp >= kProducts) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == kProducts) multiply<kDim>(sh, late);
-    else if (warp == kPlan) plan(a, sh, late);
-    else if (warp == kPages) read_pages<kDim>(a, sh, late);
+    if (warp == kProducts) multiply<kDim>(sh, sb, late);
+    else if (warp == kPlan) plan(a, sh, sb, late);
+    else if (warp == kPages) read_pages<kDim>(a, sh, sb, late);
+    else if (warp == kValues) copy_values<kDim>(a, sh, sb, late);
   } else if (warp >= kSoftmaxWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLoadRegs));
-    load_tiles<kDim, kE4m3>(a, sh, late);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWidenRegs));
+    widen_tiles<kDim, kE4m3>(sh, sb, late);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    softmax<kDim, kBf16, kE4m3>(a, sh, late);
+    softmax<kDim, kBf16, kE4m3>(a, sh, sb, late);
   }
   __syncthreads();
   if (warp == 0) {

@@ -97,27 +97,38 @@ __device__ __forceinline__ void store_block(const StoreArgs& a, const Units& u, 
     }
   }
   const float was = lo ? *scale : 0.f;
-  float turned[kTurn ? kSteps : 1][8];
   float largest;
+  // The turned rows are made twice, for their largest and for their codes: kept, they would take 64
+  // registers a thread and half of the SM's warps.
+  auto turned = [&](int i, float* y) {
+    const uint32_t row = row0 + i * kRows;
+    const bool fresh = all || (row >= lo && row < hi);  // others have no angles
+    turn8<kBf16>(*turns, row, lane % kLanes, x[i], y);
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // infinities and NaN have no code: they are held as zeros
+      const bool fine = fabsf(y[j]) <= 3.4028235e38f;
+      odd |= fresh && !fine;
+      y[j] = fresh && fine ? y[j] : 0.f;
+    }
+    return odd;
+  };
   if constexpr (kTurn) {
     largest = 0.f;
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      const uint32_t row = row0 + i * kRows;
-      const bool fresh = all || (row >= lo && row < hi);  // others have no angles
-      turn8<kBf16>(*turns, row, lane % kLanes, x[i], turned[i]);
+      float y[8];
+      odd |= turned(i, y);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        // infinities and NaN have no code: they are held as zeros
-        const bool fine = fabsf(turned[i][j]) <= 3.4028235e38f;
-        odd |= fresh && !fine;
-        turned[i][j] = fresh && fine ? turned[i][j] : 0.f;
-        largest = fmaxf(largest, fabsf(turned[i][j]));
-      }
+      for (int j = 0; j < 8; ++j) largest = fmaxf(largest, fabsf(y[j]));
     }
     if (__any_sync(~0u, odd) && lane == 0) flag_status(a.status, NETKV_DEV_EDOMAIN);
     largest = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(largest)));
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)  // not to be kept after all
+      asm volatile("" : "+r"(x[i].x), "+r"(x[i].y), "+r"(x[i].z), "+r"(x[i].w));
   } else {
     // Magnitudes are in the order of their bits, two values a word.
     constexpr uint32_t kInf = kBf16 ? 0x7f80 : 0x7c00;
@@ -156,14 +167,13 @@ __device__ __forceinline__ void store_block(const StoreArgs& a, const Units& u, 
   for (int i = 0; i < kSteps; ++i) {
     const uint32_t row = row0 + i * kRows;
     uint2* at = reinterpret_cast<uint2*>(to + i * kRows * kDim);
+    float y[8];
+    if constexpr (kTurn) turned(i, y);  // (a whole warp's work)
     if (all || (row >= lo && row < hi)) {
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-      float y[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float2 z;
-        if constexpr (kTurn) z = make_float2(turned[i][2 * j], turned[i][2 * j + 1]);
-        else z = unpack16<kBf16>(w[j]);
+        const float2 z = kTurn ? make_float2(y[2 * j], y[2 * j + 1]) : unpack16<kBf16>(w[j]);
         y[2 * j] = z.x * inv;
         y[2 * j + 1] = z.y * inv;
       }
@@ -171,7 +181,6 @@ __device__ __forceinline__ void store_block(const StoreArgs& a, const Units& u, 
     } else if (grows && row < lo) {
       // the block's scale grew: its earlier codes follow
       const uint2 old = *at;
-      float y[8];
       decode4<kE4m3>(old.x, ratio, y);
       decode4<kE4m3>(old.y, ratio, y + 4);
       *at = make_uint2(encode4<kE4m3>(y), encode4<kE4m3>(y + 4));

@@ -11,7 +11,10 @@
 namespace {
 
 constexpr uint32_t kWarps = 8;
-constexpr uint32_t kPerWarp = 2;  // heads that a warp takes where there are enough of them
+constexpr uint32_t kResident = 4;  // blocks an SM: bytes under way
+// Heads that a warp takes of 16 tokens: the more, the less the cosines and sines cost; fewer where
+// tokens are few.
+constexpr uint32_t kFewBlocks = 1216, kPerWarp[2] = {2, 10};
 
 struct RotateArgs {
   const unsigned char* x;
@@ -28,24 +31,29 @@ __device__ __forceinline__ void turn_rows(const Turns& t, const unsigned char* x
                                           unsigned char* out, uint64_t out_stride, uint32_t lo,
                                           uint32_t hi) {
   constexpr int kLanes = kDim / 8, kRows = 32 / kLanes, kSteps = kBlockTokens / kRows;
+  constexpr int kPart = kSteps < 4 ? kSteps : 4;  // loads under way at a time
   const uint32_t lane = threadIdx.x & 31, col = (lane % kLanes) * 8, row0 = lane / kLanes;
-  uint4 v[kSteps];
+#pragma unroll 1
+  for (int from = 0; from < kSteps; from += kPart) {
+    if (row0 + from * kRows - lane / kLanes >= hi) break;
+    uint4 v[kPart];
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const uint32_t row = row0 + i * kRows;
-    v[i] = make_uint4(0, 0, 0, 0);
-    if (row >= lo && row < hi)
-      v[i] = __ldcs(reinterpret_cast<const uint4*>(x + ((int64_t)(row * x_stride) + col) * 2));
-  }
+    for (int i = 0; i < kPart; ++i) {
+      const uint32_t row = row0 + (from + i) * kRows;
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (row >= lo && row < hi)
+        v[i] = __ldcs(reinterpret_cast<const uint4*>(x + ((int64_t)(row * x_stride) + col) * 2));
+    }
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const uint32_t row = row0 + i * kRows;
-    float y[8];
-    turn8<kBf16>(t, row, lane % kLanes, v[i], y);
-    if (row >= lo && row < hi)
-      *reinterpret_cast<uint4*>(out + (row * out_stride + col) * 2) =
-          make_uint4(pack16<kBf16>(y[0], y[1]), pack16<kBf16>(y[2], y[3]),
-                     pack16<kBf16>(y[4], y[5]), pack16<kBf16>(y[6], y[7]));
+    for (int i = 0; i < kPart; ++i) {
+      const uint32_t row = row0 + (from + i) * kRows;
+      float y[8];
+      turn8<kBf16>(t, row, lane % kLanes, v[i], y);
+      if (row >= lo && row < hi)
+        __stcs(reinterpret_cast<uint4*>(out + (row * out_stride + col) * 2),
+               make_uint4(pack16<kBf16>(y[0], y[1]), pack16<kBf16>(y[2], y[3]),
+                          pack16<kBf16>(y[4], y[5]), pack16<kBf16>(y[6], y[7])));
+    }
   }
 }
 
@@ -54,7 +62,7 @@ struct Table {
 };
 
 template <int kDim, bool kBf16>
-__global__ void __launch_bounds__(kWarps * 32) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, kResident) rotate_kernel(const __grid_constant__ RotateArgs a) {
   __shared__ Table table;
   const uint64_t first = (uint64_t)blockIdx.x * kBlockTokens;
   const uint32_t n = (uint32_t)min((uint64_t)kBlockTokens, a.rows - first);
@@ -113,7 +121,7 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, Table& table, 
 }
 
 template <int kDim, bool kBf16, bool kE4m3, bool kMany>
-__global__ void __launch_bounds__(kWarps * 32) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, kResident - 1) append_kernel(const __grid_constant__ AppendArgs a) {
   __shared__ Table table;
   if (blockIdx.y == 0) check_ranges(a.s);
   if constexpr (kMany) {
@@ -132,8 +140,9 @@ __global__ void __launch_bounds__(kWarps * 32) append_kernel(const __grid_consta
 }
 
 // Blocks of threads that share 16 tokens' heads.
-uint32_t shares(uint32_t units) {
-  return min((units + kWarps * kPerWarp - 1) / (kWarps * kPerWarp), 65535u);
+uint32_t shares(uint32_t units, uint64_t blocks) {
+  const uint32_t per = kWarps * kPerWarp[blocks >= kFewBlocks];
+  return min((units + per - 1) / per, 65535u);
 }
 
 }  // namespace
@@ -181,7 +190,8 @@ extern "C" netkv_status netkv_rotate(const netkv_rotary* rot, uint32_t dtype, co
     return NETKV_EINVAL;
   const RotateArgs a = {(const unsigned char*)d_x, (unsigned char*)d_out, x_stride, out_stride, rows,
                         d_pos, heads, *rot};
-  const dim3 grid((unsigned)((rows + kBlockTokens - 1) / kBlockTokens), shares(heads));
+  const uint64_t blocks = (rows + kBlockTokens - 1) / kBlockTokens;
+  const dim3 grid((unsigned)blocks, shares(heads, blocks));
   const bool bf = dtype == NETKV_BF16;
   auto go = [&](auto kernel) { kernel<<<grid, kWarps * 32, 0, (cudaStream_t)stream>>>(a); };
   if (head_dim == 64) go(bf ? rotate_kernel<64, true> : rotate_kernel<64, false>);
@@ -222,7 +232,7 @@ extern "C" netkv_status netkv_kv_append(const netkv_kv_pages* pages, const netkv
                          d_status},
                         (const unsigned char*)d_q, (unsigned char*)d_q_out, q_stride, q_out_stride,
                         d_pos, d_q ? heads : 0, *rot};
-  const dim3 grid((unsigned)blocks, shares(2 * pages->kv_heads + a.heads));
+  const dim3 grid((unsigned)blocks, shares(2 * pages->kv_heads + a.heads, blocks));
   const bool bf = dtype == NETKV_BF16, e4 = pages->format == NETKV_KV_E4M3;
   auto go = [&](auto kernel) { kernel<<<grid, kWarps * 32, 0, (cudaStream_t)stream>>>(a); };
   auto pick = [&](auto dim, auto many) {

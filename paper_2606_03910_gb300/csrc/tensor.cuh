@@ -29,6 +29,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
   return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y));
+  return d;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -163,6 +168,18 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t* r) {
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
         "r"(at)
       : "memory");
+}
+__device__ __forceinline__ void tmem_load4(uint32_t at, float* x) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(x);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at));
+}
+__device__ __forceinline__ void tmem_store4(uint32_t at, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0, %1, %2, %3};"
+               :
+               : "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(at)
+               : "memory");
 }
 __device__ __forceinline__ void tmem_loaded() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
