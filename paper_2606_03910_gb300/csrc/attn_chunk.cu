@@ -38,7 +38,7 @@ constexpr float kLag = 8.f;
 constexpr float kUp = 7.f;
 // Places on the line: a key of a row block with two tiles of rows, of one with one tile, and the
 // beginning and end of a row block.
-constexpr uint64_t kPairKey = 8, kOneKey = 5, kEdge = 1536;
+constexpr uint64_t kPairKey = 8, kOneKey = 6, kEdge = 4096;
 constexpr uint64_t kLeast = 1280;  // places of a run at least
 // Scores that may be above this (in powers of two) are rounded before the maximum is taken from them,
 // as where some are hidden: a product that is not is off the rounded maximum by 2^-24 of itself.
@@ -59,7 +59,7 @@ constexpr uint32_t kStages = kDim == 128 ? 3 : 6;  // fp16 tiles in the ring, 32
 // Key tiles whose codes are on their way or there, 32 or 16 KB each.
 template <int kDim>
 constexpr uint32_t kDeep = kDim == 128 ? 2 : 4;
-constexpr uint32_t kBatchTiles = 4, kBatches = 2;  // table entries and scales read ahead
+constexpr uint32_t kBatchTiles = 4, kBatches = 3;  // table entries and scales read ahead
 constexpr uint32_t kItems = 4;                     // items planned ahead
 
 struct Cut;
@@ -73,7 +73,8 @@ struct ChunkArgs {
   const uint32_t* len;
   const int32_t* table;
   uint32_t heads, group, n_seqs, width;
-  float scale2;  // scale * log2(e)
+  uint32_t slope;  // of the line, see Shape
+  float scale2;    // scale * log2(e)
   float* lse;
   float* part_o;   // [kCtas][2][kDim / 4][slot_rows][4]
   float2* part_ml; // [kCtas][2][slot_rows]: a row's maximum and sum
@@ -111,25 +112,40 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, uint32_t i) {
   return {r.first, r.count,
           (uint32_t)min((uint64_t)a.len[i], (uint64_t)a.width * kBlockTokens)};
 }
-// Row blocks of a sequence and KV head, and the places that they take: block b has kEdge and the keys
-// that its last row sees, up to roundings by the group's size; the last one all the sequence's keys.
+// x / y for y below 2^16, a digit of 16 bits at a time (a 64-bit division is a hundred instructions).
+__device__ __forceinline__ uint64_t divide(uint64_t x, uint32_t y) {
+  if (!(x >> 32)) return (uint32_t)x / y;
+  uint64_t q = 0;
+  uint32_t r = 0;
+#pragma unroll 1
+  for (int i = 48; i >= 0; i -= 16) {
+    const uint32_t d = r << 16 | (uint32_t)(x >> i & 0xffff);
+    q = q << 16 | d / y;
+    r = d % y;
+  }
+  return q;
+}
+// Row blocks of a sequence and KV head, and the places that they take: block b has kEdge and about the
+// keys that its last row sees, the last one all the sequence's keys.  Any rising line would do: a
+// run's ends are found in it the same way from both sides.
 struct Shape {
-  uint64_t blocks, before;  // keys before the new tokens
-  uint64_t group, last;     // places of the last row block
-  __device__ __forceinline__ Shape(const Seq& s, uint32_t g) {
-    const uint64_t rows = s.new_tokens * g;
-    group = g;
-    blocks = (rows + 2 * kRows - 1) / (2 * kRows);
-    before = s.tokens > s.new_tokens ? s.tokens - s.new_tokens : 0;
-    const uint64_t rest = rows - (blocks ? blocks - 1 : 0) * (2 * kRows);
-    last = blocks ? kEdge + s.tokens * (rest > kRows ? kPairKey : kOneKey) : 0;
+  uint32_t blocks, one;  // whether the last row block has one tile of rows
+  uint64_t before;       // places of the keys before the new tokens
+  uint64_t slope, last;  // places that a row block has more than the one before, times 32; of the last
+  __device__ __forceinline__ Shape(const Seq& s, const ChunkArgs& a) {
+    const uint64_t rows = s.new_tokens * a.group;
+    blocks = (uint32_t)((rows + 2 * kRows - 1) / (2 * kRows));
+    before = s.tokens > s.new_tokens ? (s.tokens - s.new_tokens) * kPairKey : 0;
+    slope = a.slope;
+    one = blocks && rows - (uint64_t)(blocks - 1) * (2 * kRows) <= kRows;
+    last = blocks ? kEdge + s.tokens * (one ? kOneKey : kPairKey) : 0;
   }
   // places before block b < blocks
-  __device__ __forceinline__ uint64_t upto(uint64_t b) const {
-    return b * kEdge + kPairKey * (b * before + kRows * b * (b + 1) / group);
+  __device__ __forceinline__ uint64_t upto(uint32_t b) const {
+    return b * (kEdge + before) + (slope * ((uint64_t)b * (b + 1)) >> 5);
   }
   __device__ __forceinline__ uint64_t all() const { return blocks ? upto(blocks - 1) + last : 0; }
-  __device__ __forceinline__ uint64_t of(uint64_t b) const {
+  __device__ __forceinline__ uint64_t of(uint32_t b) const {
     return b + 1 == blocks ? last : upto(b + 1) - upto(b);
   }
 };
@@ -141,14 +157,20 @@ struct Runs {
   __device__ __forceinline__ explicit Runs(uint64_t t) {
     total = t;
     count = (uint32_t)max((uint64_t)1, min((uint64_t)kCtas, t / kLeast));
-    base = t / count;
+    base = divide(t, count);
     rest = (uint32_t)(t - base * count);
   }
   __device__ __forceinline__ uint64_t start(uint32_t c) const { return base * c + min(c, rest); }
   // the run that has place p < total
   __device__ __forceinline__ uint32_t at(uint64_t p) const {
-    const uint64_t longer = (base + 1) * rest;
-    return p < longer ? (uint32_t)(p / (base + 1)) : rest + (uint32_t)((p - longer) / base);
+    uint32_t lo = 0, hi = count;
+#pragma unroll 1
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (start(mid) <= p) lo = mid;
+      else hi = mid;
+    }
+    return lo;
   }
 };
 
@@ -300,7 +322,7 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
   if (at < end) {
     for (uint32_t from = 0; from < a.n_seqs; from += 32) {
       window(from);
-      const uint64_t c = Shape(mine, a.group).all() * a.kv.heads;
+      const uint64_t c = Shape(mine, a).all() * a.kv.heads;
       uint64_t upto = c;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
@@ -321,18 +343,25 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
   }
   if (found) {  // (not with lengths that change under the call)
     Seq s = pick(seq);
-    Shape shape(s, a.group);
+    Shape shape(s, a);
     uint32_t kv_head = 0;
-    uint64_t b = 0;
+    uint32_t b = 0;
     {
       const uint64_t all = shape.all();
-      kv_head = (uint32_t)(into / all);
+      uint32_t to = a.kv.heads;
+#pragma unroll 1
+      while (to - kv_head > 1) {
+        const uint32_t mid = (kv_head + to) / 2;
+        if (mid * all <= into) kv_head = mid;
+        else to = mid;
+      }
       into -= kv_head * all;
       b = shape.blocks - 1;
       if (into < shape.upto(b)) {
-        uint64_t lo = 0, hi = b;  // upto(lo) <= into < upto(hi)
+        uint32_t lo = 0, hi = b;  // upto(lo) <= into < upto(hi)
+#pragma unroll 1
         while (hi - lo > 1) {
-          const uint64_t mid = (lo + hi) / 2;
+          const uint32_t mid = (lo + hi) / 2;
           if (shape.upto(mid) <= into) lo = mid;
           else hi = mid;
         }
@@ -343,10 +372,10 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
     bool first = true;
     while (at < end && !given_up(late)) {
       const uint64_t places = shape.of(b), upto = min(places, into + (end - at));
-      const uint64_t row0 = b * (2 * kRows);
+      const uint64_t row0 = (uint64_t)b * (2 * kRows);
       x.rows = (uint32_t)min((uint64_t)(2 * kRows), s.new_tokens * a.group - row0);
-      x.lead = (uint32_t)(row0 % a.group);
-      const uint64_t token = row0 / a.group;
+      const uint64_t token = divide(row0, a.group);
+      x.lead = (uint32_t)(row0 - token * a.group);
       x.row = s.first + token;
       x.sees = (int64_t)s.tokens - (int64_t)s.new_tokens + (int64_t)token + 1;
       x.seq = seq;
@@ -354,9 +383,10 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
       x.tokens = s.tokens;
       const int64_t most = x.sees + (x.lead + x.rows - 1) / a.group;  // of the last row
       const uint64_t tiles = most > 0 ? ((uint64_t)most + kKeys - 1) / kKeys : 0;
-      auto step = [&](uint64_t p) {
-        return p <= kEdge || places <= kEdge ? p == places ? tiles : 0
-                                             : (p - kEdge) * tiles / (places - kEdge);
+      const bool one = shape.one && b + 1 == shape.blocks;
+      auto step = [&](uint64_t p) -> uint64_t {
+        if (p == places) return tiles;
+        return p <= kEdge ? 0 : min(tiles, one ? (p - kEdge) / (kOneKey * kKeys) : (p - kEdge) / (kPairKey * kKeys));
       };
       x.first = (uint32_t)step(into);
       x.steps = (uint32_t)step(upto) - x.first;
@@ -381,7 +411,7 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
         if (++seq >= a.n_seqs) break;
         if (seq >= base + 32) window(seq);
         s = pick(seq);
-        shape = Shape(s, a.group);
+        shape = Shape(s, a);
       } while (shape.blocks == 0);
       if (seq >= a.n_seqs) break;
     }
@@ -462,6 +492,7 @@ __device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, uint32_t 
     at += b.tiles;
     return b;
   };
+  bool begun = false;
   auto scales = [&](Next& b) {
     if (!b.in) return;
     if (b.page < 0 || (uint32_t)b.page >= a.kv.n_pages) {
@@ -471,6 +502,7 @@ __device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, uint32_t 
     }
     const uint64_t part = (uint64_t)b.page * a.kv.heads + b.kv_head;
     b.scale = make_float2(a.kv.k_scale[part], a.kv.v_scale[part]);
+    if (!begun) return;  // the first are copied at once
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.kv.k + part * (kBlockTokens * kDim)),
                  "n"(kBlockTokens * kDim)
                  : "memory");
@@ -479,12 +511,15 @@ __device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, uint32_t 
                  : "memory");
   };
   uint32_t tile = 0;
-  Next b0 = take();
+  Next b0 = take(), b1 = take();
   scales(b0);
-  Next b1 = take();
+  begun = true;
   for (uint32_t n = 0; b0.tiles; ++n) {
-    scales(b1);
-    const Next b2 = take();
+    Next b2 = {};
+    if (n) {
+      scales(b1);
+      b2 = take();
+    }
     Batch& to = sh.batch[n % kBatches];
     if (n >= kBatches) wait(AT(batch_empty[n % kBatches]), (n / kBatches - 1) & 1, late);
     to.page[lane] = b0.page;
@@ -494,9 +529,14 @@ __device__ __forceinline__ void read_pages(const ChunkArgs& a, Sh& sh, uint32_t 
     if (lane == 0) to.absent = absent;
     __syncwarp();
     if (lane == 0) bar_arrive(AT(batch_full[n % kBatches]));
-    for (uint32_t q = 0; q < b0.tiles; ++q)
+    for (uint32_t q = 0; q < b0.tiles; ++q) {
       if (!copy_tile<kDim, 0>(a, sh, sb, tile++, lane / kTileBlocks == q, b0.page, b0.kv_head, late))
         return;
+      if (n == 0 && q + 1 == min(b0.tiles, kDeep<kDim>)) {  // the first batch before all else
+        scales(b1);
+        b2 = take();
+      }
+    }
     b0 = b1;
     b1 = b2;
   }
@@ -623,77 +663,52 @@ __device__ __forceinline__ void multiply(Sh& sh, uint32_t sb, volatile int* late
     wait(AT(kv_full[n % kRing]), (n / kRing) & 1, late);
     after_sync();
   };
-  auto take = [&](uint32_t t, uint32_t v, bool add) {  // P_t V from the ring's place v
-    const uint32_t parity = (t ? done1++ : done0++) & 1;
-#pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-      wait(AT(p_full[t][half]), parity, late);
-      after_sync();
-      if (leader) {
-#pragma unroll
-        for (uint32_t x = half * (kKeys / 32); x < (half + 1) * (kKeys / 32); ++x)
-          mma_tmem(kO + t * kDim, kS + t * 128 + x * 8, v0 + v * kTile + x * (2048 >> 4), kSums,
-                   add || x > 0);
-      }
-      __syncwarp();
-    }
-  };
   Items items;
   while (true) {
     const Item x = items.next(sh, sb, late);
     if (!x.valid) break;
     if (x.steps == 0) continue;
-    const uint32_t n = x.steps;
+    // Of two tiles of rows each key tile is both tiles' (a turn each), of one it is the even or the odd
+    // one's.  The ring has K 0, V 0, K 1, V 1, ... or K 0, K 1, V 0, K 2, V 1, ...
+    const uint32_t n = x.steps, turns = x.rows <= kRows ? n : 2 * n;
+    const bool one = x.rows <= kRows;
     wait(AT(q_full[0]), with_q & 1, late);
     wait(AT(q_full[1]), with_q & 1, late);
     ++with_q;
-    after_sync();
-    arrived(i);
-    scores(0, i % kRing);
-    if (x.rows <= kRows) {  // the even and the odd key tiles of one tile of rows
-      signal(AT(kv_empty[i++ % kRing]));
-      if (n > 1) {
-        arrived(i);
-        scores(1, i % kRing);
-        signal(AT(kv_empty[i++ % kRing]));
-      }
-      for (uint32_t j = 0; j < n; j += 2) {
+#pragma unroll 1
+    for (uint32_t u = 0; u < min(2u, turns) + turns; ++u) {
+      const bool first = u < min(2u, turns);  // the first scores of each tile; then P V and the next scores
+      const uint32_t w = first ? u : u - min(2u, turns), t = w & 1;
+      const bool last = one || t;  // the turn after which key tiles are left
+      const uint32_t v = i + (one ? w + min(w + 2, n) : w | 1);
+      const uint32_t k = i + (first ? (one ? w : 0) : one ? 2 * w + 3 : (w | 1) + 1);
+      const bool more = first || w + 2 < turns;
+      if (!first) {
+        if (one || t == 0) arrived(v);
+        const uint32_t parity = (t ? done1++ : done0++) & 1;
 #pragma unroll
-        for (uint32_t t = 0; t < 2; ++t) {
-          if (j + t >= n) continue;
-          arrived(i);
-          take(t, i % kRing, j > 0);
-          const bool more = j + t + 2 < n;
-          if (!more) signal(AT(o_full[t]));
-          signal(AT(kv_empty[i++ % kRing]));
-          if (more) {
-            arrived(i);
-            scores(t, i % kRing);
-            signal(AT(kv_empty[i++ % kRing]));
+        for (uint32_t half = 0; half < 2; ++half) {
+          wait(AT(p_full[t][half]), parity, late);
+          after_sync();
+          if (leader) {
+#pragma unroll
+            for (uint32_t x = 0; x < kKeys / 32; ++x)
+              mma_tmem(kO + t * kDim, kS + t * 128 + half * 32 + x * 8,
+                       v0 + v % kRing * kTile + (half * (kKeys / 32) + x) * (2048 >> 4), kSums,
+                       w >= 2 || half || x);
           }
+          __syncwarp();
         }
+        if (!more) signal(AT(o_full[t]));
+        if (last) signal(AT(kv_empty[v % kRing]));
       }
-      continue;
-    }
-    scores(1, i % kRing);
-    signal(AT(kv_empty[i++ % kRing]));
-    for (uint32_t j = 0; j < n; ++j) {
-      const uint32_t v = i++ % kRing, k = i % kRing;
-      const bool more = j + 1 < n;
-      arrived(i - 1);
-      if (more) arrived(i);
-#pragma unroll
-      for (uint32_t t = 0; t < 2; ++t) {
-        take(t, v, j > 0);
-        if (more) scores(t, k);
-        else signal(AT(o_full[t]));
-      }
-      signal(AT(kv_empty[v]));
       if (more) {
-        signal(AT(kv_empty[k]));
-        ++i;
+        if (one || t == 0) arrived(k);
+        scores(t, k % kRing);
+        if (last) signal(AT(kv_empty[k % kRing]));
       }
     }
+    i += 2 * n;
   }
   // the last signals have to reach a block that is still there
   if (i >= 1) wait(smem_addr(&sh.kv_empty[(i - 1) % kRing]), ((i - 1) / kRing) & 1, late);
@@ -738,16 +753,14 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
 #pragma unroll
         for (int i = 0; i < kDim / 8; ++i) v[i] = real ? __ldcs(from + i) : make_uint4(0, 0, 0, 0);
         by = a.scale2;
-        float largest = 0.f;
+        // magnitudes are in the order of their bits, two values a word
+        uint32_t bits = 0;
 #pragma unroll
         for (int i = 0; i < kDim / 8; ++i) {
-          const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 y = unpack16<kBf16>(w[j]);
-            largest = max3(largest, fabsf(y.x), fabsf(y.y));
-          }
+          bits = __vimax3_u16x2(bits, v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu);
+          bits = __vimax3_u16x2(bits, v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu);
         }
+        const float largest = unpack16<kBf16>(max(bits & 0xffffu, bits >> 16)).x;
         // (rows of infinities are not others' concern)
         reach = largest <= 3.4028235e38f ? largest * by * (kDim * kTop) : 0.f;
         if constexpr (kBf16) {
@@ -839,7 +852,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
             unit = above;
           }
           if (any) {  // S_t is complete, and so is P_t V before it
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < kDim / 16; ++i) {
               float o[16];
               tmem_load16(o_at + i * 16, o);
@@ -988,6 +1001,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   Shared<kDim>& sh = *reinterpret_cast<Shared<kDim>*>(smem);
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(~0u, tid / 32, 0);
   volatile int* late = &sh.late;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (warp == 0) {
     if (lane == 0) {
       sh.late = 0;
@@ -1027,7 +1041,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   // the line's length, and what is wrong with the sequences, said by the first block
   uint64_t sum = 0;
   for (uint32_t i = tid; i < a.n_seqs; i += kThreads) {
-    sum += Shape(seq_of(a, i), a.group).all();
+    sum += Shape(seq_of(a, i), a).all();
     if (blockIdx.x == 0 && (row_range(a.off, i, a.rows).bad ||
                             a.len[i] > (uint64_t)a.width * kBlockTokens))
       flag_status(a.status, NETKV_DEV_ERANGE);
@@ -1074,6 +1088,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 constexpr uint32_t kJoinThreads = 256, kJoinShares = 8;
 template <int kDim, bool kBf16>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ ChunkArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const Cut c = a.cuts[blockIdx.x + 1];
   if (c.parts == 0) return;
   const uint32_t shares = (c.parts - 1) * kJoinShares;
@@ -1167,6 +1182,7 @@ extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t d
                        heads / pages->kv_heads,
                        n_seqs,
                        table_width,
+                       (uint32_t)(kPairKey * 2 * kRows * 16 / (heads / pages->kv_heads)),
                        scale * kLog2e,
                        d_lse,
                        (float*)w,
@@ -1189,8 +1205,16 @@ extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t d
     NETKV_CUDA_TRY(allow_shared<kernel>((int)bytes));
     kernel<<<kCtas, kThreads, bytes, (cudaStream_t)stream>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;
-    join_kernel<kDim, kB>
-        <<<dim3(kCtas - 1, kJoinShares), kJoinThreads, 0, (cudaStream_t)stream>>>(a);
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(kCtas - 1, kJoinShares);
+    c.blockDim = dim3(kJoinThreads);
+    c.stream = (cudaStream_t)stream;
+    c.attrs = &early;
+    c.numAttrs = 1;
+    NETKV_CUDA_TRY(cudaLaunchKernelEx(&c, join_kernel<kDim, kB>, a));
     return netkv_launch_status();
   };
   auto types = [&](auto dim) {
