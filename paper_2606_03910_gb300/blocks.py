@@ -2,8 +2,9 @@
 
 ``BlockPool`` holds the 8-bit blocks of a batch of sequences (one slot each) and runs the
 calls of ``netkv.h`` on them: new tokens in (``append``), blocks back as rows (``read``), one
-decode step's attention (``attend``), and the eviction of the blocks that have drawn the least
-of it (``evict``).  ``move`` carries a sequence from one pool to another, as the transfer that
+decode step's attention (``attend``), a chunk of new tokens a slot, turned by their positions,
+stored and attended (``extend``, ``attend_chunk``), and the eviction of the blocks that have drawn
+the least attention (``evict``).  ``move`` carries a sequence from one pool to another, as the transfer that
 ``netkv_schedule_streams`` prices does between instances.
 
 Pages are handed out on the host; device work is enqueued on torch's current stream.  Only
@@ -11,7 +12,7 @@ Pages are handed out on the host; device work is enqueued on torch's current str
 """
 from __future__ import annotations
 
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 import torch
 
@@ -46,6 +47,7 @@ class BlockPool:
         self.length = torch.zeros(slots, dtype=torch.int32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.tokens: List[int] = [0] * slots          # length, on the host
+        self.seen: List[int] = [0] * slots            # tokens ever, evicted ones too: the next position
         self.page_of: List[List[int]] = [[] for _ in range(slots)]
         self.free = list(range(n_pages - 1, -1, -1))
         self._spare = (torch.empty_like(self.table), torch.empty_like(self.length),
@@ -53,6 +55,7 @@ class BlockPool:
                        torch.empty_like(self.length))
         self._workspace = None
         self._workspace_heads = 0
+        self._chunk_workspace = None
 
     @property
     def slots(self) -> int:
@@ -124,7 +127,11 @@ class BlockPool:
         except Exception:
             self._give_back(taken)
             raise
+        self._grow(counts)
+
+    def _grow(self, counts: List[int]) -> None:
         self.tokens = [t + c for t, c in zip(self.tokens, counts)]
+        self.seen = [t + c for t, c in zip(self.seen, counts)]
         self.length += self._dev(counts)
 
     def read(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int]) -> None:
@@ -150,6 +157,53 @@ class BlockPool:
                                 workspace=self._workspace, status=self.status)
         return out, lse
 
+    def _chunk_space(self, q: torch.Tensor, scale) -> torch.Tensor:
+        """A workspace for the queries' attention; a ValueError where that would be refused."""
+        if scale is not None and not 0.0 < scale <= 3.4e38:
+            raise ValueError(f"a scale above 0 expected, got {scale}")
+        need = netkv.netkv_attn_chunk_workspace_size(self.pages, q.shape[0], self.slots, q.shape[1])
+        if need == 0:
+            raise ValueError(f"query heads in groups of {self.pages.heads_dim[0]} expected, got {q.shape[1]}")
+        if self._chunk_workspace is None or self._chunk_workspace.nbytes < need:
+            self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
+        return self._chunk_workspace
+
+    def attend_chunk(self, q: torch.Tensor, counts: Sequence[int], scale=None):
+        """Rows q [sum(counts), heads, dim] are the queries of the last counts[i] tokens of each slot i:
+        (out, lse), each row over its own token and those before it.  The blocks' ``mass`` stays."""
+        counts = self._counts(counts, q)
+        workspace = self._chunk_space(q, scale)
+        out = torch.empty_like(q)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        netkv.netkv_attn_chunk(self.pages, q, self._offsets(counts), self.length, self.table, out, lse=lse,
+                               scale=scale, workspace=workspace, status=self.status)
+        return out, lse
+
+    def extend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int],
+               rotary: "netkv.Rotary", positions: Optional[torch.Tensor] = None, scale=None):
+        """counts[i] new tokens of each slot i, as a layer has them: queries and keys turned by their
+        positions, keys and values into blocks, and attention over the blocks: (out, lse).
+
+        positions [axes, rows] int32; by default a token's number in its slot, counting tokens that
+        have been evicted.  Nothing changes where the call is refused."""
+        counts = self._counts(counts, q, k, v)
+        self._chunk_space(q, scale)
+        if positions is None and rotary.axes > 1:
+            raise ValueError("positions of every axis expected")
+        if positions is None and any(c and s != t for c, s, t in zip(counts, self.seen, self.tokens)):
+            at = [s + i for s, c in zip(self.seen, counts) for i in range(c)]
+            positions = self._dev(at + [0] * (k.shape[0] - len(at)))
+        taken = self._take(counts)
+        try:
+            turned = torch.empty_like(q)
+            netkv.netkv_kv_append(self.pages, k, v, self._offsets(counts), self.length, self.table, rotary,
+                                  pos=positions, q=q, q_out=turned, status=self.status)
+        except Exception:
+            self._give_back(taken)
+            raise
+        self._grow(counts)
+        return self.attend_chunk(turned, counts, scale)
+
     def evict(self, budget: Sequence[int], sink: int = 4, recent: int = 4) -> List[List[int]]:
         """Cuts slot i to max(budget[i], sink + recent) blocks; the pages that became free."""
         table, length, mass, freed, n_freed = self._spare
@@ -174,7 +228,7 @@ class BlockPool:
         """Gives all of a slot's pages back."""
         self.free.extend(self.page_of[slot])
         self.page_of[slot] = []
-        self.tokens[slot] = 0
+        self.tokens[slot] = self.seen[slot] = 0
         self.table[slot].fill_(-1)
         self.length[slot].fill_(0)
 
@@ -208,5 +262,6 @@ def move(src: BlockPool, slot: int, dst: BlockPool, to: int) -> int:
         dst.pages.tensors[i][b] = src.pages.tensors[i][a]
     dst.mass[to, :blocks] = src.mass[slot, :blocks]
     dst.tokens[to] = n
+    dst.seen[to] = src.seen[slot]
     dst.length[to].fill_(n)
     return 2 * blocks * (one + src.pages.tensors[2][0].numel() * 4)
