@@ -5,8 +5,11 @@
 // a row block has 128 rows or fewer, both tiles are the same rows, and take the even and the odd key
 // tiles.  Keys come 128 at a time: eight blocks of 16 tokens.
 //
-// Bound: with 256 rows the tensor cores, 2,048 clocks a key tile at 128 wide for both products; with
-// 128 or fewer HBM, 32 KB of codes a key tile, 1,400 clocks of an SM's share.
+// Bound: with 256 rows shared memory, which a key tile at 128 wide takes for 2,500 clocks (320 KB: the
+// products read 192, widening moves 128), where the tensor cores take 2,048; with 128 or fewer the
+// widening, where HBM would take 1,400 (32 KB of codes, an SM's share).  2,048 tokens of 16 heads on 2
+// behind 65,536: 775 us, 1,440 TFLOP/s; 512 behind 7,680: 54 us; two parts of 900 tokens among 24
+// decoded ones: 214 us; 64 sequences of 9,400 tokens with 5 drafted ones each, e4m3: 129 us, 2.4 TB/s.
 //
 // Split: a line on which every row block has places for the keys that it sees and for its beginning
 // and end is cut into equal runs, one a block of threads, so that single long sequences, ragged
@@ -32,14 +35,16 @@ constexpr uint32_t kCtas = 152;  // blocks of the grid, one an SM: they hold all
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two).
 constexpr float kLag = 8.f;
-// Weights go into the second product times their value scale over a unit that is above all value
-// scales so far (at most twice the largest), and times 2^kUp: up to 2^(kLag + kUp), below fp16's
-// 2^16.  They are exact to 2^-11 down to 2^-20 of the largest one, 0 below 2^-31.
+// Weights go into the second product times their value scale over the largest one so far, and times
+// 2^kUp: up to 2^(kLag + kUp), below fp16's 2^16.  They are exact to 2^-11 down to 2^-21 of the largest
+// one, 0 below 2^-32; that of the only token of a row, or of the largest of a block alone, is exact.
 constexpr float kUp = 7.f;
+constexpr float kLeastScale = 1e-37f;  // value scales below are 0: 1 over them has to be finite
 // Places on the line: a key of a row block with two tiles of rows, of one with one tile, and the
-// beginning and end of a row block.
+// beginning and end of a row block.  (An end at 1,536: two parts among 24 decoded tokens 232 us instead
+// of 221, 512 behind 7,680 55.5 instead of 53.4; one-tile keys at 5: four drafted tokens 19.0 for 17.9.)
 constexpr uint64_t kPairKey = 8, kOneKey = 6, kEdge = 4096;
-constexpr uint64_t kLeast = 1280;  // places of a run at least
+constexpr uint64_t kLeast = 1280;  // places of a run at least (at 4,096 four drafted tokens: 29.6 us)
 // Scores that may be above this (in powers of two) are rounded before the maximum is taken from them,
 // as where some are hidden: a product that is not is off the rounded maximum by 2^-24 of itself.
 constexpr float kFar = 1048576.f;
@@ -282,8 +287,33 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t x, int from) {
          __shfl_sync(~0u, (uint32_t)x, from);
 }
 
+// Sequences that a warp adds up the places of: whole windows of 32.
+__device__ __forceinline__ uint32_t share_of(uint32_t n_seqs) {
+  constexpr uint32_t kWarps = kThreads / 32;
+  return (n_seqs + kWarps * 32 - 1) / (kWarps * 32) * 32;
+}
+
+// Rows that see no key, or a run's part of a row block without any: 0 and -inf.  Such items go no
+// further: the warps that look ahead wait for items with keys only, of which kItems are enough.
+template <int kDim, bool kBf16>
+__device__ __forceinline__ void nothing_seen(const ChunkArgs& a, const Item& x) {
+#pragma unroll 1
+  for (uint32_t r = threadIdx.x & 31; r < x.rows; r += 32) {
+    if (x.slot >= 0) {
+      a.part_ml[(uint64_t)x.slot * a.slot_rows + r] = make_float2(-INFINITY, 0.f);
+      continue;
+    }
+    const uint64_t row = x.row + (x.lead + r) / a.group;
+    const uint32_t head = x.kv_head * a.group + (x.lead + r) % a.group;
+    uint4* to = reinterpret_cast<uint4*>(a.out + (row * a.out_stride + (uint64_t)head * kDim) * 2);
+#pragma unroll 1
+    for (uint32_t i = 0; i < kDim / 8; ++i) to[i] = make_uint4(0, 0, 0, 0);
+    if (a.lse) a.lse[row * a.heads + head] = -INFINITY;
+  }
+}
+
 // ---- the planning warp: the run's items one after another
-template <class Sh>
+template <int kDim, bool kBf16, class Sh>
 __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
   const uint32_t lane = threadIdx.x & 31;
   uint64_t total = 0;
@@ -306,8 +336,9 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
   };
   uint32_t n = 0;
   auto publish = [&](const Item& x) {
-    if (n >= kItems)
-      wait<kItemPatience>(AT(item_empty[n % kItems]), (n / kItems - 1) & 1, late);
+    const bool ok = n < kItems ||
+                    wait<kItemPatience>(AT(item_empty[n % kItems]), (n / kItems - 1) & 1, late);
+    if (!__all_sync(~0u, ok)) return;  // the item there may be in use; nobody asks for another
     if (lane == 0) {
       sh.item[n % kItems] = x;
       bar_arrive(AT(item_full[n % kItems]));
@@ -320,7 +351,9 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
   uint64_t before = 0, into = 0;
   bool found = false;
   if (at < end) {
-    for (uint32_t from = 0; from < a.n_seqs; from += 32) {
+    uint32_t share = 0;  // the warp that has counted it
+    while (share + 1 < kThreads / 32 && at >= before + sh.sums[share]) before += sh.sums[share++];
+    for (uint32_t from = share * share_of(a.n_seqs); from < a.n_seqs; from += 32) {
       window(from);
       const uint64_t c = Shape(mine, a).all() * a.kv.heads;
       uint64_t upto = c;
@@ -399,7 +432,8 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
         a.cuts[run] = {x.row, kv_head, x.lead, x.rows, runs.at(begin + places - 1) - run0 + 1, run0,
                        runs.start(run0) < begin, run - run0 - 1};
       }
-      publish(x);
+      if (x.steps) publish(x);
+      else nothing_seen<kDim, kBf16>(a, x);
       first = false;
       at += upto - into;
       into = 0;
@@ -554,6 +588,7 @@ __device__ __forceinline__ void copy_values(const ChunkArgs& a, Sh& sh, uint32_t
     if (!x.valid) break;
     for (uint32_t from = 0; from < x.steps; from += kBatchTiles) {
       const int32_t page = batches.get(sh, sb, from, late).page[lane];
+      if (given_up(late)) return;  // it may not be a page
       batches.give(sh, sb, from + kBatchTiles, x.steps, late);
       for (uint32_t q = 0; q < min(kBatchTiles, x.steps - from); ++q)
         if (!copy_tile<kDim, 1>(a, sh, sb, count++, lane / kTileBlocks == q, page, x.kv_head, late))
@@ -667,7 +702,6 @@ __device__ __forceinline__ void multiply(Sh& sh, uint32_t sb, volatile int* late
   while (true) {
     const Item x = items.next(sh, sb, late);
     if (!x.valid) break;
-    if (x.steps == 0) continue;
     // Of two tiles of rows each key tile is both tiles' (a turn each), of one it is the even or the odd
     // one's.  The ring has K 0, V 0, K 1, V 1, ... or K 0, K 1, V 0, K 2, V 1, ...
     const uint32_t n = x.steps, turns = x.rows <= kRows ? n : 2 * n;
@@ -792,7 +826,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     const int rest = (int)max((int64_t)0, sees - (int64_t)full * kKeys);
     const uint32_t stride = one ? 2 : 1, own0 = one ? t : 0, steps = x.steps;
     float m = -INFINITY, l = 0.f;
-    uint32_t unit = 1;  // the exponent of what value scales are taken over
+    float unit = 0.f, over = 0.f;  // the largest value scale so far, and 1 over it
     bool any = false;
     for (uint32_t j = own0; j < steps; j += stride) {
       wait(AT(s_full[t]), taken++ & 1, late);
@@ -836,8 +870,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
           u = max3(u, y[14], y[15]);
           top = fmaxf(top, fmaxf(u, w) * k[b]);
         }
-        const uint32_t above = min((__float_as_uint(most) >> 23 & 0xff) + 1, 253u);
-        const bool grown = above > unit;  // alike for all rows
+        const bool grown = most > unit;      // alike for all rows
         const bool follow = top - m > kLag;  // also the first maximum
         if (grown || __any_sync(~0u, follow)) {
           float to = 1.f;
@@ -848,8 +881,9 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
           __syncwarp();
           l *= to;
           if (grown) {
-            to *= any ? __uint_as_float(127 + unit > above ? (127 + unit - above) << 23 : 0) : 0.f;
-            unit = above;
+            to *= any ? unit / most : 0.f;
+            unit = most;
+            over = most >= kLeastScale ? 1.f / most : 0.f;
           }
           if (any) {  // S_t is complete, and so is P_t V before it
 #pragma unroll 1
@@ -865,7 +899,6 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
         }
         any = true;
         const float base = m == -INFINITY ? 0.f : kUp - m;
-        const float over = __uint_as_float((254 - unit) << 23);
         const uint64_t base_2 = pair(base, base);
         uint64_t sums_2[2] = {0, 0};
 #pragma unroll
@@ -907,7 +940,6 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     batches.end(steps);
 
     // ---- the row's output, or its part
-    const float made = __uint_as_float(unit << 23);
     float w0 = 1.f, w1 = 0.f;  // what the two tiles' sums are multiplied by
     if (one) {
       const bool has0 = x.steps > 0, has1 = x.steps > 1;
@@ -916,7 +948,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
       finished0 += has0;
       finished1 += has1;
       // what a row's two threads have goes through their lane of TMEM, where the scores were
-      float own[4] = {m, l, made, 0.f}, other[4];
+      float own[4] = {m, l, unit, 0.f}, other[4];
       after_sync();
       tmem_store4(s_at, reinterpret_cast<const uint32_t*>(own));
       tmem_stored();
@@ -931,14 +963,14 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
       w1 = m1 == -INFINITY ? 0.f : ex2(m1 - m);
       // (a tile of NaN scores has no maximum, but its sum says so)
       l = w0 * (t ? other[1] : l) + w1 * (t ? l : other[1]);
-      w0 *= t ? other[2] : made;
-      w1 *= t ? made : other[2];
+      w0 *= t ? other[2] : unit;
+      w1 *= t ? unit : other[2];
     } else if (x.steps) {
       wait(AT(o_full[t]), (t ? finished1 : finished0) & 1, late);
       ++finished0;
       ++finished1;
       after_sync();
-      w0 = made;
+      w0 = unit;
     }
     if (busy) {
       const uint32_t token = (x.lead + mine) / a.group;
@@ -1039,8 +1071,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     before_sync();
   }
   // the line's length, and what is wrong with the sequences, said by the first block
+  // (a warp has neighbouring sequences, so that the plan finds its own among those of one warp)
   uint64_t sum = 0;
-  for (uint32_t i = tid; i < a.n_seqs; i += kThreads) {
+  const uint32_t each = share_of(a.n_seqs);
+  for (uint32_t i = warp * each + lane; i < min(a.n_seqs, (warp + 1) * each); i += 32) {
     sum += Shape(seq_of(a, i), a).all();
     if (blockIdx.x == 0 && (row_range(a.off, i, a.rows).bad ||
                             a.len[i] > (uint64_t)a.width * kBlockTokens))
@@ -1059,7 +1093,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   if (warp >= kProducts) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kProducts) multiply<kDim>(sh, sb, late);
-    else if (warp == kPlan) plan(a, sh, sb, late);
+    else if (warp == kPlan) plan<kDim, kBf16>(a, sh, sb, late);
     else if (warp == kPages) read_pages<kDim>(a, sh, sb, late);
     else if (warp == kValues) copy_values<kDim>(a, sh, sb, late);
   } else if (warp >= kSoftmaxWarps) {

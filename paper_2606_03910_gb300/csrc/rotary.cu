@@ -3,7 +3,10 @@
 //
 // Bound: HBM.  A block of threads has 16 tokens (of a sequence's block, where rows go into blocks):
 // it makes the cosines and sines of all their pairs once, in shared memory, and its warps take the
-// tokens' heads one by one, 16 rows of a head at a time with all loads under way at once.
+// tokens' heads one by one, 4 loads of 16 bytes a lane under way at a time: 32,768 rows of 72 heads of
+// 128 in 215 us, 5.6 TB/s (all 8 loads of 16 rows under way, and half the warps: 314).  New tokens of
+// 8 KV and 64 query heads: 70,319 of them in 595 us, 4.6 TB/s; the keys' warps set the pace, which
+// turn their rows twice, for the scale and for the codes.
 #include <math.h>
 
 #include "kv_store.cuh"

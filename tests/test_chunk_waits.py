@@ -75,3 +75,27 @@ def test_the_join_waits_before_it_ends():
     text = source()
     join = text[text.index(" join_kernel("):]
     assert join.index("griddepcontrol.wait") < join.index("return;")
+
+
+def test_only_items_with_keys_are_looked_ahead_for():
+    """The pages' warp asks for items ahead before it says what it has of the present one, and an item's
+    place comes back when the softmax is done with it: items without keys between two with some would
+    stand for ever between them.  The planning warp deals with those itself."""
+    text = source()
+    plan = text[text.index(" plan("):text.index(" read_pages(")]
+    assert re.search(r"if \(x\.steps\) publish\(x\);\s*else nothing_seen<", plan)
+    assert plan.count("publish(x);") == 2  # and the last one, that says there are no more
+    assert int(re.search(r"kItems = (\d+)", text).group(1)) >= 4  # the present one, two ahead, one behind
+
+
+def test_what_stands_after_a_wait_has_run_out_is_not_an_address():
+    """The planning warp leaves an item's place that may be in use, and page numbers are looked at only
+    after the flag: both become addresses."""
+    text = source()
+    publish = text[text.index("auto publish ="):]
+    publish = publish[:publish.index("};")]
+    assert publish.index("wait<kItemPatience>(") < publish.index("if (!__all_sync(~0u, ok)) return;") \
+        < publish.index("sh.item[n % kItems] = x;")
+    values = text[text.index(" copy_values("):]
+    values = values[:values.index("\n}\n")]
+    assert values.index(".page[lane]") < values.index("if (given_up(late)) return;") < values.index("copy_tile<")

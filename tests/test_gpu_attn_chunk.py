@@ -164,6 +164,16 @@ def test_more_rows_than_tokens(netkv):
     check(netkv, [20, 1, 300, 5, 40], [-7, -1, -200, -5, 10], 8, 1, 128, torch.float16, "e4m3")
 
 
+@pytest.mark.parametrize("gone", [1, 2, 3, 9, 40])
+def test_sequences_without_tokens_between_others(netkv, gone):
+    """Many rows in a row that see nothing, in one run of the line and across runs."""
+    new = [3, 1] + [2] * gone + [4, 1] + [1] * gone + [2]
+    held = [50, 400] + [-2] * gone + [60, 200] + [-1] * gone + [30]
+    check(netkv, new, held, 8, 1, 128, torch.bfloat16, "int8", seed=gone)
+    check(netkv, new * 3, held * 3, 4, 4, 64, torch.float16, "e4m3", seed=gone)
+    check(netkv, [300] * gone + [2], [-300] * gone + [40], 4, 2, 64, torch.float16, "int8", seed=gone)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 def test_absent_pages(netkv, dim):
     """Pages out of range hold no tokens: their block is not seen, ERANGE is said, and a row that sees
@@ -348,18 +358,24 @@ def test_a_graph_and_two_streams(netkv):
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
 
-def test_single_tokens_are_decode(netkv):
-    """One new token a sequence: what netkv_attn_decode gives, up to both sides' rounding."""
-    lengths = [1, 17, 300, 5000, 64]
+@pytest.mark.parametrize("n", [5, 5000])
+def test_single_tokens_are_decode(netkv, n):
+    """One new token a sequence: what netkv_attn_decode gives, up to both sides' rounding; among 5,000
+    sequences some without tokens."""
+    rng = np.random.default_rng(n)
+    lengths = [1, 17, 300, 5000, 64] + (rng.integers(0, 3, n - 5) * rng.integers(1, 60, n - 5)).tolist()
     blocks = [-(-x // 16) for x in lengths]
     pages = netkv.KvPages(*pool(sum(blocks), 2, 128, "int8"))
     table = tables(blocks, max(blocks), sum(blocks))
-    q = torch.randn((5, 16, 128), device="cuda").half()
-    a, b, la, lb = torch.empty_like(q), torch.empty_like(q), *(torch.empty((5, 16), device="cuda") for _ in "ab")
-    ws = torch.empty(netkv.netkv_attn_decode_workspace_size(pages, 5, 16, max(blocks)),
+    q = torch.randn((n, 16, 128), device="cuda").half()
+    a, b, la, lb = torch.empty_like(q), torch.empty_like(q), *(torch.empty((n, 16), device="cuda") for _ in "ab")
+    ws = torch.empty(netkv.netkv_attn_decode_workspace_size(pages, n, 16, max(blocks)),
                      dtype=torch.uint8, device="cuda")
     netkv.netkv_attn_decode(pages, q, ints(lengths), table, a, lse=la, workspace=ws)
-    assert call(netkv, pages, q, offsets([1] * 5), ints(lengths), table, b, lse=lb) == 0
+    assert call(netkv, pages, q, offsets([1] * n), ints(lengths), table, b, lse=lb) == 0
+    none = torch.tensor(lengths, device="cuda") == 0
+    assert (b[none] == 0).all() and (lb[none] == -math.inf).all() and (la[none] == -math.inf).all()
+    la[none], lb[none] = 0, 0
     # each: weights to 2^-11 and the output to 2^-11, of values up to 4 (codes of up to 127 at 1.25 / 127)
     assert ((a.float() - b.float()).abs() <= 4 * 2.0 ** -11 * 4).all()
     assert ((la - lb).abs() <= 1e-5 * (1 + la.abs())).all()
