@@ -166,3 +166,30 @@ def test_a_captured_step(blocks):
     step()
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(got, (*pool.pages.tensors, turned, out)))
+
+
+def test_pages_past_four_gigabytes(blocks):
+    """The same blocks at the end of a pool whose codes are past 32 bits, and in a small one."""
+    netkv = blocks.netkv
+    n, heads, kv_heads, dim, new = 1_200_000, 8, 2, 128, [70, 1]
+    big = [torch.empty((n, kv_heads, 16, dim), dtype=torch.int8, device="cuda") for _ in "kv"] + \
+        [torch.empty((n, kv_heads), device="cuda") for _ in "kv"]
+    small = [x[-20:].clone().zero_() for x in big]
+    for x in big:
+        x[-20:] = 0
+    q, k, v = (rows(71, h, dim, torch.bfloat16, h) for h in (heads, kv_heads, kv_heads))
+    off = torch.tensor([0, 70, 71], dtype=torch.int64, device="cuda")
+    length = torch.tensor(new, dtype=torch.int32, device="cuda")
+    outs = []
+    for codes, first in ((big, n - 20), (small, 0)):
+        pages = netkv.KvPages(*codes)
+        table = (torch.arange(20, dtype=torch.int32, device="cuda").flip(0) + first).view(2, 10).contiguous()
+        turned, out = torch.empty_like(q), torch.empty_like(q)
+        ws = torch.empty(netkv.netkv_attn_chunk_workspace_size(pages, 71, 2, heads), dtype=torch.uint8, device="cuda")
+        netkv.netkv_kv_append(pages, k, v, off, None, table, netkv.Rotary(64), q=q, q_out=turned)
+        netkv.netkv_attn_chunk(pages, turned, off, length, table, out, workspace=ws)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    for x, y in zip(big, small):
+        assert torch.equal(x[-20:], y)
