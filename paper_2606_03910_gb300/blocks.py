@@ -7,7 +7,8 @@ stored and attended (``extend``, ``attend_chunk``), and the eviction of the bloc
 the least attention (``evict``).  ``move`` carries a sequence from one pool to another, as the transfer that
 ``netkv_schedule_streams`` prices does between instances.
 
-Pages are handed out on the host; device work is enqueued on torch's current stream.  Only
+Pages are handed out on the host; device work is enqueued on torch's current stream.  Calls that
+change a pool come one after another; ``read`` and ``attend_chunk`` do not, and may overlap.  Only
 ``evict`` waits for the device: it reads which pages became free.
 """
 from __future__ import annotations
@@ -55,7 +56,6 @@ class BlockPool:
                        torch.empty_like(self.length))
         self._workspace = None
         self._workspace_heads = 0
-        self._chunk_workspace = None
 
     @property
     def slots(self) -> int:
@@ -157,22 +157,21 @@ class BlockPool:
                                 workspace=self._workspace, status=self.status)
         return out, lse
 
-    def _chunk_space(self, q: torch.Tensor, scale) -> torch.Tensor:
-        """A workspace for the queries' attention; a ValueError where that would be refused."""
+    def _chunk_bytes(self, q: torch.Tensor, scale) -> int:
+        """Workspace of the queries' attention; a ValueError where that would be refused."""
         if scale is not None and not 0.0 < scale <= 3.4e38:
             raise ValueError(f"a scale above 0 expected, got {scale}")
         need = netkv.netkv_attn_chunk_workspace_size(self.pages, q.shape[0], self.slots, q.shape[1])
         if need == 0:
             raise ValueError(f"query heads in groups of {self.pages.heads_dim[0]} expected, got {q.shape[1]}")
-        if self._chunk_workspace is None or self._chunk_workspace.nbytes < need:
-            self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
-        return self._chunk_workspace
+        return need
 
     def attend_chunk(self, q: torch.Tensor, counts: Sequence[int], scale=None):
         """Rows q [sum(counts), heads, dim] are the queries of the last counts[i] tokens of each slot i:
         (out, lse), each row over its own token and those before it.  The blocks' ``mass`` stays."""
         counts = self._counts(counts, q)
-        workspace = self._chunk_space(q, scale)
+        # a workspace of the call's own: calls on other streams may overlap with it
+        workspace = torch.empty(self._chunk_bytes(q, scale), dtype=torch.uint8, device=self.table.device)
         out = torch.empty_like(q)
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
         netkv.netkv_attn_chunk(self.pages, q, self._offsets(counts), self.length, self.table, out, lse=lse,
@@ -187,7 +186,7 @@ class BlockPool:
         positions [axes, rows] int32; by default a token's number in its slot, counting tokens that
         have been evicted.  Nothing changes where the call is refused."""
         counts = self._counts(counts, q, k, v)
-        self._chunk_space(q, scale)
+        self._chunk_bytes(q, scale)
         if positions is None and rotary.axes > 1:
             raise ValueError("positions of every axis expected")
         if positions is None and any(c and s != t for c, s, t in zip(counts, self.seen, self.tokens)):
