@@ -54,8 +54,6 @@ class BlockPool:
         self._spare = (torch.empty_like(self.table), torch.empty_like(self.length),
                        torch.empty_like(self.mass), torch.empty_like(self.table),
                        torch.empty_like(self.length))
-        self._workspace = None
-        self._workspace_heads = 0
 
     @property
     def slots(self) -> int:
@@ -145,16 +143,15 @@ class BlockPool:
     def attend(self, q: torch.Tensor, scale=None):
         """One query row a slot, [slots, heads, dim]: (out, lse); the blocks' weights add up in
         ``mass``."""
-        if self._workspace_heads != q.shape[1]:
-            need = netkv.netkv_attn_decode_workspace_size(self.pages, self.slots, q.shape[1],
-                                                          self.table.shape[1], True)
-            self._workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
-            self._workspace_heads = q.shape[1]
+        need = netkv.netkv_attn_decode_workspace_size(self.pages, self.slots, q.shape[1],
+                                                      self.table.shape[1], True)
+        # of the call's own: the last one's may still be in use on another stream
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.table.device)
         out = torch.empty_like(q)
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
         netkv.netkv_attn_decode(self.pages, q, self.length, self.table, out, lse=lse,
                                 mass_in=self.mass, mass_out=self.mass, scale=scale,
-                                workspace=self._workspace, status=self.status)
+                                workspace=workspace, status=self.status)
         return out, lse
 
     def _chunk_bytes(self, q: torch.Tensor, scale) -> int:

@@ -28,3 +28,15 @@ def test_chunks_of_two_streams_share_no_workspace(blocks, monkeypatch):
     for w, n in zip(kept, (3, 3, 60, 1)):
         assert w.nbytes >= blocks.netkv.netkv_attn_chunk_workspace_size(pool.pages, n, 3, 4)
     assert not any(x is w for x in vars(pool).values() for w in kept)
+
+
+def test_a_call_with_other_heads_frees_no_workspace_in_use(blocks, monkeypatch):
+    """A decode call on another stream than the last one's, and with other heads, while that runs."""
+    pool, kept = make(blocks), []
+    monkeypatch.setattr(blocks.netkv, "netkv_attn_decode", lambda *a, **k: kept.append(k["workspace"]))
+    for heads in (4, 8, 4, 4):
+        pool.attend(rows(3, heads))
+    assert len({w.data_ptr() for w in kept}) == 4
+    for w, heads in zip(kept, (4, 8, 4, 4)):
+        assert w.nbytes >= blocks.netkv.netkv_attn_decode_workspace_size(pool.pages, 3, heads, 5, True)
+    assert not any(x is w for x in vars(pool).values() for w in kept)
