@@ -567,8 +567,8 @@ netkv_status netkv_kv_load(const netkv_kv_pages* pages, uint32_t dtype, void* d_
  * product (fp16: to 2^-11 of themselves down to 2^-21 of the row's largest, 0 below 2^-32 of it).
  * d_lse [q_rows][heads] fp32 or NULL.  Rows outside every sequence are not written.
  * Values of a sequence's own v have to be finite: an infinity or NaN may reach rows that do
- * not see it.  What lies outside the sequence reaches nothing.  scale is finite and > 0.
- * At most 2^31 - 1 rows of either kind and 2^24 - 1 sequences. */
+ * not see it.  What lies outside the sequence reaches nothing.  scale is > 0, and scale *
+ * log2(e) finite.  At most 2^31 - 1 rows of either kind and 2^24 - 1 sequences. */
 netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint64_t q_stride,
                                const void* d_k, uint64_t k_stride, const void* d_v,
                                uint64_t v_stride, uint32_t heads, uint32_t kv_heads,
@@ -597,7 +597,8 @@ size_t netkv_attn_decode_workspace_size(const netkv_kv_pages* pages, uint32_t n_
  *               not written.  d_mass_in NULL: 0.  The two may be the same buffer.
  *   d_ws        caller-owned, netkv_attn_decode_workspace_size bytes; needs no initial value;
  *               calls that overlap on the GPU need distinct ones
- * Codes past the last token of a block reach nothing.  At most 2^24 - 1 sequences. */
+ * Codes past the last token of a block reach nothing.  scale is > 0, and scale * log2(e) finite.
+ * At most 2^24 - 1 sequences. */
 netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t dtype, const void* d_q,
                                uint64_t q_stride, uint32_t heads, uint32_t n_seqs,
                                const uint32_t* d_len, const int32_t* d_table,
@@ -691,8 +692,8 @@ size_t netkv_attn_chunk_workspace_size(const netkv_kv_pages* pages, uint64_t row
  *   d_lse [rows][heads] fp32 or NULL
  *   d_ws  caller-owned, netkv_attn_chunk_workspace_size bytes; needs no initial value; calls that
  *         overlap on the GPU need distinct ones
- * Codes past a sequence's last token reach nothing.  scale is finite and > 0.  At most 2^31 - 1 rows
- * and 2^24 - 1 sequences. */
+ * Codes past a sequence's last token reach nothing.  scale is > 0, and scale * log2(e) finite.  At most
+ * 2^31 - 1 rows and 2^24 - 1 sequences. */
 netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t dtype, const void* d_q,
                               uint64_t q_stride, uint32_t heads, uint32_t n_seqs,
                               const uint64_t* d_off, uint64_t rows, const uint32_t* d_len,

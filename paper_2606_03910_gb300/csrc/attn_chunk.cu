@@ -32,7 +32,6 @@ namespace {
 constexpr uint32_t kRows = 128, kKeys = 128;  // of a tile
 constexpr uint32_t kTileBlocks = kKeys / kBlockTokens;
 constexpr uint32_t kCtas = 152;  // blocks of the grid, one an SM: they hold all of TMEM
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two).
 constexpr float kLag = 8.f;
 // Weights go into the second product times their value scale over the largest one so far, and times
@@ -1191,7 +1190,7 @@ extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t d
                                          uint64_t out_stride, float* d_lse, void* d_ws,
                                          size_t ws_bytes, int* d_status, netkv_stream_t stream) {
   if (!sizes_ok(pages, rows, n_seqs, heads) || dtype > NETKV_BF16 || table_width == 0 ||
-      table_width >= (1u << 28) || !(scale > 0.f) || !(scale <= 3.4e38f))
+      table_width >= (1u << 28) || !scale_ok(scale))
     return NETKV_EINVAL;
   if (n_seqs == 0 || rows == 0) return NETKV_OK;
   const uint64_t row = (uint64_t)heads * pages->head_dim;

@@ -41,7 +41,6 @@ constexpr uint32_t kStages = 256 / kDim;  // pairs of pages in flight a warp: 16
 constexpr uint32_t kEdge = 8;       // see Runs; at 0 runs of short segments end last (338 us for 308)
 constexpr uint32_t kMinPages = 16;  // places of a run at least: a pair of pages for each of a block's
                                     // warps and an edge; a warp's own then cuts few short segments
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum follows the scores once one is above it by this (in powers of two):
 // weights up to 2^8 are as exact in fp16 as those up to 1, and sums are fp32.
 constexpr float kLag = 8.f;
@@ -1118,8 +1117,7 @@ extern "C" netkv_status netkv_attn_decode(const netkv_kv_pages* pages, uint32_t 
   if (!rows_ok(d_q, q_stride, row) || !rows_ok(d_out, out_stride, row) || !d_len || !d_table ||
       !d_ws || !aligned_to(d_len, 4) || !aligned_to(d_table, 4) || !aligned_to(d_lse, 4) ||
       !aligned_to(d_mass_in, 4) || !aligned_to(d_mass_out, 4) || !aligned_to(d_ws, 16) ||
-      !aligned_to(d_status, 4) || (d_mass_in && !d_mass_out) || !(scale > 0.f) ||
-      !(scale <= 3.4e38f))
+      !aligned_to(d_status, 4) || (d_mass_in && !d_mass_out) || !scale_ok(scale))
     return NETKV_EINVAL;
   const Workspace ws = workspace(pages, n_seqs, heads, table_width, d_mass_out != nullptr);
   if (ws_bytes < ws.total) return NETKV_EINVAL;

@@ -46,7 +46,6 @@ constexpr float kLag = 8.f;              // in powers of two
 // 2^-32; at 1, keys 2^-25 below a sink of small values would leave the output and not its sum.
 template <bool kBf16>
 constexpr float kUp = kBf16 ? 0.f : 7.f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Limits of waits in clocks: two seconds for what is at most a few steps away.  What may be a whole
 // item away (the next item, or a tile's scores where it has no rows in the item before) has ten times
 // what the steps of the longest one take; that others wait for the steps of that item ends it too.
@@ -791,7 +790,7 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
                                           int* d_status, netkv_stream_t stream) {
   if (dtype > NETKV_BF16 || (head_dim != 64 && head_dim != 128) || heads == 0 || heads > 65535 ||
       kv_heads == 0 || heads % kv_heads || n_seqs >> 24 || q_rows >> 31 || k_rows >> 31 ||
-      !(scale > 0.f) || !(scale <= 3.4e38f))
+      !scale_ok(scale))
     return NETKV_EINVAL;
   if (n_seqs == 0 || q_rows == 0) return NETKV_OK;
   const uint64_t row = (uint64_t)heads * head_dim, kv_row = (uint64_t)kv_heads * head_dim;

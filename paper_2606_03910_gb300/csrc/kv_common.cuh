@@ -10,6 +10,11 @@
 #include "netkv_internal.cuh"
 
 constexpr uint32_t kBlockTokens = NETKV_BLOCK_TOKENS;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// A softmax scale: the exponentials are powers of two, so its product with log2(e) has to be finite
+// too (an infinite one would make NaN of a score of 0).
+inline bool scale_ok(float scale) { return scale > 0.f && scale * kLog2e <= 3.4028235e38f; }
 
 // The pages by value, and the sizes of one page's part for one head.
 struct KvArgs {
