@@ -13,6 +13,8 @@ change a pool come one after another; ``read`` and ``attend_chunk`` do not, and 
 """
 from __future__ import annotations
 
+import ctypes
+import math
 from typing import List, Optional, Sequence
 
 import torch
@@ -20,6 +22,7 @@ import torch
 from . import netkv
 
 BLOCK = netkv.NETKV_BLOCK_TOKENS
+LOG2_E = 1.0 / math.log(2.0)
 FORMATS = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
 
 
@@ -156,8 +159,9 @@ class BlockPool:
 
     def _chunk_bytes(self, q: torch.Tensor, scale) -> int:
         """Workspace of the queries' attention; a ValueError where that would be refused."""
-        if scale is not None and not 0.0 < scale <= 3.4e38:
-            raise ValueError(f"a scale above 0 expected, got {scale}")
+        # as the call gets it: what is above 0 as a Python number may be 0 in 32 bits
+        if scale is not None and not 0.0 < ctypes.c_float(scale).value * LOG2_E <= 3.4028235e38:
+            raise ValueError(f"a scale above 0, and finite times log2(e), expected, got {scale}")
         need = netkv.netkv_attn_chunk_workspace_size(self.pages, q.shape[0], self.slots, q.shape[1])
         if need == 0:
             raise ValueError(f"query heads in groups of {self.pages.heads_dim[0]} expected, got {q.shape[1]}")
