@@ -131,9 +131,10 @@ class BlockPool:
         self._grow(counts)
 
     def _grow(self, counts: List[int]) -> None:
+        more = self._dev(counts)
         self.tokens = [t + c for t, c in zip(self.tokens, counts)]
         self.seen = [t + c for t, c in zip(self.seen, counts)]
-        self.length += self._dev(counts)
+        self.length += more
 
     def read(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int]) -> None:
         """The first counts[i] tokens of each slot into the rows k, v."""
@@ -167,17 +168,22 @@ class BlockPool:
             raise ValueError(f"query heads in groups of {self.pages.heads_dim[0]} expected, got {q.shape[1]}")
         return need
 
+    def _chunk_outputs(self, q: torch.Tensor, scale):
+        """Output, lse and workspace of the queries' attention, all that it may want of the allocator: a
+        workspace of the call's own, as calls on other streams may overlap with it."""
+        workspace = torch.empty(self._chunk_bytes(q, scale), dtype=torch.uint8, device=self.table.device)
+        return torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device=q.device), workspace
+
+    def _attend_chunk(self, q: torch.Tensor, off: torch.Tensor, scale, out, lse, workspace):
+        netkv.netkv_attn_chunk(self.pages, q, off, self.length, self.table, out, lse=lse, scale=scale,
+                               workspace=workspace, status=self.status)
+        return out, lse
+
     def attend_chunk(self, q: torch.Tensor, counts: Sequence[int], scale=None):
         """Rows q [sum(counts), heads, dim] are the queries of the last counts[i] tokens of each slot i:
         (out, lse), each row over its own token and those before it.  The blocks' ``mass`` stays."""
         counts = self._counts(counts, q)
-        # a workspace of the call's own: calls on other streams may overlap with it
-        workspace = torch.empty(self._chunk_bytes(q, scale), dtype=torch.uint8, device=self.table.device)
-        out = torch.empty_like(q)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        netkv.netkv_attn_chunk(self.pages, q, self._offsets(counts), self.length, self.table, out, lse=lse,
-                               scale=scale, workspace=workspace, status=self.status)
-        return out, lse
+        return self._attend_chunk(q, self._offsets(counts), scale, *self._chunk_outputs(q, scale))
 
     def extend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int],
                rotary: "netkv.Rotary", positions: Optional[torch.Tensor] = None, scale=None):
@@ -187,22 +193,24 @@ class BlockPool:
         positions [axes, rows] int32; by default a token's number in its slot, counting tokens that
         have been evicted.  Nothing changes where the call is refused."""
         counts = self._counts(counts, q, k, v)
-        self._chunk_bytes(q, scale)
+        outputs = self._chunk_outputs(q, scale)
         if positions is None and rotary.axes > 1:
             raise ValueError("positions of every axis expected")
         if positions is None and any(c and s != t for c, s, t in zip(counts, self.seen, self.tokens)):
             at = [s + i for s, c in zip(self.seen, counts) for i in range(c)]
             positions = self._dev(at + [0] * (k.shape[0] - len(at)))
-        taken = self._take(counts)
+        off, turned, taken, grown = self._offsets(counts), torch.empty_like(q), self._take(counts), False
         try:
-            turned = torch.empty_like(q)
-            netkv.netkv_kv_append(self.pages, k, v, self._offsets(counts), self.length, self.table, rotary,
-                                  pos=positions, q=q, q_out=turned, status=self.status)
+            netkv.netkv_kv_append(self.pages, k, v, off, self.length, self.table, rotary, pos=positions, q=q,
+                                  q_out=turned, status=self.status)
+            self._grow(counts)
+            grown = True
+            return self._attend_chunk(turned, off, scale, *outputs)
         except Exception:
+            if grown:
+                self._grow([-c for c in counts])
             self._give_back(taken)
             raise
-        self._grow(counts)
-        return self.attend_chunk(turned, counts, scale)
 
     def evict(self, budget: Sequence[int], sink: int = 4, recent: int = 4) -> List[List[int]]:
         """Cuts slot i to max(budget[i], sink + recent) blocks; the pages that became free."""
