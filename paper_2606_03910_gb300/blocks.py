@@ -168,11 +168,15 @@ class BlockPool:
             raise ValueError(f"query heads in groups of {self.pages.heads_dim[0]} expected, got {q.shape[1]}")
         return need
 
-    def _chunk_outputs(self, q: torch.Tensor, scale):
-        """Output, lse and workspace of the queries' attention, all that it may want of the allocator: a
-        workspace of the call's own, as calls on other streams may overlap with it."""
+    def _chunk_outputs(self, q: torch.Tensor, rows: int, scale):
+        """Output, lse and workspace of the attention of q's first rows, all that it may want of the
+        allocator: a workspace of the call's own, as calls on other streams may overlap with it."""
         workspace = torch.empty(self._chunk_bytes(q, scale), dtype=torch.uint8, device=self.table.device)
-        return torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device=q.device), workspace
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        if rows < len(q):  # the call leaves a padded batch's other rows as they are
+            out[rows:].zero_()
+            lse[rows:].fill_(-math.inf)
+        return out, lse, workspace
 
     def _attend_chunk(self, q: torch.Tensor, off: torch.Tensor, scale, out, lse, workspace):
         netkv.netkv_attn_chunk(self.pages, q, off, self.length, self.table, out, lse=lse, scale=scale,
@@ -181,19 +185,22 @@ class BlockPool:
 
     def attend_chunk(self, q: torch.Tensor, counts: Sequence[int], scale=None):
         """Rows q [sum(counts), heads, dim] are the queries of the last counts[i] tokens of each slot i:
-        (out, lse), each row over its own token and those before it.  The blocks' ``mass`` stays."""
+        (out, lse), each row over its own token and those before it.  Rows of q behind these, as of a padded
+        batch, give 0 and -inf.  The blocks' ``mass`` stays."""
         counts = self._counts(counts, q)
-        return self._attend_chunk(q, self._offsets(counts), scale, *self._chunk_outputs(q, scale))
+        return self._attend_chunk(q, self._offsets(counts), scale,
+                                  *self._chunk_outputs(q, sum(counts), scale))
 
     def extend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int],
                rotary: "netkv.Rotary", positions: Optional[torch.Tensor] = None, scale=None):
         """counts[i] new tokens of each slot i, as a layer has them: queries and keys turned by their
-        positions, keys and values into blocks, and attention over the blocks: (out, lse).
+        positions, keys and values into blocks, and attention over the blocks: (out, lse), with 0 and -inf
+        in rows behind these.
 
         positions [axes, rows] int32; by default a token's number in its slot, counting tokens that
         have been evicted.  Nothing changes where the call is refused."""
         counts = self._counts(counts, q, k, v)
-        outputs = self._chunk_outputs(q, scale)
+        outputs = self._chunk_outputs(q, sum(counts), scale)
         if positions is None and rotary.axes > 1:
             raise ValueError("positions of every axis expected")
         if positions is None and any(c and s != t for c, s, t in zip(counts, self.seen, self.tokens)):
