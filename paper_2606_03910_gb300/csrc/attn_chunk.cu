@@ -80,7 +80,7 @@ struct ChunkArgs {
   uint32_t slope;  // of the line, see Shape
   float scale2;    // scale * log2(e)
   float* lse;
-  float* part_o;   // [kCtas][2][kDim / 4][slot_rows][4]
+  float* part_o;   // [kCtas][2][kDim / 4][slot_rows][4], over a power of two, see over_power
   float2* part_ml; // [kCtas][2][slot_rows]: a row's maximum and sum
   Cut* cuts;       // [kCtas]
   uint32_t slot_rows;
@@ -754,6 +754,15 @@ __device__ __forceinline__ void multiply(Sh& sh, uint32_t sb, volatile int* late
   if (i >= 2) wait(smem_addr(&sh.kv_empty[(i - 2) % kRing]), ((i - 2) / kRing) & 1, late);
 }
 
+// A part's sums go to the workspace over a power of two, the one above the sum of its weights: that sum
+// is up to 2^15 times the row's tokens, and its product with a large value may pass fp32's range where
+// their quotient does not.  The powers leave the bits of whatever is a normal number as they are.
+__device__ __forceinline__ uint32_t power_of(float sum) {
+  return min(max(__float_as_uint(sum) >> 23, 1u), 252u);
+}
+__device__ __forceinline__ float over_power(float sum) { return __uint_as_float((253 - power_of(sum)) << 23); }
+__device__ __forceinline__ float times_power(float sum) { return __uint_as_float((power_of(sum) + 1) << 23); }
+
 // ---- softmax: a thread has a row of its tile
 template <int kDim, bool kBf16, bool kE4m3, class Sh>
 __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
@@ -980,7 +989,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     if (busy) {
       const uint32_t token = (x.lead + mine) / a.group;
       const uint32_t head = x.kv_head * a.group + (x.lead + mine) % a.group;
-      const float inv = l == 0.f || x.slot >= 0 ? 1.f : 1.f / l;
+      const float inv = x.slot >= 0 ? over_power(l) : l == 0.f ? 1.f : 1.f / l;
       const bool none = l == 0.f;  // NaN is not
       w0 *= inv;
       w1 *= inv;
@@ -1125,6 +1134,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 // Joins the row blocks that runs share: a run's beginning inside one has blocks of threads for a share
 // of its rows, a thread each row and 4 columns.
 constexpr uint32_t kJoinThreads = 256, kJoinShares = 8;
+static_assert(kCtas <= 256, "parts of a row block");
 template <int kDim, bool kBf16>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ ChunkArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1135,9 +1145,14 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   for (uint32_t u = (c.order * kJoinShares + blockIdx.y) * kJoinThreads + threadIdx.x;
        u < c.rows * (kDim / 4); u += shares * kJoinThreads) {
     const uint32_t row = u % c.rows, col = u / c.rows;
-    float top = -INFINITY;
-    for (uint32_t i = 0; i < c.parts; ++i)
-      top = fmaxf(top, a.part_ml[(uint64_t)slot(i) * a.slot_rows + row].x);
+    float top = -INFINITY, most = 0.f;
+    for (uint32_t i = 0; i < c.parts; ++i) {
+      const float2 ml = a.part_ml[(uint64_t)slot(i) * a.slot_rows + row];
+      top = fmaxf(top, ml.x);
+      most = fmaxf(most, ml.y);
+    }
+    // all parts over one power of two, 2^8 (they are fewer) above that of the largest
+    const float over = over_power(most) * 0x1p-8f;
     float sum = 0.f, o[4] = {};
     for (uint32_t i = 0; i < c.parts; ++i) {
       const float2 ml = a.part_ml[(uint64_t)slot(i) * a.slot_rows + row];
@@ -1146,12 +1161,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
       if (ml.y == 0.f) continue;
       const float4 y = reinterpret_cast<const float4*>(
           a.part_o)[((uint64_t)slot(i) * (kDim / 4) + col) * a.slot_rows + row];
-      o[0] += w * y.x;
-      o[1] += w * y.y;
-      o[2] += w * y.z;
-      o[3] += w * y.w;
+      const float by = w * (times_power(ml.y) * over);
+      o[0] += by * y.x;
+      o[1] += by * y.y;
+      o[2] += by * y.z;
+      o[3] += by * y.w;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum * (times_power(most) * 0x1p8f);
     const uint64_t to = c.row + (c.lead + row) / a.group;
     const uint32_t head = c.kv_head * a.group + (c.lead + row) % a.group;
     *reinterpret_cast<uint2*>(a.out + (to * a.out_stride + (uint64_t)head * kDim + col * 4) * 2) =
