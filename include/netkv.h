@@ -686,8 +686,8 @@ size_t netkv_attn_chunk_workspace_size(const netkv_kv_pages* pages, uint64_t row
  * every sequence are not written.
  * Codes go into the products as they are, queries as fp16 (bf16 rows times a power of two: channels
  * down to 2^-31 of a row's largest keep their bits), and so do the softmax weights times the blocks'
- * value scales (to 2^-11 of themselves down to 2^-21 of the largest weight at the largest scale, 0 below
- * 2^-32 of that); sums and lse are fp32.  Scales are finite and 0 or more; value scales below 1e-37
+ * value scales (to 2^-11 of themselves down to 2^-21 of the largest weight at the largest scale that the
+ * row sees, 0 below 2^-32 of that); sums and lse are fp32.  Scales are finite and 0 or more; value scales below 1e-37
  * count as 0.
  *   d_lse [rows][heads] fp32 or NULL
  *   d_ws  caller-owned, netkv_attn_chunk_workspace_size bytes; needs no initial value; calls that

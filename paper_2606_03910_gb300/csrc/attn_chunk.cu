@@ -34,8 +34,8 @@ constexpr uint32_t kTileBlocks = kKeys / kBlockTokens;
 constexpr uint32_t kCtas = 152;  // blocks of the grid, one an SM: they hold all of TMEM
 // The running maximum follows the scores once one is above it by this (in powers of two).
 constexpr float kLag = 8.f;
-// Weights go into the second product times their value scale over the largest one so far, and times
-// 2^kUp: up to 2^(kLag + kUp), below fp16's 2^16.  They are exact to 2^-11 down to 2^-21 of the largest
+// Weights go into the second product times their value scale over the largest one that the row has seen
+// so far, and times 2^kUp: up to 2^(kLag + kUp), below fp16's 2^16.  They are exact to 2^-11 down to 2^-21 of the largest
 // one, 0 below 2^-32; that of the only token of a row, or of the largest of a block alone, is exact.
 constexpr float kUp = 7.f;
 constexpr float kLeastScale = 1e-37f;  // value scales below are 0: 1 over them has to be finite
@@ -840,7 +840,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     const int rest = (int)max((int64_t)0, sees - (int64_t)full * kKeys);
     const uint32_t stride = one ? 2 : 1, own0 = one ? t : 0, steps = x.steps;
     float m = -INFINITY, l = 0.f;
-    float unit = 0.f, over = 0.f;  // the largest value scale so far, and 1 over it
+    float unit = 0.f, over = 0.f;  // the largest value scale seen so far, and 1 over it
     bool any = false;
     for (uint32_t j = own0; j < steps; j += stride) {
       wait(AT(s_full[t]), taken++ & 1, late);
@@ -857,8 +857,8 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
         const float4* v = reinterpret_cast<const float4*>(batch.v_scale + b0);
         const uint32_t absent = batch.absent >> b0 & 0xff;
         const int seen = j < full ? kKeys : j == full ? rest : 0;
-        const float most = max3(max3(v[0].x, v[0].y, v[0].z), max3(v[0].w, v[1].x, v[1].y),
-                                fmaxf(v[1].z, v[1].w));
+        float most = max3(max3(v[0].x, v[0].y, v[0].z), max3(v[0].w, v[1].x, v[1].y),
+                          fmaxf(v[1].z, v[1].w));
         const float most_k = max3(max3(k[0], k[1], k[2]), max3(k[3], k[4], k[5]), fmaxf(k[6], k[7]));
         const bool masked = __any_sync(~0u, seen < (int)kKeys || reach * most_k > kFar) || absent;
 #pragma unroll
@@ -870,6 +870,13 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
             s[i] = i < seen && !(absent >> (i / 16) & 1) ? s[i] * k[i / 16] : -INFINITY;
 #pragma unroll
           for (uint32_t b = 0; b < kTileBlocks; ++b) k[b] = 1.f;
+          // of the blocks that the row sees: a later token's scale takes no bits from its weights
+          if (seen < (int)kKeys) {
+            const float* each = reinterpret_cast<const float*>(v);
+            most = 0.f;
+#pragma unroll
+            for (int b = 0; b < (int)kTileBlocks; ++b) most = b * 16 < seen ? fmaxf(most, each[b]) : most;
+          }
         }
         float top = m;
 #pragma unroll
@@ -884,9 +891,9 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
           u = max3(u, y[14], y[15]);
           top = fmaxf(top, fmaxf(u, w) * k[b]);
         }
-        const bool grown = most > unit;      // alike for all rows
+        const bool grown = most > unit;
         const bool follow = top - m > kLag;  // also the first maximum
-        if (grown || __any_sync(~0u, follow)) {
+        if (__any_sync(~0u, grown || follow)) {
           float to = 1.f;
           if (follow) {
             to = m == -INFINITY ? 0.f : ex2(m - top);
@@ -922,7 +929,8 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
           const float scale[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            const float g = scale[b] * over, f = k[h * 4 + b];
+            // (at most 1, but of blocks that are not seen, whose weights of 0 should meet no infinity)
+            const float g = __saturatef(scale[b] * over), f = k[h * 4 + b];
             const uint64_t f_2 = pair(f, f), g_2 = pair(g, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {

@@ -4,7 +4,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_attn_chunk import call  # noqa: E402
+from tests import kv_plain as plain  # noqa: E402
+from tests.test_gpu_attn_chunk import WEIGHT_UNIT, call  # noqa: E402
 from tests.test_gpu_kv_blocks import ints, offsets, pool, tables  # noqa: E402
 
 
@@ -51,3 +52,53 @@ def test_values_times_a_power_of_two(netkv, fmt, heads, kv_heads, dim, new, held
         fine = out.abs() >= 2.0 ** -120
         assert torch.equal(back[fine], want.double()[fine])
         assert ((back - want.double()).abs()[~fine] <= 2.0 ** (-133 - power)).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(16, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("new,held", [(100, 0), (300, 0), (300, 50), (90, 3000)])
+@pytest.mark.parametrize("power", [12, 24, 40, 100])
+def test_values_of_tokens_that_a_row_does_not_see(netkv, fmt, heads, kv_heads, dim, new, held, power):
+    """A chunk whose values grow by a power of two from one of its blocks on: rows before that block are as
+    exact as without it, and are the same to the bit whatever stands there."""
+    total = new + held
+    blocks = -(-total // 16)
+    k, v, ks, vs = pool(blocks, kv_heads, dim, fmt)
+    table = torch.arange(blocks, dtype=torch.int32, device="cuda")[None]
+    q = torch.randn((new, heads, dim), device="cuda").bfloat16()
+    large = (held + new // 2) // 16   # the first block of large values
+    row = large * 16 - held           # the first row that sees it
+    outs = []
+    for p in (0, power):
+        more = vs.clone()
+        more[large:] *= 2.0 ** p
+        out, lse = torch.full_like(q, 5), torch.empty((new, heads), device="cuda")
+        assert call(netkv, netkv.KvPages(k, v, ks, more), q, offsets([new]), ints([total]), table, out,
+                    lse=lse) == 0
+        outs.append((out, lse, more))
+    assert torch.equal(outs[0][0][:row], outs[1][0][:row]) and torch.equal(outs[0][1], outs[1][1])
+    out, _, more = outs[1]
+    see = torch.arange(total, device="cuda")[None] <= torch.arange(new, device="cuda")[:, None] + held
+    for h in (0, heads - 1):
+        hk = h // (heads // kv_heads)
+        kh, vh = ((x[:, hk].double() * s[:, hk].double()[:, None, None]).flatten(0, 1)[:total]
+                  for x, s in ((k, ks), (v, more)))
+        o, _, _, weight, size = plain.attention(q[:, h].double(), kh, vh, dim ** -0.5, see)
+        # weights below fp16's smallest step: half of it, times the largest value that the row sees
+        for lo, hi in ((0, row), (row, new)):
+            top = float(more[:large if lo == 0 else blocks, hk].max()) * plain.TOP[fmt]
+            plain.close_out(out[lo:hi, h], o[lo:hi], weight[lo:hi], size, dim, torch.bfloat16, WEIGHT_UNIT,
+                            total * 2.0 ** -25 * top)
+
+
+def test_scales_at_both_ends_of_fp32(netkv):
+    """The quotient of a hidden block's scale by a visible one's is past fp32's range."""
+    k, v, ks, vs = pool(4, 1, 64, "int8")
+    vs[:2], vs[2:] = 1e-30, 1e36
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    q = torch.randn((64, 4, 64), device="cuda").bfloat16()
+    out = torch.full_like(q, 5)
+    assert call(netkv, netkv.KvPages(k, v, ks, vs), q, offsets([64]), ints([64]), table, out) == 0
+    assert torch.isfinite(out.float()).all()
+    # values of up to 127 * 1e-30 in the rows before, of up to 127 * 1e36 behind
+    assert 0 < out[:32].abs().max() < 1.3e-28 and out[32:].abs().amax((1, 2)).min() > 1e30
