@@ -1260,11 +1260,7 @@ extern "C" netkv_status netkv_attn_chunk(const netkv_kv_pages* pages, uint32_t d
     constexpr size_t bytes = sizeof(Shared<kDim>);
     static_assert(bytes <= 227 * 1024, "shared memory");
     // a launch with fewer registers than the warps share out would never end
-    static const int regs = [] {
-      cudaFuncAttributes has;
-      return cudaFuncGetAttributes(&has, kernel) == cudaSuccess ? has.numRegs : 0;
-    }();
-    if (regs < kLaunchRegs) return NETKV_ECUDA;
+    if (launch_registers<kernel>() < kLaunchRegs) return NETKV_ECUDA;
     NETKV_CUDA_TRY(allow_shared<kernel>((int)bytes));
     kernel<<<kCtas, kThreads, bytes, (cudaStream_t)stream>>>(a);
     if (netkv_launch_status() != NETKV_OK) return NETKV_ECUDA;

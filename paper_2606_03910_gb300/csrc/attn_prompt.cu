@@ -848,11 +848,7 @@ extern "C" netkv_status netkv_attn_prompt(uint32_t dtype, const void* d_q, uint6
     constexpr auto kernel = prompt_kernel<decltype(dim)::value, decltype(b)::value>;
     constexpr size_t bytes = sizeof(Shared<decltype(dim)::value>);
     // a launch with fewer registers than the warps share out would never end
-    static const int regs = [] {
-      cudaFuncAttributes has;
-      return cudaFuncGetAttributes(&has, kernel) == cudaSuccess ? has.numRegs : 0;
-    }();
-    if (regs < kLaunchRegs) return NETKV_ECUDA;
+    if (launch_registers<kernel>() < kLaunchRegs) return NETKV_ECUDA;
     NETKV_CUDA_TRY(allow_shared<kernel>((int)bytes));
     kernel<<<(unsigned)grid, kThreads, bytes, (cudaStream_t)stream>>>(a, q, k, v);
     return netkv_launch_status();

@@ -52,6 +52,21 @@ inline cudaError_t allow_shared(int bytes) {
   return e;
 }
 
+// Registers a thread of a kernel's launches; 0 where the runtime does not say, as for want of memory to
+// load the kernel, which a later call asks again.
+template <auto kKernel>
+inline int launch_registers() {
+  static std::atomic<int> known{0};
+  int n = known.load(std::memory_order_relaxed);
+  if (n) return n;
+  cudaFuncAttributes has;
+  if (cudaFuncGetAttributes(&has, kKernel) == cudaSuccess)
+    known.store(n = has.numRegs, std::memory_order_relaxed);
+  else
+    cudaGetLastError();  // or the next call's launch would be taken for the one that failed
+  return n;
+}
+
 // Rows of heads * dim 16-bit values: 16-byte aligned, strides in values.
 inline bool rows_ok(const void* p, uint64_t stride, uint64_t width) {
   return p && aligned_to(p, 16) && stride % 8 == 0 && stride >= width && stride < (1ull << 40);
