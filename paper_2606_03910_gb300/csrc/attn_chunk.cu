@@ -35,8 +35,9 @@ constexpr uint32_t kCtas = 152;  // blocks of the grid, one an SM: they hold all
 // The running maximum follows the scores once one is above it by this (in powers of two).
 constexpr float kLag = 8.f;
 // Weights go into the second product times their value scale over the largest one that the row has seen
-// so far, and times 2^kUp: up to 2^(kLag + kUp), below fp16's 2^16.  They are exact to 2^-11 down to 2^-21 of the largest
-// one, 0 below 2^-32; that of the only token of a row, or of the largest of a block alone, is exact.
+// so far, and times 2^kUp: up to 2^(kLag + kUp), below fp16's 2^16.  They are exact to 2^-11 down to
+// 2^-21 of the largest one, 0 below 2^-32; that of the only token of a row, or of the largest of a block
+// alone, is exact.
 constexpr float kUp = 7.f;
 constexpr float kLeastScale = 1e-37f;  // value scales below are 0: 1 over them has to be finite
 // Places on the line: a key of a row block with two tiles of rows, of one with one tile, and the
@@ -186,7 +187,7 @@ struct Item {
   uint32_t lead;      // heads of the first token that are another row block's
   uint32_t rows;      // 1 .. 256
   uint32_t tokens;    // of the sequence
-  uint32_t first, steps;
+  uint32_t first, steps;  // of an item that is sent on, steps >= 1
   int32_t slot;       // of the workspace; -1: the row block is all this item's
   int32_t valid;      // 0: no more items
 };
@@ -294,7 +295,7 @@ __device__ __forceinline__ uint32_t share_of(uint32_t n_seqs) {
 
 // Rows that see no key, or a run's part of a row block without any: 0 and -inf.  Such items go no
 // further: the warps that look ahead wait for items with keys only, of which kItems are enough.
-template <int kDim, bool kBf16>
+template <int kDim>
 __device__ __forceinline__ void nothing_seen(const ChunkArgs& a, const Item& x) {
 #pragma unroll 1
   for (uint32_t r = threadIdx.x & 31; r < x.rows; r += 32) {
@@ -312,7 +313,7 @@ __device__ __forceinline__ void nothing_seen(const ChunkArgs& a, const Item& x) 
 }
 
 // ---- the planning warp: the run's items one after another
-template <int kDim, bool kBf16, class Sh>
+template <int kDim, class Sh>
 __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, volatile int* late) {
   const uint32_t lane = threadIdx.x & 31;
   uint64_t total = 0;
@@ -432,7 +433,7 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
                        runs.start(run0) < begin, run - run0 - 1};
       }
       if (x.steps) publish(x);
-      else nothing_seen<kDim, kBf16>(a, x);
+      else nothing_seen<kDim>(a, x);
       first = false;
       at += upto - into;
       into = 0;
@@ -441,8 +442,8 @@ __device__ __forceinline__ void plan(const ChunkArgs& a, Sh& sh, uint32_t sb, vo
       if (++kv_head < a.kv.heads) continue;
       kv_head = 0;
       // the next sequence with rows, a window at a time: of a pool's slots few may have some.  (One by
-      // one, and by runs that had ended too, four tokens of two of 4,096 sequences took 311 us; now 47, and 21
-      // where they are neighbours.)
+      // one, and by runs that had ended too, four tokens of two of 4,096 sequences took 311 us; now 47,
+      // and 21 where they are neighbours.)
       if (at >= end) break;
       uint32_t later = seq + 1 - base < 32 ? ~0u << (seq + 1 - base) : 0u, hit;
       while (!(hit = __ballot_sync(~0u, mine.new_tokens != 0) & later) && base + 32 < a.n_seqs) {
@@ -773,7 +774,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
   const uint32_t s_at = kS + t * 128 + lanes, o_at = kO + t * kDim + lanes;
   Items items;
   Batches batches;
-  uint32_t taken = 0, finished0 = 0, finished1 = 0, meetings = 0;  // steps; items of each tile; meetings
+  uint32_t taken = 0, finished = 0, meetings = 0;  // of the tile: steps, items with any; meetings
   auto meet = [&]() {
     __syncwarp();
     if (lane == 0) bar_arrive(AT(met));
@@ -790,49 +791,47 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     const bool busy = __any_sync(~0u, real);
     float by = 0.f;  // what brings a sum of products to a score in powers of two, but for the scales
     float reach = 0.f;  // no score is above this times the scales
-    if (x.steps) {
-      // the row's queries as fp16, 16 bytes of row r in place (c ^ r) of 8
-      if (busy) {
-        const uint32_t token = (x.lead + mine) / a.group;
-        const uint32_t head = x.kv_head * a.group + (x.lead + mine) % a.group;
-        const uint4* from = reinterpret_cast<const uint4*>(
-            a.q + ((x.row + token) * a.q_stride + (uint64_t)head * kDim) * 2);
-        uint4 v[kDim / 8];
+    // the row's queries as fp16, 16 bytes of row r in place (c ^ r) of 8
+    if (busy) {
+      const uint32_t token = (x.lead + mine) / a.group;
+      const uint32_t head = x.kv_head * a.group + (x.lead + mine) % a.group;
+      const uint4* from = reinterpret_cast<const uint4*>(
+          a.q + ((x.row + token) * a.q_stride + (uint64_t)head * kDim) * 2);
+      uint4 v[kDim / 8];
 #pragma unroll
-        for (int i = 0; i < kDim / 8; ++i) v[i] = real ? __ldcs(from + i) : make_uint4(0, 0, 0, 0);
-        by = a.scale2;
-        // magnitudes are in the order of their bits, two values a word
-        uint32_t bits = 0;
+      for (int i = 0; i < kDim / 8; ++i) v[i] = real ? __ldcs(from + i) : make_uint4(0, 0, 0, 0);
+      by = a.scale2;
+      // magnitudes are in the order of their bits, two values a word
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < kDim / 8; ++i) {
+        bits = __vimax3_u16x2(bits, v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu);
+        bits = __vimax3_u16x2(bits, v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu);
+      }
+      const float largest = unpack16<kBf16>(max(bits & 0xffffu, bits >> 16)).x;
+      // (rows of infinities are not others' concern)
+      reach = largest <= 3.4028235e38f ? largest * by * (kDim * kTop) : 0.f;
+      if constexpr (kBf16) {
+        // 2^14 over the largest value's power of two, and the reverse; both are normal numbers
+        const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);
+        const float inv = __uint_as_float((254 + 14 - e) << 23);
+        by *= __uint_as_float((e - 14) << 23);
 #pragma unroll
         for (int i = 0; i < kDim / 8; ++i) {
-          bits = __vimax3_u16x2(bits, v[i].x & 0x7fff7fffu, v[i].y & 0x7fff7fffu);
-          bits = __vimax3_u16x2(bits, v[i].z & 0x7fff7fffu, v[i].w & 0x7fff7fffu);
-        }
-        const float largest = unpack16<kBf16>(max(bits & 0xffffu, bits >> 16)).x;
-        // (rows of infinities are not others' concern)
-        reach = largest <= 3.4028235e38f ? largest * by * (kDim * kTop) : 0.f;
-        if constexpr (kBf16) {
-          // 2^14 over the largest value's power of two, and the reverse; both are normal numbers
-          const uint32_t e = max(__float_as_uint(largest) >> 23, 15u);
-          const float inv = __uint_as_float((254 + 14 - e) << 23);
-          by *= __uint_as_float((e - 14) << 23);
+          uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
 #pragma unroll
-          for (int i = 0; i < kDim / 8; ++i) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float2 y = unpack16<true>(w[j]);
-              w[j] = pack16<false>(y.x * inv, y.y * inv);
-            }
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = unpack16<true>(w[j]);
+            w[j] = pack16<false>(y.x * inv, y.y * inv);
           }
         }
-#pragma unroll
-        for (int i = 0; i < kDim / 8; ++i)
-          *reinterpret_cast<uint4*>(sh.q[t] + i / 8 * kBox + row * 128 + ((i % 8) ^ (row & 7)) * 16) = v[i];
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      bar_arrive(AT(q_full[t]));
+#pragma unroll
+      for (int i = 0; i < kDim / 8; ++i)
+        *reinterpret_cast<uint4*>(sh.q[t] + i / 8 * kBox + row * 128 + ((i % 8) ^ (row & 7)) * 16) = v[i];
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    bar_arrive(AT(q_full[t]));
     // tokens that this row sees: of its key tiles all of the first `full`, and `rest` of the next
     const int64_t sees = (real ? x.sees + (x.lead + mine) / a.group : (int64_t)x.tokens) -
                          (int64_t)x.first * kKeys;
@@ -964,11 +963,7 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
     // ---- the row's output, or its part
     float w0 = 1.f, w1 = 0.f;  // what the two tiles' sums are multiplied by
     if (one) {
-      const bool has0 = x.steps > 0, has1 = x.steps > 1;
-      if (t == 0 && has0) wait(AT(o_full[0]), finished0 & 1, late);
-      if (t == 1 && has1) wait(AT(o_full[1]), finished1 & 1, late);
-      finished0 += has0;
-      finished1 += has1;
+      if (steps > t) wait(AT(o_full[t]), finished++ & 1, late);
       // what a row's two threads have goes through their lane of TMEM, where the scores were
       float own[4] = {m, l, unit, 0.f}, other[4];
       after_sync();
@@ -987,10 +982,8 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
       l = w0 * (t ? other[1] : l) + w1 * (t ? l : other[1]);
       w0 *= t ? other[2] : unit;
       w1 *= t ? unit : other[2];
-    } else if (x.steps) {
-      wait(AT(o_full[t]), (t ? finished1 : finished0) & 1, late);
-      ++finished0;
-      ++finished1;
+    } else {
+      wait(AT(o_full[t]), finished++ & 1, late);
       after_sync();
       w0 = unit;
     }
@@ -1006,16 +999,14 @@ __device__ __forceinline__ void softmax(const ChunkArgs& a, Sh& sh, uint32_t sb,
       const uint32_t c0 = one ? t * (kDim / 2) : 0, c1 = one ? c0 + kDim / 2 : kDim;
 #pragma unroll 1
       for (uint32_t c = c0; c < c1; c += kCols) {
-        float o[kCols] = {}, y[kCols];
-        if (x.steps) {
-          tmem_load16(kO + lanes + (one ? 0 : t * kDim) + c, o);
-          if (one && x.steps > 1) tmem_load16(kO + lanes + kDim + c, y);
-          tmem_loaded();
+        float o[kCols], y[kCols];
+        tmem_load16(kO + lanes + (one ? 0 : t * kDim) + c, o);
+        if (one && x.steps > 1) tmem_load16(kO + lanes + kDim + c, y);
+        tmem_loaded();
 #pragma unroll
-          for (int i = 0; i < kCols; ++i) {
-            o[i] = none ? 0.f : o[i] * w0;
-            if (one && x.steps > 1) o[i] += none ? 0.f : y[i] * w1;
-          }
+        for (int i = 0; i < kCols; ++i) {
+          o[i] = none ? 0.f : o[i] * w0;
+          if (one && x.steps > 1) o[i] += none ? 0.f : y[i] * w1;
         }
         if (!real) {
         } else if (x.slot >= 0) {
@@ -1115,7 +1106,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   if (warp >= kProducts) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kProducts) multiply<kDim>(sh, sb, late);
-    else if (warp == kPlan) plan<kDim, kBf16>(a, sh, sb, late);
+    else if (warp == kPlan) plan<kDim>(a, sh, sb, late);
     else if (warp == kPages) read_pages<kDim>(a, sh, sb, late);
     else if (warp == kValues) copy_values<kDim>(a, sh, sb, late);
   } else if (warp >= kSoftmaxWarps) {
