@@ -94,3 +94,27 @@ def test_three_axes(blocks, fmt, dtype):  # noqa: F811
         assert ((got - x).abs() <= tol).all()
         row += c
     check_outputs(pool, turned, counts, out, lse, dtype)
+
+
+def test_chunks_on_two_streams(blocks):  # noqa: F811
+    """attend_chunk() changes nothing in the pool: calls on two streams at once, small ones and ones that
+    need more in turn, give what they give one after another."""
+    heads, kv_heads, dim = 8, 2, 128
+    pool = blocks.BlockPool(700, kv_heads, dim, 2, 400)
+    k, v = (rows(8000, kv_heads, dim, torch.bfloat16, j) for j in range(2))
+    pool.append(k, v, [5000, 3000])
+    calls = [(rows(sum(c), heads, dim, torch.bfloat16, i), c)
+             for i, c in enumerate([[4, 0], [600, 1], [1, 3], [90, 700], [2, 2], [1000, 1000]])]
+    want = [pool.attend_chunk(q, c) for q, c in calls]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for turn in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for j in range(len(calls)):
+                    at = (j + turn + 3 * i) % len(calls)
+                    got.append((at, pool.attend_chunk(*calls[at])))
+    torch.cuda.synchronize()
+    assert int(pool.status) == 0
+    for at, (out, lse) in got:
+        assert torch.equal(out, want[at][0]) and torch.equal(lse, want[at][1])
