@@ -566,6 +566,7 @@ netkv_status netkv_kv_load(const netkv_kv_pages* pages, uint32_t dtype, void* d_
  * sums; the softmax is in fp32; its weights are rounded to the inputs' type for the second
  * product (fp16: to 2^-11 of themselves down to 2^-21 of the row's largest, 0 below 2^-32 of it).
  * d_lse [q_rows][heads] fp32 or NULL.  Rows outside every sequence are not written.
+ * Weighted sums of values are divided at the end, in fp32: values up to 2^80 stay in its range.
  * Values of a sequence's own v have to be finite: an infinity or NaN may reach rows that do
  * not see it.  What lies outside the sequence reaches nothing.  scale is > 0, and scale *
  * log2(e) finite.  At most 2^31 - 1 rows of either kind and 2^24 - 1 sequences. */
@@ -589,7 +590,8 @@ size_t netkv_attn_decode_workspace_size(const netkv_kv_pages* pages, uint32_t n_
  * Codes go into the products as they are, queries as fp16 (bf16 rows times a power of two: channels
  * down to 2^-31 of a row's largest keep their bits), and so do the softmax weights times the blocks'
  * value scales (to 2^-11 of themselves down to 2^-20 of the largest, 0 below 2^-31 of it); sums,
- * lse and block weights are fp32.
+ * lse and block weights are fp32.  Weighted sums of values are divided at the end: values up to 2^80
+ * stay in fp32's range.
  *   d_lse       [n_seqs][heads] fp32 or NULL
  *   d_mass_in, d_mass_out  [n_seqs][table_width] fp32 or NULL (both or d_mass_in only NULL):
  *               mass_out[i][j] = mass_in[i][j] + the softmax weights of block j's tokens,
@@ -634,7 +636,7 @@ netkv_status netkv_kv_evict(uint32_t n_seqs, const int32_t* d_table, const uint3
  * channels from 2 * pairs on are left as they are.  With the token's position t on the pair's axis
  * and a = t * step[p] / 2^64 turns,
  *     (x, y) -> (x cos a - y sin a, y cos a + x sin a)
- * in fp32.  Several axes: time, height and width of a token of an image or a video, for example. */
+ * in fp32, a to |t| * frequency * 2^-52 + 2^-23 of a radian.  Several axes: time, height and width of a token of an image or a video, for example. */
 typedef struct {
   uint64_t step[64];    /* of pair p: the part of a whole turn that a position is, times 2^64 */
   uint8_t axis[64];     /* of pair p: the axis whose positions it goes by, < axes */
@@ -687,8 +689,9 @@ size_t netkv_attn_chunk_workspace_size(const netkv_kv_pages* pages, uint64_t row
  * Codes go into the products as they are, queries as fp16 (bf16 rows times a power of two: channels
  * down to 2^-31 of a row's largest keep their bits), and so do the softmax weights times the blocks'
  * value scales (to 2^-11 of themselves down to 2^-21 of the largest weight at the largest scale that the
- * row sees, 0 below 2^-32 of that); sums and lse are fp32.  Scales are finite and 0 or more; value scales below 1e-37
- * count as 0.
+ * row sees, 0 below 2^-32 of that); sums and lse are fp32.  Scales are finite and 0 or more; value
+ * scales below 1e-37 count as 0.  A sequence's own codes have to be finite: e4m3's NaN, which
+ * netkv_kv_store does not write, may reach rows that do not see it.
  *   d_lse [rows][heads] fp32 or NULL
  *   d_ws  caller-owned, netkv_attn_chunk_workspace_size bytes; needs no initial value; calls that
  *         overlap on the GPU need distinct ones

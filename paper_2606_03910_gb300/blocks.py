@@ -198,7 +198,8 @@ class BlockPool:
         in rows behind these.
 
         positions [axes, rows] int32; by default a token's number in its slot, counting tokens that
-        have been evicted.  Nothing changes where the call is refused."""
+        have been evicted.  The blocks' ``mass`` stays: where only extend() runs, evict() takes the oldest
+        blocks between the first and the last ones.  Nothing changes where the call is refused."""
         counts = self._counts(counts, q, k, v)
         outputs = self._chunk_outputs(q, sum(counts), scale)
         if positions is None and rotary.axes > 1:

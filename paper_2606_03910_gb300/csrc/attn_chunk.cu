@@ -8,8 +8,9 @@
 // Bound: with 256 rows shared memory, which a key tile at 128 wide takes for 2,500 clocks (320 KB: the
 // products read 192, widening moves 128), where the tensor cores take 2,048; with 128 or fewer the
 // widening, where HBM would take 1,400 (32 KB of codes, an SM's share).  2,048 tokens of 16 heads on 2
-// behind 65,536: 775 to 806 us, 1,410 TFLOP/s; 512 behind 7,680: 55 us; two parts of 900 tokens among 24
-// decoded ones: 217 us; 64 sequences of 9,400 tokens with 5 drafted ones each, e4m3: 131 us, 2.4 TB/s.
+// behind 65,536: 800 to 816 us, 1,370 to 1,400 TFLOP/s; 512 behind 7,680: 54 us; two parts of 900 tokens
+// among 24 decoded ones: 217 us; 64 sequences of 9,400 tokens with 5 drafted ones each, e4m3: 133 us, 2.3
+// TB/s.
 //
 // Split: a line on which every row block has places for the keys that it sees and for its beginning
 // and end is cut into equal runs, one a block of threads, so that single long sequences, ragged

@@ -3,8 +3,10 @@
 //
 // An angle is needed only up to whole turns, and a 64-bit product wraps exactly there: a pair's
 // frequency is held as the part of a turn that one position is, times 2^64, and position * step
-// mod 2^64 is the angle, to 2^-22 of a radian at the last of 2^31 positions (an fp32 product of a
-// position near 2^20 would be 2^-4 off).  Its upper half goes to sincospif.
+// mod 2^64 is the angle.  A step is off by 2^-52 of itself at most (2 pi and the division, in doubles), so
+// the angle of position t at frequency f by t * f * 2^-52 of a radian, and by 2^-23 more where its upper
+// half becomes fp32 for sincospif: 2^-21 at the last of 2^31 positions for frequencies up to 1.  (An fp32
+// product of a position near 2^20 would be 2^-4 off.)
 #pragma once
 
 #include "kv_common.cuh"
